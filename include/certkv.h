@@ -73,6 +73,13 @@ enum {
 
 enum { CERTKV_F32 = 0, CERTKV_BF16 = 1 };
 
+/* How the rows of a packed cache are held. */
+enum {
+  CERTKV_CACHE_BF16 = 0,  /* bf16 values                                   */
+  CERTKV_CACHE_MXFP8 = 1, /* e4m3 codes, a scale byte for every 32 dims    */
+  CERTKV_CACHE_MXFP4 = 2  /* e2m1 codes, a scale byte for every 32 dims    */
+};
+
 enum {
   CERTKV_CAUSAL = 1u << 0,  /* window rows see only keys at or before them  */
   CERTKV_DRY_RUN = 1u << 1, /* validate arguments, launch nothing           */
@@ -374,6 +381,92 @@ certkv_status certkv_decode(const certkv_problem* p, certkv_tensor q_new,
                             const int64_t* packed_offsets, float* out,
                             float* lse, void* ws, size_t ws_bytes,
                             void* stream);
+
+/* ---- The packed cache in microscaled codes, and drafted tokens ---------------
+ * A packed cache in one of the CERTKV_CACHE_ formats.  bf16: k, v [rows][d], no
+ * scales.  mxfp8 and mxfp4: a row is d/32 blocks of 32 consecutive dims, a block
+ * its codes c_i and a scale byte x, the values c_i 2^(x - 127).
+ *   mxfp8   e4m3 codes (largest 448), k, v [rows][d] bytes
+ *   mxfp4   e2m1 codes (largest 6), k, v [rows][d/2] bytes, the even dim in the
+ *           low half of a byte
+ *   scales  [rows][d/32] bytes, 27 to 246 (mxfp8) or 252 (mxfp4), or 255: a
+ *           block that held a non-finite value, all of it NaN
+ *   offsets [L*B*H+1] int64, start of each unit's rows
+ * k and v must be 16-byte aligned, the scales 4-byte aligned. */
+typedef struct certkv_cache {
+  int32_t format;
+  const void* k;
+  const void* v;
+  const uint8_t* k_scales; /* NULL for bf16 */
+  const uint8_t* v_scales;
+  const int64_t* offsets;
+} certkv_cache;
+
+/* certkv_compact with the rows quantised as they are written: same kept sets,
+ * slots, order, positions and offsets; format CERTKV_CACHE_MXFP8 or _MXFP4.
+ * A block's exponent x - 127 is the smallest under which its largest magnitude
+ * is at most the largest code, within [-100, 119] (mxfp8) or [-100, 125]
+ * (mxfp4); codes are rounded to nearest, ties to even, from the source's own
+ * values (a slot's from its fp32 k*, v*), and saturate only beyond 1.75 x 2^127
+ * (mxfp8) or 1.5 x 2^127 (mxfp4).  Sources in kv_dtype, bf16 or fp32.  A
+ * non-finite value sets the status word.  k_star, v_star are 16-byte aligned
+ * and may be NULL under CERTKV_NO_SLOT.  Rows of the outputs past the last packed one are not
+ * written. */
+certkv_status certkv_compact_mx(const certkv_problem* p, int32_t format, certkv_tensor k,
+                                certkv_tensor v, const int64_t* kept_offsets,
+                                const int32_t* kept_idx, const float* k_star,
+                                const float* v_star, void* k_codes, uint8_t* k_scales,
+                                void* v_codes, uint8_t* v_scales, int32_t* pos_packed,
+                                int64_t* packed_offsets, void* stream);
+
+/* certkv_compress with a packed cache in microscaled codes, written as
+ * certkv_compact_mx does.  out->k_packed and out->v_packed are not written and
+ * may be NULL, out->k_star and out->v_star are 16-byte aligned; everything else
+ * as certkv_compress. */
+certkv_status certkv_compress_mx(const certkv_problem* p, int32_t format, certkv_tensor q_win,
+                                 certkv_tensor k, certkv_tensor v, const float* lse_in,
+                                 const int32_t* n_keep_host, double alpha, int32_t steps,
+                                 const certkv_outputs* out, void* k_codes, uint8_t* k_scales,
+                                 void* v_codes, uint8_t* v_scales, void* ws, size_t ws_bytes,
+                                 void* stream);
+
+/* The values of rows first_row .. first_row + rows - 1 of a microscaled cache
+ * (cache.offsets is not read), exact in bf16 and fp32.
+ *   k_out, v_out   [rows][d] in out_dtype (CERTKV_BF16 or CERTKV_F32), 16-byte
+ *                  aligned; either may be NULL */
+certkv_status certkv_read_mx(const certkv_problem* p, certkv_cache cache, int64_t first_row,
+                             int64_t rows, int32_t out_dtype, void* k_out, void* v_out,
+                             void* stream);
+
+/* certkv_decode over a microscaled cache (mxfp8 or mxfp4): the same queries,
+ * sums and outputs, over the values that the codes stand for.  A segment longer
+ * than its bound of max_rows stores CERTKV_ERANGE in *dev_status and its rows
+ * past the bound are left out.  A row with no packed row to see is out = 0, lse =
+ * -infinity.  The workspace is certkv_decode_cache_workspace_size(p, format, tq, 0,
+ * max_rows) bytes, 256-byte aligned. */
+size_t certkv_decode_cache_workspace_size(const certkv_problem* p, int32_t format, int32_t tq,
+                                          int32_t tn, int32_t max_rows);
+certkv_status certkv_decode_mx(const certkv_problem* p, certkv_tensor q_new, int32_t tq,
+                               int32_t max_rows, certkv_cache cache, float* out, float* lse,
+                               void* ws, size_t ws_bytes, void* stream);
+
+/* Attention of drafted tokens: certkv_decode over a packed cache of any format
+ * and, beside it, over tn new rows per sequence that each query sees or not: the
+ * tokens since the compression, a tree of drafted tokens.
+ *   q_new        [L][B*tq][Hq][d] bf16, tq * G <= 512
+ *   k_new, v_new [L][B*tn][H][d] bf16, stride rules as for q_new; 1 <= tn <= 65536
+ *   mask         [B][tq][tn] bytes: query t of sequence b sees new row j where
+ *                mask[b][t][j] != 0 (for a tree: its ancestors and itself).
+ *                NULL: j <= tn - tq + t, the last tq rows being the queries' own
+ *                (tn >= tq)
+ * Every packed row is visible to every query.  A new row that a query does not
+ * see has no part in its output, whatever it holds (a padded batch's rows may be
+ * NaN).  A query that sees nothing is out = 0, lse = -infinity.  The workspace is
+ * certkv_decode_cache_workspace_size(p, cache.format, tq, tn, max_rows) bytes. */
+certkv_status certkv_decode_tree(const certkv_problem* p, certkv_tensor q_new, int32_t tq,
+                                 int32_t max_rows, certkv_cache cache, certkv_tensor k_new,
+                                 certkv_tensor v_new, int32_t tn, const uint8_t* mask, float* out,
+                                 float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* Clustered tail summaries (appendix, deterministic output-error bound for
  * clustered tail summaries): per head, the evicted ranks b_h..n-1 in the

@@ -31,6 +31,9 @@ CERTKV_ALLOC_GREEDY = 1 << 6
 CERTKV_NO_SLOT = 1 << 7
 CERTKV_SELECT_BUDGET = 0
 CERTKV_SELECT_COVERAGE = 1
+CERTKV_CACHE_BF16 = 0
+CERTKV_CACHE_MXFP8 = 1
+CERTKV_CACHE_MXFP4 = 2
 
 STAGE_SCORE = 1
 STAGE_ALLOCATE = 2
@@ -46,6 +49,8 @@ EXPORTS = [
     "certkv_decode_clustered", "certkv_profile_enable",
     "certkv_profile_read", "certkv_profile_reset",
     "certkv_score_noalloc", "certkv_score_noalloc_max_bytes",
+    "certkv_compact_mx", "certkv_compress_mx", "certkv_read_mx",
+    "certkv_decode_cache_workspace_size", "certkv_decode_mx", "certkv_decode_tree",
 ]
 
 
@@ -72,6 +77,17 @@ class Tensor(ctypes.Structure):
         ("s_layer", ctypes.c_int64),
         ("s_token", ctypes.c_int64),
         ("s_head", ctypes.c_int64),
+    ]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [
+        ("format", ctypes.c_int32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p),
+        ("v_scales", ctypes.c_void_p),
+        ("offsets", ctypes.c_void_p),
     ]
 
 
@@ -125,6 +141,15 @@ def lib():
     L.certkv_cluster_tail.argtypes = [P, Tensor, Tensor, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
     L.certkv_decode_clustered.argtypes = [P, Tensor, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp,
                                           vp, vp, vp, vp, vp, vp, sz, vp]
+    L.certkv_compact_mx.argtypes = [P, i32, Tensor, Tensor] + [vp] * 11
+    L.certkv_compress_mx.argtypes = [P, i32, Tensor, Tensor, Tensor, vp, vp, dbl, i32,
+                                     ctypes.POINTER(Outputs), vp, vp, vp, vp, vp, sz, vp]
+    L.certkv_read_mx.argtypes = [P, Cache, i64, i64, i32, vp, vp, vp]
+    L.certkv_decode_cache_workspace_size.argtypes = [P, i32, i32, i32, i32]
+    L.certkv_decode_cache_workspace_size.restype = sz
+    L.certkv_decode_mx.argtypes = [P, Tensor, i32, i32, Cache, vp, vp, vp, sz, vp]
+    L.certkv_decode_tree.argtypes = [P, Tensor, i32, i32, Cache, Tensor, Tensor, i32, vp, vp, vp,
+                                     vp, sz, vp]
     L.certkv_profile_enable.argtypes = [i32]
     L.certkv_profile_read.argtypes = [vp, vp, vp, i32]
     L.certkv_profile_read.restype = i32
@@ -133,7 +158,8 @@ def lib():
     for name in EXPORTS:
         if name not in ("certkv_status_string", "certkv_workspace_size",
                         "certkv_decode_workspace_size", "certkv_profile_read",
-                        "certkv_profile_reset", "certkv_score_noalloc_max_bytes"):
+                        "certkv_profile_reset", "certkv_score_noalloc_max_bytes",
+                        "certkv_decode_cache_workspace_size"):
             getattr(L, name).restype = i32
     _LIB = L
     return L

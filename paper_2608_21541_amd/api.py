@@ -269,9 +269,12 @@ def decode_workspace_size(spec: ProblemSpec, tq: int, max_rows: int = 0) -> int:
 
 
 class DecodeBuffers:
-    """Preallocated outputs and workspace of certkv_decode (reusable)."""
+    """Preallocated outputs and workspace of certkv_decode (reusable); with fmt
+    ("bf16", "mxfp8" or "mxfp4") those of certkv_decode_mx and certkv_decode_tree
+    over a cache of that format and tn new rows per sequence."""
 
-    def __init__(self, spec: ProblemSpec, tq: int, device, with_lse=False, max_rows=0):
+    def __init__(self, spec: ProblemSpec, tq: int, device, with_lse=False, max_rows=0, tn=0,
+                 fmt=None):
         self.tq = int(tq)
         self.max_rows = int(max_rows)
         rows = spec.layers * spec.batch * self.tq
@@ -280,7 +283,12 @@ class DecodeBuffers:
                                dtype=torch.float32, device=device)
         self.lse = torch.empty((spec.layers, spec.batch * self.tq, hq), dtype=torch.float32,
                                device=device) if with_lse else None
-        self.ws_bytes = decode_workspace_size(spec, self.tq, self.max_rows)
+        self.tn = int(tn)
+        self.fmt = fmt
+        if fmt is None:
+            self.ws_bytes = decode_workspace_size(spec, self.tq, self.max_rows)
+        else:
+            self.ws_bytes = decode_cache_workspace_size(spec, fmt, self.tq, self.tn, self.max_rows)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
         assert self.ws.data_ptr() % 256 == 0 and rows > 0
 
@@ -343,11 +351,183 @@ def decode_clustered(spec: ProblemSpec, q_new, k_packed, v_packed, packed_offset
     return bufs.out, bufs.lse, bound
 
 
+_FORMATS = {"bf16": _lib.CERTKV_CACHE_BF16, "mxfp8": _lib.CERTKV_CACHE_MXFP8,
+            "mxfp4": _lib.CERTKV_CACHE_MXFP4}
+
+
+def _format_code(fmt):
+    if fmt not in _FORMATS:
+        raise ValueError(f"unsupported cache format {fmt!r}")
+    return _FORMATS[fmt]
+
+
+@dataclass
+class MxCache:
+    """A packed cache in microscaled codes ("mxfp8": k, v [rows][d] uint8; "mxfp4":
+    [rows][d/2], the even dim in the low half of a byte), a scale byte for every 32 dims
+    (k_scales, v_scales [rows][d/32]), the units' offsets [U+1] int64 and, where
+    compact_mx wrote it, the rows' positions [rows] int32."""
+    format: str
+    k: torch.Tensor
+    k_scales: torch.Tensor
+    v: torch.Tensor
+    v_scales: torch.Tensor
+    offsets: torch.Tensor
+    pos: Optional[torch.Tensor] = None
+
+    @staticmethod
+    def empty(spec: ProblemSpec, rows: int, fmt: str, device):
+        """Buffers for a cache of `rows` packed rows."""
+        if _format_code(fmt) == _lib.CERTKV_CACHE_BF16:
+            raise ValueError("a microscaled cache is mxfp8 or mxfp4")
+        d = spec.head_dim
+        codes = (rows, d if fmt == "mxfp8" else d // 2)
+        u8 = dict(dtype=torch.uint8, device=device)
+        return MxCache(fmt, torch.empty(codes, **u8), torch.empty((rows, d // 32), **u8),
+                       torch.empty(codes, **u8), torch.empty((rows, d // 32), **u8),
+                       torch.empty(spec.units + 1, dtype=torch.int64, device=device),
+                       torch.empty(rows, dtype=torch.int32, device=device))
+
+    @property
+    def rows(self):
+        return self.k.shape[0]
+
+    @property
+    def head_dim(self):
+        return self.k.shape[1] * (1 if self.format == "mxfp8" else 2)
+
+    def c_cache(self):
+        for t in (self.k, self.k_scales, self.v, self.v_scales):
+            assert t.dtype == torch.uint8 and t.is_contiguous() and t.shape[0] == self.rows
+        assert self.v.shape == self.k.shape
+        assert self.k_scales.shape[1] == self.v_scales.shape[1] == self.head_dim // 32
+        return _lib.Cache(_format_code(self.format), self.k.data_ptr(), self.v.data_ptr(),
+                          self.k_scales.data_ptr(), self.v_scales.data_ptr(),
+                          self.offsets.data_ptr())
+
+
+def compact_mx(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star, fmt, cache=None):
+    """compact with the packed rows quantised as they are written: an MxCache of format fmt
+    ("mxfp8" or "mxfp4"), `cache` if one is given (its rows past the last packed one are left
+    as they are)."""
+    L = _lib.lib()
+    dev = k.device
+    if cache is None:
+        rows = int(kept_offsets[-1].item()) + (spec.units if spec.slot else 0)
+        cache = MxCache.empty(spec, rows, fmt, dev)
+    assert cache.format == fmt and cache.pos is not None and cache.head_dim == spec.head_dim
+    p, c = spec.c_problem(), cache.c_cache()
+    with torch.cuda.device(dev):
+        _check(L.certkv_compact_mx(ctypes.byref(p), c.format, _tensor(k), _tensor(v),
+                                   _ptr(kept_offsets), _ptr(kept_idx), _ptr(k_star), _ptr(v_star),
+                                   c.k, c.k_scales, c.v, c.v_scales, _ptr(cache.pos),
+                                   _ptr(cache.offsets), _stream(dev)), "certkv_compact_mx")
+    return cache
+
+
+def read_mx(cache: MxCache, dtype=torch.bfloat16, first_row=0, rows=None, out=None):
+    """The values (k, v) [rows][d] of a cache's rows first_row .. first_row + rows - 1 (all
+    from first_row on by default), exact in bf16 and fp32; out: the two tensors to write."""
+    L = _lib.lib()
+    dev = cache.k.device
+    d = cache.head_dim
+    n = cache.rows - first_row if rows is None else int(rows)
+    assert 0 <= first_row and 0 <= n and first_row + n <= cache.rows
+    if out is None:
+        out = [torch.empty((n, d), dtype=dtype, device=dev) for _ in range(2)]
+    for t in out:
+        assert t.is_contiguous() and tuple(t.shape) == (n, d) and t.dtype == out[0].dtype
+    p = ProblemSpec(1, 1, 1, d, 1, [1]).c_problem()
+    with torch.cuda.device(dev):
+        _check(L.certkv_read_mx(ctypes.byref(p), cache.c_cache(), int(first_row), n,
+                                _dtype_code(out[0].dtype), _ptr(out[0]), _ptr(out[1]),
+                                _stream(dev)), "certkv_read_mx")
+    return out[0], out[1]
+
+
+def decode_cache_workspace_size(spec: ProblemSpec, fmt: str, tq: int, tn: int = 0,
+                                max_rows: int = 0) -> int:
+    p = spec.c_problem()
+    return int(_lib.lib().certkv_decode_cache_workspace_size(
+        ctypes.byref(p), _format_code(fmt), int(tq), int(tn), int(max_rows)))
+
+
+def _check_queries(spec, q_new, tq):
+    assert q_new.dtype == torch.bfloat16
+    assert tuple(q_new.shape) == (spec.layers, spec.batch * int(tq), spec.kv_heads * spec.group,
+                                  spec.head_dim)
+
+
+def _cache_buffers(spec, fmt, tq, tn, dev, with_lse, bufs, max_rows):
+    if bufs is None:
+        bufs = DecodeBuffers(spec, tq, dev, with_lse=with_lse, max_rows=max_rows, tn=tn, fmt=fmt)
+    assert bufs.fmt == fmt and bufs.tq == int(tq) and bufs.tn == int(tn)
+    return bufs
+
+
+def decode_mx(spec: ProblemSpec, q_new, cache: MxCache, tq, with_lse=False, bufs=None, max_rows=0):
+    """decode over a microscaled packed cache: out [L][B*tq][Hq][d] fp32 (and the natural-log
+    lse [L][B*tq][Hq] with_lse).  bufs: DecodeBuffers(..., fmt=cache.format)."""
+    L = _lib.lib()
+    dev = q_new.device
+    _check_queries(spec, q_new, tq)
+    assert cache.head_dim == spec.head_dim and cache.offsets.numel() == spec.units + 1
+    bufs = _cache_buffers(spec, cache.format, tq, 0, dev, with_lse, bufs, max_rows)
+    p = spec.c_problem()
+    with torch.cuda.device(dev):
+        _check(L.certkv_decode_mx(ctypes.byref(p), _tensor(q_new), int(tq), bufs.max_rows,
+                                  cache.c_cache(), _ptr(bufs.out), _ptr(bufs.lse), _ptr(bufs.ws),
+                                  bufs.ws_bytes, _stream(dev)), "certkv_decode_mx")
+    return (bufs.out, bufs.lse) if with_lse else bufs.out
+
+
+def decode_tree(spec: ProblemSpec, q_new, cache, tq, k_new, v_new, mask=None, with_lse=False,
+                bufs=None, max_rows=0):
+    """Attention of tq drafted tokens per sequence (q_new [L][B*tq][Hq][d]) over the packed
+    cache and tn new rows per sequence (k_new, v_new [L][B*tn][H][d]): the tokens since the
+    compression, a tree of drafted ones.  cache: an MxCache, or (k_packed, v_packed,
+    packed_offsets) of a bf16 one.  mask [B][tq][tn] bool or uint8: the new rows that each
+    query sees; None: j <= tn - tq + t, the last tq rows being the queries' own.  Returns out
+    [L][B*tq][Hq][d] fp32 (and lse [L][B*tq][Hq] with_lse); a query that sees nothing is out 0,
+    lse -inf.  bufs: DecodeBuffers(..., tn=tn, fmt=format of the cache)."""
+    L = _lib.lib()
+    dev = q_new.device
+    _check_queries(spec, q_new, tq)
+    tn = k_new.shape[1] // spec.batch
+    for t in (k_new, v_new):
+        assert t.dtype == torch.bfloat16
+        assert tuple(t.shape) == (spec.layers, spec.batch * tn, spec.kv_heads, spec.head_dim)
+    if mask is not None:
+        assert mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous()
+        assert tuple(mask.shape) == (spec.batch, int(tq), tn)
+    if isinstance(cache, MxCache):
+        fmt, offsets, c = cache.format, cache.offsets, cache.c_cache()
+        assert cache.head_dim == spec.head_dim
+    else:
+        kp, vp, offsets = cache
+        assert kp.is_contiguous() and vp.is_contiguous() and kp.shape == vp.shape
+        assert kp.dtype == vp.dtype == torch.bfloat16 and kp.shape[1] == spec.head_dim
+        fmt = "bf16"
+        c = _lib.Cache(_format_code(fmt), kp.data_ptr(), vp.data_ptr(), None, None,
+                       offsets.data_ptr())
+    assert offsets.dtype == torch.int64 and offsets.numel() == spec.units + 1
+    bufs = _cache_buffers(spec, fmt, tq, tn, dev, with_lse, bufs, max_rows)
+    p = spec.c_problem()
+    with torch.cuda.device(dev):
+        _check(L.certkv_decode_tree(ctypes.byref(p), _tensor(q_new), int(tq), bufs.max_rows, c,
+                                    _tensor(k_new), _tensor(v_new), tn, _ptr(mask),
+                                    _ptr(bufs.out), _ptr(bufs.lse), _ptr(bufs.ws), bufs.ws_bytes,
+                                    _stream(dev)), "certkv_decode_tree")
+    return (bufs.out, bufs.lse) if with_lse else bufs.out
+
+
 class CompressBuffers:
-    """Preallocated outputs and workspace of the fused pass (reusable)."""
+    """Preallocated outputs and workspace of the fused pass (reusable); with fmt
+    ("mxfp8" or "mxfp4") the packed cache is an MxCache, `mx`, in place of
+    k_packed and v_packed, and shares pos_packed and packed_offsets."""
 
     def __init__(self, spec: ProblemSpec, n_keep, device, with_curves=False, with_perm=False,
-                 with_mask=False, with_lse=False):
+                 with_mask=False, with_lse=False, fmt=None):
         self.spec = spec
         self.n_keep = [int(x) for x in n_keep]
         H, D = spec.kv_heads, spec.head_dim
@@ -364,10 +544,15 @@ class CompressBuffers:
         self.k_star = torch.empty((U, D), dtype=torch.float32, device=device)
         self.v_star = torch.empty((U, D), dtype=torch.float32, device=device)
         self.tail_mass = torch.empty(U, dtype=torch.float64, device=device)
-        self.k_packed = torch.empty((rows, D), dtype=dt, device=device)
-        self.v_packed = torch.empty((rows, D), dtype=dt, device=device)
-        self.pos_packed = torch.empty(rows, dtype=torch.int32, device=device)
-        self.packed_offsets = torch.empty(U + 1, dtype=torch.int64, device=device)
+        self.mx = MxCache.empty(spec, rows, fmt, device) if fmt is not None else None
+        if self.mx is None:
+            self.k_packed = torch.empty((rows, D), dtype=dt, device=device)
+            self.v_packed = torch.empty((rows, D), dtype=dt, device=device)
+            self.pos_packed = torch.empty(rows, dtype=torch.int32, device=device)
+            self.packed_offsets = torch.empty(U + 1, dtype=torch.int64, device=device)
+        else:
+            self.k_packed = self.v_packed = None
+            self.pos_packed, self.packed_offsets = self.mx.pos, self.mx.offsets
         self.curves = torch.empty(shape, dtype=torch.float32, device=device) if with_curves else None
         self.perm = torch.empty(shape, dtype=torch.int32, device=device) if with_perm else None
         self.alloc_stats = torch.zeros((spec.layers * spec.batch, 3), dtype=torch.int64,
@@ -393,16 +578,29 @@ class CompressBuffers:
 
 
 def compress(spec: ProblemSpec, q_win, k, v, n_keep, alpha=0.2, steps=40, bufs=None,
-             with_curves=False, with_perm=False, with_mask=False, with_lse=False, lse_in=None):
-    """The whole pass; returns the CompressBuffers holding every output."""
+             with_curves=False, with_perm=False, with_mask=False, with_lse=False, lse_in=None,
+             fmt=None):
+    """The whole pass; returns the CompressBuffers holding every output.  fmt ("mxfp8" or
+    "mxfp4"): the packed cache in microscaled codes (bufs.mx)."""
     L = _lib.lib()
     dev = k.device
     if bufs is None:
         bufs = CompressBuffers(spec, n_keep, dev, with_curves=with_curves, with_perm=with_perm,
-                               with_mask=with_mask, with_lse=with_lse)
+                               with_mask=with_mask, with_lse=with_lse, fmt=fmt)
     if lse_in is not None:
         assert lse_in.dtype == torch.float32 and lse_in.is_contiguous()
         assert tuple(lse_in.shape) == _lse_shape(spec)
+    if fmt is not None:
+        assert bufs.mx is not None and bufs.mx.format == fmt
+    if bufs.mx is not None:
+        c = bufs.mx.c_cache()
+        with torch.cuda.device(dev):
+            _check(L.certkv_compress_mx(ctypes.byref(bufs._p), c.format, _tensor(q_win),
+                                        _tensor(k), _tensor(v), _ptr(lse_in), bufs._nk,
+                                        float(alpha), int(steps), ctypes.byref(bufs._out), c.k,
+                                        c.k_scales, c.v, c.v_scales, _ptr(bufs.ws), bufs.ws_bytes,
+                                        _stream(dev)), "certkv_compress_mx")
+        return bufs
     _check(L.certkv_compress(ctypes.byref(bufs._p), _tensor(q_win), _tensor(k), _tensor(v),
                              _ptr(lse_in), bufs._nk, float(alpha), int(steps),
                              ctypes.byref(bufs._out), _ptr(bufs.ws), bufs.ws_bytes, _stream(dev)),

@@ -6,6 +6,7 @@
 #include <string>
 #include <vector>
 
+#include "mx.h"
 #include "stages.h"
 
 namespace certkv {
@@ -996,20 +997,205 @@ certkv_status certkv_cluster_tail(const certkv_problem* p, certkv_tensor k, cert
   return CERTKV_OK;
 }
 
-certkv_status certkv_compress(const certkv_problem* p, certkv_tensor q_win, certkv_tensor k,
-                              certkv_tensor v, const float* lse_in, const int32_t* n_keep_host,
-                              double alpha, int32_t steps, const certkv_outputs* out, void* ws,
-                              size_t ws_bytes, void* stream) {
+// The outputs of a microscaled packed cache, and the launches that write them.
+struct MxOut {
+  int32_t format;
+  void* k_codes;
+  uint8_t* k_scales;
+  void* v_codes;
+  uint8_t* v_scales;
+};
+static certkv_status check_mx_out(const MxOut& o) {
+  if (o.format != CERTKV_CACHE_MXFP8 && o.format != CERTKV_CACHE_MXFP4) return CERTKV_EINVAL;
+  if (!o.k_codes || !o.k_scales || !o.v_codes || !o.v_scales) return CERTKV_EINVAL;
+  if (((uintptr_t)o.k_codes & 15u) || ((uintptr_t)o.v_codes & 15u)) return CERTKV_EINVAL;
+  if (((uintptr_t)o.k_scales & 3u) || ((uintptr_t)o.v_scales & 3u)) return CERTKV_EINVAL;
+  return CERTKV_OK;
+}
+static certkv_status do_compact_mx(const Plan& P, const MxOut& o, certkv_tensor k, certkv_tensor v,
+                                   const int64_t* kept_offsets, const int32_t* kept_idx,
+                                   const float* k_star, const float* v_star, int32_t* pos_packed,
+                                   int64_t* packed_offsets, hipStream_t s) {
+  CompactMxArgs a;
+  a.g = P.g;
+  a.dtype = P.dtype;
+  a.format = o.format;
+  a.k = k;
+  a.v = v;
+  a.kept_offsets = kept_offsets;
+  a.kept_idx = kept_idx;
+  a.k_star = k_star;
+  a.v_star = v_star;
+  a.k_codes = static_cast<uint8_t*>(o.k_codes);
+  a.k_scales = o.k_scales;
+  a.v_codes = static_cast<uint8_t*>(o.v_codes);
+  a.v_scales = o.v_scales;
+  a.pos_packed = pos_packed;
+  a.packed_offsets = packed_offsets;
+  for (int b0 = 0; b0 < P.g.B; b0 += kMaxSeq) {
+    SeqTab t;
+    memset(&t, 0, sizeof(t));
+    t.first = b0;
+    t.count = P.g.B - b0 < kMaxSeq ? P.g.B - b0 : kMaxSeq;
+    for (int i = 0; i < t.count; ++i) {
+      t.start[i] = P.cu[b0 + i];
+      t.len[i] = (int32_t)(P.cu[b0 + i + 1] - P.cu[b0 + i]);
+    }
+    TRY(run_compact_mx(a, t, s));
+  }
+  return CERTKV_OK;
+}
+
+certkv_status certkv_compact_mx(const certkv_problem* p, int32_t format, certkv_tensor k,
+                                certkv_tensor v, const int64_t* kept_offsets,
+                                const int32_t* kept_idx, const float* k_star,
+                                const float* v_star, void* k_codes, uint8_t* k_scales,
+                                void* v_codes, uint8_t* v_scales, int32_t* pos_packed,
+                                int64_t* packed_offsets, void* stream) {
+  Plan P;
+  TRY(make_plan(p, &P));
+  TRY(check_tensor(k, P));
+  TRY(check_tensor(v, P));
+  const MxOut o{format, k_codes, k_scales, v_codes, v_scales};
+  TRY(check_mx_out(o));
+  if (!kept_offsets || !kept_idx || !pos_packed || !packed_offsets) return CERTKV_EINVAL;
+  if (P.g.slot && (!k_star || !v_star)) return CERTKV_EINVAL;
+  if (((uintptr_t)k_star & 15u) || ((uintptr_t)v_star & 15u)) return CERTKV_EINVAL;
+  if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
+  return do_compact_mx(P, o, k, v, kept_offsets, kept_idx, k_star, v_star, pos_packed,
+                       packed_offsets, (hipStream_t)stream);
+}
+
+static certkv_status check_cache(const certkv_cache& c, bool scales_only) {
+  const bool mx = c.format == CERTKV_CACHE_MXFP8 || c.format == CERTKV_CACHE_MXFP4;
+  if (!mx && (scales_only || c.format != CERTKV_CACHE_BF16)) return CERTKV_EINVAL;
+  if (!c.k || !c.v || ((uintptr_t)c.k & 15u) || ((uintptr_t)c.v & 15u)) return CERTKV_EINVAL;
+  if (mx && (!c.k_scales || !c.v_scales || ((uintptr_t)c.k_scales & 3u) ||
+             ((uintptr_t)c.v_scales & 3u)))
+    return CERTKV_EINVAL;
+  return CERTKV_OK;
+}
+
+certkv_status certkv_read_mx(const certkv_problem* p, certkv_cache cache, int64_t first_row,
+                             int64_t rows, int32_t out_dtype, void* k_out, void* v_out,
+                             void* stream) {
+  Plan P;
+  TRY(make_plan(p, &P));
+  TRY(check_cache(cache, true));
+  if (out_dtype != CERTKV_BF16 && out_dtype != CERTKV_F32) return CERTKV_EUNSUPPORTED;
+  if (first_row < 0 || rows < 0 || first_row > INT32_MAX || rows > INT32_MAX) return CERTKV_EINVAL;
+  if ((rows > 0 && !k_out && !v_out) || ((uintptr_t)k_out & 15u) || ((uintptr_t)v_out & 15u))
+    return CERTKV_EINVAL;
+  if ((p->flags & CERTKV_DRY_RUN) || rows == 0) return CERTKV_OK;
+  const int64_t code = first_row * mx_row_bytes(cache.format, P.g.D);
+  const int64_t scale = first_row * (P.g.D / kMxBlock);
+  ReadMxArgs a;
+  a.format = cache.format;
+  a.f32 = out_dtype == CERTKV_F32;
+  a.items = rows * (P.g.D / 8);
+  a.k_codes = static_cast<const uint8_t*>(cache.k) + code;
+  a.k_scales = cache.k_scales + scale;
+  a.v_codes = static_cast<const uint8_t*>(cache.v) + code;
+  a.v_scales = cache.v_scales + scale;
+  a.k_out = k_out;
+  a.v_out = v_out;
+  return run_read_mx(a, (hipStream_t)stream);
+}
+
+// New rows of a query at most: their tiles are counted in 32 bits.
+constexpr int32_t kMaxNewRows = 65536;
+
+size_t certkv_decode_cache_workspace_size(const certkv_problem* p, int32_t format, int32_t tq,
+                                          int32_t tn, int32_t max_rows) {
+  Plan P;
+  if (make_plan(p, &P) != CERTKV_OK || tq < 1 || tn < 0 || tn > kMaxNewRows || max_rows < 0)
+    return 0;
+  if (format < CERTKV_CACHE_BF16 || format > CERTKV_CACHE_MXFP4) return 0;
+  return 256;
+}
+
+static certkv_status check_rows(const certkv_tensor& t) {
+  if (!t.ptr || ((uintptr_t)t.ptr & 15u)) return CERTKV_EINVAL;
+  if ((t.s_layer % 8) || (t.s_token % 8) || (t.s_head % 8)) return CERTKV_EINVAL;
+  if (t.s_layer < 0 || t.s_token < 0 || t.s_head < 0) return CERTKV_EINVAL;
+  return CERTKV_OK;
+}
+
+static certkv_status attend_impl(const certkv_problem* p, certkv_tensor q_new, int32_t tq,
+                                 int32_t max_rows, const certkv_cache& cache, certkv_tensor k_new,
+                                 certkv_tensor v_new, int32_t tn, const uint8_t* mask, float* out,
+                                 float* lse, void* ws, size_t ws_bytes, void* stream) {
+  Plan P;
+  TRY(make_plan(p, &P));
+  if (tq < 1 || max_rows < 0) return CERTKV_EINVAL;
+  if (P.dtype != CERTKV_BF16) return CERTKV_EUNSUPPORTED;
+  if ((int64_t)tq * P.g.G > 512) return CERTKV_EUNSUPPORTED;
+  TRY(check_rows(q_new));
+  if (!cache.offsets || !out) return CERTKV_EINVAL;
+  if (!ws) return CERTKV_EWORKSPACE;
+  if (((uintptr_t)ws & 255u) != 0) return CERTKV_EINVAL;
+  if (ws_bytes < certkv_decode_cache_workspace_size(p, cache.format, tq, tn, max_rows))
+    return CERTKV_EWORKSPACE;
+  if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
+  AttendArgs a;
+  a.g = P.g;
+  a.U = P.U;
+  a.tq = tq;
+  a.tn = tn;
+  a.cover = decode_rows_bound(P, max_rows);
+  a.q = q_new;
+  a.cache = cache;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.mask = mask;
+  a.out = out;
+  a.lse = lse;
+  return run_attend(a, (hipStream_t)stream);
+}
+
+certkv_status certkv_decode_mx(const certkv_problem* p, certkv_tensor q_new, int32_t tq,
+                               int32_t max_rows, certkv_cache cache, float* out, float* lse,
+                               void* ws, size_t ws_bytes, void* stream) {
+  TRY(check_cache(cache, true));
+  const certkv_tensor none{nullptr, 0, 0, 0};
+  return attend_impl(p, q_new, tq, max_rows, cache, none, none, 0, nullptr, out, lse, ws, ws_bytes,
+                     stream);
+}
+
+certkv_status certkv_decode_tree(const certkv_problem* p, certkv_tensor q_new, int32_t tq,
+                                 int32_t max_rows, certkv_cache cache, certkv_tensor k_new,
+                                 certkv_tensor v_new, int32_t tn, const uint8_t* mask, float* out,
+                                 float* lse, void* ws, size_t ws_bytes, void* stream) {
+  TRY(check_cache(cache, false));
+  TRY(check_rows(k_new));
+  TRY(check_rows(v_new));
+  if (tn < 1 || (!mask && tn < tq)) return CERTKV_EINVAL;
+  if (tn > kMaxNewRows) return CERTKV_EUNSUPPORTED;
+  return attend_impl(p, q_new, tq, max_rows, cache, k_new, v_new, tn, mask, out, lse, ws, ws_bytes,
+                     stream);
+}
+
+// The whole pass; mx: the packed cache in microscaled codes, or NULL.
+static certkv_status compress_impl(const certkv_problem* p, certkv_tensor q_win, certkv_tensor k,
+                                   certkv_tensor v, const float* lse_in,
+                                   const int32_t* n_keep_host, double alpha, int32_t steps,
+                                   const certkv_outputs* out, const MxOut* mx, void* ws,
+                                   size_t ws_bytes, void* stream) {
   Plan P;
   TRY(make_plan(p, &P));
   TRY(check_tensor(q_win, P));
   TRY(check_tensor(k, P));
   TRY(check_tensor(v, P));
   if (!out || !out->scores || !out->budgets || !out->kept_offsets || !out->kept_idx ||
-      !out->k_star || !out->v_star || !out->tail_mass || !out->k_packed || !out->v_packed ||
-      !out->pos_packed || !out->packed_offsets)
+      !out->k_star || !out->v_star || !out->tail_mass || !out->pos_packed || !out->packed_offsets)
     return CERTKV_EINVAL;
-  if (((uintptr_t)out->k_packed & 15u) || ((uintptr_t)out->v_packed & 15u)) return CERTKV_EINVAL;
+  if (mx) {
+    TRY(check_mx_out(*mx));
+    if (((uintptr_t)out->k_star & 15u) || ((uintptr_t)out->v_star & 15u)) return CERTKV_EINVAL;
+  } else {
+    if (!out->k_packed || !out->v_packed) return CERTKV_EINVAL;
+    if (((uintptr_t)out->k_packed & 15u) || ((uintptr_t)out->v_packed & 15u)) return CERTKV_EINVAL;
+  }
   if ((uintptr_t)out->kept_mask & 15u) return CERTKV_EINVAL;
   if (P.dtype == CERTKV_F32 && P.g.D != 64) return CERTKV_EUNSUPPORTED;
   TRY(check_budget(P, n_keep_host, alpha, steps));
@@ -1030,9 +1216,31 @@ certkv_status certkv_compress(const certkv_problem* p, certkv_tensor q_win, cert
   TRY(do_select(P, out->scores, w.keysA, pm, out->budgets, CERTKV_SELECT_BUDGET, 0.0,
                 out->kept_offsets, out->packed_offsets, out->kept_idx, cap, out->kept_mask, &w, s));
   TRY(do_tail(P, out->scores, k, v, out->kept_offsets, out->kept_idx, w.ksum, w.vsum, out->k_star,
-              out->v_star, out->tail_mass, out->k_packed, out->v_packed, out->pos_packed, true, true,
+              out->v_star, out->tail_mass, out->k_packed, out->v_packed, out->pos_packed, true, !mx,
               true, w, s));
+  if (mx)
+    TRY(do_compact_mx(P, *mx, k, v, out->kept_offsets, out->kept_idx, out->k_star, out->v_star,
+                      out->pos_packed, out->packed_offsets, s));
   return CERTKV_OK;
+}
+
+certkv_status certkv_compress(const certkv_problem* p, certkv_tensor q_win, certkv_tensor k,
+                              certkv_tensor v, const float* lse_in, const int32_t* n_keep_host,
+                              double alpha, int32_t steps, const certkv_outputs* out, void* ws,
+                              size_t ws_bytes, void* stream) {
+  return compress_impl(p, q_win, k, v, lse_in, n_keep_host, alpha, steps, out, nullptr, ws,
+                       ws_bytes, stream);
+}
+
+certkv_status certkv_compress_mx(const certkv_problem* p, int32_t format, certkv_tensor q_win,
+                                 certkv_tensor k, certkv_tensor v, const float* lse_in,
+                                 const int32_t* n_keep_host, double alpha, int32_t steps,
+                                 const certkv_outputs* out, void* k_codes, uint8_t* k_scales,
+                                 void* v_codes, uint8_t* v_scales, void* ws, size_t ws_bytes,
+                                 void* stream) {
+  const MxOut mx{format, k_codes, k_scales, v_codes, v_scales};
+  return compress_impl(p, q_win, k, v, lse_in, n_keep_host, alpha, steps, out, &mx, ws, ws_bytes,
+                       stream);
 }
 
 certkv_status certkv_profile_enable(int32_t enable) {

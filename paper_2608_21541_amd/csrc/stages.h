@@ -223,6 +223,54 @@ certkv_status run_decode(const DecodeArgs& a, hipStream_t s);
 DecodeChunks decode_chunks(int D, int tq, int G, int64_t cover_rows, int64_t rows);
 int64_t decode_partials(const DecodeChunks& c, int64_t U);  // partials of a call at most
 
+// The packed cache written in microscaled codes (see mx.h).
+struct CompactMxArgs {
+  Geo g;
+  int32_t dtype;
+  int32_t format;
+  certkv_tensor k, v;
+  const int64_t* kept_offsets;
+  const int32_t* kept_idx;
+  const float* k_star;          // [U][d] (not read without slot rows)
+  const float* v_star;
+  uint8_t* k_codes;             // [rows][d or d/2]
+  uint8_t* k_scales;            // [rows][d/32]
+  uint8_t* v_codes;
+  uint8_t* v_scales;
+  int32_t* pos_packed;
+  int64_t* packed_offsets;
+};
+certkv_status run_compact_mx(const CompactMxArgs& a, const SeqTab& st, hipStream_t s);
+
+struct ReadMxArgs {
+  int32_t format;
+  bool f32;                     // out: fp32, or bf16
+  int64_t items;                // of eight dims
+  const uint8_t* k_codes;
+  const uint8_t* k_scales;
+  const uint8_t* v_codes;
+  const uint8_t* v_scales;
+  void* k_out;                  // either may be NULL
+  void* v_out;
+};
+certkv_status run_read_mx(const ReadMxArgs& a, hipStream_t s);
+
+// Attention of new queries over a packed cache of any format and rows of their own.
+struct AttendArgs {
+  Geo g;
+  int64_t U;
+  int32_t tq;                   // new queries per sequence
+  int32_t tn;                   // new rows per sequence (0: none)
+  int64_t cover;                // rows of a segment that are attended
+  certkv_tensor q;              // [L][B*tq][Hq][d] bf16
+  certkv_cache cache;
+  certkv_tensor k_new, v_new;   // [L][B*tn][H][d] bf16
+  const uint8_t* mask;          // [B][tq][tn], or NULL: causal
+  float* out;                   // [L][B*tq][Hq][d]
+  float* lse;                   // optional [L][B*tq][Hq]
+};
+certkv_status run_attend(const AttendArgs& a, hipStream_t s);
+
 certkv_status run_packed_from_kept(int64_t U, int32_t slot, const int64_t* kept_offsets,
                                    int64_t* packed_offsets, hipStream_t s);
 }  // namespace certkv
