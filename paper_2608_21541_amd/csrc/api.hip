@@ -1105,13 +1105,37 @@ certkv_status certkv_read_mx(const certkv_problem* p, certkv_cache cache, int64_
 // New rows of a query at most: their tiles are counted in 32 bits.
 constexpr int32_t kMaxNewRows = 65536;
 
+// Attention's workspace: partials (output rows, then (max, sum) pairs), each 256-byte
+// aligned.
+struct AttendWs {
+  AttendChunks ck;
+  size_t ml_off, total;
+};
+static bool attend_ws_layout(const Plan& P, int32_t format, int32_t tq, int32_t tn,
+                             int32_t max_rows, AttendWs* w) {
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const int64_t bound = decode_rows_bound(P, max_rows);
+  int64_t rows = 0;  // of all segments: b_h <= n_b kept rows and the slot row
+  for (int b = 0; b < P.g.B; ++b) {
+    const int64_t n = P.cu[b + 1] - P.cu[b] + P.g.slot;
+    rows += n < bound ? n : bound;
+  }
+  if ((int64_t)tq * P.g.G > 512) return false;
+  if (!attend_chunks(format, P.g.D, tq, P.g.G, tn, rows * P.g.L * P.g.H, P.U, &w->ck)) return false;
+  const size_t part = (size_t)(w->ck.most + P.U) * w->ck.mp;
+  w->ml_off = up(part * (size_t)P.g.D * sizeof(float));
+  w->total = up(w->ml_off + part * sizeof(float2));
+  return true;
+}
+
 size_t certkv_decode_cache_workspace_size(const certkv_problem* p, int32_t format, int32_t tq,
                                           int32_t tn, int32_t max_rows) {
   Plan P;
   if (make_plan(p, &P) != CERTKV_OK || tq < 1 || tn < 0 || tn > kMaxNewRows || max_rows < 0)
     return 0;
   if (format < CERTKV_CACHE_BF16 || format > CERTKV_CACHE_MXFP4) return 0;
-  return 256;
+  AttendWs w;
+  return attend_ws_layout(P, format, tq, tn, max_rows, &w) ? w.total : 0;
 }
 
 static certkv_status check_rows(const certkv_tensor& t) {
@@ -1134,8 +1158,9 @@ static certkv_status attend_impl(const certkv_problem* p, certkv_tensor q_new, i
   if (!cache.offsets || !out) return CERTKV_EINVAL;
   if (!ws) return CERTKV_EWORKSPACE;
   if (((uintptr_t)ws & 255u) != 0) return CERTKV_EINVAL;
-  if (ws_bytes < certkv_decode_cache_workspace_size(p, cache.format, tq, tn, max_rows))
-    return CERTKV_EWORKSPACE;
+  AttendWs W;
+  if (!attend_ws_layout(P, cache.format, tq, tn, max_rows, &W)) return CERTKV_EUNSUPPORTED;
+  if (ws_bytes < W.total) return CERTKV_EWORKSPACE;
   if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
   AttendArgs a;
   a.g = P.g;
@@ -1143,11 +1168,14 @@ static certkv_status attend_impl(const certkv_problem* p, certkv_tensor q_new, i
   a.tq = tq;
   a.tn = tn;
   a.cover = decode_rows_bound(P, max_rows);
+  a.ck = W.ck;
   a.q = q_new;
   a.cache = cache;
   a.k_new = k_new;
   a.v_new = v_new;
   a.mask = mask;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + W.ml_off);
   a.out = out;
   a.lse = lse;
   return run_attend(a, (hipStream_t)stream);

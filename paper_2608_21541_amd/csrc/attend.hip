@@ -1,156 +1,148 @@
-// Attention of new queries over a packed cache of any format and new rows.
-//
-// For query row (t, head h G + g) of sequence b, over the unit's packed rows and the
-// sequence's new rows j that mask[b][t][j] admits:
-//   z_i = scale <q, k_i>,  out = sum_i softmax(z)_i v_i,  lse = log sum_i e^z_i,
-// with out = 0 and lse = -inf where no row is visible.
-//
-// A workgroup per (unit, query row): each wave takes 64 rows at a time, a row to a
-// lane for the dot products, dims to lanes for the weighted sum, with a running
-// maximum and sum; the four waves are joined in LDS.
-#include "mx.h"
-#include "stages.h"
+// Attention over a packed cache of any format: chunks, dispatch, and the partials joined.
+#include "attend.h"
 
 namespace certkv {
 
-// Dims 8 c .. 8 c + 7 of packed row r as floats.
-template <int D, int F>
-__device__ __forceinline__ void attend_load8(const void* codes, const uint8_t* scales, int64_t r,
-                                             int c, float x[8]) {
-  uint4 v;
-  if constexpr (F == CERTKV_CACHE_BF16) {
-    v = reinterpret_cast<const uint4*>(codes)[r * (D / 8) + c];
-  } else {
-    uint2 w = make_uint2(0u, 0u);
-    if constexpr (F == CERTKV_CACHE_MXFP8)
-      w = reinterpret_cast<const uint2*>(codes)[r * (D / 8) + c];
-    else
-      w.x = reinterpret_cast<const uint32_t*>(codes)[r * (D / 8) + c];
-    const uint32_t b = scales[r * (D / kMxBlock) + c / 4];
-    v = mx_decode8<F>(w, mx_scale(b == 255u ? 127u : b));
-    if (b == 255u) v = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
-  }
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = bf16_lo(w[i]);
-    x[2 * i + 1] = bf16_hi(w[i]);
-  }
+bool attend_chunks(int format, int D, int tq, int G, int tn, int64_t rows, int64_t U,
+                   AttendChunks* c) {
+  (void)format;
+  (void)D;
+  const int M = tq * G;
+  c->shape = M <= 16 ? kAtOne : M <= 32 ? kAtTwo : M <= 64 ? kAtFour : M <= 128 ? kAtEight : kAtSixteen;
+  const int held = 16 << c->shape;
+  c->qgroups = (M + held - 1) / held;
+  c->mp = c->qgroups * held;
+  c->parts = 256 * (c->shape == kAtSixteen ? 1 : 2);
+  const int64_t gap = 64 + (tn + 31) / 32 * 32;
+  const int64_t total = (rows + 31) / 32 * 32 + U * gap;
+  if (U > INT32_MAX || total > INT32_MAX) return false;
+  c->gap = (int32_t)gap;
+  const int64_t shortest = (total + kAtMinKeys - 1) / kAtMinKeys;
+  int64_t most = (total + kAtMaxKeys - 1) / kAtMaxKeys;
+  if (most < c->parts) most = c->parts;
+  if (most > shortest) most = shortest;
+  c->most = (int32_t)(most > 0 ? most : 1);
+  return true;
 }
 
-template <int D, int F>
-__global__ __launch_bounds__(256) void attend_kernel(
-    Geo g, int32_t tq, int32_t tn, int64_t cover, const uint16_t* __restrict__ qn, int64_t q_sl,
-    int64_t q_st, int64_t q_sh, certkv_cache cache, const uint16_t* __restrict__ kn, int64_t kn_sl,
-    int64_t kn_st, int64_t kn_sh, const uint16_t* __restrict__ vn, int64_t vn_sl, int64_t vn_st,
-    int64_t vn_sh, const uint8_t* __restrict__ mask, float* __restrict__ out,
-    float* __restrict__ lse) {
-  __shared__ float q_s[D];
-  __shared__ float o_s[4][D];
-  __shared__ float2 ml_s[4];
+constexpr int kAtJoinThreads = 256;
+
+// The partials of each (unit, query row) joined in row order: D / 4 threads fold one
+// row's, four in flight; S groups of them share the partials of a row (with few rows),
+// or take a row each (S = 1).
+template <int D, int S>
+__global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs a) {
+  constexpr int C4 = D / 4, GR = kAtJoinThreads / C4, RW = GR / S;
+  __shared__ float4 acc_s[GR][C4];
+  __shared__ float2 ml_s[GR];
+  const Geo& g = a.g;
   const int64_t u = blockIdx.x;
-  const int row = blockIdx.y;
+  const int grp = threadIdx.x / C4, c4 = threadIdx.x % C4;
+  const int row = blockIdx.y * RW + grp / S, sg = grp % S;
+  const int M = a.tq * g.G;
+  const int64_t* off = a.cache.offsets;
+  const int64_t base = off[0], full = off[u + 1] - off[u];
+  const AtCut cut = at_cut(a.ck, (uint32_t)(off[a.U] - base), a.U);
+  const uint32_t vs = at_place(off, base, u, a.ck.gap);
+  const uint32_t len = (uint32_t)min(full, a.cover);
+  // rows of the unit in the common order
+  const uint32_t used = a.tn ? at_up32(len) + (uint32_t)a.tn : len;
+  const uint32_t s0 = vs / cut.keys, nv = used ? (vs + used - 1) / cut.keys - s0 + 1 : 0;
+  if (full > a.cover && blockIdx.y == 0 && threadIdx.x == 0) report_range(g);
+  float m = -INFINITY, L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (row < M) {
+    const int64_t first = ((int64_t)s0 + u) * a.ck.mp + row;
+    constexpr int Q = 4;
+    for (uint32_t i0 = sg; i0 < nv; i0 += Q * S) {
+      float2 ml[Q];
+      float4 x[Q];
+#pragma unroll
+      for (int i = 0; i < Q; ++i) {
+        const int64_t pr = first + (int64_t)min(i0 + i * S, nv - 1) * a.ck.mp;
+        ml[i] = a.part_ml[pr];
+        x[i] = reinterpret_cast<const float4*>(a.part_o + pr * D)[c4];
+      }
+#pragma unroll
+      for (int i = 0; i < Q; ++i) {
+        if (i0 + i * S >= nv || (ml[i].x == -INFINITY && ml[i].y == 0.f)) continue;
+        const float mn = fmaxf(m, ml[i].x);
+        const float e = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        const float w = __builtin_amdgcn_exp2f(ml[i].x - mn);
+        m = mn;
+        L = fmaf(L, e, ml[i].y * w);
+        o.x = fmaf(o.x, e, x[i].x * w);
+        o.y = fmaf(o.y, e, x[i].y * w);
+        o.z = fmaf(o.z, e, x[i].z * w);
+        o.w = fmaf(o.w, e, x[i].w * w);
+      }
+    }
+  }
+  if constexpr (S > 1) {
+    acc_s[grp][c4] = o;
+    if (c4 == 0) ml_s[grp] = make_float2(m, L);
+    __syncthreads();
+    if (sg != 0) return;
+    float mx = m;
+#pragma unroll
+    for (int k = 1; k < S; ++k) mx = fmaxf(mx, ml_s[grp + k].x);
+    const float e = m == -INFINITY ? (L == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - mx);
+    L *= e;
+    o.x *= e, o.y *= e, o.z *= e, o.w *= e;
+#pragma unroll
+    for (int k = 1; k < S; ++k) {
+      const float2 ml = ml_s[grp + k];
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;
+      const float w = __builtin_amdgcn_exp2f(ml.x - mx);
+      const float4 x = acc_s[grp + k][c4];
+      L = fmaf(ml.y, w, L);
+      o.x = fmaf(x.x, w, o.x);
+      o.y = fmaf(x.y, w, o.y);
+      o.z = fmaf(x.z, w, o.z);
+      o.w = fmaf(x.w, w, o.w);
+    }
+    m = mx;
+  }
+  if (row >= M) return;
   const int h = (int)(u % g.H);
   const int64_t lb = u / g.H;
   const int b = (int)(lb % g.B);
   const int l = (int)(lb / g.B);
   const int t = row / g.G, gq = row % g.G;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t p0 = cache.offsets[u];
-  const int64_t full = cache.offsets[u + 1] - p0;
-  const int64_t len = full < cover ? full : cover;
-  if (full > cover && row == 0 && tid == 0) report_range(g);
-  if (tid < D)
-    q_s[tid] = bf16_to_f32(qn[l * q_sl + (int64_t)(b * tq + t) * q_st +
-                              (int64_t)(h * g.G + gq) * q_sh + tid]) * g.scale;
-  __syncthreads();
-  float m = -INFINITY, sum = 0.f, o[D / 64];
-  for (int i = 0; i < D / 64; ++i) o[i] = 0.f;
-  for (int64_t j0 = wave * 64; j0 < len + tn; j0 += 256) {
-    const int64_t j = j0 + lane;
-    float z = -INFINITY;
-    bool see = j < len;
-    const int64_t jn = j - len;
-    if (!see && jn < tn)
-      see = mask ? mask[((int64_t)b * tq + t) * tn + jn] != 0 : jn <= tn - tq + t;
-    if (see) {
-      z = 0.f;
-      for (int c = 0; c < D / 8; ++c) {
-        float x[8];
-        if (j < len)
-          attend_load8<D, F>(cache.k, cache.k_scales, p0 + j, c, x);
-        else
-          for (int e = 0; e < 8; ++e)
-            x[e] = bf16_to_f32(kn[l * kn_sl + (b * (int64_t)tn + jn) * kn_st + h * kn_sh + c * 8 + e]);
-        for (int e = 0; e < 8; ++e) z = fmaf(q_s[c * 8 + e], x[e], z);
-      }
-    }
-    const float mx = fmaxf(m, wave_max(z));
-    if (mx == -INFINITY && !__any(z != z)) continue;
-    const float a = m == -INFINITY ? 0.f : expf(m - mx), p = see ? expf(z - mx) : 0.f;
-    m = mx;
-    sum = sum * a + wave_sum(p);
-    for (int i = 0; i < D / 64; ++i) o[i] *= a;
-    for (int k = 0; k < 64; ++k) {
-      const float pk = __shfl(p, k, 64);
-      const int64_t jk = j0 + k;
-      if (!__shfl((int)see, k, 64)) continue;
-      for (int i = 0; i < D / 64; ++i) {
-        const int d = i * 64 + lane;
-        float v;
-        if (jk < len) {
-          float x[8];
-          attend_load8<D, F>(cache.v, cache.v_scales, p0 + jk, d / 8, x);
-          v = 0.f;
-          for (int e = 0; e < 8; ++e) v = (d & 7) == e ? x[e] : v;
-        } else {
-          v = bf16_to_f32(vn[l * vn_sl + (b * (int64_t)tn + jk - len) * vn_st + h * vn_sh + d]);
-        }
-        o[i] = fmaf(pk, v, o[i]);
-      }
-    }
+  const int64_t orow = ((int64_t)l * g.B * a.tq + (int64_t)b * a.tq + t) * (g.H * g.G) + h * g.G + gq;
+  const float inv = L == 0.f ? 0.f : 1.f / L;  // (nothing visible: out 0, lse -inf)
+  const float y[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+  bool fine = true;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    fine = fine && isfinite(y[i]);
+    a.out[orow * D + 4 * c4 + i] = y[i];
   }
-  for (int i = 0; i < D / 64; ++i) o_s[wave][i * 64 + lane] = o[i];
-  if (lane == 0) ml_s[wave] = make_float2(m, sum);
-  __syncthreads();
-  float mx = -INFINITY, tot = 0.f, x = 0.f;
-  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, ml_s[w].x);
-  for (int w = 0; w < 4; ++w) {
-    if (ml_s[w].y == 0.f) continue;
-    const float a = expf(ml_s[w].x - mx);
-    tot += ml_s[w].y * a;
-    if (tid < D) x += o_s[w][tid] * a;
-  }
-  if (tid >= D) return;
-  const int64_t orow = ((int64_t)l * g.B * tq + (int64_t)b * tq + t) * (g.H * g.G) + h * g.G + gq;
-  const float y = tot == 0.f ? 0.f : x / tot;
-  if (!isfinite(y)) report_nonfinite(g);
-  out[orow * D + tid] = y;
-  if (lse && tid == 0) lse[orow] = tot == 0.f ? -INFINITY : mx + logf(tot);
-}
-
-template <int D, int F>
-static certkv_status launch_attend(const AttendArgs& a, hipStream_t s) {
-  CERTKV_LAUNCH("attend", (attend_kernel<D, F>),
-                dim3((unsigned)a.U, (unsigned)(a.tq * a.g.G)), dim3(256), 0, s, a.g, a.tq, a.tn,
-                a.cover, static_cast<const uint16_t*>(a.q.ptr), a.q.s_layer, a.q.s_token,
-                a.q.s_head, a.cache, static_cast<const uint16_t*>(a.k_new.ptr), a.k_new.s_layer,
-                a.k_new.s_token, a.k_new.s_head, static_cast<const uint16_t*>(a.v_new.ptr),
-                a.v_new.s_layer, a.v_new.s_token, a.v_new.s_head, a.mask, a.out, a.lse);
-  return CERTKV_OK;
+  if (!fine) report_nonfinite(g);
+  if (a.lse && c4 == 0)
+    a.lse[orow] = L == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(L)) * kAtLn2;
 }
 
 template <int D>
-static certkv_status launch_attend_f(const AttendArgs& a, hipStream_t s) {
-  switch (a.cache.format) {
-    case CERTKV_CACHE_MXFP8: return launch_attend<D, CERTKV_CACHE_MXFP8>(a, s);
-    case CERTKV_CACHE_MXFP4: return launch_attend<D, CERTKV_CACHE_MXFP4>(a, s);
-    default: return launch_attend<D, CERTKV_CACHE_BF16>(a, s);
-  }
+static certkv_status launch_attend_join(const AttendArgs& a, hipStream_t s) {
+  constexpr int GR = kAtJoinThreads / (D / 4);
+  const int M = a.tq * a.g.G;
+  // (as for certkv_decode: the partials of few rows are dealt out, of many taken row by row)
+  if (a.U * M < 8192)
+    CERTKV_LAUNCH("attend_join", (attend_join_kernel<D, GR>), dim3((unsigned)a.U, (unsigned)M),
+                  dim3(kAtJoinThreads), 0, s, a);
+  else
+    CERTKV_LAUNCH("attend_join", (attend_join_kernel<D, 1>),
+                  dim3((unsigned)a.U, (unsigned)((M + GR - 1) / GR)), dim3(kAtJoinThreads), 0, s, a);
+  return CERTKV_OK;
 }
 
 certkv_status run_attend(const AttendArgs& a, hipStream_t s) {
-  return a.g.D == 128 ? launch_attend_f<128>(a, s) : launch_attend_f<64>(a, s);
+  const certkv_status st = a.cache.format == CERTKV_CACHE_MXFP8   ? run_attend_mxfp8(a, s)
+                           : a.cache.format == CERTKV_CACHE_MXFP4 ? run_attend_mxfp4(a, s)
+                                                                  : run_attend_bf16(a, s);
+  if (st != CERTKV_OK) return st;
+  return a.g.D == 128 ? launch_attend_join<128>(a, s) : launch_attend_join<64>(a, s);
 }
 
 }  // namespace certkv

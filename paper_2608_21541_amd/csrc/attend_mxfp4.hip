@@ -1,0 +1,11 @@
+// Attention over a packed cache of mxfp4 rows (the kernel is in attend.h).
+#include "attend.h"
+
+namespace certkv {
+
+certkv_status run_attend_mxfp4(const AttendArgs& a, hipStream_t s) {
+  return a.g.D == 128 ? launch_attend_d<CERTKV_CACHE_MXFP4, 128>(a, s)
+                      : launch_attend_d<CERTKV_CACHE_MXFP4, 64>(a, s);
+}
+
+}  // namespace certkv

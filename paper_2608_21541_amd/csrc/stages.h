@@ -255,6 +255,21 @@ struct ReadMxArgs {
 };
 certkv_status run_read_mx(const ReadMxArgs& a, hipStream_t s);
 
+// How the rows of a call are cut into chunks, and the workgroup's shape (attend.h).
+constexpr int kAtMinKeys = 128;    // shortest chunk, and the unit of its length
+constexpr int kAtMaxKeys = 16384;  // longest: a bound on how long an fp32 sum gets
+// Query rows of a workgroup: 16 and 32 of one wave (four waves take tiles in turn), 64 of
+// two (twice), 128 of four, 256 of eight.
+enum { kAtOne, kAtTwo, kAtFour, kAtEight, kAtSixteen };
+struct AttendChunks {
+  int32_t shape;
+  int32_t qgroups;              // workgroups of a chunk: by query rows
+  int32_t mp;                   // query rows of a partial, with padding
+  int32_t parts;                // chunks taken at once
+  int32_t most;                 // chunks the workspace has room for
+  int32_t gap;                  // rows between units' places beside their packed ones
+};
+
 // Attention of new queries over a packed cache of any format and rows of their own.
 struct AttendArgs {
   Geo g;
@@ -262,14 +277,23 @@ struct AttendArgs {
   int32_t tq;                   // new queries per sequence
   int32_t tn;                   // new rows per sequence (0: none)
   int64_t cover;                // rows of a segment that are attended
+  AttendChunks ck;
   certkv_tensor q;              // [L][B*tq][Hq][d] bf16
   certkv_cache cache;
   certkv_tensor k_new, v_new;   // [L][B*tn][H][d] bf16
   const uint8_t* mask;          // [B][tq][tn], or NULL: causal
+  float* part_o;                // [most + U][mp][d]
+  float2* part_ml;              // [most + U][mp]
   float* out;                   // [L][B*tq][Hq][d]
   float* lse;                   // optional [L][B*tq][Hq]
 };
 certkv_status run_attend(const AttendArgs& a, hipStream_t s);
+certkv_status run_attend_bf16(const AttendArgs& a, hipStream_t s);   // by format
+certkv_status run_attend_mxfp8(const AttendArgs& a, hipStream_t s);
+certkv_status run_attend_mxfp4(const AttendArgs& a, hipStream_t s);
+// rows: of all segments together, at most.  false: too many to count.
+bool attend_chunks(int format, int D, int tq, int G, int tn, int64_t rows, int64_t U,
+                   AttendChunks* c);
 
 certkv_status run_packed_from_kept(int64_t U, int32_t slot, const int64_t* kept_offsets,
                                    int64_t* packed_offsets, hipStream_t s);
