@@ -57,6 +57,15 @@ class ProblemSpec:
         return cu
 
     def c_problem(self):
+        # built anew when a field has changed (a call of a small problem would take longer
+        # to describe than to run)
+        key = (self.layers, self.kv_heads, self.group, self.head_dim, self.window,
+               tuple(self.seqlens), self.dtype, self.softmax_scale, self.causal, self.dry_run,
+               self.keep_window, self.statistic, self.allocator, self.slot,
+               self.status.data_ptr() if self.status is not None else None)
+        kept = self.__dict__.get("_c")
+        if kept is not None and kept[0] == key:
+            return kept[1]
         cu = self.cu_seqlens()
         self._cu = (ctypes.c_int64 * len(cu))(*cu)  # kept alive with the spec
         dt = _dtype_code(self.dtype)
@@ -68,10 +77,14 @@ class ProblemSpec:
             "lagrangian": 0, "uniform": _lib.CERTKV_ALLOC_UNIFORM,
             "greedy": _lib.CERTKV_ALLOC_GREEDY}[self.allocator] | (
             0 if self.slot else _lib.CERTKV_NO_SLOT)
-        st = self.status.data_ptr() if self.status is not None else None
-        return _lib.Problem(self.layers, self.batch, self.kv_heads, self.group, self.head_dim,
-                            self.window, ctypes.cast(self._cu, ctypes.POINTER(ctypes.c_int64)),
-                            dt, dt, float(self.softmax_scale), flags, st)
+        p = _lib.Problem(self.layers, self.batch, self.kv_heads, self.group, self.head_dim,
+                         self.window, ctypes.cast(self._cu, ctypes.POINTER(ctypes.c_int64)),
+                         dt, dt, float(self.softmax_scale), flags, key[-1])
+        self.__dict__["_c"] = (key, p)
+        return p
+
+    def __getstate__(self):  # (a copy describes itself anew)
+        return {k: v for k, v in self.__dict__.items() if k != "_c"}
 
 
 def _dtype_code(dt):
@@ -83,9 +96,10 @@ def _dtype_code(dt):
 
 
 def _tensor(t: torch.Tensor) -> _lib.Tensor:
-    if t.dim() != 4 or t.stride(3) != 1:
+    s = t.stride()
+    if len(s) != 4 or s[3] != 1:
         raise ValueError("expected a [layers][tokens][heads][head_dim] tensor with contiguous last dim")
-    return _lib.Tensor(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return _lib.Tensor(t.data_ptr(), s[0], s[1], s[2])
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -94,6 +108,19 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _stream(device):
     return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+
+
+def _run(dev, what, *args):
+    """The entry point `what` with args and the current stream of dev, dev being current."""
+    fn = getattr(_lib.lib(), what)
+    index = dev.index
+    if index is None:
+        raise ValueError(f"{what}: expected tensors on a GPU")
+    if index == torch.cuda.current_device():
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(index)), what)
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, torch._C._cuda_getCurrentRawStream(index)), what)
 
 
 def _check(st, what):
@@ -397,52 +424,57 @@ class MxCache:
         return self.k.shape[1] * (1 if self.format == "mxfp8" else 2)
 
     def c_cache(self):
-        for t in (self.k, self.k_scales, self.v, self.v_scales):
-            assert t.dtype == torch.uint8 and t.is_contiguous() and t.shape[0] == self.rows
-        assert self.v.shape == self.k.shape
-        assert self.k_scales.shape[1] == self.v_scales.shape[1] == self.head_dim // 32
-        return _lib.Cache(_format_code(self.format), self.k.data_ptr(), self.v.data_ptr(),
-                          self.k_scales.data_ptr(), self.v_scales.data_ptr(),
-                          self.offsets.data_ptr())
+        k, ks, v, vs = self.k, self.k_scales, self.v, self.v_scales
+        rows, wide = k.shape
+        scales = (rows, wide // (32 if self.format == "mxfp8" else 16))
+        assert v.shape == k.shape and ks.shape == scales and vs.shape == scales
+        assert k.dtype == v.dtype == ks.dtype == vs.dtype == torch.uint8
+        assert k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()
+        assert self.offsets.dtype == torch.int64 and self.offsets.is_contiguous()
+        return _lib.Cache(_format_code(self.format), k.data_ptr(), v.data_ptr(), ks.data_ptr(),
+                          vs.data_ptr(), self.offsets.data_ptr())
+
+
+_READ_SPECS = {}
 
 
 def compact_mx(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star, fmt, cache=None):
     """compact with the packed rows quantised as they are written: an MxCache of format fmt
     ("mxfp8" or "mxfp4"), `cache` if one is given (its rows past the last packed one are left
     as they are)."""
-    L = _lib.lib()
     dev = k.device
     if cache is None:
         rows = int(kept_offsets[-1].item()) + (spec.units if spec.slot else 0)
         cache = MxCache.empty(spec, rows, fmt, dev)
+    assert k.dtype == v.dtype == spec.dtype and k.device == v.device == cache.k.device
+    assert kept_offsets.dtype == torch.int64 and kept_idx.dtype == cache.pos.dtype == torch.int32
+    assert cache.offsets.numel() == kept_offsets.numel() == spec.units + 1
     assert cache.format == fmt and cache.pos is not None and cache.head_dim == spec.head_dim
-    p, c = spec.c_problem(), cache.c_cache()
-    with torch.cuda.device(dev):
-        _check(L.certkv_compact_mx(ctypes.byref(p), c.format, _tensor(k), _tensor(v),
-                                   _ptr(kept_offsets), _ptr(kept_idx), _ptr(k_star), _ptr(v_star),
-                                   c.k, c.k_scales, c.v, c.v_scales, _ptr(cache.pos),
-                                   _ptr(cache.offsets), _stream(dev)), "certkv_compact_mx")
+    c = cache.c_cache()
+    _run(dev, "certkv_compact_mx", ctypes.byref(spec.c_problem()), c.format, _tensor(k),
+         _tensor(v), kept_offsets.data_ptr(), kept_idx.data_ptr(), _ptr(k_star), _ptr(v_star), c.k,
+         c.k_scales, c.v, c.v_scales, cache.pos.data_ptr(), c.offsets)
     return cache
 
 
 def read_mx(cache: MxCache, dtype=torch.bfloat16, first_row=0, rows=None, out=None):
     """The values (k, v) [rows][d] of a cache's rows first_row .. first_row + rows - 1 (all
     from first_row on by default), exact in bf16 and fp32; out: the two tensors to write."""
-    L = _lib.lib()
-    dev = cache.k.device
-    d = cache.head_dim
-    n = cache.rows - first_row if rows is None else int(rows)
+    c = cache.c_cache()
+    n, d = cache.k.shape
+    d = d if cache.format == "mxfp8" else 2 * d
+    n = n - first_row if rows is None else int(rows)
     assert 0 <= first_row and 0 <= n and first_row + n <= cache.rows
     if out is None:
-        out = [torch.empty((n, d), dtype=dtype, device=dev) for _ in range(2)]
-    for t in out:
-        assert t.is_contiguous() and tuple(t.shape) == (n, d) and t.dtype == out[0].dtype
-    p = ProblemSpec(1, 1, 1, d, 1, [1]).c_problem()
-    with torch.cuda.device(dev):
-        _check(L.certkv_read_mx(ctypes.byref(p), cache.c_cache(), int(first_row), n,
-                                _dtype_code(out[0].dtype), _ptr(out[0]), _ptr(out[1]),
-                                _stream(dev)), "certkv_read_mx")
-    return out[0], out[1]
+        out = [torch.empty((n, d), dtype=dtype, device=cache.k.device) for _ in range(2)]
+    ko, vo = out
+    assert ko.shape == vo.shape == (n, d) and ko.dtype == vo.dtype
+    assert ko.is_contiguous() and vo.is_contiguous() and ko.device == vo.device == cache.k.device
+    if d not in _READ_SPECS:  # (of the problem only the row length is read)
+        _READ_SPECS[d] = ProblemSpec(1, 1, 1, d, 1, [1])
+    _run(cache.k.device, "certkv_read_mx", ctypes.byref(_READ_SPECS[d].c_problem()), c,
+         int(first_row), n, _dtype_code(ko.dtype), ko.data_ptr(), vo.data_ptr())
+    return ko, vo
 
 
 def decode_cache_workspace_size(spec: ProblemSpec, fmt: str, tq: int, tn: int = 0,
@@ -454,8 +486,8 @@ def decode_cache_workspace_size(spec: ProblemSpec, fmt: str, tq: int, tn: int = 
 
 def _check_queries(spec, q_new, tq):
     assert q_new.dtype == torch.bfloat16
-    assert tuple(q_new.shape) == (spec.layers, spec.batch * int(tq), spec.kv_heads * spec.group,
-                                  spec.head_dim)
+    assert q_new.shape == (spec.layers, spec.batch * int(tq), spec.kv_heads * spec.group,
+                           spec.head_dim)
 
 
 def _cache_buffers(spec, fmt, tq, tn, dev, with_lse, bufs, max_rows):
@@ -468,16 +500,14 @@ def _cache_buffers(spec, fmt, tq, tn, dev, with_lse, bufs, max_rows):
 def decode_mx(spec: ProblemSpec, q_new, cache: MxCache, tq, with_lse=False, bufs=None, max_rows=0):
     """decode over a microscaled packed cache: out [L][B*tq][Hq][d] fp32 (and the natural-log
     lse [L][B*tq][Hq] with_lse).  bufs: DecodeBuffers(..., fmt=cache.format)."""
-    L = _lib.lib()
     dev = q_new.device
     _check_queries(spec, q_new, tq)
     assert cache.head_dim == spec.head_dim and cache.offsets.numel() == spec.units + 1
+    assert cache.k.device == dev
     bufs = _cache_buffers(spec, cache.format, tq, 0, dev, with_lse, bufs, max_rows)
-    p = spec.c_problem()
-    with torch.cuda.device(dev):
-        _check(L.certkv_decode_mx(ctypes.byref(p), _tensor(q_new), int(tq), bufs.max_rows,
-                                  cache.c_cache(), _ptr(bufs.out), _ptr(bufs.lse), _ptr(bufs.ws),
-                                  bufs.ws_bytes, _stream(dev)), "certkv_decode_mx")
+    _run(dev, "certkv_decode_mx", ctypes.byref(spec.c_problem()), _tensor(q_new), bufs.tq,
+         bufs.max_rows, cache.c_cache(), bufs.out.data_ptr(), _ptr(bufs.lse), bufs.ws.data_ptr(),
+         bufs.ws_bytes)
     return (bufs.out, bufs.lse) if with_lse else bufs.out
 
 
@@ -490,16 +520,17 @@ def decode_tree(spec: ProblemSpec, q_new, cache, tq, k_new, v_new, mask=None, wi
     query sees; None: j <= tn - tq + t, the last tq rows being the queries' own.  Returns out
     [L][B*tq][Hq][d] fp32 (and lse [L][B*tq][Hq] with_lse); a query that sees nothing is out 0,
     lse -inf.  bufs: DecodeBuffers(..., tn=tn, fmt=format of the cache)."""
-    L = _lib.lib()
     dev = q_new.device
     _check_queries(spec, q_new, tq)
     tn = k_new.shape[1] // spec.batch
-    for t in (k_new, v_new):
-        assert t.dtype == torch.bfloat16
-        assert tuple(t.shape) == (spec.layers, spec.batch * tn, spec.kv_heads, spec.head_dim)
+    new = (spec.layers, spec.batch * tn, spec.kv_heads, spec.head_dim)
+    assert k_new.shape == new and v_new.shape == new
+    assert k_new.dtype == v_new.dtype == torch.bfloat16
+    assert k_new.device == v_new.device == dev
     if mask is not None:
+        assert mask.device == dev
         assert mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous()
-        assert tuple(mask.shape) == (spec.batch, int(tq), tn)
+        assert mask.shape == (spec.batch, int(tq), tn)
     if isinstance(cache, MxCache):
         fmt, offsets, c = cache.format, cache.offsets, cache.c_cache()
         assert cache.head_dim == spec.head_dim
@@ -511,13 +542,11 @@ def decode_tree(spec: ProblemSpec, q_new, cache, tq, k_new, v_new, mask=None, wi
         c = _lib.Cache(_format_code(fmt), kp.data_ptr(), vp.data_ptr(), None, None,
                        offsets.data_ptr())
     assert offsets.dtype == torch.int64 and offsets.numel() == spec.units + 1
+    assert offsets.device == dev
     bufs = _cache_buffers(spec, fmt, tq, tn, dev, with_lse, bufs, max_rows)
-    p = spec.c_problem()
-    with torch.cuda.device(dev):
-        _check(L.certkv_decode_tree(ctypes.byref(p), _tensor(q_new), int(tq), bufs.max_rows, c,
-                                    _tensor(k_new), _tensor(v_new), tn, _ptr(mask),
-                                    _ptr(bufs.out), _ptr(bufs.lse), _ptr(bufs.ws), bufs.ws_bytes,
-                                    _stream(dev)), "certkv_decode_tree")
+    _run(dev, "certkv_decode_tree", ctypes.byref(spec.c_problem()), _tensor(q_new), bufs.tq,
+         bufs.max_rows, c, _tensor(k_new), _tensor(v_new), tn, _ptr(mask), bufs.out.data_ptr(),
+         _ptr(bufs.lse), bufs.ws.data_ptr(), bufs.ws_bytes)
     return (bufs.out, bufs.lse) if with_lse else bufs.out
 
 
@@ -594,12 +623,10 @@ def compress(spec: ProblemSpec, q_win, k, v, n_keep, alpha=0.2, steps=40, bufs=N
         assert bufs.mx is not None and bufs.mx.format == fmt
     if bufs.mx is not None:
         c = bufs.mx.c_cache()
-        with torch.cuda.device(dev):
-            _check(L.certkv_compress_mx(ctypes.byref(bufs._p), c.format, _tensor(q_win),
-                                        _tensor(k), _tensor(v), _ptr(lse_in), bufs._nk,
-                                        float(alpha), int(steps), ctypes.byref(bufs._out), c.k,
-                                        c.k_scales, c.v, c.v_scales, _ptr(bufs.ws), bufs.ws_bytes,
-                                        _stream(dev)), "certkv_compress_mx")
+        _run(dev, "certkv_compress_mx", ctypes.byref(bufs._p), c.format, _tensor(q_win),
+             _tensor(k), _tensor(v), _ptr(lse_in), bufs._nk, float(alpha), int(steps),
+             ctypes.byref(bufs._out), c.k, c.k_scales, c.v, c.v_scales, _ptr(bufs.ws),
+             bufs.ws_bytes)
         return bufs
     _check(L.certkv_compress(ctypes.byref(bufs._p), _tensor(q_win), _tensor(k), _tensor(v),
                              _ptr(lse_in), bufs._nk, float(alpha), int(steps),
