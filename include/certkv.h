@@ -454,7 +454,8 @@ certkv_status certkv_decode_mx(const certkv_problem* p, certkv_tensor q_new, int
  * and, beside it, over tn new rows per sequence that each query sees or not: the
  * tokens since the compression, a tree of drafted tokens.
  *   q_new        [L][B*tq][Hq][d] bf16, tq * G <= 512
- *   k_new, v_new [L][B*tn][H][d] bf16, stride rules as for q_new; 1 <= tn <= 65536
+ *   k_new, v_new [L][B*tn][H][d] bf16, stride rules as for q_new; 1 <= tn <= 65536;
+ *                tn * s_token below 2^31 - 256 elements, else CERTKV_EUNSUPPORTED
  *   mask         [B][tq][tn] bytes: query t of sequence b sees new row j where
  *                mask[b][t][j] != 0 (for a tree: its ancestors and itself).
  *                NULL: j <= tn - tq + t, the last tq rows being the queries' own

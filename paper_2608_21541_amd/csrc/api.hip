@@ -1122,7 +1122,7 @@ static bool attend_ws_layout(const Plan& P, int32_t format, int32_t tq, int32_t 
   }
   if ((int64_t)tq * P.g.G > 512) return false;
   if (!attend_chunks(format, P.g.D, tq, P.g.G, tn, rows * P.g.L * P.g.H, P.U, &w->ck)) return false;
-  const size_t part = (size_t)(w->ck.most + P.U) * w->ck.mp;
+  const size_t part = (size_t)attend_partials(w->ck, P.U, tn) * w->ck.mp;
   w->ml_off = up(part * (size_t)P.g.D * sizeof(float));
   w->total = up(w->ml_off + part * sizeof(float2));
   return true;
@@ -1199,6 +1199,9 @@ certkv_status certkv_decode_tree(const certkv_problem* p, certkv_tensor q_new, i
   TRY(check_rows(v_new));
   if (tn < 1 || (!mask && tn < tq)) return CERTKV_EINVAL;
   if (tn > kMaxNewRows) return CERTKV_EUNSUPPORTED;
+  // the new rows of one (layer, head, sequence) are addressed with 32-bit byte offsets
+  for (const int64_t st : {k_new.s_token, v_new.s_token})
+    if (st > (int64_t)0x7FFFFF00 / tn) return CERTKV_EUNSUPPORTED;
   return attend_impl(p, q_new, tq, max_rows, cache, k_new, v_new, tn, mask, out, lse, ws, ws_bytes,
                      stream);
 }

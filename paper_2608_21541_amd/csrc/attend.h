@@ -38,32 +38,40 @@ typedef float at_f32x2 __attribute__((ext_vector_type(2)));
 typedef short at_s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) at_s16x4 at_lds_s16x4;
 
-constexpr int kAtTile = 32;
 constexpr float kAtLog2e = 1.4426950408889634f;
 constexpr float kAtLn2 = 0.6931471805599453f;
 constexpr float kAtSlack = 8.f;  // log2 growth of a row maximum absorbed without rescaling
 
-// How the rows of all units are laid out in one order and cut into chunks.  A unit
-// takes the tiles of its packed rows and, after them, those of its new rows, from
-// a place that follows from its first row alone (a sum over the units before would
-// need a pass): at least `gap` further per unit, so that tiles never straddle units
-// or formats.  The chunks are of equal length, one for each workgroup that is
-// resident at once; a chunk that crosses from one unit to the next is two pieces,
-// and a unit's gap also stands for what a piece costs beside its tiles.
+// The rows of all units in one order, cut into chunks of equal length, one for each
+// workgroup that is resident at once: the packed rows, each unit's from a place that
+// follows from its first row alone (a sum over the units before would need a pass), and
+// apart from them the new rows, tn of each unit.  Places are multiples of 32, so that no
+// tile straddles units; a unit's place is at least `gap` rows beyond the rows before it,
+// which stand for what a piece costs beside its tiles.  A chunk that crosses from one
+// unit to the next is two pieces.
 __device__ __forceinline__ uint32_t at_up32(uint32_t x) { return (x + 31u) & ~31u; }
 struct AtCut {
   uint32_t keys, total;
 };
-__device__ __forceinline__ AtCut at_cut(const AttendChunks& c, uint32_t rows, int64_t U) {
-  AtCut cut;
-  cut.total = at_up32(rows) + (uint32_t)U * (uint32_t)c.gap;
-  uint32_t k = (cut.total + (uint32_t)c.parts - 1u) / (uint32_t)c.parts;
-  k = min(max(k, (uint32_t)kAtMinKeys), (uint32_t)kAtMaxKeys);
+__device__ __forceinline__ AtCut at_cut(uint32_t total, uint32_t parts, uint32_t most,
+                                        uint32_t least) {
+  uint32_t k = (total + parts - 1u) / parts;
+  k = min(max(k, least), (uint32_t)kAtMaxKeys);
   // (more rows than the caller's bound allows for: longer chunks, so that the partials
   // stay within the workspace)
-  if (cut.total > (uint64_t)c.most * k) k = (cut.total + (uint32_t)c.most - 1u) / (uint32_t)c.most;
-  cut.keys = (k + kAtMinKeys - 1u) / kAtMinKeys * kAtMinKeys;
-  return cut;
+  if (total > (uint64_t)most * k) k = (total + most - 1u) / most;
+  return AtCut{(k + least - 1u) / least * least, total};
+}
+__device__ __forceinline__ uint32_t at_place(const int64_t* __restrict__ off, int64_t base,
+                                             int64_t u, int32_t gap) {
+  return at_up32((uint32_t)(off[u] - base)) + (uint32_t)u * (uint32_t)gap;
+}
+__device__ __forceinline__ AtCut at_cut_packed(const AttendArgs& a) {
+  return at_cut(at_place(a.cache.offsets, a.cache.offsets[0], a.U, a.ck.gap), a.ck.parts,
+                a.ck.most, kAtMinKeys);
+}
+__device__ __forceinline__ AtCut at_cut_new(const AttendArgs& a) {
+  return at_cut((uint32_t)a.U * at_up32((uint32_t)a.tn), a.ck.parts, a.ck.most_new, kAtTile);
 }
 
 // How a lane holds eight or more consecutive dims of a row in format F.
@@ -109,28 +117,34 @@ __device__ __forceinline__ uint32_t at_pack(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2){a, b}, at_bf16x2));
 }
 
-// LDS tiles: 32 rows of D bf16 in natural order, 16-byte chunks swizzled within a row.
-// Keys are read a chunk per lane, sixteen rows at a time; values by transposing reads,
-// eight rows of 32 bytes per half-wave: each spreads over all banks.
+// LDS tiles: 32 rows of D bf16 in natural order.  Keys are read a 16-byte chunk per
+// lane, sixteen rows at a time; values by transposing reads, eight rows of 32 bytes per
+// half-wave: rows padded by 16 and by 32 bytes spread either over all banks, and leave
+// every access at a constant distance from one address.
+template <int D>
+struct AtTile {
+  static constexpr int KROW = D / 8 + 1, VROW = D / 8 + 2;  // 16-byte chunks per row
+  static constexpr int K = kAtTile * KROW * 8, V = kAtTile * VROW * 8;  // bf16 elements
+};
 template <int D>
 __device__ __forceinline__ int at_key_chunk(int r, int c) {
-  return r * (D / 8) + (c ^ ((D == 128 ? r : (r >> 1)) & (D / 8 - 1)));
+  return r * AtTile<D>::KROW + c;
 }
 template <int D>
 __device__ __forceinline__ int at_value_chunk(int r, int c) {
-  return r * (D / 8) + (c ^ (2 * ((D == 128 ? r : (r >> 1)) & (D / 16 - 1))));
+  return r * AtTile<D>::VROW + c;
 }
 
-template <int F, int D, int NQ, int QT>
+template <int D, int NQ, int QT>
 struct AtShape {
   static constexpr int KS = NQ == 1 ? 4 : NQ == 2 ? 2 : 1;
   static constexpr int NT = 64 * NQ * KS;
-  static constexpr int TILE = kAtTile * D;            // bf16 elements of an LDS tile
   static constexpr int KT = NQ == 1 ? 0 : 2;          // key tiles of a group in LDS
   static constexpr int VT = NQ == 1 ? 1 : 2;          // value tiles
   static constexpr int ROW = D + 4;                   // floats of a joined output row
   static constexpr int JOIN = KS == 1 ? 0 : 2 * KS * NQ * 16 * ROW;  // bf16 elements
-  static constexpr int TILES = KS * (KT + VT) * TILE;
+  static constexpr int GROUP = KT * AtTile<D>::K + VT * AtTile<D>::V;  // bf16 elements
+  static constexpr int TILES = KS * GROUP;
   static constexpr int LDS = TILES > JOIN ? TILES : JOIN;
 };
 
@@ -205,12 +219,8 @@ __device__ __forceinline__ void at_values(AtAcc<D, QT>& a, const uint16_t* vt, c
 }
 
 
-// The unit whose place holds row r of the common order (at_cut), by a wave: 64 units'
-// ends per step.
-__device__ __forceinline__ uint32_t at_place(const int64_t* __restrict__ off, int64_t base,
-                                             int64_t u, int32_t gap) {
-  return at_up32((uint32_t)(off[u] - base)) + (uint32_t)u * (uint32_t)gap;
-}
+// The unit whose place holds row r of the packed rows' order, by a wave: 64 units' ends
+// per step.
 __device__ __forceinline__ int64_t at_find_unit(const int64_t* __restrict__ off, int64_t base,
                                                 int64_t U, int32_t gap, uint32_t r, int lane) {
   int64_t lo = 0, n = U;  // the answer is one of [lo, lo + n]
@@ -233,32 +243,27 @@ __device__ __forceinline__ bool at_bad8(uint4 x) {
   return bad;
 }
 
-template <int F, int D, int NQ, int QT>
-__global__ __launch_bounds__((AtShape<F, D, NQ, QT>::NT)) __attribute__((amdgpu_waves_per_eu(2)))
-void attend_kernel(AttendArgs a) {
-  using Shape = AtShape<F, D, NQ, QT>;
-  constexpr int KS = Shape::KS, NT = Shape::NT, TILE = Shape::TILE;
-  constexpr int RB = mx_row_bytes(F, D), BITS = F == CERTKV_CACHE_BF16 ? 16 : F == CERTKV_CACHE_MXFP8 ? 8 : 4;
+// The packed rows of the workgroup's chunks (F: their format), or the new rows (NEW, bf16).
+template <int F, int D, int NQ, int QT, bool NEW>
+__device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, float2* ml_s,
+                                            uint32_t* bad_s) {
+  using Shape = AtShape<D, NQ, QT>;
+  constexpr int KS = Shape::KS, NT = Shape::NT;
+  constexpr int BITS = F == CERTKV_CACHE_BF16 ? 16 : F == CERTKV_CACHE_MXFP8 ? 8 : 4;
   constexpr bool MX = F != CERTKV_CACHE_BF16;
+  constexpr int RB = mx_row_bytes(F, D);  // bytes of a row
   constexpr int KSTEP = D / 32;
   // keys read straight into operands (NQ = 1): lane (g, c) holds WK bytes of row c at a
   // time, EK dims, so that the four groups read 4 WK consecutive bytes
   constexpr int WK = 32 * RB / 128 >= 16 ? 16 : 8, EK = NQ == 1 ? WK * 8 / BITS : 8;
   constexpr int SK = EK / 8, NLK = KSTEP / SK;
-  // a row-major tile: W bytes of a lane, the tile in NL pieces of a wave; alone, a wave
+  // a row-major tile: W bytes of a lane, the tile in NLT pieces of a wave; alone, a wave
   // takes the values, in a group the waves take turns at the keys' and the values' pieces
   constexpr int TB = kAtTile * RB;
   constexpr int W = NQ == 1 || !MX || 2 * TB / (64 * 16) >= NQ ? 16
                     : F == CERTKV_CACHE_MXFP8 || 2 * TB / (64 * 8) >= NQ ? 8 : 4;
-  constexpr int EV = W * 8 / BITS, LPR = RB / W, NLT = TB / (64 * W);
+  constexpr int EV = W * 8 / BITS, LPR = RB / W, NLT = TB / (64 * W), RPL = 64 / LPR;
   constexpr int PER = NQ == 1 ? NLT : (2 * NLT + NQ - 1) / NQ;
-  // and of new rows, bf16 in 16-byte pieces
-  constexpr int LPRN = D / 8, NLN = kAtTile * D * 2 / 1024;
-  constexpr int PERN = NQ == 1 ? NLN : (2 * NLN + NQ - 1) / NQ;
-
-  __shared__ __align__(16) uint16_t lds[Shape::LDS];
-  __shared__ float2 ml_s[KS == 1 ? 1 : KS * NQ * 16];
-  __shared__ uint32_t bad_s[NQ == 1 ? 1 : 2 * KS * NQ];
 
   const Geo& gm = a.g;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -269,12 +274,11 @@ void attend_kernel(AttendArgs a) {
   const float c2 = gm.scale * kAtLog2e;
   const int64_t U = a.U;
   const int64_t* __restrict__ off = a.cache.offsets;
-  const int32_t gap = a.ck.gap;
-  const uint32_t tnp = at_up32((uint32_t)a.tn);
 
   // Query groups (more rows than a workgroup holds) of a chunk: eight workgroups apart, on
-  // the same XCD, whose L2 then serves all but the first.
-  const int wgx = blockIdx.x;
+  // the same XCD, whose L2 then serves all but the first.  New rows' chunks are dealt from
+  // the other end: with few of either no workgroup has both.
+  const int wgx = NEW ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
   const int qg = (wgx >> 3) % a.ck.qgroups;
   const uint32_t x0 = a.ck.qgroups == 1 ? wgx : (wgx >> 3) / a.ck.qgroups * 8 + (wgx & 7);
   const uint32_t xstep = gridDim.x / a.ck.qgroups;
@@ -282,44 +286,49 @@ void attend_kernel(AttendArgs a) {
   const bool active = row0 < M;
   auto kdim = [&](int ks) { return (ks / SK) * 4 * EK + g * EK + 8 * (ks % SK); };
 
-  uint16_t* const group_lds = lds + kg * (Shape::KT + Shape::VT) * TILE;
-  auto key_tile = [&](int buf) { return group_lds + buf * TILE; };
-  auto value_tile = [&](int buf) { return group_lds + (Shape::KT + (NQ == 1 ? 0 : buf)) * TILE; };
+  uint16_t* const group_lds = lds + kg * Shape::GROUP;
+  auto key_tile = [&](int buf) { return group_lds + buf * AtTile<D>::K; };
+  auto value_tile = [&](int buf) {
+    return group_lds + Shape::KT * AtTile<D>::K + (NQ == 1 ? 0 : buf) * AtTile<D>::V;
+  };
 
   const int64_t base = off[0];
-  const AtCut cut = at_cut(a.ck, (uint32_t)(off[U] - base), U);
+  const AtCut cut = NEW ? at_cut_new(a) : at_cut_packed(a);
+  const uint32_t tnp = at_up32((uint32_t)a.tn);
   const uint32_t nch = (cut.total + cut.keys - 1) / cut.keys;
   for (uint32_t x = x0; x < nch; x += xstep) {
     const uint32_t r0 = x * cut.keys, r1 = min(cut.total, r0 + cut.keys);
-    for (int64_t u = at_find_unit(off, base, U, gap, r0, lane); u < U; ++u) {
-      const uint32_t vs = at_place(off, base, u, gap);
+    int64_t u = NEW ? r0 / tnp : at_find_unit(off, base, U, a.ck.gap, r0, lane);
+    for (; u < U; ++u) {
+      const uint32_t vs = NEW ? (uint32_t)u * tnp : at_place(off, base, u, a.ck.gap);
       if (vs >= r1) break;
-      const int64_t p0 = off[u];
-      const uint32_t len = (uint32_t)min(off[u + 1] - p0, a.cover), pt = at_up32(len);
-      const uint32_t lo = max(r0, vs) - vs, hi = r1 - vs;
-      // the piece: packed rows [lo, lo + np), then new rows [n0, n0 + nn)
-      const int np = (int)min(hi, len) - (int)lo;
-      const uint32_t nlo = max(lo, pt) - pt, nhi = hi > pt ? min(hi - pt, (uint32_t)a.tn) : 0u;
-      const int nn = (int)nhi - (int)nlo;
-      if (np <= 0 && nn <= 0) continue;  // (only what lies between units)
-      const int ntp = np > 0 ? (np + 31) / 32 : 0, ntn = nn > 0 ? (nn + 31) / 32 : 0;
+      // the piece: rows [lo, lo + np) of the unit's
+      const int64_t p0 = NEW ? 0 : off[u];
+      const uint32_t len = NEW ? (uint32_t)a.tn : (uint32_t)min(off[u + 1] - p0, a.cover);
+      const uint32_t lo = max(r0, vs) - vs;
+      const int np = (int)min(r1 - vs, len) - (int)lo;
+      if (np <= 0) continue;  // (only what lies between units)
+      const int ntp = (np + kAtTile - 1) / kAtTile;
       const int h = (int)(u % gm.H);
       const int64_t lb = u / gm.H;
       const int b = (int)(lb % gm.B);
       const int l = (int)(lb / gm.B);
 
-      // packed rows of the piece (reads past them return zero)
-      const uint32_t rows = np > 0 ? np : 0;
+      // Its rows; reads past them return zero.  (New rows keep their strides; what lies past
+      // the last one is not used.)
       const int64_t at = p0 + lo;
-      const BufRsrc kr = make_rsrc(static_cast<const uint8_t*>(a.cache.k) + at * RB, rows * RB);
-      const BufRsrc vr = make_rsrc(static_cast<const uint8_t*>(a.cache.v) + at * RB, rows * RB);
-      const BufRsrc ksr = make_rsrc(a.cache.k_scales + (MX ? at * (D / 32) : 0), MX ? rows * (D / 32) : 0);
-      const BufRsrc vsr = make_rsrc(a.cache.v_scales + (MX ? at * (D / 32) : 0), MX ? rows * (D / 32) : 0);
-      // new rows of the unit
-      const uint16_t* kn = static_cast<const uint16_t*>(a.k_new.ptr) + l * a.k_new.s_layer +
-                           (int64_t)b * a.tn * a.k_new.s_token + h * a.k_new.s_head;
+      const uint32_t kst = NEW ? (uint32_t)a.k_new.s_token * 2u : RB;
+      const uint32_t vst = NEW ? (uint32_t)a.v_new.s_token * 2u : RB;
       const uint16_t* vn = static_cast<const uint16_t*>(a.v_new.ptr) + l * a.v_new.s_layer +
-                           (int64_t)b * a.tn * a.v_new.s_token + h * a.v_new.s_head;
+                           ((int64_t)b * a.tn + lo) * a.v_new.s_token + h * a.v_new.s_head;
+      const uint16_t* kn = static_cast<const uint16_t*>(a.k_new.ptr) + l * a.k_new.s_layer +
+                           ((int64_t)b * a.tn + lo) * a.k_new.s_token + h * a.k_new.s_head;
+      const BufRsrc kr = NEW ? make_rsrc(kn, (np - 1) * kst + RB)
+                             : make_rsrc(static_cast<const uint8_t*>(a.cache.k) + at * RB, np * RB);
+      const BufRsrc vr = NEW ? make_rsrc(vn, (np - 1) * vst + RB)
+                             : make_rsrc(static_cast<const uint8_t*>(a.cache.v) + at * RB, np * RB);
+      const BufRsrc ksr = make_rsrc(a.cache.k_scales + (MX ? at * (D / 32) : 0), MX ? np * (D / 32) : 0);
+      const BufRsrc vsr = make_rsrc(a.cache.v_scales + (MX ? at * (D / 32) : 0), MX ? np * (D / 32) : 0);
 
       AtAcc<D, QT> acc;
 #pragma unroll
@@ -345,8 +354,7 @@ void attend_kernel(AttendArgs a) {
         }
       };
 
-      // Scores of a tile whose keys' operands are kf(kb, ks), masked to `left` rows, or by
-      // the bits seen[qt] (of the lane's eight keys).
+      // Scores of a tile whose keys' operands are kf(kb, ks).
       auto scores = [&](auto kf, at_f32x4 s[QT][2]) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -362,48 +370,43 @@ void attend_kernel(AttendArgs a) {
           }
         }
       };
-      auto packed_weights = [&](at_f32x4 s[QT][2], int left, uint4 ph[QT], uint4 pl[QT]) {
-        if (left < kAtTile) {
-#pragma unroll
-          for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (16 * (i >> 2) + 4 * g + (i & 3) >= left) s[qt][i >> 2][i & 3] = -INFINITY;
-        }
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          float p[8];
-          at_softmax<D, QT, false>(acc, qt, s[qt], c2, ph[qt], pl[qt], p);
-        }
-      };
-      // Weights of new rows j0 .. j0 + 31, and their values added; `bad`: rows whose values
-      // are not all finite, zero in the tile, which reach only the queries that see them.
-      auto new_tile = [&](at_f32x4 s[QT][2], const uint16_t* vt, int j0, uint32_t bad) {
+      // The tile's weights from its scores and its values added.  Of the packed rows, those
+      // past the piece are masked; of new rows, those that a query does not see.  `bad`: new
+      // rows whose values are not all finite; they are zero in the tile and reach only the
+      // queries that see them.
+      auto finish = [&](at_f32x4 s[QT][2], const uint16_t* vt, int t, uint32_t bad) {
         uint4 ph[QT], pl[QT];
         float p[QT][8];
         uint32_t seen[QT];
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
-          const int row = row0 + qt * 16 + c, t = min(row, M - 1) / gm.G;
-          const uint8_t* mrow = a.mask + ((int64_t)b * a.tq + t) * a.tn;
-          seen[qt] = 0;
+          if constexpr (NEW) {
+            const int row = row0 + qt * 16 + c, tt = min(row, M - 1) / gm.G;
+            const uint8_t* mrow = a.mask + ((int64_t)b * a.tq + tt) * a.tn;
+            seen[qt] = 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int j = j0 + 16 * (i >> 2) + 4 * g + (i & 3);
-            bool see = j <= a.tn - a.tq + t;
-            if (a.mask) see = mrow[min(j, a.tn - 1)] != 0;
-            see = see && j < a.tn && row < M;
-            seen[qt] |= (uint32_t)see << i;
-            if (!see) s[qt][i >> 2][i & 3] = -INFINITY;
+            for (int i = 0; i < 8; ++i) {
+              const int j = (int)lo + t * kAtTile + 16 * (i >> 2) + 4 * g + (i & 3);
+              bool see = j <= a.tn - a.tq + tt;
+              if (a.mask) see = mrow[min(j, a.tn - 1)] != 0;
+              see = see && j < a.tn && row < M;
+              seen[qt] |= (uint32_t)see << i;
+              if (!see) s[qt][i >> 2][i & 3] = -INFINITY;
+            }
+          } else if (np - t * kAtTile < kAtTile) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (16 * (i >> 2) + 4 * g + (i & 3) >= np - t * kAtTile)
+                s[qt][i >> 2][i & 3] = -INFINITY;
           }
-          at_softmax<D, QT, true>(acc, qt, s[qt], c2, ph[qt], pl[qt], p[qt]);
+          at_softmax<D, QT, NEW>(acc, qt, s[qt], c2, ph[qt], pl[qt], p[qt]);
         }
         at_values<D, QT>(acc, vt, ph, pl, lane);
-        while (bad) {  // (rare)
+        while (NEW && bad) {  // (rare)
           const int r = __builtin_ctz(bad);
           bad &= bad - 1;
           const int i = 4 * (r >> 4) + (r & 3), src = ((r >> 2) & 3) * 16 + c;
-          const uint16_t* vrow = vn + (int64_t)min(j0 + r, a.tn - 1) * a.v_new.s_token;
+          const uint16_t* vrow = vn + (int64_t)(t * kAtTile + r) * a.v_new.s_token;
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) {
             float w = p[qt][0];
@@ -422,6 +425,21 @@ void attend_kernel(AttendArgs a) {
           }
         }
       };
+      // A lane's part of the tile's row r of new values: zero past the last row, and where the
+      // row holds a value that is not finite, whose rows' bits are returned.
+      auto finite_rows = [&](uint4& v, int t, int n) {
+        const bool past = t * kAtTile + n * RPL + lane / LPR >= np;
+        const uint64_t any = __ballot(!past && at_bad8(v));
+        const uint64_t own = any >> (lane / LPR * LPR) & ((1ull << LPR) - 1);
+        if (own || past) v = make_uint4(0u, 0u, 0u, 0u);
+        uint32_t bad = 0;
+        if (any) {
+#pragma unroll
+          for (int i = 0; i < RPL; ++i)
+            if (any >> (i * LPR) & ((1ull << LPR) - 1)) bad |= 1u << (n * RPL + i);
+        }
+        return bad;
+      };
 
       if constexpr (NQ == 1) {
         uint16_t* const vt = value_tile(0);
@@ -433,26 +451,29 @@ void attend_kernel(AttendArgs a) {
           for (int kb = 0; kb < 2; ++kb) {
             const uint32_t r = t * kAtTile + kb * 16 + c;
 #pragma unroll
-            for (int i = 0; i < NLK; ++i) kx[kb][i].load(kr, r * RB + g * WK + i * 4 * WK);
+            for (int i = 0; i < NLK; ++i) kx[kb][i].load(kr, r * kst + g * WK + i * 4 * WK);
             if constexpr (MX) ksc[kb] = D == 128 ? buf_load_u32(ksr, r * 4) : buf_load_u16(ksr, r * 2);
           }
         };
         auto load_values = [&](int t) {
 #pragma unroll
           for (int n = 0; n < PER; ++n) {
-            const uint32_t r = t * kAtTile + n * (64 / LPR) + lane / LPR;
-            vx[n].load(vr, r * RB + (lane % LPR) * W);
+            const uint32_t r = t * kAtTile + n * RPL + lane / LPR;
+            vx[n].load(vr, r * vst + (lane % LPR) * W);
             if constexpr (MX)
               vsc[n] = __builtin_amdgcn_raw_buffer_load_b8(
                   vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
           }
         };
-        if (kg < ntp) {
+        // (new rows of 128 dims beside two query tiles: registers for either keys or values)
+        constexpr bool AHEAD = !(NEW && D == 128 && QT == 2);
+        if (AHEAD && kg < ntp) {
           load_keys(kg);
           load_values(kg);
         }
         load_queries();
         for (int t = kg; t < ntp; t += KS) {
+          if (!AHEAD) load_keys(t);
           at_f32x4 s[QT][2];
           scores(
               [&](int kb, int ks) {
@@ -462,185 +483,95 @@ void attend_kernel(AttendArgs a) {
                 return at_bf16<F, WK>(kx[kb][i], ks % SK, f);
               },
               s);
-          if (t + KS < ntp) load_keys(t + KS);
+          if (AHEAD && t + KS < ntp) load_keys(t + KS);
+          if (!AHEAD) load_values(t);
+          uint32_t bad = 0;
 #pragma unroll
           for (int n = 0; n < PER; ++n) {
-            const int r = n * (64 / LPR) + lane / LPR;
+            const int r = n * RPL + lane / LPR;
             const float f = MX ? mx_scale(vsc[n]) : 1.f;
+            if constexpr (NEW) bad |= finite_rows(vx[n].x, t, n);
 #pragma unroll
             for (int e = 0; e < EV / 8; ++e)
               reinterpret_cast<uint4*>(vt)[at_value_chunk<D>(r, (lane % LPR) * (EV / 8) + e)] =
                   at_bf16<F, W>(vx[n], e, f);
           }
           __builtin_amdgcn_wave_barrier();
-          if (t + KS < ntp) load_values(t + KS);
-          uint4 ph[QT], pl[QT];
-          packed_weights(s, np - t * kAtTile, ph, pl);
-          at_values<D, QT>(acc, vt, ph, pl, lane);
-          __builtin_amdgcn_wave_barrier();
-        }
-        // the new rows go on where the packed ones' turn ended
-        for (int t = (kg - ntp % KS + KS) % KS; t < ntn; t += KS) {
-          const int j0 = (int)nlo + t * kAtTile;
-          uint4 kf[2][KSTEP], vf[NLN];
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb) {
-            const uint16_t* src = kn + (int64_t)min(j0 + kb * 16 + c, a.tn - 1) * a.k_new.s_token;
-#pragma unroll
-            for (int ks = 0; ks < KSTEP; ++ks)
-              kf[kb][ks] = *reinterpret_cast<const uint4*>(src + kdim(ks));
-          }
-#pragma unroll
-          for (int n = 0; n < NLN; ++n) {
-            const int r = n * (64 / LPRN) + lane / LPRN;
-            vf[n] = *reinterpret_cast<const uint4*>(
-                vn + (int64_t)min(j0 + r, a.tn - 1) * a.v_new.s_token + (lane % LPRN) * 8);
-          }
-          at_f32x4 s[QT][2];
-          scores([&](int kb, int ks) { return kf[kb][ks]; }, s);
-          uint32_t bad = 0;
-#pragma unroll
-          for (int n = 0; n < NLN; ++n) {
-            const int r = n * (64 / LPRN) + lane / LPRN;
-            const uint64_t any = __ballot(j0 + r < a.tn && at_bad8(vf[n]));
-            const uint64_t own = any >> (lane / LPRN * LPRN) & ((1ull << LPRN) - 1);
-            if (own || j0 + r >= a.tn) vf[n] = make_uint4(0u, 0u, 0u, 0u);
-            if (any) {
-#pragma unroll
-              for (int i = 0; i < 64 / LPRN; ++i)
-                if (any >> (i * LPRN) & ((1ull << LPRN) - 1)) bad |= 1u << (n * (64 / LPRN) + i);
-            }
-            reinterpret_cast<uint4*>(vt)[at_value_chunk<D>(r, lane % LPRN)] = vf[n];
-          }
-          __builtin_amdgcn_wave_barrier();
-          new_tile(s, vt, j0, bad);
+          if (AHEAD && t + KS < ntp) load_values(t + KS);
+          finish(s, vt, t, bad);
           __builtin_amdgcn_wave_barrier();
         }
       } else {
         // A group's waves convert a tile together; while they compute with one pair of LDS
         // tiles, the next tile's share waits in registers or is written to the other.
-        auto lds_keys = [&](int buf) {
-          return [&, buf](int kb, int ks) {
-            return reinterpret_cast<const uint4*>(
-                key_tile(buf))[at_key_chunk<D>(kb * 16 + c, ks * 4 + g)];
-          };
+        AtRaw<F, W> raw[PER];
+        uint32_t sc[PER] = {};
+        auto load = [&](int t) {
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            const int n = qw + NQ * i;
+            if (n >= 2 * NLT) continue;
+            const uint32_t r = t * kAtTile + (n % NLT) * RPL + lane / LPR;
+            raw[i].load(n < NLT ? kr : vr, r * (n < NLT ? kst : vst) + (lane % LPR) * W);
+            if constexpr (MX)
+              sc[i] = __builtin_amdgcn_raw_buffer_load_b8(
+                  n < NLT ? ksr : vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
+          }
         };
-        {
-          AtRaw<F, W> raw[PER];
-          uint32_t sc[PER] = {};
-          auto load = [&](int t) {
+        auto store = [&](int t, int buf) {
+          uint32_t bad = 0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-              const int n = qw + NQ * i;
-              if (n >= 2 * NLT) continue;
-              const uint32_t r = t * kAtTile + (n % NLT) * (64 / LPR) + lane / LPR;
-              raw[i].load(n < NLT ? kr : vr, r * RB + (lane % LPR) * W);
-              if constexpr (MX)
-                sc[i] = __builtin_amdgcn_raw_buffer_load_b8(
-                    n < NLT ? ksr : vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
+          for (int i = 0; i < PER; ++i) {
+            const int n = qw + NQ * i;
+            if (n >= 2 * NLT) continue;
+            const int r = (n % NLT) * RPL + lane / LPR;
+            const float f = MX ? mx_scale(sc[i]) : 1.f;
+            if constexpr (NEW) {
+              if (n >= NLT) bad |= finite_rows(raw[i].x, t, n - NLT);
             }
-          };
-          auto store = [&](int buf) {
+            uint4* dst = reinterpret_cast<uint4*>(n < NLT ? key_tile(buf) : value_tile(buf));
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-              const int n = qw + NQ * i;
-              if (n >= 2 * NLT) continue;
-              const int r = (n % NLT) * (64 / LPR) + lane / LPR;
-              const float f = MX ? mx_scale(sc[i]) : 1.f;
-              uint4* dst = reinterpret_cast<uint4*>(n < NLT ? key_tile(buf) : value_tile(buf));
-#pragma unroll
-              for (int e = 0; e < EV / 8; ++e) {
-                const int ch = (lane % LPR) * (EV / 8) + e;
-                dst[n < NLT ? at_key_chunk<D>(r, ch) : at_value_chunk<D>(r, ch)] =
-                    at_bf16<F, W>(raw[i], e, f);
-              }
+            for (int e = 0; e < EV / 8; ++e) {
+              const int ch = (lane % LPR) * (EV / 8) + e;
+              dst[n < NLT ? at_key_chunk<D>(r, ch) : at_value_chunk<D>(r, ch)] =
+                  at_bf16<F, W>(raw[i], e, f);
             }
-          };
-          const int its = (ntp + KS - 1) / KS;
-          if (kg < ntp) load(kg);
-          load_queries();
-          if (kg < ntp) store(0);
-          if (kg + KS < ntp) load(kg + KS);
-          __syncthreads();
-          for (int it = 0; it < its; ++it) {
-            const int t = it * KS + kg;
-            if (t + KS < ntp) store((it + 1) & 1);
-            if (t + 2 * KS < ntp) load(t + 2 * KS);
-            if (active && t < ntp) {
-              at_f32x4 s[QT][2];
-              scores(lds_keys(it & 1), s);
-              uint4 ph[QT], pl[QT];
-              packed_weights(s, np - t * kAtTile, ph, pl);
-              at_values<D, QT>(acc, value_tile(it & 1), ph, pl, lane);
-            }
-            __syncthreads();
           }
-        }
-        if (ntn) {
-          uint4 raw[PERN];
-          auto load = [&](int t) {
-#pragma unroll
-            for (int i = 0; i < PERN; ++i) {
-              const int n = qw + NQ * i;
-              if (n >= 2 * NLN) continue;
-              const int r = (int)nlo + t * kAtTile + (n % NLN) * (64 / LPRN) + lane / LPRN;
-              raw[i] = *reinterpret_cast<const uint4*>(
-                  (n < NLN ? kn : vn) + (lane % LPRN) * 8 +
-                  (int64_t)min(r, a.tn - 1) * (n < NLN ? a.k_new.s_token : a.v_new.s_token));
-            }
-          };
-          auto store = [&](int t, int buf) {
+          if (NEW && lane == 0) bad_s[(buf * KS + kg) * NQ + qw] = bad;
+        };
+        const int its = (ntp + KS - 1) / KS;
+        if (kg < ntp) load(kg);
+        load_queries();
+        if (kg < ntp) store(kg, 0);
+        if (kg + KS < ntp) load(kg + KS);
+        __syncthreads();
+        for (int it = 0; it < its; ++it) {
+          const int t = it * KS + kg, buf = it & 1;
+          if (t + KS < ntp) store(t + KS, buf ^ 1);
+          if (t + 2 * KS < ntp) load(t + 2 * KS);
+          if (active && t < ntp) {
             uint32_t bad = 0;
+            if constexpr (NEW) {
 #pragma unroll
-            for (int i = 0; i < PERN; ++i) {
-              const int n = qw + NQ * i;
-              if (n >= 2 * NLN) continue;
-              const int r = (n % NLN) * (64 / LPRN) + lane / LPRN, ch = lane % LPRN;
-              if (n < NLN) {
-                reinterpret_cast<uint4*>(key_tile(buf))[at_key_chunk<D>(r, ch)] = raw[i];
-                continue;
-              }
-              const bool past = (int)nlo + t * kAtTile + r >= a.tn;
-              const uint64_t any = __ballot(!past && at_bad8(raw[i]));
-              const uint64_t own = any >> (lane / LPRN * LPRN) & ((1ull << LPRN) - 1);
-              if (own || past) raw[i] = make_uint4(0u, 0u, 0u, 0u);
-              if (any) {
-#pragma unroll
-                for (int k = 0; k < 64 / LPRN; ++k)
-                  if (any >> (k * LPRN) & ((1ull << LPRN) - 1))
-                    bad |= 1u << ((n - NLN) * (64 / LPRN) + k);
-              }
-              reinterpret_cast<uint4*>(value_tile(buf))[at_value_chunk<D>(r, ch)] = raw[i];
-            }
-            if (lane == 0) bad_s[(buf * KS + kg) * NQ + qw] = bad;
-          };
-          const int its = (ntn + KS - 1) / KS;
-          if (kg < ntn) load(kg);
-          if (ntp == 0) load_queries();
-          if (kg < ntn) store(kg, 0);
-          if (kg + KS < ntn) load(kg + KS);
-          __syncthreads();
-          for (int it = 0; it < its; ++it) {
-            const int t = it * KS + kg;
-            if (t + KS < ntn) store(t + KS, (it + 1) & 1);
-            if (t + 2 * KS < ntn) load(t + 2 * KS);
-            if (active && t < ntn) {
-              uint32_t bad = 0;
-#pragma unroll
-              for (int w = 0; w < NQ; ++w) bad |= bad_s[((it & 1) * KS + kg) * NQ + w];
+              for (int w = 0; w < NQ; ++w) bad |= bad_s[(buf * KS + kg) * NQ + w];
               bad = __builtin_amdgcn_readfirstlane(bad);
-              at_f32x4 s[QT][2];
-              scores(lds_keys(it & 1), s);
-              new_tile(s, value_tile(it & 1), (int)nlo + t * kAtTile, bad);
             }
-            __syncthreads();
+            at_f32x4 s[QT][2];
+            scores(
+                [&](int kb, int ks) {
+                  return reinterpret_cast<const uint4*>(
+                      key_tile(buf))[at_key_chunk<D>(kb * 16 + c, ks * 4 + g)];
+                },
+                s);
+            finish(s, value_tile(buf), t, bad);
           }
+          __syncthreads();
         }
       }
 
       // The piece's partial: (maximum, sum, unnormalized output) of each query row, the KS
       // groups joined in LDS.
-      const int64_t slot = (int64_t)x + u;
+      const int64_t slot = (NEW ? a.ck.most + U : 0) + x + u;
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
         float l_row = acc.l[qt];
@@ -705,23 +636,46 @@ void attend_kernel(AttendArgs a) {
   }
 }
 
-template <int F, int D, int NQ, int QT>
+// TREE: with new rows.
+template <int F, int D, int SHAPE, bool TREE>
+__global__ __launch_bounds__((64 * attend_wg_waves(SHAPE)))
+__attribute__((amdgpu_waves_per_eu(attend_waves(F, D, SHAPE, TREE)))) void attend_kernel(
+    AttendArgs a) {
+  constexpr int NQ = SHAPE <= kAtTwo ? 1 : SHAPE == kAtFour ? 2 : SHAPE == kAtEight ? 4 : 8;
+  constexpr int QT = SHAPE == kAtOne ? 1 : 2;
+  using Shape = AtShape<D, NQ, QT>;
+  static_assert(Shape::NT == 64 * attend_wg_waves(SHAPE), "the workgroup's waves");
+  __shared__ __align__(16) uint16_t lds[Shape::LDS];
+  __shared__ float2 ml_s[Shape::KS == 1 ? 1 : Shape::KS * NQ * 16];
+  __shared__ uint32_t bad_s[TREE && NQ > 1 ? 2 * Shape::KS * NQ : 1];
+  attend_rows<F, D, NQ, QT, false>(a, lds, ml_s, bad_s);
+  if constexpr (TREE) attend_rows<CERTKV_CACHE_BF16, D, NQ, QT, true>(a, lds, ml_s, bad_s);
+}
+
+template <int F, int D, int SHAPE>
 static certkv_status launch_attend(const AttendArgs& a, hipStream_t s) {
-  const int wgs = a.ck.most < a.ck.parts ? a.ck.most : a.ck.parts;
+  const int chunks = a.tn && a.ck.most_new > a.ck.most ? a.ck.most_new : a.ck.most;
+  const int wgs = chunks < a.ck.parts ? chunks : a.ck.parts;
   const int grid = a.ck.qgroups == 1 ? wgs : (wgs + 7) / 8 * 8 * a.ck.qgroups;
-  CERTKV_LAUNCH("attend", (attend_kernel<F, D, NQ, QT>), dim3(grid),
-                dim3(AtShape<F, D, NQ, QT>::NT), 0, s, a);
+  constexpr int NT = 64 * attend_wg_waves(SHAPE);
+  if constexpr (F != CERTKV_CACHE_BF16) {
+    if (a.tn == 0) {
+      CERTKV_LAUNCH("attend", (attend_kernel<F, D, SHAPE, false>), dim3(grid), dim3(NT), 0, s, a);
+      return CERTKV_OK;
+    }
+  }
+  CERTKV_LAUNCH("attend", (attend_kernel<F, D, SHAPE, true>), dim3(grid), dim3(NT), 0, s, a);
   return CERTKV_OK;
 }
 
 template <int F, int D>
 static certkv_status launch_attend_d(const AttendArgs& a, hipStream_t s) {
   switch (a.ck.shape) {
-    case kAtOne: return launch_attend<F, D, 1, 1>(a, s);
-    case kAtTwo: return launch_attend<F, D, 1, 2>(a, s);
-    case kAtFour: return launch_attend<F, D, 2, 2>(a, s);
-    case kAtEight: return launch_attend<F, D, 4, 2>(a, s);
-    default: return launch_attend<F, D, 8, 2>(a, s);
+    case kAtOne: return launch_attend<F, D, kAtOne>(a, s);
+    case kAtTwo: return launch_attend<F, D, kAtTwo>(a, s);
+    case kAtFour: return launch_attend<F, D, kAtFour>(a, s);
+    case kAtEight: return launch_attend<F, D, kAtEight>(a, s);
+    default: return launch_attend<F, D, kAtSixteen>(a, s);
   }
 }
 

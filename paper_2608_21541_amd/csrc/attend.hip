@@ -5,23 +5,26 @@ namespace certkv {
 
 bool attend_chunks(int format, int D, int tq, int G, int tn, int64_t rows, int64_t U,
                    AttendChunks* c) {
-  (void)format;
-  (void)D;
   const int M = tq * G;
   c->shape = M <= 16 ? kAtOne : M <= 32 ? kAtTwo : M <= 64 ? kAtFour : M <= 128 ? kAtEight : kAtSixteen;
   const int held = 16 << c->shape;
   c->qgroups = (M + held - 1) / held;
   c->mp = c->qgroups * held;
-  c->parts = 256 * (c->shape == kAtSixteen ? 1 : 2);
-  const int64_t gap = 64 + (tn + 31) / 32 * 32;
-  const int64_t total = (rows + 31) / 32 * 32 + U * gap;
-  if (U > INT32_MAX || total > INT32_MAX) return false;
-  c->gap = (int32_t)gap;
-  const int64_t shortest = (total + kAtMinKeys - 1) / kAtMinKeys;
-  int64_t most = (total + kAtMaxKeys - 1) / kAtMaxKeys;
-  if (most < c->parts) most = c->parts;
-  if (most > shortest) most = shortest;
-  c->most = (int32_t)(most > 0 ? most : 1);
+  // as many chunks as workgroups stay resident: 256 compute units of four SIMDs
+  c->parts = 256 * 4 * attend_waves(format, D, c->shape, tn > 0) / attend_wg_waves(c->shape);
+  if (c->shape == kAtFour && D == 128) c->parts = 512;  // (by LDS)
+  c->gap = 64;
+  auto chunks = [&](int64_t total, int64_t least) {
+    const int64_t shortest = (total + least - 1) / least;
+    int64_t most = (total + kAtMaxKeys - 1) / kAtMaxKeys;
+    if (most < c->parts) most = c->parts;
+    if (most > shortest) most = shortest;
+    return (int32_t)(most > 0 ? most : 1);
+  };
+  const int64_t total = (rows + 31) / 32 * 32 + U * c->gap, fresh = U * ((tn + 31) / 32 * 32);
+  if (U > INT32_MAX || total > INT32_MAX || fresh > INT32_MAX) return false;
+  c->most = chunks(total, kAtMinKeys);
+  c->most_new = chunks(fresh, kAtTile);
   return true;
 }
 
@@ -41,25 +44,19 @@ __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs 
   const int row = blockIdx.y * RW + grp / S, sg = grp % S;
   const int M = a.tq * g.G;
   const int64_t* off = a.cache.offsets;
-  const int64_t base = off[0], full = off[u + 1] - off[u];
-  const AtCut cut = at_cut(a.ck, (uint32_t)(off[a.U] - base), a.U);
-  const uint32_t vs = at_place(off, base, u, a.ck.gap);
-  const uint32_t len = (uint32_t)min(full, a.cover);
-  // rows of the unit in the common order
-  const uint32_t used = a.tn ? at_up32(len) + (uint32_t)a.tn : len;
-  const uint32_t s0 = vs / cut.keys, nv = used ? (vs + used - 1) / cut.keys - s0 + 1 : 0;
+  const int64_t full = off[u + 1] - off[u];
   if (full > a.cover && blockIdx.y == 0 && threadIdx.x == 0) report_range(g);
   float m = -INFINITY, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (row < M) {
-    const int64_t first = ((int64_t)s0 + u) * a.ck.mp + row;
+  // nv partials from `first` on
+  auto fold = [&](int64_t first, uint32_t nv) {
     constexpr int Q = 4;
     for (uint32_t i0 = sg; i0 < nv; i0 += Q * S) {
       float2 ml[Q];
       float4 x[Q];
 #pragma unroll
       for (int i = 0; i < Q; ++i) {
-        const int64_t pr = first + (int64_t)min(i0 + i * S, nv - 1) * a.ck.mp;
+        const int64_t pr = (first + min(i0 + i * S, nv - 1)) * a.ck.mp + row;
         ml[i] = a.part_ml[pr];
         x[i] = reinterpret_cast<const float4*>(a.part_o + pr * D)[c4];
       }
@@ -76,6 +73,17 @@ __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs 
         o.z = fmaf(o.z, e, x[i].z * w);
         o.w = fmaf(o.w, e, x[i].w * w);
       }
+    }
+  };
+  if (row < M) {
+    const AtCut cut = at_cut_packed(a);
+    const uint32_t vs = at_place(off, off[0], u, a.ck.gap), s0 = vs / cut.keys;
+    const uint32_t len = (uint32_t)min(full, a.cover);
+    fold((int64_t)s0 + u, len ? (vs + len - 1) / cut.keys - s0 + 1 : 0);
+    if (a.tn) {
+      const AtCut fresh = at_cut_new(a);
+      const uint32_t ns = (uint32_t)u * at_up32((uint32_t)a.tn), n0 = ns / fresh.keys;
+      fold(a.ck.most + a.U + n0 + u, (ns + a.tn - 1) / fresh.keys - n0 + 1);
     }
   }
   if constexpr (S > 1) {

@@ -256,17 +256,33 @@ struct ReadMxArgs {
 certkv_status run_read_mx(const ReadMxArgs& a, hipStream_t s);
 
 // How the rows of a call are cut into chunks, and the workgroup's shape (attend.h).
-constexpr int kAtMinKeys = 128;    // shortest chunk, and the unit of its length
+constexpr int kAtTile = 32;        // rows per tile
+constexpr int kAtMinKeys = 128;    // shortest chunk of packed rows, and the unit of its length
 constexpr int kAtMaxKeys = 16384;  // longest: a bound on how long an fp32 sum gets
 // Query rows of a workgroup: 16 and 32 of one wave (four waves take tiles in turn), 64 of
 // two (twice), 128 of four, 256 of eight.
 enum { kAtOne, kAtTwo, kAtFour, kAtEight, kAtSixteen };
+// Waves per SIMD that the kernel of a shape leaves registers for.
+constexpr int attend_waves(int format, int D, int shape, bool tree) {
+#ifdef ATW
+  return ATW;
+#else
+  if (D == 128)
+    return shape == kAtOne && !tree ? (format == CERTKV_CACHE_MXFP4 ? 4 : 3) : 2;
+  if (shape == kAtOne) return 4;
+  if (shape <= kAtFour) return tree ? 2 : 3;
+  return tree ? 3 : 4;
+#endif
+}
+// Waves of a workgroup.
+constexpr int attend_wg_waves(int shape) { return shape == kAtSixteen ? 8 : 4; }
 struct AttendChunks {
   int32_t shape;
   int32_t qgroups;              // workgroups of a chunk: by query rows
   int32_t mp;                   // query rows of a partial, with padding
   int32_t parts;                // chunks taken at once
-  int32_t most;                 // chunks the workspace has room for
+  int32_t most;                 // chunks of packed rows that the workspace has room for
+  int32_t most_new;             // and of new rows
   int32_t gap;                  // rows between units' places beside their packed ones
 };
 
@@ -282,11 +298,15 @@ struct AttendArgs {
   certkv_cache cache;
   certkv_tensor k_new, v_new;   // [L][B*tn][H][d] bf16
   const uint8_t* mask;          // [B][tq][tn], or NULL: causal
-  float* part_o;                // [most + U][mp][d]
-  float2* part_ml;              // [most + U][mp]
+  float* part_o;                // [attend_partials()][mp][d]: of packed rows, then of new rows
+  float2* part_ml;              // [attend_partials()][mp]
   float* out;                   // [L][B*tq][Hq][d]
   float* lse;                   // optional [L][B*tq][Hq]
 };
+// Partials of a call at most: a chunk has one, and one more for each unit that begins in it.
+inline int64_t attend_partials(const AttendChunks& c, int64_t U, int tn) {
+  return c.most + U + (tn ? c.most_new + U : 0);
+}
 certkv_status run_attend(const AttendArgs& a, hipStream_t s);
 certkv_status run_attend_bf16(const AttendArgs& a, hipStream_t s);   // by format
 certkv_status run_attend_mxfp8(const AttendArgs& a, hipStream_t s);
