@@ -9,8 +9,9 @@
 //   S^T = K Q^T on v_mfma_f32_16x16x32_bf16 with the keys as the A operand, so that
 //     lane (g, c) = (lane / 16, lane % 16) holds query c and keys 4 g + i and
 //     16 + 4 g + i (i = 0..3) of the tile;
-//   a running maximum and sum in log2 units, the maximum moved (and the sums
-//     rescaled) only when a row's grows by more than 2^8;
+//   a running sum in log2 units against a reference, the row's maximum when it was
+//     last moved: only when a weight exceeds 2^8 (and the sums are rescaled), so that
+//     no maximum is waited for between scores and weights;
 //   O^T += V^T P^T on the same instruction: P^T (the B operand) is the lane's own
 //     eight weights, as the bf16 of each and the bf16 of the remainder (16 bits of
 //     the fp32 weight: one bf16 alone would leave 2^-9), V^T (the A operand) comes from
@@ -40,7 +41,8 @@ typedef __attribute__((address_space(3))) at_s16x4 at_lds_s16x4;
 
 constexpr float kAtLog2e = 1.4426950408889634f;
 constexpr float kAtLn2 = 0.6931471805599453f;
-constexpr float kAtSlack = 8.f;  // log2 growth of a row maximum absorbed without rescaling
+constexpr float kAtMost = 256.f;   // a weight beyond it moves the row's reference
+constexpr float kAtNone = -3e38f;  // the reference of a row that has seen nothing
 
 // The rows of all units in one order, cut into chunks of equal length, one for each
 // workgroup that is resident at once: the packed rows, each unit's from a place that
@@ -139,8 +141,9 @@ template <int D, int NQ, int QT>
 struct AtShape {
   static constexpr int KS = NQ == 1 ? 4 : NQ == 2 ? 2 : 1;
   static constexpr int NT = 64 * NQ * KS;
-  static constexpr int KT = NQ == 1 ? 0 : 2;          // key tiles of a group in LDS
-  static constexpr int VT = NQ == 1 ? 1 : 2;          // value tiles
+  static constexpr int SUB = NQ == 1 ? 1 : 2;         // tiles that a group takes at a time
+  static constexpr int KT = NQ == 1 ? 0 : 2 * SUB;    // key tiles of a group in LDS
+  static constexpr int VT = NQ == 1 ? 1 : 2 * SUB;    // value tiles
   static constexpr int ROW = D + 4;                   // floats of a joined output row
   static constexpr int JOIN = KS == 1 ? 0 : 2 * KS * NQ * 16 * ROW;  // bf16 elements
   static constexpr int GROUP = KT * AtTile<D>::K + VT * AtTile<D>::V;  // bf16 elements
@@ -155,69 +158,88 @@ struct AtAcc {
   at_f32x4 o[QT][D / 16];
 };
 
-// Running maximum and weights of one query tile's scores s (raw products; c2 > 0 turns
-// them into log2 units), and the sums rescaled where a maximum has moved.
-template <int D, int QT, bool MASKED>
-__device__ __forceinline__ void at_softmax(AtAcc<D, QT>& a, int qt, const at_f32x4 s[2], float c2,
-                                           uint4& hi, uint4& lo, float p[8]) {
-  float mt = s[0][0];
+// Two weights (i even) of one query tile's scores s (raw products; c2 > 0 turns them into
+// log2 units) against the row's reference: the bf16 of each and of the remainder.  most:
+// the largest weight so far.
+template <int D, int QT>
+__device__ __forceinline__ void at_weights2(AtAcc<D, QT>& a, int qt, int i, const at_f32x4 s[2],
+                                            float c2, uint4& hi, uint4& lo, float p[8],
+                                            float& most) {
+  p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -a.m[qt]));
+  p[i + 1] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][(i + 1) & 3], c2, -a.m[qt]));
+  a.l[qt] += p[i] + p[i + 1];
+  most = fmaxf(most, fmaxf(p[i], p[i + 1]));
+  const uint32_t h = at_pack(p[i], p[i + 1]);
+  (&hi.x)[i >> 1] = h;
+  (&lo.x)[i >> 1] = at_pack(p[i] - __uint_as_float(h << 16), p[i + 1] - __uint_as_float(h & 0xffff0000u));
+  // (made here, not where they are used, after the reference has been looked at)
+  asm volatile("" : "+v"((&lo.x)[i >> 1]));
+}
+// Once the weights are there: where one is beyond 2^8, as in a row's first tile, the
+// references move to the maxima, the sums are rescaled and the weights made anew (l_old:
+// the sums before them).  Rows that have seen nothing keep kAtNone, under which a masked
+// score's weight is zero and any other's is infinite.
+template <int D, int QT>
+__device__ __forceinline__ void at_reference(AtAcc<D, QT>& a, const at_f32x4 s[QT][2], float c2,
+                                             const float l_old[QT], uint4 hi[QT], uint4 lo[QT],
+                                             float p[QT][8], float most) {
+  if (__builtin_amdgcn_ballot_w64(most > kAtMost) == 0) return;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) mt = fmaxf(mt, s[i >> 2][i & 3]);
-  mt *= c2;
-  if (__builtin_amdgcn_ballot_w64(mt > a.m[qt] + kAtSlack) != 0) {
+  for (int qt = 0; qt < QT; ++qt) {
+    float mt = s[qt][0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) mt = fmaxf(mt, s[qt][i >> 2][i & 3]);
+    mt *= c2;
     mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
     mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
     const float mnew = fmaxf(a.m[qt], mt);
-    // (a row that has seen nothing yet stays at -inf)
-    const float alpha = mnew == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.m[qt] - mnew);
+    const float alpha = __builtin_amdgcn_exp2f(a.m[qt] - mnew);
     a.m[qt] = mnew;
-    a.l[qt] *= alpha;
+    a.l[qt] = l_old[qt] * alpha;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) a.o[qt][db] *= alpha;
-  }
-  const float mref = MASKED && a.m[qt] == -INFINITY ? 0.f : a.m[qt];
-  uint32_t h[4], r[4];
 #pragma unroll
-  for (int i = 0; i < 8; i += 2) {
-    p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -mref));
-    p[i + 1] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][(i + 1) & 3], c2, -mref));
-    a.l[qt] += p[i] + p[i + 1];
-    h[i >> 1] = at_pack(p[i], p[i + 1]);
-    r[i >> 1] = at_pack(p[i] - __uint_as_float(h[i >> 1] << 16),
-                        p[i + 1] - __uint_as_float(h[i >> 1] & 0xffff0000u));
+    for (int i = 0; i < 8; i += 2)
+      at_weights2<D, QT>(a, qt, i, s[qt], c2, hi[qt], lo[qt], p[qt], most);
   }
-  hi = make_uint4(h[0], h[1], h[2], h[3]);
-  lo = make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// O^T += V^T P^T over the value tile at vt.
+// V^T of block db of 16 dims: lane c of group g is to hold dim c of the block at keys
+// 4 g + i, 16 + 4 g + i.  In a transposing read, lane c addresses key c / 4 of the four at
+// dims 4 (c % 4) .. + 3.
+template <int D>
+__device__ __forceinline__ at_bf16x8 at_value_block(const uint16_t* vt, int db, int lane) {
+  const int g = lane >> 4, c = lane & 15;
+  uint2 v[2];
+#pragma unroll
+  for (int rd = 0; rd < 2; ++rd) {
+    const int r = 16 * rd + 4 * g + (c >> 2), dim = 16 * db + 4 * (c & 3);
+    const uint16_t* src = vt + at_value_chunk<D>(r, dim >> 3) * 8 + (dim & 7);
+    v[rd] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (at_lds_s16x4*)(__attribute__((address_space(3))) uint16_t*)src));
+  }
+  return __builtin_bit_cast(at_bf16x8, make_uint4(v[0].x, v[0].y, v[1].x, v[1].y));
+}
+// O^T += V^T P^T of a block.
+template <int D, int QT>
+__device__ __forceinline__ void at_value_products(AtAcc<D, QT>& a, int db, at_bf16x8 vf,
+                                                  const uint4 hi[QT], const uint4 lo[QT]) {
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt)
+    a.o[qt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+        vf, __builtin_bit_cast(at_bf16x8, hi[qt]), a.o[qt][db], 0, 0, 0);
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt)
+    a.o[qt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+        vf, __builtin_bit_cast(at_bf16x8, lo[qt]), a.o[qt][db], 0, 0, 0);
+}
 template <int D, int QT>
 __device__ __forceinline__ void at_values(AtAcc<D, QT>& a, const uint16_t* vt, const uint4 hi[QT],
                                           const uint4 lo[QT], int lane) {
-  const int g = lane >> 4, c = lane & 15;
 #pragma unroll
-  for (int db = 0; db < D / 16; ++db) {
-    // lane c of group g is to hold dim c of the block at keys 4 g + i, 16 + 4 g + i: in a
-    // transposing read, lane c addresses key c / 4 of the four at dims 4 (c % 4) .. + 3
-    uint2 v[2];
-#pragma unroll
-    for (int rd = 0; rd < 2; ++rd) {
-      const int r = 16 * rd + 4 * g + (c >> 2), dim = 16 * db + 4 * (c & 3);
-      const uint16_t* src = vt + at_value_chunk<D>(r, dim >> 3) * 8 + (dim & 7);
-      v[rd] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (at_lds_s16x4*)(__attribute__((address_space(3))) uint16_t*)src));
-    }
-    const at_bf16x8 vf = __builtin_bit_cast(at_bf16x8, make_uint4(v[0].x, v[0].y, v[1].x, v[1].y));
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      a.o[qt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-          vf, __builtin_bit_cast(at_bf16x8, hi[qt]), a.o[qt][db], 0, 0, 0);
-      a.o[qt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-          vf, __builtin_bit_cast(at_bf16x8, lo[qt]), a.o[qt][db], 0, 0, 0);
-    }
-  }
+  for (int db = 0; db < D / 16; ++db)
+    at_value_products<D, QT>(a, db, at_value_block<D>(vt, db, lane), hi, lo);
 }
-
 
 // The unit whose place holds row r of the packed rows' order, by a wave: 64 units' ends
 // per step.
@@ -287,9 +309,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
   auto kdim = [&](int ks) { return (ks / SK) * 4 * EK + g * EK + 8 * (ks % SK); };
 
   uint16_t* const group_lds = lds + kg * Shape::GROUP;
-  auto key_tile = [&](int buf) { return group_lds + buf * AtTile<D>::K; };
-  auto value_tile = [&](int buf) {
-    return group_lds + Shape::KT * AtTile<D>::K + (NQ == 1 ? 0 : buf) * AtTile<D>::V;
+  auto key_tile = [&](int buf, int j) { return group_lds + (buf * Shape::SUB + j) * AtTile<D>::K; };
+  auto value_tile = [&](int buf, int j) {
+    return group_lds + Shape::KT * AtTile<D>::K + (buf * Shape::SUB + j) * AtTile<D>::V;
   };
 
   const int64_t base = off[0];
@@ -333,7 +355,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
       AtAcc<D, QT> acc;
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        acc.m[qt] = -INFINITY;
+        acc.m[qt] = kAtNone;
         acc.l[qt] = 0.f;
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) acc.o[qt][db] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
@@ -370,39 +392,38 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           }
         }
       };
-      // The tile's weights from its scores and its values added.  Of the packed rows, those
-      // past the piece are masked; of new rows, those that a query does not see.  `bad`: new
-      // rows whose values are not all finite; they are zero in the tile and reach only the
-      // queries that see them.
-      auto finish = [&](at_f32x4 s[QT][2], const uint16_t* vt, int t, uint32_t bad) {
-        uint4 ph[QT], pl[QT];
-        float p[QT][8];
-        uint32_t seen[QT];
+      // Scores masked: of the packed rows, those past the piece; of new rows, those that a
+      // query does not see (the others' bits: seen).
+      auto mask_scores = [&](at_f32x4 s[QT][2], int t, uint32_t seen[QT]) {
+        if constexpr (NEW) {
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          if constexpr (NEW) {
+          for (int qt = 0; qt < QT; ++qt) {
             const int row = row0 + qt * 16 + c, tt = min(row, M - 1) / gm.G;
             const uint8_t* mrow = a.mask + ((int64_t)b * a.tq + tt) * a.tn;
             seen[qt] = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              const int j = (int)lo + t * kAtTile + 16 * (i >> 2) + 4 * g + (i & 3);
+              const int r = t * kAtTile + 16 * (i >> 2) + 4 * g + (i & 3), j = (int)lo + r;
               bool see = j <= a.tn - a.tq + tt;
               if (a.mask) see = mrow[min(j, a.tn - 1)] != 0;
-              see = see && j < a.tn && row < M;
+              see = see && r < np && row < M;
               seen[qt] |= (uint32_t)see << i;
               if (!see) s[qt][i >> 2][i & 3] = -INFINITY;
             }
-          } else if (np - t * kAtTile < kAtTile) {
+          }
+        } else if (np - t * kAtTile < kAtTile) {
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               if (16 * (i >> 2) + 4 * g + (i & 3) >= np - t * kAtTile)
                 s[qt][i >> 2][i & 3] = -INFINITY;
-          }
-          at_softmax<D, QT, NEW>(acc, qt, s[qt], c2, ph[qt], pl[qt], p[qt]);
         }
-        at_values<D, QT>(acc, vt, ph, pl, lane);
-        while (NEW && bad) {  // (rare)
+      };
+      // New rows whose values are not all finite (rare) are zero in the tile; their bits are
+      // `bad`, and they reach only the queries that see them.
+      auto add_bad = [&](uint32_t bad, int t, const float p[QT][8], const uint32_t seen[QT]) {
+        while (bad) {
           const int r = __builtin_ctz(bad);
           bad &= bad - 1;
           const int i = 4 * (r >> 4) + (r & 3), src = ((r >> 2) & 3) * 16 + c;
@@ -442,7 +463,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
       };
 
       if constexpr (NQ == 1) {
-        uint16_t* const vt = value_tile(0);
+        uint16_t* const vt = value_tile(0, 0);
         AtRaw<F, WK> kx[2][NLK];
         AtRaw<F, W> vx[PER];
         uint32_t ksc[2] = {}, vsc[PER] = {};
@@ -498,73 +519,152 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           }
           __builtin_amdgcn_wave_barrier();
           if (AHEAD && t + KS < ntp) load_values(t + KS);
-          finish(s, vt, t, bad);
+          uint32_t seen[QT];
+          mask_scores(s, t, seen);
+          uint4 ph[QT], pl[QT];
+          float p[QT][8], l_old[QT], most = 0.f;
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) {
+            l_old[qt] = acc.l[qt];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2)
+              at_weights2<D, QT>(acc, qt, i, s[qt], c2, ph[qt], pl[qt], p[qt], most);
+          }
+          at_reference<D, QT>(acc, s, c2, l_old, ph, pl, p, most);
+          at_values<D, QT>(acc, vt, ph, pl, lane);
+          if constexpr (NEW) add_bad(bad, t, p, seen);
           __builtin_amdgcn_wave_barrier();
         }
       } else {
-        // A group's waves convert a tile together; while they compute with one pair of LDS
-        // tiles, the next tile's share waits in registers or is written to the other.
-        AtRaw<F, W> raw[PER];
-        uint32_t sc[PER] = {};
-        auto load = [&](int t) {
+        // A group's waves convert two tiles at a time together.  Tile after tile a wave
+        // multiplies the next one's keys while it turns the current scores into weights,
+        // then the current values while the keys after those are read; the group's next but
+        // one pair of key tiles and next pair of value tiles are written in between, and
+        // what follows those is on its way to registers.
+        constexpr int SUB = Shape::SUB;
+        AtRaw<F, W> raw[SUB][PER];
+        uint32_t sc[SUB][PER] = {};
+        auto load = [&](int t, bool keys, bool values) {  // keys of stage t + KS, values of t
 #pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            const int n = qw + NQ * i;
-            if (n >= 2 * NLT) continue;
-            const uint32_t r = t * kAtTile + (n % NLT) * RPL + lane / LPR;
-            raw[i].load(n < NLT ? kr : vr, r * (n < NLT ? kst : vst) + (lane % LPR) * W);
-            if constexpr (MX)
-              sc[i] = __builtin_amdgcn_raw_buffer_load_b8(
-                  n < NLT ? ksr : vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
+          for (int j = 0; j < SUB; ++j)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+              const int n = qw + NQ * i;
+              const bool key = n < NLT;
+              if (n >= 2 * NLT || !(key ? keys : values)) continue;
+              const uint32_t r = ((key ? t + KS : t) * SUB + j) * kAtTile + (n % NLT) * RPL + lane / LPR;
+              raw[j][i].load(key ? kr : vr, r * (key ? kst : vst) + (lane % LPR) * W);
+              if constexpr (MX)
+                sc[j][i] = __builtin_amdgcn_raw_buffer_load_b8(
+                    key ? ksr : vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
+            }
+        };
+        auto store = [&](int t, int buf, bool keys, bool values) {  // values to buf, keys to the other
+#pragma unroll
+          for (int j = 0; j < SUB; ++j) {
+            uint32_t bad = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+              const int n = qw + NQ * i;
+              const bool key = n < NLT;
+              if (n >= 2 * NLT || !(key ? keys : values)) continue;
+              const int r = (n % NLT) * RPL + lane / LPR;
+              const float f = MX ? mx_scale(sc[j][i]) : 1.f;
+              if constexpr (NEW) {
+                if (!key) bad |= finite_rows(raw[j][i].x, t * SUB + j, n - NLT);
+              }
+              uint4* dst = reinterpret_cast<uint4*>(key ? key_tile(buf ^ 1, j) : value_tile(buf, j));
+#pragma unroll
+              for (int e = 0; e < EV / 8; ++e) {
+                const int ch = (lane % LPR) * (EV / 8) + e;
+                dst[key ? at_key_chunk<D>(r, ch) : at_value_chunk<D>(r, ch)] =
+                    at_bf16<F, W>(raw[j][i], e, f);
+              }
+            }
+            if (NEW && values && lane == 0) bad_s[((buf * SUB + j) * KS + kg) * NQ + qw] = bad;
           }
         };
-        auto store = [&](int t, int buf) {
-          uint32_t bad = 0;
+        uint4 kf[2][KSTEP];
+        auto read_keys = [&](int buf, int j) {
 #pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            const int n = qw + NQ * i;
-            if (n >= 2 * NLT) continue;
-            const int r = (n % NLT) * RPL + lane / LPR;
-            const float f = MX ? mx_scale(sc[i]) : 1.f;
-            if constexpr (NEW) {
-              if (n >= NLT) bad |= finite_rows(raw[i].x, t, n - NLT);
-            }
-            uint4* dst = reinterpret_cast<uint4*>(n < NLT ? key_tile(buf) : value_tile(buf));
+          for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int e = 0; e < EV / 8; ++e) {
-              const int ch = (lane % LPR) * (EV / 8) + e;
-              dst[n < NLT ? at_key_chunk<D>(r, ch) : at_value_chunk<D>(r, ch)] =
-                  at_bf16<F, W>(raw[i], e, f);
-            }
-          }
-          if (NEW && lane == 0) bad_s[(buf * KS + kg) * NQ + qw] = bad;
+            for (int ks = 0; ks < KSTEP; ++ks)
+              kf[kb][ks] = reinterpret_cast<const uint4*>(
+                  key_tile(buf, j))[at_key_chunk<D>(kb * 16 + c, ks * 4 + g)];
         };
-        const int its = (ntp + KS - 1) / KS;
-        if (kg < ntp) load(kg);
+        const int its = (ntp + KS * SUB - 1) / (KS * SUB);
+        load(kg - KS, true, false);
         load_queries();
-        if (kg < ntp) store(kg, 0);
-        if (kg + KS < ntp) load(kg + KS);
+        store(kg - KS, 1, true, false);
+        load(kg, true, true);
+        __syncthreads();
+        at_f32x4 s[QT][2];
+        if (active) {
+          read_keys(0, 0);
+          scores([&](int kb, int ks) { return kf[kb][ks]; }, s);
+          read_keys(0, 1);
+        }
+        store(kg, 0, true, true);
+        load(kg + KS, true, true);
         __syncthreads();
         for (int it = 0; it < its; ++it) {
           const int t = it * KS + kg, buf = it & 1;
-          if (t + KS < ntp) store(t + KS, buf ^ 1);
-          if (t + 2 * KS < ntp) load(t + 2 * KS);
-          if (active && t < ntp) {
-            uint32_t bad = 0;
-            if constexpr (NEW) {
+          if (active && t * SUB < ntp) {
 #pragma unroll
-              for (int w = 0; w < NQ; ++w) bad |= bad_s[(buf * KS + kg) * NQ + w];
-              bad = __builtin_amdgcn_readfirstlane(bad);
+            for (int j = 0; j < SUB; ++j) {
+              uint32_t seen[QT], bad = 0;
+              mask_scores(s, t * SUB + j, seen);
+              if constexpr (NEW) {
+#pragma unroll
+                for (int w = 0; w < NQ; ++w) bad |= bad_s[((buf * SUB + j) * KS + kg) * NQ + w];
+                bad = __builtin_amdgcn_readfirstlane(bad);
+              }
+              at_f32x4 next[QT][2];
+              uint4 ph[QT], pl[QT];
+              float p[QT][8], l_old[QT], most = 0.f;
+              at_bf16x8 vf[3];
+#pragma unroll
+              for (int qt = 0; qt < QT; ++qt) {
+                next[qt][0] = next[qt][1] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
+                l_old[qt] = acc.l[qt];
+              }
+              // the matrix unit takes KSTEP / 2 products while the vector unit turns two scores
+              // into weights (the fences keep the compiler from taking them apart)
+#pragma unroll
+              for (int pr = 0; pr < 4 * QT; ++pr) {
+#pragma unroll
+                for (int m = pr * KSTEP / 2; m < (pr + 1) * KSTEP / 2; ++m) {
+                  const int ks = m / (2 * QT), kb = m / QT % 2, qt = m % QT;
+                  next[qt][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                      __builtin_bit_cast(at_bf16x8, kf[kb][ks]),
+                      __builtin_bit_cast(at_bf16x8, q[qt][ks]), next[qt][kb], 0, 0, 0);
+                }
+                const int qt = pr / 4;
+                at_weights2<D, QT>(acc, qt, 2 * (pr % 4), s[qt], c2, ph[qt], pl[qt], p[qt], most);
+                if (pr >= 4 * QT - 2)
+                  vf[pr - (4 * QT - 2)] = at_value_block<D>(value_tile(buf, j), pr - (4 * QT - 2), lane);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+              at_reference<D, QT>(acc, s, c2, l_old, ph, pl, p, most);
+              // and the values' products, their operands two blocks ahead
+#pragma unroll
+              for (int db = 0; db < D / 16; ++db) {
+                if (db + 2 < D / 16)
+                  vf[(db + 2) % 3] = at_value_block<D>(value_tile(buf, j), db + 2, lane);
+                if (db == D / 32) read_keys(buf ^ 1, j);
+                at_value_products<D, QT>(acc, db, vf[db % 3], ph, pl);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+              if constexpr (NEW) add_bad(bad, t * SUB + j, p, seen);
+#pragma unroll
+              for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) s[qt][kb] = next[qt][kb];
             }
-            at_f32x4 s[QT][2];
-            scores(
-                [&](int kb, int ks) {
-                  return reinterpret_cast<const uint4*>(
-                      key_tile(buf))[at_key_chunk<D>(kb * 16 + c, ks * 4 + g)];
-                },
-                s);
-            finish(s, value_tile(buf), t, bad);
           }
+          store(t + KS, buf ^ 1, true, true);
+          load(t + 2 * KS, true, true);
           __syncthreads();
         }
       }
@@ -593,10 +693,10 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           __syncthreads();  // every wave is done with its tiles (and with the tile before)
           if (g == 0) ml_s[wave * 16 + c] = make_float2(acc.m[qt], l_row);
           __syncthreads();
-          float mx = -INFINITY;
+          float mx = kAtNone;
 #pragma unroll
           for (int k = 0; k < KS; ++k) mx = fmaxf(mx, ml_s[(k * NQ + qw) * 16 + c].x);
-          const float w = acc.m[qt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(acc.m[qt] - mx);
+          const float w = __builtin_amdgcn_exp2f(acc.m[qt] - mx);
 #pragma unroll
           for (int db = 0; db < D / 16; ++db) {
             const at_f32x4 o = acc.o[qt][db];
@@ -618,13 +718,13 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
             const int64_t pr = slot * mp + row;
             reinterpret_cast<float4*>(a.part_o + pr * D)[d4] = o;
             if (d4 == 0) {
-              float mm = -INFINITY, sum = 0.f;
+              float mm = kAtNone, sum = 0.f;
 #pragma unroll
               for (int k = 0; k < KS; ++k) mm = fmaxf(mm, ml_s[k * NQ * 16 + r].x);
 #pragma unroll
               for (int k = 0; k < KS; ++k) {
                 const float2 ml = ml_s[k * NQ * 16 + r];
-                if (ml.x != -INFINITY || ml.y != 0.f) sum += ml.y * __builtin_amdgcn_exp2f(ml.x - mm);
+                sum += ml.y * __builtin_amdgcn_exp2f(ml.x - mm);
               }
               a.part_ml[pr] = make_float2(mm, sum);
             }
@@ -647,7 +747,7 @@ __attribute__((amdgpu_waves_per_eu(attend_waves(F, D, SHAPE, TREE)))) void atten
   static_assert(Shape::NT == 64 * attend_wg_waves(SHAPE), "the workgroup's waves");
   __shared__ __align__(16) uint16_t lds[Shape::LDS];
   __shared__ float2 ml_s[Shape::KS == 1 ? 1 : Shape::KS * NQ * 16];
-  __shared__ uint32_t bad_s[TREE && NQ > 1 ? 2 * Shape::KS * NQ : 1];
+  __shared__ uint32_t bad_s[TREE && NQ > 1 ? 2 * Shape::SUB * Shape::KS * NQ : 1];
   attend_rows<F, D, NQ, QT, false>(a, lds, ml_s, bad_s);
   if constexpr (TREE) attend_rows<CERTKV_CACHE_BF16, D, NQ, QT, true>(a, lds, ml_s, bad_s);
 }

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs 
   const int64_t* off = a.cache.offsets;
   const int64_t full = off[u + 1] - off[u];
   if (full > a.cover && blockIdx.y == 0 && threadIdx.x == 0) report_range(g);
-  float m = -INFINITY, L = 0.f;
+  float m = kAtNone, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   // nv partials from `first` on
   auto fold = [&](int64_t first, uint32_t nv) {
@@ -62,9 +62,9 @@ __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs 
       }
 #pragma unroll
       for (int i = 0; i < Q; ++i) {
-        if (i0 + i * S >= nv || (ml[i].x == -INFINITY && ml[i].y == 0.f)) continue;
+        if (i0 + i * S >= nv) continue;
         const float mn = fmaxf(m, ml[i].x);
-        const float e = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        const float e = __builtin_amdgcn_exp2f(m - mn);
         const float w = __builtin_amdgcn_exp2f(ml[i].x - mn);
         m = mn;
         L = fmaf(L, e, ml[i].y * w);
@@ -94,13 +94,12 @@ __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs 
     float mx = m;
 #pragma unroll
     for (int k = 1; k < S; ++k) mx = fmaxf(mx, ml_s[grp + k].x);
-    const float e = m == -INFINITY ? (L == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - mx);
+    const float e = __builtin_amdgcn_exp2f(m - mx);
     L *= e;
     o.x *= e, o.y *= e, o.z *= e, o.w *= e;
 #pragma unroll
     for (int k = 1; k < S; ++k) {
       const float2 ml = ml_s[grp + k];
-      if (ml.x == -INFINITY && ml.y == 0.f) continue;
       const float w = __builtin_amdgcn_exp2f(ml.x - mx);
       const float4 x = acc_s[grp + k][c4];
       L = fmaf(ml.y, w, L);
