@@ -544,54 +544,58 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
         constexpr int SUB = Shape::SUB;
         AtRaw<F, W> raw[SUB][PER];
         uint32_t sc[SUB][PER] = {};
-        auto load = [&](int t, bool keys, bool values) {  // keys of stage t + KS, values of t
+        auto load_piece = [&](int t, int j, int i, bool keys, bool values) {
+          const int n = qw + NQ * i;
+          const bool key = n < NLT;
+          if (n >= 2 * NLT || !(key ? keys : values)) return;
+          const uint32_t r = ((key ? t + KS : t) * SUB + j) * kAtTile + (n % NLT) * RPL + lane / LPR;
+          raw[j][i].load(key ? kr : vr, r * (key ? kst : vst) + (lane % LPR) * W);
+          if constexpr (MX)
+            sc[j][i] = __builtin_amdgcn_raw_buffer_load_b8(
+                key ? ksr : vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
+        };
+        auto store_piece = [&](int t, int buf, int j, int i, bool keys, bool values) {
+          uint32_t bad = 0;
+          const int n = qw + NQ * i;
+          const bool key = n < NLT;
+          if (n >= 2 * NLT || !(key ? keys : values)) return bad;
+          const int r = (n % NLT) * RPL + lane / LPR;
+          const float f = MX ? mx_scale(sc[j][i]) : 1.f;
+          if constexpr (NEW) {
+            if (!key) bad = finite_rows(raw[j][i].x, t * SUB + j, n - NLT);
+          }
+          uint4* dst = reinterpret_cast<uint4*>(key ? key_tile(buf ^ 1, j) : value_tile(buf, j));
+#pragma unroll
+          for (int e = 0; e < EV / 8; ++e) {
+            const int ch = (lane % LPR) * (EV / 8) + e;
+            dst[key ? at_key_chunk<D>(r, ch) : at_value_chunk<D>(r, ch)] =
+                at_bf16<F, W>(raw[j][i], e, f);
+          }
+          return bad;
+        };
+        // keys of stage t + KS and values of t
+        auto load = [&](int t, bool keys, bool values) {
 #pragma unroll
           for (int j = 0; j < SUB; ++j)
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-              const int n = qw + NQ * i;
-              const bool key = n < NLT;
-              if (n >= 2 * NLT || !(key ? keys : values)) continue;
-              const uint32_t r = ((key ? t + KS : t) * SUB + j) * kAtTile + (n % NLT) * RPL + lane / LPR;
-              raw[j][i].load(key ? kr : vr, r * (key ? kst : vst) + (lane % LPR) * W);
-              if constexpr (MX)
-                sc[j][i] = __builtin_amdgcn_raw_buffer_load_b8(
-                    key ? ksr : vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
-            }
+            for (int i = 0; i < PER; ++i) load_piece(t, j, i, keys, values);
         };
-        auto store = [&](int t, int buf, bool keys, bool values) {  // values to buf, keys to the other
+        // values to buf, keys to the other
+        auto store = [&](int t, int buf, bool keys, bool values) {
 #pragma unroll
           for (int j = 0; j < SUB; ++j) {
             uint32_t bad = 0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-              const int n = qw + NQ * i;
-              const bool key = n < NLT;
-              if (n >= 2 * NLT || !(key ? keys : values)) continue;
-              const int r = (n % NLT) * RPL + lane / LPR;
-              const float f = MX ? mx_scale(sc[j][i]) : 1.f;
-              if constexpr (NEW) {
-                if (!key) bad |= finite_rows(raw[j][i].x, t * SUB + j, n - NLT);
-              }
-              uint4* dst = reinterpret_cast<uint4*>(key ? key_tile(buf ^ 1, j) : value_tile(buf, j));
-#pragma unroll
-              for (int e = 0; e < EV / 8; ++e) {
-                const int ch = (lane % LPR) * (EV / 8) + e;
-                dst[key ? at_key_chunk<D>(r, ch) : at_value_chunk<D>(r, ch)] =
-                    at_bf16<F, W>(raw[j][i], e, f);
-              }
-            }
+            for (int i = 0; i < PER; ++i) bad |= store_piece(t, buf, j, i, keys, values);
             if (NEW && values && lane == 0) bad_s[((buf * SUB + j) * KS + kg) * NQ + qw] = bad;
           }
         };
         uint4 kf[2][KSTEP];
-        auto read_keys = [&](int buf, int j) {
+        auto read_keys = [&](int buf, int j, int kb) {
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int ks = 0; ks < KSTEP; ++ks)
-              kf[kb][ks] = reinterpret_cast<const uint4*>(
-                  key_tile(buf, j))[at_key_chunk<D>(kb * 16 + c, ks * 4 + g)];
+          for (int ks = 0; ks < KSTEP; ++ks)
+            kf[kb][ks] = reinterpret_cast<const uint4*>(
+                key_tile(buf, j))[at_key_chunk<D>(kb * 16 + c, ks * 4 + g)];
         };
         const int its = (ntp + KS * SUB - 1) / (KS * SUB);
         load(kg - KS, true, false);
@@ -601,9 +605,11 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
         __syncthreads();
         at_f32x4 s[QT][2];
         if (active) {
-          read_keys(0, 0);
+          read_keys(0, 0, 0);
+          read_keys(0, 0, 1);
           scores([&](int kb, int ks) { return kf[kb][ks]; }, s);
-          read_keys(0, 1);
+          read_keys(0, 1, 0);
+          read_keys(0, 1, 1);
         }
         store(kg, 0, true, true);
         load(kg + KS, true, true);
@@ -629,13 +635,15 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                 next[qt][0] = next[qt][1] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
                 l_old[qt] = acc.l[qt];
               }
-              // the matrix unit takes KSTEP / 2 products while the vector unit turns two scores
-              // into weights (the fences keep the compiler from taking them apart)
+              // The matrix unit takes KSTEP / 2 products while the vector unit turns two scores
+              // into weights (the fences keep the compiler from taking them apart); the keys
+              // are those of the tile after this one, read before the barrier that lets their
+              // buffer be written again.
 #pragma unroll
               for (int pr = 0; pr < 4 * QT; ++pr) {
 #pragma unroll
                 for (int m = pr * KSTEP / 2; m < (pr + 1) * KSTEP / 2; ++m) {
-                  const int ks = m / (2 * QT), kb = m / QT % 2, qt = m % QT;
+                  const int kb = m / (KSTEP * QT), ks = m / QT % KSTEP, qt = m % QT;
                   next[qt][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                       __builtin_bit_cast(at_bf16x8, kf[kb][ks]),
                       __builtin_bit_cast(at_bf16x8, q[qt][ks]), next[qt][kb], 0, 0, 0);
@@ -647,13 +655,22 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                 __builtin_amdgcn_sched_barrier(0);
               }
               at_reference<D, QT>(acc, s, c2, l_old, ph, pl, p, most);
-              // and the values' products, their operands two blocks ahead
+              // And the values' products, their operands two blocks ahead, while the wave's
+              // share of the tiles to come is converted.
 #pragma unroll
               for (int db = 0; db < D / 16; ++db) {
                 if (db + 2 < D / 16)
                   vf[(db + 2) % 3] = at_value_block<D>(value_tile(buf, j), db + 2, lane);
-                if (db == D / 32) read_keys(buf ^ 1, j);
+                if (db >= D / 16 - 2) read_keys(buf ^ 1, j, db - (D / 16 - 2));
                 at_value_products<D, QT>(acc, db, vf[db % 3], ph, pl);
+                if constexpr (!NEW) {
+#pragma unroll
+                  for (int i = 0; i < PER; ++i)
+                    if (db == i * (D / 16) / PER) {
+                      store_piece(t + KS, buf ^ 1, j, i, true, true);
+                      load_piece(t + 2 * KS, j, i, true, true);
+                    }
+                }
                 __builtin_amdgcn_sched_barrier(0);
               }
               if constexpr (NEW) add_bad(bad, t * SUB + j, p, seen);
@@ -663,8 +680,10 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                 for (int kb = 0; kb < 2; ++kb) s[qt][kb] = next[qt][kb];
             }
           }
-          store(t + KS, buf ^ 1, true, true);
-          load(t + 2 * KS, true, true);
+          if (NEW || !(active && t * SUB < ntp)) {
+            store(t + KS, buf ^ 1, true, true);
+            load(t + 2 * KS, true, true);
+          }
           __syncthreads();
         }
       }
