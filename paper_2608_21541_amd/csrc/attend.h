@@ -10,8 +10,7 @@
 //     lane (g, c) = (lane / 16, lane % 16) holds query c and keys 4 g + i and
 //     16 + 4 g + i (i = 0..3) of the tile;
 //   a running sum in log2 units against a reference, the row's maximum when it was
-//     last moved: only when a weight exceeds 2^8 (and the sums are rescaled), so that
-//     no maximum is waited for between scores and weights;
+//     last moved: only when a weight would exceed 2^8 (and the sums are rescaled);
 //   O^T += V^T P^T on the same instruction: P^T (the B operand) is the lane's own
 //     eight weights, as the bf16 of each and the bf16 of the remainder (16 bits of
 //     the fp32 weight: one bf16 alone would leave 2^-9), V^T (the A operand) comes from
@@ -19,11 +18,11 @@
 // Codes become bf16 values, exactly, on the way from memory to the matrix unit: a
 // conversion takes the block's scale as its operand (one instruction for two codes).
 //
-// A workgroup is NQ waves, each with QT query tiles, times KS groups that take the
-// tiles in turn.  Up to 32 query rows (NQ = 1) every wave is a group by itself and
-// reads keys straight into MFMA operands; only values pass through its LDS tile, and
-// no wave waits for another until the groups are joined at the end.  With more rows the waves of
-// a group convert a tile together, each its share, into one of two LDS buffers while
+// A workgroup is NQ waves, each with QT query tiles.  With up to 32 query rows (NQ = 1)
+// it is four such groups that take the tiles in turn (KS), every wave a group by itself:
+// it reads keys straight into MFMA operands, only values pass through its LDS tile, and
+// no wave waits for another until the groups are joined at the end.  With more rows its
+// waves convert the tiles together, each its share, into one pair of LDS buffers while
 // they work on the other.
 #pragma once
 
@@ -41,7 +40,7 @@ typedef __attribute__((address_space(3))) at_s16x4 at_lds_s16x4;
 
 constexpr float kAtLog2e = 1.4426950408889634f;
 constexpr float kAtLn2 = 0.6931471805599453f;
-constexpr float kAtMost = 256.f;   // a weight beyond it moves the row's reference
+constexpr float kAtSlack = 8.f;    // log2 of the weight beyond which a row's reference moves
 constexpr float kAtNone = -3e38f;  // the reference of a row that has seen nothing
 
 // The rows of all units in one order, cut into chunks of equal length, one for each
@@ -64,26 +63,27 @@ __device__ __forceinline__ AtCut at_cut(uint32_t total, uint32_t parts, uint32_t
   if (total > (uint64_t)most * k) k = (total + most - 1u) / most;
   return AtCut{(k + least - 1u) / least * least, total};
 }
-__device__ __forceinline__ uint32_t at_place(const int64_t* __restrict__ off, int64_t base,
-                                             int64_t u, int32_t gap) {
-  return at_up32((uint32_t)(off[u] - base)) + (uint32_t)u * (uint32_t)gap;
+__device__ __forceinline__ uint32_t at_place(int64_t rows_before, uint32_t u, int32_t gap) {
+  return at_up32((uint32_t)rows_before) + u * (uint32_t)gap;
 }
-__device__ __forceinline__ AtCut at_cut_packed(const AttendArgs& a) {
-  return at_cut(at_place(a.cache.offsets, a.cache.offsets[0], a.U, a.ck.gap), a.ck.parts,
-                a.ck.most, kAtMinKeys);
+__device__ __forceinline__ AtCut at_cut_packed(const AttendArgs& a, int64_t rows) {
+  return at_cut(at_place(rows, (uint32_t)a.U, a.ck.gap), a.ck.parts, a.ck.most, kAtMinKeys);
 }
 __device__ __forceinline__ AtCut at_cut_new(const AttendArgs& a) {
   return at_cut((uint32_t)a.U * at_up32((uint32_t)a.tn), a.ck.parts, a.ck.most_new, kAtTile);
 }
 
-// How a lane holds eight or more consecutive dims of a row in format F.
+// How a lane holds W bytes of a row in format F: eight or more consecutive dims.  NT:
+// loaded non-temporally.
+constexpr int kAtNT = 2;  // (the instruction's bit)
 template <int F, int W>
 struct AtRaw;
 template <int F>
 struct AtRaw<F, 16> {
   uint4 x;
+  template <bool NT>
   __device__ __forceinline__ void load(BufRsrc r, uint32_t off) {
-    const auto v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0);
+    const auto v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, NT ? kAtNT : 0);
     x = make_uint4(v[0], v[1], v[2], v[3]);
   }
   __device__ __forceinline__ uint2 codes8(int s) const {
@@ -94,7 +94,11 @@ struct AtRaw<F, 16> {
 template <int F>
 struct AtRaw<F, 8> {
   uint2 x;
-  __device__ __forceinline__ void load(BufRsrc r, uint32_t off) { x = buf_load_u64(r, off); }
+  template <bool NT>
+  __device__ __forceinline__ void load(BufRsrc r, uint32_t off) {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, 0, NT ? kAtNT : 0);
+    x = make_uint2(v[0], v[1]);
+  }
   __device__ __forceinline__ uint2 codes8(int s) const {
     return F == CERTKV_CACHE_MXFP8 ? x : make_uint2((&x.x)[s], 0u);
   }
@@ -102,7 +106,10 @@ struct AtRaw<F, 8> {
 template <int F>
 struct AtRaw<F, 4> {
   uint32_t x;
-  __device__ __forceinline__ void load(BufRsrc r, uint32_t off) { x = buf_load_u32(r, off); }
+  template <bool NT>
+  __device__ __forceinline__ void load(BufRsrc r, uint32_t off) {
+    x = __builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, NT ? kAtNT : 0);
+  }
   __device__ __forceinline__ uint2 codes8(int) const { return make_uint2(x, 0u); }
 };
 // Dims 8 s .. 8 s + 7 of a lane's piece as bf16.
@@ -139,7 +146,7 @@ __device__ __forceinline__ int at_value_chunk(int r, int c) {
 
 template <int D, int NQ, int QT>
 struct AtShape {
-  static constexpr int KS = NQ == 1 ? 4 : NQ == 2 ? 2 : 1;
+  static constexpr int KS = NQ == 1 ? 4 : 1;
   static constexpr int NT = 64 * NQ * KS;
   static constexpr int SUB = NQ == 1 ? 1 : 2;         // tiles that a group takes at a time
   static constexpr int KT = NQ == 1 ? 0 : 2 * SUB;    // key tiles of a group in LDS
@@ -158,50 +165,46 @@ struct AtAcc {
   at_f32x4 o[QT][D / 16];
 };
 
-// Two weights (i even) of one query tile's scores s (raw products; c2 > 0 turns them into
-// log2 units) against the row's reference: the bf16 of each and of the remainder.  most:
-// the largest weight so far.
-template <int D, int QT>
-__device__ __forceinline__ void at_weights2(AtAcc<D, QT>& a, int qt, int i, const at_f32x4 s[2],
-                                            float c2, uint4& hi, uint4& lo, float p[8],
-                                            float& most) {
-  p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -a.m[qt]));
-  p[i + 1] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][(i + 1) & 3], c2, -a.m[qt]));
-  a.l[qt] += p[i] + p[i + 1];
-  most = fmaxf(most, fmaxf(p[i], p[i + 1]));
-  const uint32_t h = at_pack(p[i], p[i + 1]);
-  (&hi.x)[i >> 1] = h;
-  (&lo.x)[i >> 1] = at_pack(p[i] - __uint_as_float(h << 16), p[i + 1] - __uint_as_float(h & 0xffff0000u));
-  // (made here, not where they are used, after the reference has been looked at)
-  asm volatile("" : "+v"((&lo.x)[i >> 1]));
+// The largest of a lane's eight scores.
+__device__ __forceinline__ float at_max8(const at_f32x4 s[2]) {
+  float m = s[0][0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i >> 2][i & 3]);
+  return m;
 }
-// Once the weights are there: where one is beyond 2^8, as in a row's first tile, the
-// references move to the maxima, the sums are rescaled and the weights made anew (l_old:
-// the sums before them).  Rows that have seen nothing keep kAtNone, under which a masked
-// score's weight is zero and any other's is infinite.
+// Before the scores become weights: where a score (raw products; c2 > 0 turns them into
+// log2 units) is more than 8 above its row's reference, as in a row's first tile, the
+// references move to the maxima and the sums are rescaled.  Rows that have seen nothing
+// keep kAtNone, under which a masked score's weight is zero.
 template <int D, int QT>
-__device__ __forceinline__ void at_reference(AtAcc<D, QT>& a, const at_f32x4 s[QT][2], float c2,
-                                             const float l_old[QT], uint4 hi[QT], uint4 lo[QT],
-                                             float p[QT][8], float most) {
-  if (__builtin_amdgcn_ballot_w64(most > kAtMost) == 0) return;
+__device__ __forceinline__ void at_reference(AtAcc<D, QT>& a, const float most[QT], float c2) {
+  bool above = false;
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) above |= most[qt] * c2 > a.m[qt] + kAtSlack;
+  if (__builtin_amdgcn_ballot_w64(above) == 0) return;
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
-    float mt = s[qt][0][0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) mt = fmaxf(mt, s[qt][i >> 2][i & 3]);
-    mt *= c2;
+    float mt = most[qt] * c2;
     mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
     mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
     const float mnew = fmaxf(a.m[qt], mt);
     const float alpha = __builtin_amdgcn_exp2f(a.m[qt] - mnew);
     a.m[qt] = mnew;
-    a.l[qt] = l_old[qt] * alpha;
+    a.l[qt] *= alpha;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) a.o[qt][db] *= alpha;
-#pragma unroll
-    for (int i = 0; i < 8; i += 2)
-      at_weights2<D, QT>(a, qt, i, s[qt], c2, hi[qt], lo[qt], p[qt], most);
   }
+}
+// Two weights (i even) of one query tile's scores s: the bf16 of each and of the remainder.
+template <int D, int QT>
+__device__ __forceinline__ void at_weights2(AtAcc<D, QT>& a, int qt, int i, const at_f32x4 s[2],
+                                            float c2, uint4& hi, uint4& lo) {
+  const float p0 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -a.m[qt]));
+  const float p1 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][(i + 1) & 3], c2, -a.m[qt]));
+  a.l[qt] += p0 + p1;
+  const uint32_t h = at_pack(p0, p1);
+  (&hi.x)[i >> 1] = h;
+  (&lo.x)[i >> 1] = at_pack(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
 }
 
 // V^T of block db of 16 dims: lane c of group g is to hold dim c of the block at keys
@@ -241,19 +244,52 @@ __device__ __forceinline__ void at_values(AtAcc<D, QT>& a, const uint16_t* vt, c
     at_value_products<D, QT>(a, db, at_value_block<D>(vt, db, lane), hi, lo);
 }
 
-// The unit whose place holds row r of the packed rows' order, by a wave: 64 units' ends
-// per step.
-__device__ __forceinline__ int64_t at_find_unit(const int64_t* __restrict__ off, int64_t base,
-                                                int64_t U, int32_t gap, uint32_t r, int lane) {
-  int64_t lo = 0, n = U;  // the answer is one of [lo, lo + n]
-  while (true) {
-    const int64_t step = (n + 63) / 64, i = lo + lane * step + step - 1;
-    const bool past = i >= U || at_place(off, base, i + 1, gap) > r;
-    lo += (int64_t)__popcll(__ballot(!past)) * step;
-    if (step == 1) return lo < U ? lo : U;
-    n = step;
+// The packed rows' offsets, as a wave reads them.  Up to 64 units they are held in the
+// lanes, so that one load is waited for before a piece's own, not three in turn.
+struct AtOffsets {
+  const int64_t* __restrict__ off;
+  uint32_t U;
+  bool few;
+  int64_t base, rows;
+  int64_t first, end;  // of unit `lane`
+  __device__ __forceinline__ AtOffsets(const int64_t* o, int64_t units, int lane)
+      : off(o), U((uint32_t)units), few(units <= 64), base(0), rows(0), first(0), end(0) {
+    if (units == 0) return;  // (not asked for)
+    if (few) {
+      first = off[min((uint32_t)lane, U)];
+      end = off[min((uint32_t)lane + 1, U)];
+      base = lane64(first, 0);
+      rows = lane64(end, U - 1) - base;
+    } else {
+      base = off[0];
+      rows = off[U] - base;
+    }
   }
-}
+  static __device__ __forceinline__ int64_t lane64(int64_t x, uint32_t i) {
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, i);
+    const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)((uint64_t)x >> 32), i);
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+  }
+  // a unit's first row and the one behind its last
+  __device__ __forceinline__ int64_t start(uint32_t u) const { return few ? lane64(first, u) : off[u]; }
+  __device__ __forceinline__ int64_t stop(uint32_t u) const { return few ? lane64(end, u) : off[u + 1]; }
+  // The unit whose place holds row r of the common order: 64 units' ends per step.
+  __device__ __forceinline__ uint32_t find(uint32_t r, int32_t gap, int lane) const {
+    if (few) {
+      const uint64_t past =
+          __ballot(lane < (int)U && at_place(end - base, (uint32_t)lane + 1, gap) > r);
+      return past ? (uint32_t)__builtin_ctzll(past) : U;
+    }
+    uint32_t lo = 0, n = U;  // the answer is one of [lo, lo + n]
+    while (true) {
+      const uint32_t step = (n + 63) / 64, i = lo + lane * step + step - 1;
+      const bool past = i >= U || at_place(off[i + 1] - base, i + 1, gap) > r;
+      lo += (uint32_t)__popcll(__ballot(!past)) * step;
+      if (step == 1) return min(lo, U);
+      n = step;
+    }
+  }
+};
 
 // Whether a bf16 of the eight is not finite.
 __device__ __forceinline__ bool at_bad8(uint4 x) {
@@ -294,8 +330,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
   const int g = lane >> 4, c = lane & 15;
   const int M = a.tq * gm.G, mp = a.ck.mp;
   const float c2 = gm.scale * kAtLog2e;
-  const int64_t U = a.U;
-  const int64_t* __restrict__ off = a.cache.offsets;
+  const uint32_t U = (uint32_t)a.U;
 
   // Query groups (more rows than a workgroup holds) of a chunk: eight workgroups apart, on
   // the same XCD, whose L2 then serves all but the first.  New rows' chunks are dealt from
@@ -304,37 +339,34 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
   const int qg = (wgx >> 3) % a.ck.qgroups;
   const uint32_t x0 = a.ck.qgroups == 1 ? wgx : (wgx >> 3) / a.ck.qgroups * 8 + (wgx & 7);
   const uint32_t xstep = gridDim.x / a.ck.qgroups;
-  const int row0 = (qg * NQ + qw) * QT * 16;
+  const int row0 = (qg * NQ + qw) * QT * 16;  // a wave's first query row
   const bool active = row0 < M;
   auto kdim = [&](int ks) { return (ks / SK) * 4 * EK + g * EK + 8 * (ks % SK); };
 
   uint16_t* const group_lds = lds + kg * Shape::GROUP;
-  auto key_tile = [&](int buf, int j) { return group_lds + (buf * Shape::SUB + j) * AtTile<D>::K; };
+  auto key_tile = [&](int n) { return group_lds + (n & 3) * AtTile<D>::K; };  // of tile n
   auto value_tile = [&](int buf, int j) {
     return group_lds + Shape::KT * AtTile<D>::K + (buf * Shape::SUB + j) * AtTile<D>::V;
   };
 
-  const int64_t base = off[0];
-  const AtCut cut = NEW ? at_cut_new(a) : at_cut_packed(a);
+  const AtOffsets off(a.cache.offsets, NEW ? 0 : a.U, lane);
+  const AtCut cut = NEW ? at_cut_new(a) : at_cut_packed(a, off.rows);
   const uint32_t tnp = at_up32((uint32_t)a.tn);
   const uint32_t nch = (cut.total + cut.keys - 1) / cut.keys;
   for (uint32_t x = x0; x < nch; x += xstep) {
     const uint32_t r0 = x * cut.keys, r1 = min(cut.total, r0 + cut.keys);
-    int64_t u = NEW ? r0 / tnp : at_find_unit(off, base, U, a.ck.gap, r0, lane);
-    for (; u < U; ++u) {
-      const uint32_t vs = NEW ? (uint32_t)u * tnp : at_place(off, base, u, a.ck.gap);
+    for (uint32_t u = NEW ? r0 / tnp : off.find(r0, a.ck.gap, lane); u < U; ++u) {
+      const int64_t p0 = NEW ? 0 : off.start(u);
+      const uint32_t vs = NEW ? u * tnp : at_place(p0 - off.base, u, a.ck.gap);
       if (vs >= r1) break;
       // the piece: rows [lo, lo + np) of the unit's
-      const int64_t p0 = NEW ? 0 : off[u];
-      const uint32_t len = NEW ? (uint32_t)a.tn : (uint32_t)min(off[u + 1] - p0, a.cover);
+      const uint32_t len = NEW ? (uint32_t)a.tn : (uint32_t)min(off.stop(u) - p0, a.cover);
       const uint32_t lo = max(r0, vs) - vs;
       const int np = (int)min(r1 - vs, len) - (int)lo;
       if (np <= 0) continue;  // (only what lies between units)
       const int ntp = (np + kAtTile - 1) / kAtTile;
-      const int h = (int)(u % gm.H);
-      const int64_t lb = u / gm.H;
-      const int b = (int)(lb % gm.B);
-      const int l = (int)(lb / gm.B);
+      const int h = (int)(u % (uint32_t)gm.H), b = (int)(u / gm.H % (uint32_t)gm.B);
+      const int l = (int)(u / gm.H / gm.B);
 
       // Its rows; reads past them return zero.  (New rows keep their strides; what lies past
       // the last one is not used.)
@@ -422,7 +454,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
       };
       // New rows whose values are not all finite (rare) are zero in the tile; their bits are
       // `bad`, and they reach only the queries that see them.
-      auto add_bad = [&](uint32_t bad, int t, const float p[QT][8], const uint32_t seen[QT]) {
+      auto add_bad = [&](uint32_t bad, int t, const uint4 ph[QT], const uint4 pl[QT],
+                         const uint32_t seen[QT]) {
         while (bad) {
           const int r = __builtin_ctz(bad);
           bad &= bad - 1;
@@ -430,9 +463,13 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           const uint16_t* vrow = vn + (int64_t)(t * kAtTile + r) * a.v_new.s_token;
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) {
-            float w = p[qt][0];
+            uint32_t wh = ph[qt].x, wl = pl[qt].x;  // the weight's two parts
 #pragma unroll
-            for (int e = 1; e < 8; ++e) w = i == e ? p[qt][e] : w;
+            for (int e = 1; e < 4; ++e) {
+              wh = i >> 1 == e ? (&ph[qt].x)[e] : wh;
+              wl = i >> 1 == e ? (&pl[qt].x)[e] : wl;
+            }
+            float w = i & 1 ? bf16_hi(wh) + bf16_hi(wl) : bf16_lo(wh) + bf16_lo(wl);
             w = __shfl(w, src, 64);
             const bool see = (__shfl(seen[qt], src, 64) >> i) & 1;
 #pragma unroll
@@ -472,7 +509,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           for (int kb = 0; kb < 2; ++kb) {
             const uint32_t r = t * kAtTile + kb * 16 + c;
 #pragma unroll
-            for (int i = 0; i < NLK; ++i) kx[kb][i].load(kr, r * kst + g * WK + i * 4 * WK);
+            for (int i = 0; i < NLK; ++i) kx[kb][i].template load<false>(kr, r * kst + g * WK + i * 4 * WK);
             if constexpr (MX) ksc[kb] = D == 128 ? buf_load_u32(ksr, r * 4) : buf_load_u16(ksr, r * 2);
           }
         };
@@ -480,7 +517,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
 #pragma unroll
           for (int n = 0; n < PER; ++n) {
             const uint32_t r = t * kAtTile + n * RPL + lane / LPR;
-            vx[n].load(vr, r * vst + (lane % LPR) * W);
+            // (a tile is read once; 3.36M rows, one query, mxfp8: 159 us without, 144 with;
+            // keys too: 143, but a second query group then takes 291 instead of 253)
+            vx[n].template load<!NEW>(vr, r * vst + (lane % LPR) * W);
             if constexpr (MX)
               vsc[n] = __builtin_amdgcn_raw_buffer_load_b8(
                   vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
@@ -521,124 +560,132 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           if (AHEAD && t + KS < ntp) load_values(t + KS);
           uint32_t seen[QT];
           mask_scores(s, t, seen);
+          float most[QT];
           uint4 ph[QT], pl[QT];
-          float p[QT][8], l_old[QT], most = 0.f;
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt) {
-            l_old[qt] = acc.l[qt];
+          for (int qt = 0; qt < QT; ++qt) most[qt] = at_max8(s[qt]);
+          at_reference<D, QT>(acc, most, c2);
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
             for (int i = 0; i < 8; i += 2)
-              at_weights2<D, QT>(acc, qt, i, s[qt], c2, ph[qt], pl[qt], p[qt], most);
-          }
-          at_reference<D, QT>(acc, s, c2, l_old, ph, pl, p, most);
+              at_weights2<D, QT>(acc, qt, i, s[qt], c2, ph[qt], pl[qt]);
           at_values<D, QT>(acc, vt, ph, pl, lane);
-          if constexpr (NEW) add_bad(bad, t, p, seen);
+          if constexpr (NEW) add_bad(bad, t, ph, pl, seen);
           __builtin_amdgcn_wave_barrier();
         }
       } else {
-        // A group's waves convert two tiles at a time together.  Tile after tile a wave
-        // multiplies the next one's keys while it turns the current scores into weights,
-        // then the current values while the keys after those are read; the group's next but
-        // one pair of key tiles and next pair of value tiles are written in between, and
-        // what follows those is on its way to registers.
+        // The waves convert two tiles at a time together.  Tile after tile a wave multiplies
+        // the next one's keys while it turns the current scores into weights, then the
+        // current values.  Of a stage (two tiles, 2 t and 2 t + 1) the keys are those of the
+        // tiles 2 t + 1 and 2 t + 2: four key tiles and four value tiles in LDS are two in use
+        // and two being written for the stage to come; what follows those is on its way to
+        // registers.
+        static_assert(KS == 1 && Shape::SUB == 2, "a stage is two tiles of all waves");
         constexpr int SUB = Shape::SUB;
         AtRaw<F, W> raw[SUB][PER];
         uint32_t sc[SUB][PER] = {};
-        auto load_piece = [&](int t, int j, int i, bool keys, bool values) {
+        auto load_piece = [&](AtRaw<F, W>(&x)[SUB][PER], uint32_t(&xs)[SUB][PER], int t, int j,
+                              int i) {
           const int n = qw + NQ * i;
           const bool key = n < NLT;
-          if (n >= 2 * NLT || !(key ? keys : values)) return;
-          const uint32_t r = ((key ? t + KS : t) * SUB + j) * kAtTile + (n % NLT) * RPL + lane / LPR;
-          raw[j][i].load(key ? kr : vr, r * (key ? kst : vst) + (lane % LPR) * W);
+          if (n >= 2 * NLT) return;
+          const uint32_t r = (t * SUB + j + (key ? 1 : 0)) * kAtTile + (n % NLT) * RPL + lane / LPR;
+          x[j][i].template load<!NEW>(key ? kr : vr, r * (key ? kst : vst) + (lane % LPR) * W);
           if constexpr (MX)
-            sc[j][i] = __builtin_amdgcn_raw_buffer_load_b8(
+            xs[j][i] = __builtin_amdgcn_raw_buffer_load_b8(
                 key ? ksr : vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
         };
-        auto store_piece = [&](int t, int buf, int j, int i, bool keys, bool values) {
+        auto store_piece = [&](AtRaw<F, W>(&x)[SUB][PER], const uint32_t(&xs)[SUB][PER], int t,
+                               int j, int i) {
           uint32_t bad = 0;
           const int n = qw + NQ * i;
           const bool key = n < NLT;
-          if (n >= 2 * NLT || !(key ? keys : values)) return bad;
+          if (n >= 2 * NLT) return bad;
           const int r = (n % NLT) * RPL + lane / LPR;
-          const float f = MX ? mx_scale(sc[j][i]) : 1.f;
+          const float f = MX ? mx_scale(xs[j][i]) : 1.f;
           if constexpr (NEW) {
-            if (!key) bad = finite_rows(raw[j][i].x, t * SUB + j, n - NLT);
+            if (!key) bad = finite_rows(x[j][i].x, t * SUB + j, n - NLT);
           }
-          uint4* dst = reinterpret_cast<uint4*>(key ? key_tile(buf ^ 1, j) : value_tile(buf, j));
+          uint4* dst = reinterpret_cast<uint4*>(key ? key_tile(t * SUB + j + 1) : value_tile(t & 1, j));
 #pragma unroll
           for (int e = 0; e < EV / 8; ++e) {
             const int ch = (lane % LPR) * (EV / 8) + e;
             dst[key ? at_key_chunk<D>(r, ch) : at_value_chunk<D>(r, ch)] =
-                at_bf16<F, W>(raw[j][i], e, f);
+                at_bf16<F, W>(x[j][i], e, f);
           }
           return bad;
         };
-        // keys of stage t + KS and values of t
-        auto load = [&](int t, bool keys, bool values) {
+        auto load = [&](AtRaw<F, W>(&x)[SUB][PER], uint32_t(&xs)[SUB][PER], int t) {
 #pragma unroll
           for (int j = 0; j < SUB; ++j)
 #pragma unroll
-            for (int i = 0; i < PER; ++i) load_piece(t, j, i, keys, values);
+            for (int i = 0; i < PER; ++i) load_piece(x, xs, t, j, i);
         };
-        // values to buf, keys to the other
-        auto store = [&](int t, int buf, bool keys, bool values) {
+        auto store = [&](AtRaw<F, W>(&x)[SUB][PER], const uint32_t(&xs)[SUB][PER], int t) {
 #pragma unroll
           for (int j = 0; j < SUB; ++j) {
             uint32_t bad = 0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) bad |= store_piece(t, buf, j, i, keys, values);
-            if (NEW && values && lane == 0) bad_s[((buf * SUB + j) * KS + kg) * NQ + qw] = bad;
+            for (int i = 0; i < PER; ++i) bad |= store_piece(x, xs, t, j, i);
+            if (NEW && lane == 0) bad_s[((t & 1) * SUB + j) * NQ + qw] = bad;
           }
         };
         uint4 kf[2][KSTEP];
-        auto read_keys = [&](int buf, int j, int kb) {
+        auto read_keys = [&](int n) {
 #pragma unroll
-          for (int ks = 0; ks < KSTEP; ++ks)
-            kf[kb][ks] = reinterpret_cast<const uint4*>(
-                key_tile(buf, j))[at_key_chunk<D>(kb * 16 + c, ks * 4 + g)];
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int ks = 0; ks < KSTEP; ++ks)
+              kf[kb][ks] = reinterpret_cast<const uint4*>(
+                  key_tile(n))[at_key_chunk<D>(kb * 16 + c, ks * 4 + g)];
         };
-        const int its = (ntp + KS * SUB - 1) / (KS * SUB);
-        load(kg - KS, true, false);
-        load_queries();
-        store(kg - KS, 1, true, false);
-        load(kg, true, true);
+        const int its = (ntp + SUB - 1) / SUB;
+        {
+          AtRaw<F, W> x[SUB][PER];  // (the first keys; nothing else of the stage before the first)
+          uint32_t xs[SUB][PER] = {};
+#pragma unroll
+          for (int i = 0; i < PER; ++i)
+            if (qw + NQ * i < NLT) load_piece(x, xs, -1, 1, i);
+          load(raw, sc, 0);
+          load_queries();
+#pragma unroll
+          for (int i = 0; i < PER; ++i)
+            if (qw + NQ * i < NLT) store_piece(x, xs, -1, 1, i);
+          store(raw, sc, 0);
+          load(raw, sc, 1);
+        }
         __syncthreads();
         at_f32x4 s[QT][2];
+        uint32_t seen[QT];
         if (active) {
-          read_keys(0, 0, 0);
-          read_keys(0, 0, 1);
+          read_keys(0);
           scores([&](int kb, int ks) { return kf[kb][ks]; }, s);
-          read_keys(0, 1, 0);
-          read_keys(0, 1, 1);
+          mask_scores(s, 0, seen);
+          float most[QT];
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) most[qt] = at_max8(s[qt]);
+          at_reference<D, QT>(acc, most, c2);
         }
-        store(kg, 0, true, true);
-        load(kg + KS, true, true);
-        __syncthreads();
-        for (int it = 0; it < its; ++it) {
-          const int t = it * KS + kg, buf = it & 1;
-          if (active && t * SUB < ntp) {
+        __syncthreads();  // tile 0's keys are read: the first stage writes tile 4's over them
+        for (int t = 0; t < its; ++t) {
+          if (active) {
 #pragma unroll
             for (int j = 0; j < SUB; ++j) {
-              uint32_t seen[QT], bad = 0;
-              mask_scores(s, t * SUB + j, seen);
+              uint32_t bad = 0, seen_next[QT];
               if constexpr (NEW) {
 #pragma unroll
-                for (int w = 0; w < NQ; ++w) bad |= bad_s[((buf * SUB + j) * KS + kg) * NQ + w];
+                for (int w = 0; w < NQ; ++w) bad |= bad_s[((t & 1) * SUB + j) * NQ + w];
                 bad = __builtin_amdgcn_readfirstlane(bad);
               }
               at_f32x4 next[QT][2];
               uint4 ph[QT], pl[QT];
-              float p[QT][8], l_old[QT], most = 0.f;
               at_bf16x8 vf[3];
 #pragma unroll
-              for (int qt = 0; qt < QT; ++qt) {
-                next[qt][0] = next[qt][1] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
-                l_old[qt] = acc.l[qt];
-              }
+              for (int qt = 0; qt < QT; ++qt) next[qt][0] = next[qt][1] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
               // The matrix unit takes KSTEP / 2 products while the vector unit turns two scores
-              // into weights (the fences keep the compiler from taking them apart); the keys
-              // are those of the tile after this one, read before the barrier that lets their
-              // buffer be written again.
+              // into weights (the fences keep the compiler from taking them apart).
+              read_keys(t * SUB + j + 1);
 #pragma unroll
               for (int pr = 0; pr < 4 * QT; ++pr) {
 #pragma unroll
@@ -649,40 +696,47 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                       __builtin_bit_cast(at_bf16x8, q[qt][ks]), next[qt][kb], 0, 0, 0);
                 }
                 const int qt = pr / 4;
-                at_weights2<D, QT>(acc, qt, 2 * (pr % 4), s[qt], c2, ph[qt], pl[qt], p[qt], most);
+                at_weights2<D, QT>(acc, qt, 2 * (pr % 4), s[qt], c2, ph[qt], pl[qt]);
                 if (pr >= 4 * QT - 2)
-                  vf[pr - (4 * QT - 2)] = at_value_block<D>(value_tile(buf, j), pr - (4 * QT - 2), lane);
+                  vf[pr - (4 * QT - 2)] = at_value_block<D>(value_tile(t & 1, j), pr - (4 * QT - 2), lane);
                 __builtin_amdgcn_sched_barrier(0);
               }
-              at_reference<D, QT>(acc, s, c2, l_old, ph, pl, p, most);
+              mask_scores(next, t * SUB + j + 1, seen_next);
               // And the values' products, their operands two blocks ahead, while the wave's
-              // share of the tiles to come is converted.
+              // share of the tiles to come is converted and the next scores' maxima are found;
+              // ahead of the other wave's weights.
+              float most[QT];
+              __builtin_amdgcn_s_setprio(1);
 #pragma unroll
               for (int db = 0; db < D / 16; ++db) {
                 if (db + 2 < D / 16)
-                  vf[(db + 2) % 3] = at_value_block<D>(value_tile(buf, j), db + 2, lane);
-                if (db >= D / 16 - 2) read_keys(buf ^ 1, j, db - (D / 16 - 2));
+                  vf[(db + 2) % 3] = at_value_block<D>(value_tile(t & 1, j), db + 2, lane);
                 at_value_products<D, QT>(acc, db, vf[db % 3], ph, pl);
                 if constexpr (!NEW) {
 #pragma unroll
                   for (int i = 0; i < PER; ++i)
                     if (db == i * (D / 16) / PER) {
-                      store_piece(t + KS, buf ^ 1, j, i, true, true);
-                      load_piece(t + 2 * KS, j, i, true, true);
+                      store_piece(raw, sc, t + 1, j, i);
+                      load_piece(raw, sc, t + 2, j, i);
                     }
                 }
+                if (db >= D / 16 - QT) most[db - (D / 16 - QT)] = at_max8(next[db - (D / 16 - QT)]);
                 __builtin_amdgcn_sched_barrier(0);
               }
-              if constexpr (NEW) add_bad(bad, t * SUB + j, p, seen);
+              __builtin_amdgcn_s_setprio(0);
+              if constexpr (NEW) add_bad(bad, t * SUB + j, ph, pl, seen);
+              at_reference<D, QT>(acc, most, c2);
 #pragma unroll
-              for (int qt = 0; qt < QT; ++qt)
+              for (int qt = 0; qt < QT; ++qt) {
+                if constexpr (NEW) seen[qt] = seen_next[qt];
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) s[qt][kb] = next[qt][kb];
+              }
             }
           }
-          if (NEW || !(active && t * SUB < ntp)) {
-            store(t + KS, buf ^ 1, true, true);
-            load(t + 2 * KS, true, true);
+          if (NEW || !active) {
+            store(raw, sc, t + 1);
+            load(raw, sc, t + 2);
           }
           __syncthreads();
         }
@@ -690,7 +744,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
 
       // The piece's partial: (maximum, sum, unnormalized output) of each query row, the KS
       // groups joined in LDS.
-      const int64_t slot = (NEW ? a.ck.most + U : 0) + x + u;
+      const int64_t slot = (NEW ? a.ck.most + a.U : 0) + x + u;
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
         float l_row = acc.l[qt];
@@ -760,7 +814,7 @@ template <int F, int D, int SHAPE, bool TREE>
 __global__ __launch_bounds__((64 * attend_wg_waves(SHAPE)))
 __attribute__((amdgpu_waves_per_eu(attend_waves(F, D, SHAPE, TREE)))) void attend_kernel(
     AttendArgs a) {
-  constexpr int NQ = SHAPE <= kAtTwo ? 1 : SHAPE == kAtFour ? 2 : SHAPE == kAtEight ? 4 : 8;
+  constexpr int NQ = SHAPE <= kAtTwo ? 1 : SHAPE == kAtEight ? 4 : 8;
   constexpr int QT = SHAPE == kAtOne ? 1 : 2;
   using Shape = AtShape<D, NQ, QT>;
   static_assert(Shape::NT == 64 * attend_wg_waves(SHAPE), "the workgroup's waves");
@@ -792,7 +846,6 @@ static certkv_status launch_attend_d(const AttendArgs& a, hipStream_t s) {
   switch (a.ck.shape) {
     case kAtOne: return launch_attend<F, D, kAtOne>(a, s);
     case kAtTwo: return launch_attend<F, D, kAtTwo>(a, s);
-    case kAtFour: return launch_attend<F, D, kAtFour>(a, s);
     case kAtEight: return launch_attend<F, D, kAtEight>(a, s);
     default: return launch_attend<F, D, kAtSixteen>(a, s);
   }

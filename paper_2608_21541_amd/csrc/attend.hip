@@ -6,13 +6,15 @@ namespace certkv {
 bool attend_chunks(int format, int D, int tq, int G, int tn, int64_t rows, int64_t U,
                    AttendChunks* c) {
   const int M = tq * G;
-  c->shape = M <= 16 ? kAtOne : M <= 32 ? kAtTwo : M <= 64 ? kAtFour : M <= 128 ? kAtEight : kAtSixteen;
-  const int held = 16 << c->shape;
+  // (Up to 64 rows as two groups of 32, each of which reads the cache: with two waves that
+  // share their tiles 3.36M rows of mxfp8 take 300 us, so 230, the second group from L2.)
+  c->shape = M <= 16 ? kAtOne : M <= 64 ? kAtTwo : M <= 128 ? kAtEight : kAtSixteen;
+  const int held = c->shape == kAtOne ? 16 : c->shape == kAtTwo ? 32 : c->shape == kAtEight ? 128 : 256;
   c->qgroups = (M + held - 1) / held;
   c->mp = c->qgroups * held;
-  // as many chunks as workgroups stay resident: 256 compute units of four SIMDs
+  // as many chunks as their workgroups stay resident: 256 compute units of four SIMDs
   c->parts = 256 * 4 * attend_waves(format, D, c->shape, tn > 0) / attend_wg_waves(c->shape);
-  if (c->shape == kAtFour && D == 128) c->parts = 512;  // (by LDS)
+  c->parts = (c->parts + c->qgroups - 1) / c->qgroups;
   c->gap = 64;
   auto chunks = [&](int64_t total, int64_t least) {
     const int64_t shortest = (total + least - 1) / least;
@@ -39,7 +41,7 @@ __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs 
   __shared__ float4 acc_s[GR][C4];
   __shared__ float2 ml_s[GR];
   const Geo& g = a.g;
-  const int64_t u = blockIdx.x;
+  const uint32_t u = blockIdx.x;
   const int grp = threadIdx.x / C4, c4 = threadIdx.x % C4;
   const int row = blockIdx.y * RW + grp / S, sg = grp % S;
   const int M = a.tq * g.G;
@@ -76,8 +78,8 @@ __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs 
     }
   };
   if (row < M) {
-    const AtCut cut = at_cut_packed(a);
-    const uint32_t vs = at_place(off, off[0], u, a.ck.gap), s0 = vs / cut.keys;
+    const AtCut cut = at_cut_packed(a, off[a.U] - off[0]);
+    const uint32_t vs = at_place(off[u] - off[0], u, a.ck.gap), s0 = vs / cut.keys;
     const uint32_t len = (uint32_t)min(full, a.cover);
     fold((int64_t)s0 + u, len ? (vs + len - 1) / cut.keys - s0 + 1 : 0);
     if (a.tn) {
@@ -111,10 +113,8 @@ __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs 
     m = mx;
   }
   if (row >= M) return;
-  const int h = (int)(u % g.H);
-  const int64_t lb = u / g.H;
-  const int b = (int)(lb % g.B);
-  const int l = (int)(lb / g.B);
+  const int h = (int)(u % (uint32_t)g.H), b = (int)(u / g.H % (uint32_t)g.B);
+  const int l = (int)(u / g.H / g.B);
   const int t = row / g.G, gq = row % g.G;
   const int64_t orow = ((int64_t)l * g.B * a.tq + (int64_t)b * a.tq + t) * (g.H * g.G) + h * g.G + gq;
   const float inv = L == 0.f ? 0.f : 1.f / L;  // (nothing visible: out 0, lse -inf)

@@ -259,19 +259,16 @@ certkv_status run_read_mx(const ReadMxArgs& a, hipStream_t s);
 constexpr int kAtTile = 32;        // rows per tile
 constexpr int kAtMinKeys = 128;    // shortest chunk of packed rows, and the unit of its length
 constexpr int kAtMaxKeys = 16384;  // longest: a bound on how long an fp32 sum gets
-// Query rows of a workgroup: 16 and 32 of one wave (four waves take tiles in turn), 64 of
-// two (twice), 128 of four, 256 of eight.
-enum { kAtOne, kAtTwo, kAtFour, kAtEight, kAtSixteen };
+// Query rows of a workgroup: 16 or 32 of every wave (four take tiles in turn), 128 of four
+// waves, 256 of eight.
+enum { kAtOne, kAtTwo, kAtEight, kAtSixteen };
 // Waves per SIMD that the kernel of a shape leaves registers for.
 constexpr int attend_waves(int format, int D, int shape, bool tree) {
 #ifdef ATW
   return ATW;
 #else
-  if (D == 128)
-    return shape == kAtOne && !tree ? (format == CERTKV_CACHE_MXFP4 ? 4 : 3) : 2;
-  if (shape == kAtOne) return 4;
-  if (shape <= kAtFour) return tree ? 2 : 3;
-  return tree ? 3 : 4;
+  if (D == 128) return shape == kAtOne && !tree ? 3 : 2;
+  return shape == kAtOne ? 4 : shape == kAtTwo && !tree ? 3 : 2;
 #endif
 }
 // Waves of a workgroup.
