@@ -49,12 +49,17 @@ __device__ __forceinline__ void mx_store8(const Geo& g, const float x[8], int64_
   if (bad) report_nonfinite(g);
 }
 
+typedef uint32_t MxU4 __attribute__((ext_vector_type(4)));
+typedef float MxF4 __attribute__((ext_vector_type(4)));
 template <typename T>
 struct MxRaw;  // eight values as they are loaded
 template <>
 struct MxRaw<uint16_t> {
   uint4 a;
-  __device__ __forceinline__ void load(const uint16_t* p) { a = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    const MxU4 v = __builtin_nontemporal_load(reinterpret_cast<const MxU4*>(p));
+    a = make_uint4(v[0], v[1], v[2], v[3]);
+  }
   __device__ __forceinline__ void values(float x[8]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -68,8 +73,10 @@ template <>
 struct MxRaw<float> {
   float4 a, b;
   __device__ __forceinline__ void load(const float* p) {
-    a = reinterpret_cast<const float4*>(p)[0];
-    b = reinterpret_cast<const float4*>(p)[1];
+    const MxF4 v = __builtin_nontemporal_load(reinterpret_cast<const MxF4*>(p));
+    const MxF4 w = __builtin_nontemporal_load(reinterpret_cast<const MxF4*>(p) + 1);
+    a = make_float4(v[0], v[1], v[2], v[3]);
+    b = make_float4(w[0], w[1], w[2], w[3]);
   }
   __device__ __forceinline__ void values(float x[8]) const {
     x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
@@ -88,80 +95,89 @@ __global__ __launch_bounds__(kMxThreads) void compact_mx_kernel(
     int64_t* __restrict__ packed_offsets) {
   constexpr int LPR = D / 8;              // lanes per row
   constexpr int RPS = kMxThreads / LPR;   // rows per step of the workgroup
-  constexpr int UR = sizeof(T) == 2 ? 4 : 2;  // rows of a lane in flight
-  const int64_t U = (int64_t)g.L * g.B * g.H;
-  auto seg = [&](int64_t u) { return kept_offsets[u] + g.slot * u; };  // a unit's first packed row
-  for (int64_t u = (int64_t)blockIdx.x * kMxThreads + threadIdx.x; u <= U;
-       u += (int64_t)gridDim.x * kMxThreads)
+  // Rows of a lane in flight.  (1.15M rows of 16 layers: 4 rows 230 us, 2 205, 1 205; the
+  // source rows non-temporally, 2 171: a tenth of the cache in 256-byte pieces is read at
+  // 3.4 TB/s at most.)
+  constexpr int UR = 2;
+  const uint32_t U = (uint32_t)(g.L * g.B * g.H);
+  auto seg = [&](uint32_t u) { return kept_offsets[u] + (int64_t)g.slot * u; };  // first packed row
+  for (uint32_t u = blockIdx.x * kMxThreads + threadIdx.x; u <= U; u += gridDim.x * kMxThreads)
     packed_offsets[u] = seg(u);
   const int64_t base = seg(0), rows = seg(U) - base;
   const int64_t per = ((rows + gridDim.x - 1) / gridDim.x + RPS - 1) / RPS * RPS;
   const int64_t r0 = base + blockIdx.x * per, r1 = min(base + rows, r0 + per);
   if (r0 >= r1) return;
   // the unit of row r0, 64 units' ends per step
-  int64_t u = 0;
-  for (int64_t n = U; n > 0;) {
-    const int64_t step = (n + 63) / 64, i = u + (threadIdx.x & 63) * step + step - 1;
+  uint32_t u = 0;
+  for (uint32_t n = U; n > 0;) {
+    const uint32_t step = (n + 63) / 64, i = u + (threadIdx.x & 63) * step + step - 1;
     const bool past = i >= U || seg(i + 1) > r0;
-    u += (int64_t)__popcll(__ballot(!past)) * step;
+    u += (uint32_t)__popcll(__ballot(!past)) * step;
     if (step == 1) break;
     n = step;
   }
   u = min(u, U - 1);
   const int ri = threadIdx.x / LPR, ci = threadIdx.x % LPR;
-  int64_t first = seg(u), end = seg(u + 1);  // the current unit's rows
+  // The lane's current unit: the row behind its last, and where its source rows are.
+  // (Worked out when the unit changes: its divisions would be the time of a row.)
+  int64_t end = 0, k_at = 0, v_at = 0;
+  int32_t n = 0;  // source rows; 0: another launch's sequence
+  auto enter = [&]() {
+    end = seg(u + 1);
+    const uint32_t h = u % (uint32_t)g.H, lb = u / (uint32_t)g.H;
+    const uint32_t l = lb / (uint32_t)g.B;
+    const int b = (int)(lb - l * (uint32_t)g.B) - st.first;
+    const bool mine = b >= 0 && b < st.count;
+    const int64_t tok = mine ? st.start[b] : 0;
+    n = mine ? st.len[b] : 0;
+    k_at = l * k_sl + tok * k_st + h * k_sh + ci * 8;
+    v_at = l * v_sl + tok * v_st + h * v_sh + ci * 8;
+  };
+  enter();
   for (int64_t r = r0 + ri; r < r1; r += RPS * UR) {
-    // Row by row its unit and source; rows past the run, slots and other launches'
-    // sequences fetch the run's first source row that is at hand, unused.
-    const T *kr[UR], *vr[UR];
-    int64_t unit[UR];
+    // The rows' sources, then the rows, in flight together; rows past the run and other
+    // launches' fetch the unit's first row (or the tensor's), unused.
+    int64_t ka[UR], va[UR];
     int32_t j[UR];
+    uint32_t unit[UR];
     bool slot[UR], mine[UR];
-    int l[UR], b[UR], h[UR];
 #pragma unroll
     for (int q = 0; q < UR; ++q) {
       const int64_t x = r + q * RPS;
       while (x >= end && u + 1 < U) {
         ++u;
-        first = end;
-        end = seg(u + 1);
+        enter();
       }
-      h[q] = (int)(u % g.H);
-      const int64_t lb = u / g.H;
-      l[q] = (int)(lb / g.B);
-      b[q] = (int)(lb % g.B) - st.first;
       unit[q] = u;
-      mine[q] = x < r1 && b[q] >= 0 && b[q] < st.count;
+      mine[q] = x < r1 && n > 0;
       slot[q] = mine[q] && g.slot && x + 1 == end;
-      const bool kept = mine[q] && !slot[q];
-      j[q] = kept ? kept_idx[x - g.slot * u] : 0;
-      if (!kept) b[q] = 0;
+      j[q] = mine[q] && !slot[q] ? min(max(kept_idx[x - (int64_t)g.slot * u], 0), n - 1) : 0;  // caller indices clamped
+      ka[q] = k_at;
+      va[q] = v_at;
     }
-    MxRaw<T> ka[UR], va[UR];
+    MxRaw<T> kx[UR], vx[UR];
 #pragma unroll
     for (int q = 0; q < UR; ++q) {
-      j[q] = min(max(j[q], 0), st.len[b[q]] - 1);  // caller indices clamped
-      const int64_t tok = st.start[b[q]] + j[q];
-      ka[q].load(kc + l[q] * k_sl + tok * k_st + h[q] * k_sh + ci * 8);
-      va[q].load(vc + l[q] * v_sl + tok * v_st + h[q] * v_sh + ci * 8);
+      kx[q].load(kc + ka[q] + j[q] * k_st);
+      vx[q].load(vc + va[q] + j[q] * v_st);
     }
 #pragma unroll
     for (int q = 0; q < UR; ++q) {
       const int64_t x = r + q * RPS;
       if (!mine[q]) continue;  // (a whole row's lanes)
-      float kx[8], vx[8];
+      float ky[8], vy[8];
       if (slot[q]) {
         MxRaw<float> s;
-        s.load(k_star + unit[q] * D + ci * 8);
-        s.values(kx);
-        s.load(v_star + unit[q] * D + ci * 8);
-        s.values(vx);
+        s.load(k_star + (int64_t)unit[q] * D + ci * 8);
+        s.values(ky);
+        s.load(v_star + (int64_t)unit[q] * D + ci * 8);
+        s.values(vy);
       } else {
-        ka[q].values(kx);
-        va[q].values(vx);
+        kx[q].values(ky);
+        vx[q].values(vy);
       }
-      mx_store8<F>(g, kx, x * D + ci * 8, k_codes, k_scales);
-      mx_store8<F>(g, vx, x * D + ci * 8, v_codes, v_scales);
+      mx_store8<F>(g, ky, x * D + ci * 8, k_codes, k_scales);
+      mx_store8<F>(g, vy, x * D + ci * 8, v_codes, v_scales);
       if (ci == 0) pos_packed[x] = slot[q] ? -1 : j[q];
     }
   }
@@ -194,8 +210,9 @@ certkv_status run_compact_mx(const CompactMxArgs& a, const SeqTab& st, hipStream
 
 // Codes back to values, eight dims a lane: the rows of both arrays are contiguous,
 // so an item is eight dims of either and its scale byte the item's quarter.  Bound
-// by the writes (mxfp8: 1.03 bytes read for 2 written as bf16).  blockIdx.y: keys
-// or values.
+// by the writes (mxfp8: 1.03 bytes read for 2 written as bf16), which are made
+// non-temporally (1.15M rows of mxfp4 after they were written 153 us without, 113
+// with; 3.36M of mxfp8 by themselves 510 and 504, 5.2 TB/s).  blockIdx.y: keys or values.
 template <int F, bool F32>
 __global__ __launch_bounds__(kMxThreads) void read_mx_kernel(
     int64_t items, const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_scales,
@@ -216,11 +233,11 @@ __global__ __launch_bounds__(kMxThreads) void read_mx_kernel(
     uint4 v = mx_decode8<F>(c, mx_scale(x == 255u ? 127u : x));
     if (x == 255u) v = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
     if constexpr (F32) {
-      float4* o = reinterpret_cast<float4*>(out) + 2 * i;
-      o[0] = make_float4(bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y));
-      o[1] = make_float4(bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w));
+      MxF4* o = reinterpret_cast<MxF4*>(out) + 2 * i;
+      __builtin_nontemporal_store((MxF4){bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y)}, o);
+      __builtin_nontemporal_store((MxF4){bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)}, o + 1);
     } else {
-      reinterpret_cast<uint4*>(out)[i] = v;
+      __builtin_nontemporal_store((MxU4){v.x, v.y, v.z, v.w}, reinterpret_cast<MxU4*>(out) + i);
     }
   }
 }
