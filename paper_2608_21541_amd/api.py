@@ -116,7 +116,7 @@ def _run(dev, what, *args):
     index = dev.index
     if index is None:
         raise ValueError(f"{what}: expected tensors on a GPU")
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():
         _check(fn(*args, torch._C._cuda_getCurrentRawStream(index)), what)
     else:
         with torch.cuda.device(dev):
@@ -423,7 +423,11 @@ class MxCache:
     def head_dim(self):
         return self.k.shape[1] * (1 if self.format == "mxfp8" else 2)
 
-    def c_cache(self):
+    def __setattr__(self, name, value):
+        object.__setattr__(self, "_checked", False)
+        object.__setattr__(self, name, value)
+
+    def _check_tensors(self):
         k, ks, v, vs = self.k, self.k_scales, self.v, self.v_scales
         rows, wide = k.shape
         scales = (rows, wide // (32 if self.format == "mxfp8" else 16))
@@ -431,8 +435,14 @@ class MxCache:
         assert k.dtype == v.dtype == ks.dtype == vs.dtype == torch.uint8
         assert k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()
         assert self.offsets.dtype == torch.int64 and self.offsets.is_contiguous()
-        return _lib.Cache(_format_code(self.format), k.data_ptr(), v.data_ptr(), ks.data_ptr(),
-                          vs.data_ptr(), self.offsets.data_ptr())
+        object.__setattr__(self, "_checked", True)
+
+    def c_cache(self):
+        if not self._checked:  # (again when a field has changed)
+            self._check_tensors()
+        return _lib.Cache(_format_code(self.format), self.k.data_ptr(), self.v.data_ptr(),
+                          self.k_scales.data_ptr(), self.v_scales.data_ptr(),
+                          self.offsets.data_ptr())
 
 
 _READ_SPECS = {}

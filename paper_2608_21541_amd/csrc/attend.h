@@ -424,33 +424,33 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           }
         }
       };
-      // Scores masked: of the packed rows, those past the piece; of new rows, those that a
-      // query does not see (the others' bits: seen).
-      auto mask_scores = [&](at_f32x4 s[QT][2], int t, uint32_t seen[QT]) {
-        if constexpr (NEW) {
+      // Which of the lane's eight keys of new tile t each query sees, a bit each.
+      auto see = [&](int t, uint32_t seen[QT]) {
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt) {
-            const int row = row0 + qt * 16 + c, tt = min(row, M - 1) / gm.G;
-            const uint8_t* mrow = a.mask + ((int64_t)b * a.tq + tt) * a.tn;
-            seen[qt] = 0;
+        for (int qt = 0; qt < QT; ++qt) {
+          seen[qt] = 0;
+          const int row = row0 + qt * 16 + c, tt = min(row, M - 1) / gm.G;
+          const uint8_t* mrow = a.mask + ((int64_t)b * a.tq + tt) * a.tn;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int r = t * kAtTile + 16 * (i >> 2) + 4 * g + (i & 3), j = (int)lo + r;
-              bool see = j <= a.tn - a.tq + tt;
-              if (a.mask) see = mrow[min(j, a.tn - 1)] != 0;
-              see = see && r < np && row < M;
-              seen[qt] |= (uint32_t)see << i;
-              if (!see) s[qt][i >> 2][i & 3] = -INFINITY;
-            }
+          for (int i = 0; i < 8; ++i) {
+            const int r = t * kAtTile + 16 * (i >> 2) + 4 * g + (i & 3), j = (int)lo + r;
+            bool sees = j <= a.tn - a.tq + tt;
+            if (a.mask) sees = mrow[min(j, a.tn - 1)] != 0;
+            seen[qt] |= (uint32_t)(sees && r < np && row < M) << i;
           }
-        } else if (np - t * kAtTile < kAtTile) {
-#pragma unroll
-          for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (16 * (i >> 2) + 4 * g + (i & 3) >= np - t * kAtTile)
-                s[qt][i >> 2][i & 3] = -INFINITY;
         }
+      };
+      // Scores masked: of the packed rows, those past the piece; of new rows, those that a
+      // query does not see.
+      auto mask_scores = [&](at_f32x4 s[QT][2], int t, const uint32_t seen[QT]) {
+        if (!NEW && np - t * kAtTile >= kAtTile) return;
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (NEW ? !(seen[qt] >> i & 1)
+                    : 16 * (i >> 2) + 4 * g + (i & 3) >= np - t * kAtTile)
+              s[qt][i >> 2][i & 3] = -INFINITY;
       };
       // New rows whose values are not all finite (rare) are zero in the tile; their bits are
       // `bad`, and they reach only the queries that see them.
@@ -534,6 +534,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
         load_queries();
         for (int t = kg; t < ntp; t += KS) {
           if (!AHEAD) load_keys(t);
+          uint32_t seen[QT];
+          if constexpr (NEW) see(t, seen);
+          if (!AHEAD) load_values(t);
           at_f32x4 s[QT][2];
           scores(
               [&](int kb, int ks) {
@@ -544,7 +547,6 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
               },
               s);
           if (AHEAD && t + KS < ntp) load_keys(t + KS);
-          if (!AHEAD) load_values(t);
           uint32_t bad = 0;
 #pragma unroll
           for (int n = 0; n < PER; ++n) {
@@ -558,7 +560,6 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           }
           __builtin_amdgcn_wave_barrier();
           if (AHEAD && t + KS < ntp) load_values(t + KS);
-          uint32_t seen[QT];
           mask_scores(s, t, seen);
           float most[QT];
           uint4 ph[QT], pl[QT];
@@ -658,6 +659,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
         __syncthreads();
         at_f32x4 s[QT][2];
         uint32_t seen[QT];
+        if (NEW && active) see(0, seen);
         if (active) {
           read_keys(0);
           scores([&](int kb, int ks) { return kf[kb][ks]; }, s);
@@ -686,6 +688,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
               // The matrix unit takes KSTEP / 2 products while the vector unit turns two scores
               // into weights (the fences keep the compiler from taking them apart).
               read_keys(t * SUB + j + 1);
+              if constexpr (NEW) see(t * SUB + j + 1, seen_next);
 #pragma unroll
               for (int pr = 0; pr < 4 * QT; ++pr) {
 #pragma unroll
