@@ -244,26 +244,26 @@ __device__ __forceinline__ void at_values(AtAcc<D, QT>& a, const uint16_t* vt, c
     at_value_products<D, QT>(a, db, at_value_block<D>(vt, db, lane), hi, lo);
 }
 
-// The packed rows' offsets, as a wave reads them.  Up to 64 units they are held in the
-// lanes, so that one load is waited for before a piece's own, not three in turn.
+// The packed rows' offsets, as a wave reads them: those of 64 units at a time in its lanes,
+// so that a unit's place, its rows and the next unit's are one load to wait for, not three
+// in turn; up to 64 units the same load tells the rows in all.
 struct AtOffsets {
   const int64_t* __restrict__ off;
   uint32_t U;
-  bool few;
+  uint32_t at;         // the first of the 64
   int64_t base, rows;
-  int64_t first, end;  // of unit `lane`
+  int64_t first, end;  // rows of unit at + lane
   __device__ __forceinline__ AtOffsets(const int64_t* o, int64_t units, int lane)
-      : off(o), U((uint32_t)units), few(units <= 64), base(0), rows(0), first(0), end(0) {
+      : off(o), U((uint32_t)units), at(0), base(0), rows(0), first(0), end(0) {
     if (units == 0) return;  // (not asked for)
-    if (few) {
-      first = off[min((uint32_t)lane, U)];
-      end = off[min((uint32_t)lane + 1, U)];
-      base = lane64(first, 0);
-      rows = lane64(end, U - 1) - base;
-    } else {
-      base = off[0];
-      rows = off[U] - base;
-    }
+    window(0, lane);
+    base = lane64(first, 0);
+    rows = (units <= 64 ? lane64(end, U - 1) : off[U]) - base;
+  }
+  __device__ __forceinline__ void window(uint32_t u, int lane) {
+    at = u;
+    first = off[min(u + lane, U)];
+    end = off[min(u + lane + 1, U)];
   }
   static __device__ __forceinline__ int64_t lane64(int64_t x, uint32_t i) {
     const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, i);
@@ -271,23 +271,24 @@ struct AtOffsets {
     return (int64_t)(((uint64_t)hi << 32) | lo);
   }
   // a unit's first row and the one behind its last
-  __device__ __forceinline__ int64_t start(uint32_t u) const { return few ? lane64(first, u) : off[u]; }
-  __device__ __forceinline__ int64_t stop(uint32_t u) const { return few ? lane64(end, u) : off[u + 1]; }
+  __device__ __forceinline__ void unit(uint32_t u, int lane, int64_t& p0, int64_t& p1) {
+    if (u - at >= 64) window(u, lane);
+    p0 = lane64(first, u - at);
+    p1 = lane64(end, u - at);
+  }
   // The unit whose place holds row r of the common order: 64 units' ends per step.
-  __device__ __forceinline__ uint32_t find(uint32_t r, int32_t gap, int lane) const {
-    if (few) {
-      const uint64_t past =
-          __ballot(lane < (int)U && at_place(end - base, (uint32_t)lane + 1, gap) > r);
-      return past ? (uint32_t)__builtin_ctzll(past) : U;
-    }
+  __device__ __forceinline__ uint32_t find(uint32_t r, int32_t gap, int lane) {
     uint32_t lo = 0, n = U;  // the answer is one of [lo, lo + n]
-    while (true) {
+    while (n > 64) {
       const uint32_t step = (n + 63) / 64, i = lo + lane * step + step - 1;
-      const bool past = i >= U || at_place(off[i + 1] - base, i + 1, gap) > r;
+      const bool past = i >= U || at_place(off[min(i + 1, U)] - base, i + 1, gap) > r;
       lo += (uint32_t)__popcll(__ballot(!past)) * step;
-      if (step == 1) return min(lo, U);
       n = step;
     }
+    if (lo != at) window(lo, lane);
+    const uint32_t i = lo + lane;
+    const uint64_t past = __ballot(i >= U || at_place(end - base, i + 1, gap) > r);
+    return past ? min(lo + (uint32_t)__builtin_ctzll(past), U) : U;
   }
 };
 
@@ -349,18 +350,19 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
     return group_lds + Shape::KT * AtTile<D>::K + (buf * Shape::SUB + j) * AtTile<D>::V;
   };
 
-  const AtOffsets off(a.cache.offsets, NEW ? 0 : a.U, lane);
+  AtOffsets off(a.cache.offsets, NEW ? 0 : a.U, lane);
   const AtCut cut = NEW ? at_cut_new(a) : at_cut_packed(a, off.rows);
   const uint32_t tnp = at_up32((uint32_t)a.tn);
   const uint32_t nch = (cut.total + cut.keys - 1) / cut.keys;
   for (uint32_t x = x0; x < nch; x += xstep) {
     const uint32_t r0 = x * cut.keys, r1 = min(cut.total, r0 + cut.keys);
     for (uint32_t u = NEW ? r0 / tnp : off.find(r0, a.ck.gap, lane); u < U; ++u) {
-      const int64_t p0 = NEW ? 0 : off.start(u);
+      int64_t p0 = 0, p1 = 0;
+      if constexpr (!NEW) off.unit(u, lane, p0, p1);
       const uint32_t vs = NEW ? u * tnp : at_place(p0 - off.base, u, a.ck.gap);
       if (vs >= r1) break;
       // the piece: rows [lo, lo + np) of the unit's
-      const uint32_t len = NEW ? (uint32_t)a.tn : (uint32_t)min(off.stop(u) - p0, a.cover);
+      const uint32_t len = NEW ? (uint32_t)a.tn : (uint32_t)min(p1 - p0, a.cover);
       const uint32_t lo = max(r0, vs) - vs;
       const int np = (int)min(r1 - vs, len) - (int)lo;
       if (np <= 0) continue;  // (only what lies between units)
