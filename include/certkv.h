@@ -442,7 +442,8 @@ certkv_status certkv_read_mx(const certkv_problem* p, certkv_cache cache, int64_
  * sums and outputs, over the values that the codes stand for.  A segment longer
  * than its bound of max_rows stores CERTKV_ERANGE in *dev_status and its rows
  * past the bound are left out.  A row with no packed row to see is out = 0, lse =
- * -infinity.  The workspace is certkv_decode_cache_workspace_size(p, format, tq, 0,
+ * -infinity.  The rows of all segments by their bounds, and 64 for each unit, must
+ * be fewer than 2^31 (else CERTKV_EUNSUPPORTED; max_rows bounds them).  The workspace is certkv_decode_cache_workspace_size(p, format, tq, 0,
  * max_rows) bytes, 256-byte aligned. */
 size_t certkv_decode_cache_workspace_size(const certkv_problem* p, int32_t format, int32_t tq,
                                           int32_t tn, int32_t max_rows);
@@ -462,7 +463,8 @@ certkv_status certkv_decode_mx(const certkv_problem* p, certkv_tensor q_new, int
  *                (tn >= tq)
  * Every packed row is visible to every query.  A new row that a query does not
  * see has no part in its output, whatever it holds (a padded batch's rows may be
- * NaN).  A query that sees nothing is out = 0, lse = -infinity.  The workspace is
+ * NaN).  A query that sees nothing is out = 0, lse = -infinity.  The new rows of all
+ * units, each unit's rounded up to 32, must be fewer than 2^31.  The workspace is
  * certkv_decode_cache_workspace_size(p, cache.format, tq, tn, max_rows) bytes. */
 certkv_status certkv_decode_tree(const certkv_problem* p, certkv_tensor q_new, int32_t tq,
                                  int32_t max_rows, certkv_cache cache, certkv_tensor k_new,

@@ -504,6 +504,9 @@ def _cache_buffers(spec, fmt, tq, tn, dev, with_lse, bufs, max_rows):
     if bufs is None:
         bufs = DecodeBuffers(spec, tq, dev, with_lse=with_lse, max_rows=max_rows, tn=tn, fmt=fmt)
     assert bufs.fmt == fmt and bufs.tq == int(tq) and bufs.tn == int(tn)
+    assert bufs.out.shape == (spec.layers, spec.batch * bufs.tq, spec.kv_heads * spec.group,
+                              spec.head_dim) and bufs.out.device == dev
+    assert bufs.lse is not None or not with_lse
     return bufs
 
 
