@@ -1111,8 +1111,8 @@ struct AttendWs {
   AttendChunks ck;
   size_t ml_off, total;
 };
-static bool attend_ws_layout(const Plan& P, int32_t format, int32_t tq, int32_t tn,
-                             int32_t max_rows, AttendWs* w) {
+static bool attend_ws_layout(const Plan& P, int32_t tq, int32_t tn, int32_t max_rows,
+                             AttendWs* w) {
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const int64_t bound = decode_rows_bound(P, max_rows);
   int64_t rows = 0;  // of all segments: b_h <= n_b kept rows and the slot row
@@ -1121,7 +1121,7 @@ static bool attend_ws_layout(const Plan& P, int32_t format, int32_t tq, int32_t 
     rows += n < bound ? n : bound;
   }
   if ((int64_t)tq * P.g.G > 512) return false;
-  if (!attend_chunks(format, P.g.D, tq, P.g.G, tn, rows * P.g.L * P.g.H, P.U, &w->ck)) return false;
+  if (!attend_chunks(P.g.D, tq, P.g.G, tn, rows * P.g.L * P.g.H, P.U, &w->ck)) return false;
   const size_t part = (size_t)attend_partials(w->ck, P.U, tn) * w->ck.mp;
   w->ml_off = up(part * (size_t)P.g.D * sizeof(float));
   w->total = up(w->ml_off + part * sizeof(float2));
@@ -1135,7 +1135,7 @@ size_t certkv_decode_cache_workspace_size(const certkv_problem* p, int32_t forma
     return 0;
   if (format < CERTKV_CACHE_BF16 || format > CERTKV_CACHE_MXFP4) return 0;
   AttendWs w;
-  return attend_ws_layout(P, format, tq, tn, max_rows, &w) ? w.total : 0;
+  return attend_ws_layout(P, tq, tn, max_rows, &w) ? w.total : 0;
 }
 
 static certkv_status check_rows(const certkv_tensor& t) {
@@ -1159,7 +1159,7 @@ static certkv_status attend_impl(const certkv_problem* p, certkv_tensor q_new, i
   if (!ws) return CERTKV_EWORKSPACE;
   if (((uintptr_t)ws & 255u) != 0) return CERTKV_EINVAL;
   AttendWs W;
-  if (!attend_ws_layout(P, cache.format, tq, tn, max_rows, &W)) return CERTKV_EUNSUPPORTED;
+  if (!attend_ws_layout(P, tq, tn, max_rows, &W)) return CERTKV_EUNSUPPORTED;
   if (ws_bytes < W.total) return CERTKV_EWORKSPACE;
   if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
   AttendArgs a;

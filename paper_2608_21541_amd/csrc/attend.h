@@ -817,7 +817,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
 // TREE: with new rows.
 template <int F, int D, int SHAPE, bool TREE>
 __global__ __launch_bounds__((64 * attend_wg_waves(SHAPE)))
-__attribute__((amdgpu_waves_per_eu(attend_waves(F, D, SHAPE, TREE)))) void attend_kernel(
+__attribute__((amdgpu_waves_per_eu(attend_waves(D, SHAPE)))) void attend_kernel(
     AttendArgs a) {
   constexpr int NQ = SHAPE <= kAtTwo ? 1 : SHAPE == kAtEight ? 4 : 8;
   constexpr int QT = SHAPE == kAtOne ? 1 : 2;

@@ -3,8 +3,7 @@
 
 namespace certkv {
 
-bool attend_chunks(int format, int D, int tq, int G, int tn, int64_t rows, int64_t U,
-                   AttendChunks* c) {
+bool attend_chunks(int D, int tq, int G, int tn, int64_t rows, int64_t U, AttendChunks* c) {
   const int M = tq * G;
   // (Up to 64 rows as two groups of 32, each of which reads the cache: with two waves that
   // share their tiles 3.36M rows of mxfp8 take 300 us, so 230, the second group from L2.)
@@ -13,9 +12,12 @@ bool attend_chunks(int format, int D, int tq, int G, int tn, int64_t rows, int64
   c->qgroups = (M + held - 1) / held;
   c->mp = c->qgroups * held;
   // as many chunks as their workgroups stay resident: 256 compute units of four SIMDs
-  c->parts = 256 * 4 * attend_waves(format, D, c->shape, tn > 0) / attend_wg_waves(c->shape);
+  c->parts = 256 * 4 * attend_waves(D, c->shape) / attend_wg_waves(c->shape);
   c->parts = (c->parts + c->qgroups - 1) / c->qgroups;
-  c->gap = 64;
+  // (What a piece costs beside its tiles, in rows; one value for all shapes, though few query
+  // rows would take any.  Eight ragged sequences, 192 query rows, 64: 137 us, 256: 124, 512:
+  // 131; 32 query rows, mxfp8: 187, 178, 181; 4 query rows, mxfp4: 75, 73, 75.)
+  c->gap = 256;
   auto chunks = [&](int64_t total, int64_t least) {
     const int64_t shortest = (total + least - 1) / least;
     int64_t most = (total + kAtMaxKeys - 1) / kAtMaxKeys;

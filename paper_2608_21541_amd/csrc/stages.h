@@ -262,15 +262,11 @@ constexpr int kAtMaxKeys = 16384;  // longest: a bound on how long an fp32 sum g
 // Query rows of a workgroup: 16 or 32 of every wave (four take tiles in turn), 128 of four
 // waves, 256 of eight.
 enum { kAtOne, kAtTwo, kAtEight, kAtSixteen };
-// Waves per SIMD that the kernel of a shape leaves registers for.
-constexpr int attend_waves(int format, int D, int shape, bool tree) {
-#ifdef ATW
-  return ATW;
-#else
-  if (D == 128) return shape == kAtOne && !tree ? 3 : 2;
-  return shape == kAtOne ? 4 : shape == kAtTwo && !tree ? 3 : 2;
-#endif
-}
+// Waves per SIMD that the kernel of a shape leaves registers for, which is also how many are
+// launched.  Two have 256 registers each.  More would hide more latency, but spill where the
+// operands need them (128 dims, 32 query rows, mxfp8: 161 us with two, 273 with three; 16: 145
+// and 148); only 16 query rows of 64 dims gain (many short pieces: 36 us with four, 39 with two).
+constexpr int attend_waves(int D, int shape) { return D == 64 && shape == kAtOne ? 4 : 2; }
 // Waves of a workgroup.
 constexpr int attend_wg_waves(int shape) { return shape == kAtSixteen ? 8 : 4; }
 struct AttendChunks {
@@ -309,8 +305,7 @@ certkv_status run_attend_bf16(const AttendArgs& a, hipStream_t s);   // by forma
 certkv_status run_attend_mxfp8(const AttendArgs& a, hipStream_t s);
 certkv_status run_attend_mxfp4(const AttendArgs& a, hipStream_t s);
 // rows: of all segments together, at most.  false: too many to count.
-bool attend_chunks(int format, int D, int tq, int G, int tn, int64_t rows, int64_t U,
-                   AttendChunks* c);
+bool attend_chunks(int D, int tq, int G, int tn, int64_t rows, int64_t U, AttendChunks* c);
 
 certkv_status run_packed_from_kept(int64_t U, int32_t slot, const int64_t* kept_offsets,
                                    int64_t* packed_offsets, hipStream_t s);
