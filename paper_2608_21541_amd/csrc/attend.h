@@ -18,12 +18,21 @@
 // Codes become bf16 values, exactly, on the way from memory to the matrix unit: a
 // conversion takes the block's scale as its operand (one instruction for two codes).
 //
-// A workgroup is NQ waves, each with QT query tiles.  With up to 32 query rows (NQ = 1)
-// it is four such groups that take the tiles in turn (KS), every wave a group by itself:
-// it reads keys straight into MFMA operands, only values pass through its LDS tile, and
-// no wave waits for another until the groups are joined at the end.  With more rows its
-// waves convert the tiles together, each its share, into one pair of LDS buffers while
-// they work on the other.
+// A workgroup has the query rows of NQ waves, each with QT query tiles.  With up to 64 query
+// rows (NQ = 1, of which QT = 2 tiles are 32) it is four such groups that take the tiles in
+// turn (KS), every wave a group by itself: it reads keys straight into MFMA operands, only
+// values pass through its LDS tile, and no wave waits for another until the groups are joined
+// at the end.  With more rows (NQ = 4 or 8, QT = 2) its waves convert the tiles together, each
+// its share, two tiles to a stage, into LDS buffers ahead of those that they multiply, with
+// one barrier for a stage.
+//
+// Bounds: one to sixteen query rows, the reads (3.36M rows of 128 dims, mxfp4, 4 query rows
+// of each: 459 MB in 74 us, 6.2 TB/s; mxfp8 148); many, the issue of matrix and vector
+// instructions, of which a SIMD's matrix unit is busy 45 % of the cycles and its vector unit
+// about as many, with little of either under the other (the same rows of mxfp8, 128 query
+// rows: 353 us; 256 and as many new rows: 655 us, 1.0 PFLOP/s with the weights' second part
+// counted, where a library's plain product of 8192^3 reaches 1.2).  One layer's call is
+// latency: 6.5 us for 13.1k rows.
 #pragma once
 
 #include "mx.h"
@@ -149,7 +158,8 @@ struct AtShape {
   static constexpr int KS = NQ == 1 ? 4 : 1;
   static constexpr int NT = 64 * NQ * KS;
   static constexpr int SUB = NQ == 1 ? 1 : 2;         // tiles that a group takes at a time
-  static constexpr int KT = NQ == 1 ? 0 : 2 * SUB;    // key tiles of a group in LDS
+  static constexpr int KT = NQ == 1 ? 0 : 2 * SUB;    // key tiles of a group in LDS: half are
+                                                      // read, half written
   static constexpr int VT = NQ == 1 ? 1 : 2 * SUB;    // value tiles
   static constexpr int ROW = D + 4;                   // floats of a joined output row
   static constexpr int JOIN = KS == 1 ? 0 : 2 * KS * NQ * 16 * ROW;  // bf16 elements

@@ -5,8 +5,11 @@ namespace certkv {
 
 bool attend_chunks(int D, int tq, int G, int tn, int64_t rows, int64_t U, AttendChunks* c) {
   const int M = tq * G;
-  // (Up to 64 rows as two groups of 32, each of which reads the cache: with two waves that
-  // share their tiles 3.36M rows of mxfp8 take 300 us, so 230, the second group from L2.)
+  // By the query rows: each shape's padded rows cost as much as real ones.  (Over 3.36M rows of
+  // mxfp8: up to 64 query rows as two groups of 32, each of which reads the cache, take 230 us,
+  // the second group's reads from L2; two waves that share their tiles 300.  128 query rows
+  // with eight waves, half of them idle, 437, with four 357.  256 with eight 670, as two groups
+  // of 128 707.)
   c->shape = M <= 16 ? kAtOne : M <= 64 ? kAtTwo : M <= 128 ? kAtEight : kAtSixteen;
   const int held = c->shape == kAtOne ? 16 : c->shape == kAtTwo ? 32 : c->shape == kAtEight ? 128 : 256;
   c->qgroups = (M + held - 1) / held;
@@ -34,9 +37,12 @@ bool attend_chunks(int D, int tq, int G, int tn, int64_t rows, int64_t U, Attend
 
 constexpr int kAtJoinThreads = 256;
 
-// The partials of each (unit, query row) joined in row order: D / 4 threads fold one
+// The partials of each (unit, query row) joined in row order: with m the largest of their
+// maxima m_k, out = sum_k 2^(m_k - m) o_k / sum_k 2^(m_k - m) l_k.  D / 4 threads fold one
 // row's, four in flight; S groups of them share the partials of a row (with few rows),
-// or take a row each (S = 1).
+// or take a row each (S = 1).  Bound by the reads of the partials (256 units, 256 query rows:
+// 135 MB read and written in 27 us, 5.0 TB/s; of 192 rows and three pieces to a unit 97 MB in
+// 20 us); for one layer by their latency (5 us).
 template <int D, int S>
 __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs a) {
   constexpr int C4 = D / 4, GR = kAtJoinThreads / C4, RW = GR / S;
@@ -136,7 +142,8 @@ template <int D>
 static certkv_status launch_attend_join(const AttendArgs& a, hipStream_t s) {
   constexpr int GR = kAtJoinThreads / (D / 4);
   const int M = a.tq * a.g.G;
-  // (as for certkv_decode: the partials of few rows are dealt out, of many taken row by row)
+  // The partials of few rows are dealt out, of many taken row by row (in us, dealt and not:
+  // 256 rows 9 and 24, 1024 7 and 10, 4096 10 and 10, 8192 15 and 10).
   if (a.U * M < 8192)
     CERTKV_LAUNCH("attend_join", (attend_join_kernel<D, GR>), dim3((unsigned)a.U, (unsigned)M),
                   dim3(kAtJoinThreads), 0, s, a);

