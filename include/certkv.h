@@ -410,8 +410,8 @@ typedef struct certkv_cache {
  * values (a slot's from its fp32 k*, v*), and saturate only beyond 1.75 x 2^127
  * (mxfp8) or 1.5 x 2^127 (mxfp4).  Sources in kv_dtype, bf16 or fp32.  A
  * non-finite value sets the status word.  k_star, v_star are 16-byte aligned
- * and may be NULL under CERTKV_NO_SLOT.  Rows of the outputs past the last packed one are not
- * written. */
+ * and may be NULL under CERTKV_NO_SLOT.  Rows of the outputs past the last packed
+ * one are not written. */
 certkv_status certkv_compact_mx(const certkv_problem* p, int32_t format, certkv_tensor k,
                                 certkv_tensor v, const int64_t* kept_offsets,
                                 const int32_t* kept_idx, const float* k_star,
@@ -442,9 +442,10 @@ certkv_status certkv_read_mx(const certkv_problem* p, certkv_cache cache, int64_
  * sums and outputs, over the values that the codes stand for.  A segment longer
  * than its bound of max_rows stores CERTKV_ERANGE in *dev_status and its rows
  * past the bound are left out.  A row with no packed row to see is out = 0, lse =
- * -infinity.  The rows of all segments by their bounds, and 64 for each unit, must
- * be fewer than 2^31 (else CERTKV_EUNSUPPORTED; max_rows bounds them).  The workspace is certkv_decode_cache_workspace_size(p, format, tq, 0,
- * max_rows) bytes, 256-byte aligned. */
+ * -infinity.  The rows of all segments by their bounds, and 256 for each unit, must
+ * be fewer than 2^31 (else CERTKV_EUNSUPPORTED; max_rows bounds them).  The
+ * workspace is certkv_decode_cache_workspace_size(p, format, tq, 0, max_rows)
+ * bytes, 256-byte aligned. */
 size_t certkv_decode_cache_workspace_size(const certkv_problem* p, int32_t format, int32_t tq,
                                           int32_t tn, int32_t max_rows);
 certkv_status certkv_decode_mx(const certkv_problem* p, certkv_tensor q_new, int32_t tq,

@@ -12,9 +12,12 @@
 //   a running sum in log2 units against a reference, the row's maximum when it was
 //     last moved: only when a weight would exceed 2^8 (and the sums are rescaled);
 //   O^T += V^T P^T on the same instruction: P^T (the B operand) is the lane's own
-//     eight weights, as the bf16 of each and the bf16 of the remainder (16 bits of
-//     the fp32 weight: one bf16 alone would leave 2^-9), V^T (the A operand) comes from
-//     transposing LDS reads of the row-major value tile along the same key order.
+//     eight weights, V^T (the A operand) comes from transposing LDS reads of the
+//     row-major value tile along the same key order.
+// A weight is three bf16 whose sum it is exactly, eight of its 24 bits in each.  (Two,
+// rounded, leave an error of 2e-6 against 64 bits where fp32 sums leave 4e-7, and one
+// 1e-3; 128 query rows over 3.36M rows of mxfp8 take 433 us with three, 356 with two, and
+// 4 query rows of mxfp4 76 and 72.)
 // Codes become bf16 values, exactly, on the way from memory to the matrix unit: a
 // conversion takes the block's scale as its operand (one instruction for two codes).
 //
@@ -27,10 +30,9 @@
 // one barrier for a stage.
 //
 // Bounds: one to sixteen query rows, the reads (3.36M rows of 128 dims, mxfp4, 4 query rows
-// of each: 459 MB in 74 us, 6.2 TB/s; mxfp8 148); many, the issue of matrix and vector
-// instructions, of which a SIMD's matrix unit is busy 45 % of the cycles and its vector unit
-// about as many, with little of either under the other (the same rows of mxfp8, 128 query
-// rows: 353 us; 256 and as many new rows: 655 us, 1.0 PFLOP/s with the weights' second part
+// of each: 459 MB in 76 us, 6.0 TB/s; mxfp8: 144); many, the issue of matrix and vector
+// instructions, with little of either under the other (the same rows of mxfp8, 128 query
+// rows: 433 us; 256 and as many new rows: 795 us, 1.1 PFLOP/s with the weights' three parts
 // counted, where a library's plain product of 8192^3 reaches 1.2).  One layer's call is
 // latency: 6.5 us for 13.1k rows.
 #pragma once
@@ -42,8 +44,6 @@ namespace certkv {
 
 typedef __bf16 at_bf16x8 __attribute__((__vector_size__(8 * sizeof(__bf16))));
 typedef float at_f32x4 __attribute__((__vector_size__(4 * sizeof(float))));
-typedef __bf16 at_bf16x2 __attribute__((ext_vector_type(2)));
-typedef float at_f32x2 __attribute__((ext_vector_type(2)));
 typedef short at_s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) at_s16x4 at_lds_s16x4;
 
@@ -130,9 +130,9 @@ __device__ __forceinline__ uint4 at_bf16(const AtRaw<F, W>& r, int s, float scal
     return mx_decode8<F>(r.codes8(s), scale);
 }
 
-// Two floats to bf16 (round to nearest even), a in the low half.
-__device__ __forceinline__ uint32_t at_pack(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2){a, b}, at_bf16x2));
+// The upper halves of two floats, a's in the low half: bf16, cut off.
+__device__ __forceinline__ uint32_t at_upper(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 
 // LDS tiles: 32 rows of D bf16 in natural order.  Keys are read a 16-byte chunk per
@@ -161,6 +161,7 @@ struct AtShape {
   static constexpr int KT = NQ == 1 ? 0 : 2 * SUB;    // key tiles of a group in LDS: half are
                                                       // read, half written
   static constexpr int VT = NQ == 1 ? 1 : 2 * SUB;    // value tiles
+  static constexpr int PARTS = 3;                     // bf16 parts of a weight
   static constexpr int ROW = D + 4;                   // floats of a joined output row
   static constexpr int JOIN = KS == 1 ? 0 : 2 * KS * NQ * 16 * ROW;  // bf16 elements
   static constexpr int GROUP = KT * AtTile<D>::K + VT * AtTile<D>::V;  // bf16 elements
@@ -205,16 +206,25 @@ __device__ __forceinline__ void at_reference(AtAcc<D, QT>& a, const float most[Q
     for (int db = 0; db < D / 16; ++db) a.o[qt][db] *= alpha;
   }
 }
-// Two weights (i even) of one query tile's scores s: the bf16 of each and of the remainder.
-template <int D, int QT>
+// The parts of a query tile's weights, eight of a lane: the upper half of each, of the
+// remainder, and so on.
+template <int PARTS>
+struct AtParts {
+  uint4 p[PARTS];
+};
+// Two weights (i even) of one query tile's scores s.
+template <int D, int QT, int PARTS>
 __device__ __forceinline__ void at_weights2(AtAcc<D, QT>& a, int qt, int i, const at_f32x4 s[2],
-                                            float c2, uint4& hi, uint4& lo) {
-  const float p0 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -a.m[qt]));
-  const float p1 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][(i + 1) & 3], c2, -a.m[qt]));
+                                            float c2, AtParts<PARTS>& w) {
+  float p0 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -a.m[qt]));
+  float p1 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][(i + 1) & 3], c2, -a.m[qt]));
   a.l[qt] += p0 + p1;
-  const uint32_t h = at_pack(p0, p1);
-  (&hi.x)[i >> 1] = h;
-  (&lo.x)[i >> 1] = at_pack(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    (&w.p[k].x)[i >> 1] = at_upper(p0, p1);
+    p0 -= __uint_as_float(__float_as_uint(p0) & 0xffff0000u);
+    p1 -= __uint_as_float(__float_as_uint(p1) & 0xffff0000u);
+  }
 }
 
 // V^T of block db of 16 dims: lane c of group g is to hold dim c of the block at keys
@@ -234,24 +244,22 @@ __device__ __forceinline__ at_bf16x8 at_value_block(const uint16_t* vt, int db, 
   return __builtin_bit_cast(at_bf16x8, make_uint4(v[0].x, v[0].y, v[1].x, v[1].y));
 }
 // O^T += V^T P^T of a block.
-template <int D, int QT>
+template <int D, int QT, int PARTS>
 __device__ __forceinline__ void at_value_products(AtAcc<D, QT>& a, int db, at_bf16x8 vf,
-                                                  const uint4 hi[QT], const uint4 lo[QT]) {
+                                                  const AtParts<PARTS> w[QT]) {
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt)
-    a.o[qt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-        vf, __builtin_bit_cast(at_bf16x8, hi[qt]), a.o[qt][db], 0, 0, 0);
+  for (int k = 0; k < PARTS; ++k)
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt)
-    a.o[qt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-        vf, __builtin_bit_cast(at_bf16x8, lo[qt]), a.o[qt][db], 0, 0, 0);
+    for (int qt = 0; qt < QT; ++qt)
+      a.o[qt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          vf, __builtin_bit_cast(at_bf16x8, w[qt].p[k]), a.o[qt][db], 0, 0, 0);
 }
-template <int D, int QT>
-__device__ __forceinline__ void at_values(AtAcc<D, QT>& a, const uint16_t* vt, const uint4 hi[QT],
-                                          const uint4 lo[QT], int lane) {
+template <int D, int QT, int PARTS>
+__device__ __forceinline__ void at_values(AtAcc<D, QT>& a, const uint16_t* vt,
+                                          const AtParts<PARTS> w[QT], int lane) {
 #pragma unroll
   for (int db = 0; db < D / 16; ++db)
-    at_value_products<D, QT>(a, db, at_value_block<D>(vt, db, lane), hi, lo);
+    at_value_products<D, QT, PARTS>(a, db, at_value_block<D>(vt, db, lane), w);
 }
 
 // The packed rows' offsets, as a wave reads them: those of 64 units at a time in its lanes,
@@ -317,7 +325,7 @@ template <int F, int D, int NQ, int QT, bool NEW>
 __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, float2* ml_s,
                                             uint32_t* bad_s) {
   using Shape = AtShape<D, NQ, QT>;
-  constexpr int KS = Shape::KS, NT = Shape::NT;
+  constexpr int KS = Shape::KS, NT = Shape::NT, PARTS = Shape::PARTS;
   constexpr int BITS = F == CERTKV_CACHE_BF16 ? 16 : F == CERTKV_CACHE_MXFP8 ? 8 : 4;
   constexpr bool MX = F != CERTKV_CACHE_BF16;
   constexpr int RB = mx_row_bytes(F, D);  // bytes of a row
@@ -466,8 +474,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
       };
       // New rows whose values are not all finite (rare) are zero in the tile; their bits are
       // `bad`, and they reach only the queries that see them.
-      auto add_bad = [&](uint32_t bad, int t, const uint4 ph[QT], const uint4 pl[QT],
-                         const uint32_t seen[QT]) {
+      auto add_bad = [&](uint32_t bad, int t, const AtParts<PARTS> w[QT], const uint32_t seen[QT]) {
         while (bad) {
           const int r = __builtin_ctz(bad);
           bad &= bad - 1;
@@ -475,14 +482,16 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           const uint16_t* vrow = vn + (int64_t)(t * kAtTile + r) * a.v_new.s_token;
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) {
-            uint32_t wh = ph[qt].x, wl = pl[qt].x;  // the weight's two parts
+            float p = 0.f;  // the weight: the sum of its parts
 #pragma unroll
-            for (int e = 1; e < 4; ++e) {
-              wh = i >> 1 == e ? (&ph[qt].x)[e] : wh;
-              wl = i >> 1 == e ? (&pl[qt].x)[e] : wl;
+            for (int k = PARTS - 1; k >= 0; --k) {
+              const uint4 v = w[qt].p[k];
+              uint32_t x = i >> 1 == 1 ? v.y : v.x;
+              x = i >> 1 == 2 ? v.z : x;
+              x = i >> 1 == 3 ? v.w : x;
+              p += i & 1 ? bf16_hi(x) : bf16_lo(x);
             }
-            float w = i & 1 ? bf16_hi(wh) + bf16_hi(wl) : bf16_lo(wh) + bf16_lo(wl);
-            w = __shfl(w, src, 64);
+            p = __shfl(p, src, 64);
             const bool see = (__shfl(seen[qt], src, 64) >> i) & 1;
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) {
@@ -490,7 +499,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
               const float e[4] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y)};
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if (see) acc.o[qt][db][k] = fmaf(w, e[k], acc.o[qt][db][k]);
+                if (see) acc.o[qt][db][k] = fmaf(p, e[k], acc.o[qt][db][k]);
             }
           }
         }
@@ -537,7 +546,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                   vsr, (int)(r * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
           }
         };
-        // (new rows of 128 dims beside two query tiles: registers for either keys or values)
+        // (new rows of 128 dims beside two query tiles: registers for either keys or values; 404k
+        // packed and 26k new rows, 32 query rows: 55 us, with both ahead 56)
         constexpr bool AHEAD = !(NEW && D == 128 && QT == 2);
         if (AHEAD && kg < ntp) {
           load_keys(kg);
@@ -574,7 +584,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           if (AHEAD && t + KS < ntp) load_values(t + KS);
           mask_scores(s, t, seen);
           float most[QT];
-          uint4 ph[QT], pl[QT];
+          AtParts<PARTS> w[QT];
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) most[qt] = at_max8(s[qt]);
           at_reference<D, QT>(acc, most, c2);
@@ -582,9 +592,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
             for (int i = 0; i < 8; i += 2)
-              at_weights2<D, QT>(acc, qt, i, s[qt], c2, ph[qt], pl[qt]);
-          at_values<D, QT>(acc, vt, ph, pl, lane);
-          if constexpr (NEW) add_bad(bad, t, ph, pl, seen);
+              at_weights2<D, QT, PARTS>(acc, qt, i, s[qt], c2, w[qt]);
+          at_values<D, QT, PARTS>(acc, vt, w, lane);
+          if constexpr (NEW) add_bad(bad, t, w, seen);
           __builtin_amdgcn_wave_barrier();
         }
       } else {
@@ -693,7 +703,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                 bad = __builtin_amdgcn_readfirstlane(bad);
               }
               at_f32x4 next[QT][2];
-              uint4 ph[QT], pl[QT];
+              AtParts<PARTS> w[QT];
               at_bf16x8 vf[3];
 #pragma unroll
               for (int qt = 0; qt < QT; ++qt) next[qt][0] = next[qt][1] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
@@ -711,7 +721,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                       __builtin_bit_cast(at_bf16x8, q[qt][ks]), next[qt][kb], 0, 0, 0);
                 }
                 const int qt = pr / 4;
-                at_weights2<D, QT>(acc, qt, 2 * (pr % 4), s[qt], c2, ph[qt], pl[qt]);
+                at_weights2<D, QT, PARTS>(acc, qt, 2 * (pr % 4), s[qt], c2, w[qt]);
                 if (pr >= 4 * QT - 2)
                   vf[pr - (4 * QT - 2)] = at_value_block<D>(value_tile(t & 1, j), pr - (4 * QT - 2), lane);
                 __builtin_amdgcn_sched_barrier(0);
@@ -726,7 +736,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
               for (int db = 0; db < D / 16; ++db) {
                 if (db + 2 < D / 16)
                   vf[(db + 2) % 3] = at_value_block<D>(value_tile(t & 1, j), db + 2, lane);
-                at_value_products<D, QT>(acc, db, vf[db % 3], ph, pl);
+                at_value_products<D, QT, PARTS>(acc, db, vf[db % 3], w);
                 if constexpr (!NEW) {
 #pragma unroll
                   for (int i = 0; i < PER; ++i)
@@ -739,7 +749,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                 __builtin_amdgcn_sched_barrier(0);
               }
               __builtin_amdgcn_s_setprio(0);
-              if constexpr (NEW) add_bad(bad, t * SUB + j, ph, pl, seen);
+              if constexpr (NEW) add_bad(bad, t * SUB + j, w, seen);
               at_reference<D, QT>(acc, most, c2);
 #pragma unroll
               for (int qt = 0; qt < QT; ++qt) {

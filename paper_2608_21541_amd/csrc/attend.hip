@@ -6,10 +6,10 @@ namespace certkv {
 bool attend_chunks(int D, int tq, int G, int tn, int64_t rows, int64_t U, AttendChunks* c) {
   const int M = tq * G;
   // By the query rows: each shape's padded rows cost as much as real ones.  (Over 3.36M rows of
-  // mxfp8: up to 64 query rows as two groups of 32, each of which reads the cache, take 230 us,
-  // the second group's reads from L2; two waves that share their tiles 300.  128 query rows
-  // with eight waves, half of them idle, 437, with four 357.  256 with eight 670, as two groups
-  // of 128 707.)
+  // mxfp8: up to 64 query rows as two groups of 32, each of which reads the cache, take 288 us,
+  // the second group's reads from L2, with four waves that share their tiles 338.  128 query
+  // rows with eight waves, half of them idle, 476, with four 432.  256 with eight 770, as two
+  // groups of 128 835.)
   c->shape = M <= 16 ? kAtOne : M <= 64 ? kAtTwo : M <= 128 ? kAtEight : kAtSixteen;
   const int held = c->shape == kAtOne ? 16 : c->shape == kAtTwo ? 32 : c->shape == kAtEight ? 128 : 256;
   c->qgroups = (M + held - 1) / held;
@@ -18,8 +18,9 @@ bool attend_chunks(int D, int tq, int G, int tn, int64_t rows, int64_t U, Attend
   c->parts = 256 * 4 * attend_waves(D, c->shape) / attend_wg_waves(c->shape);
   c->parts = (c->parts + c->qgroups - 1) / c->qgroups;
   // (What a piece costs beside its tiles, in rows; one value for all shapes, though few query
-  // rows would take any.  Eight ragged sequences, 192 query rows, 64: 137 us, 256: 124, 512:
-  // 131; 32 query rows, mxfp8: 187, 178, 181; 4 query rows, mxfp4: 75, 73, 75.)
+  // rows would take any.  With weights in two parts: eight ragged sequences, 192 query rows,
+  // 64: 137 us, 256: 124, 512: 131; 32 query rows, mxfp8: 187, 178, 181; 4 query rows, mxfp4:
+  // 75, 73, 75.)
   c->gap = 256;
   auto chunks = [&](int64_t total, int64_t least) {
     const int64_t shortest = (total + least - 1) / least;

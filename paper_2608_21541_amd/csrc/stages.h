@@ -261,14 +261,14 @@ constexpr int kAtTile = 32;        // rows per tile
 // query, the attention and its join: 32 rows 20.3 us, 128 17.4, 256 17.6).
 constexpr int kAtMinKeys = 128;
 constexpr int kAtMaxKeys = 16384;  // longest: a bound on how long an fp32 sum gets
-// Query rows of a workgroup: 16 or 32 of every wave (four take tiles in turn), 128 of four
+// Query rows of a workgroup: 16 or 32 (four waves that take tiles in turn), 128 of four
 // waves, 256 of eight.
 enum { kAtOne, kAtTwo, kAtEight, kAtSixteen };
 // Waves per SIMD that the kernel of a shape leaves registers for, which is also how many are
 // launched.  Two have 256 registers each.  More would hide more latency, but spill where the
 // operands need them (128 dims, 32 query rows, mxfp8: 161 us with two, 273 with three; 16: 145
-// and 148); only 16 query rows of 64 dims gain (many short pieces: 36 us with four, 39 with two).
-constexpr int attend_waves(int D, int shape) { return D == 64 && shape == kAtOne ? 4 : 2; }
+// and 148); only 16 query rows of 64 dims gain (many short pieces: 36 us with three, 39 with two).
+constexpr int attend_waves(int D, int shape) { return D == 64 && shape == kAtOne ? 3 : 2; }
 // Waves of a workgroup.
 constexpr int attend_wg_waves(int shape) { return shape == kAtSixteen ? 8 : 4; }
 struct AttendChunks {

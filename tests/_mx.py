@@ -79,9 +79,9 @@ def attend(q, k, v, scale, seen=None):
 def bound(size, dz, rows, d):
     """What an output element may be off by, and lse: a weight is off by its logit's error
     (fp32 sums of d products, each addition by half a unit of the running sum, plus the scale,
-    the logarithm's base and the exponential: 8 more), by 2^-17 for its two bf16 parts, and
+    the logarithm's base and the exponential: 8 more; its bf16 parts sum to it exactly), and
     the sums over the rows by half a unit for each 16 of them (of at most 16384 rows in turn),
     64 more for joining parts and the division.  Halved units are 2^-24."""
     u = 2.0 ** -24
-    rel = (d + 8) * u * dz + 2.0 ** -17 + (min(rows, 16384) / 16 + 64) * u
+    rel = (d + 8) * u * dz + (min(rows, 16384) / 16 + 64) * u
     return 2 * rel[:, None] * size + 1e-30, (d + 8) * u * dz + (min(rows, 16384) / 16 + 72) * u + u * 16

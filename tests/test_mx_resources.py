@@ -19,8 +19,8 @@ KERNELS = [("cache.hip", "_ZN6certkv17compact_mx_kernelI", 96),
            ("attend.hip", "_ZN6certkv18attend_join_kernelI", 64)]
 for fmt, name in ((0, "bf16"), (1, "mxfp8"), (2, "mxfp4")):
     for tree in ((1,) if fmt == 0 else (0, 1)):
-        for d, shape, most in ((128, 0, 256 if tree else 168), (128, 1, 256), (64, 0, 128),
-                               (64, 1, 256 if tree else 168), (64, 2, 256), (64, 3, 256)):
+        for d, shape, most in ((128, 0, 256), (128, 1, 256), (64, 0, 168),
+                               (64, 1, 256), (64, 2, 256), (64, 3, 256)):
             KERNELS.append((f"attend_{name}.hip",
                             f"_ZN6certkv13attend_kernelILi{fmt}ELi{d}ELi{shape}ELb{tree}E", most))
 
