@@ -435,6 +435,10 @@ class MxCache:
         assert k.dtype == v.dtype == ks.dtype == vs.dtype == torch.uint8
         assert k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()
         assert self.offsets.dtype == torch.int64 and self.offsets.is_contiguous()
+        assert v.device == ks.device == vs.device == self.offsets.device == k.device
+        if self.pos is not None:
+            assert self.pos.dtype == torch.int32 and self.pos.is_contiguous()
+            assert self.pos.numel() >= rows and self.pos.device == k.device
         object.__setattr__(self, "_checked", True)
 
     def c_cache(self):
@@ -457,9 +461,17 @@ def compact_mx(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star, 
         rows = int(kept_offsets[-1].item()) + (spec.units if spec.slot else 0)
         cache = MxCache.empty(spec, rows, fmt, dev)
     assert k.dtype == v.dtype == spec.dtype and k.device == v.device == cache.k.device
-    assert kept_offsets.dtype == torch.int64 and kept_idx.dtype == cache.pos.dtype == torch.int32
+    shape = (spec.layers, sum(spec.seqlens), spec.kv_heads, spec.head_dim)
+    assert k.shape == shape and v.shape == shape
+    assert kept_offsets.dtype == torch.int64 and kept_idx.dtype == torch.int32
+    assert kept_offsets.is_contiguous() and kept_idx.is_contiguous()
+    assert v.device == kept_offsets.device == kept_idx.device == dev
     assert cache.offsets.numel() == kept_offsets.numel() == spec.units + 1
     assert cache.format == fmt and cache.pos is not None and cache.head_dim == spec.head_dim
+    for t in (k_star, v_star):
+        if t is not None:
+            assert t.dtype == torch.float32 and t.is_contiguous() and t.device == dev
+            assert t.numel() == spec.units * spec.head_dim
     c = cache.c_cache()
     _run(dev, "certkv_compact_mx", ctypes.byref(spec.c_problem()), c.format, _tensor(k),
          _tensor(v), kept_offsets.data_ptr(), kept_idx.data_ptr(), _ptr(k_star), _ptr(v_star), c.k,
@@ -551,6 +563,7 @@ def decode_tree(spec: ProblemSpec, q_new, cache, tq, k_new, v_new, mask=None, wi
         kp, vp, offsets = cache
         assert kp.is_contiguous() and vp.is_contiguous() and kp.shape == vp.shape
         assert kp.dtype == vp.dtype == torch.bfloat16 and kp.shape[1] == spec.head_dim
+        assert kp.device == vp.device == dev and offsets.is_contiguous()
         fmt = "bf16"
         c = _lib.Cache(_format_code(fmt), kp.data_ptr(), vp.data_ptr(), None, None,
                        offsets.data_ptr())

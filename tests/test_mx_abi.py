@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import _mx
+import paper_2608_21541_amd as ck
 from paper_2608_21541_amd import _lib
 from test_abi import FAKE, problem, tensor
 
@@ -129,3 +130,51 @@ def test_plain_quantiser():
     v, s = _mx.quantise(x, "mxfp4")
     assert s[2:, 0].tolist() == [127, 128, 27, 255]
     assert v[2, 1] == 2.0 and v[3, 0] == 8.0 and v[3, 1] == -4.0
+
+
+def _spec_and_cache(fmt="mxfp8", **other):
+    spec = ck.ProblemSpec(1, 2, 2, 64, 4, [40], dtype=torch.bfloat16)
+    cache = ck.MxCache.empty(spec, 30, fmt, "cpu")
+    for name, device in other.items():
+        setattr(cache, name, getattr(cache, name).to(device))
+    return spec, cache
+
+
+@pytest.mark.parametrize("name", ["v", "k_scales", "v_scales", "offsets", "pos"])
+def test_a_cache_is_on_one_device(name):
+    spec, cache = _spec_and_cache()
+    cache.c_cache()
+    spec, cache = _spec_and_cache(**{name: "meta"})
+    with pytest.raises(AssertionError):
+        cache.c_cache()
+
+
+@pytest.mark.parametrize("name,wrong", [
+    ("k", lambda t: t[:, :39]), ("v", lambda t: t[:, :, :1]), ("kept_idx", lambda t: t.long()),
+    ("kept_idx", lambda t: t.to("meta")), ("kept_offsets", lambda t: t.to("meta")),
+    ("kept_offsets", lambda t: t[:-1]), ("k_star", lambda t: t.double()),
+    ("v_star", lambda t: t.to("meta")), ("v_star", lambda t: t[:1])])
+def test_compact_mx_refuses_other_tensors(name, wrong):
+    spec, cache = _spec_and_cache()
+    rows = torch.zeros((1, 40, 2, 64), dtype=torch.bfloat16)
+    star = torch.zeros((2, 64))
+    a = dict(k=rows, v=rows, kept_offsets=torch.tensor([0, 14, 28]),
+             kept_idx=torch.zeros(28, dtype=torch.int32), k_star=star, v_star=star)
+    with pytest.raises(ValueError, match="expected tensors on a GPU"):  # (these would do)
+        ck.compact_mx(spec, fmt="mxfp8", cache=cache, **a)
+    a[name] = wrong(a[name])
+    with pytest.raises(AssertionError):
+        ck.compact_mx(spec, fmt="mxfp8", cache=cache, **a)
+
+
+@pytest.mark.parametrize("name", ["k", "v", "offsets", "k_new", "v_new", "mask"])
+def test_decode_tree_refuses_other_devices(name):
+    spec, _ = _spec_and_cache()
+    packed = torch.zeros((30, 64), dtype=torch.bfloat16)
+    new = torch.zeros((1, 3, 2, 64), dtype=torch.bfloat16)
+    a = dict(k=packed, v=packed, offsets=torch.tensor([0, 15, 30]), k_new=new, v_new=new,
+             mask=torch.ones((1, 2, 3), dtype=torch.bool))
+    a[name] = a[name].to("meta")
+    with pytest.raises(AssertionError):
+        ck.decode_tree(spec, torch.zeros((1, 2, 4, 64), dtype=torch.bfloat16),
+                       (a["k"], a["v"], a["offsets"]), 2, a["k_new"], a["v_new"], a["mask"])
