@@ -460,22 +460,24 @@ def compact_mx(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star, 
     if cache is None:
         rows = int(kept_offsets[-1].item()) + (spec.units if spec.slot else 0)
         cache = MxCache.empty(spec, rows, fmt, dev)
-    assert k.dtype == v.dtype == spec.dtype and k.device == v.device == cache.k.device
-    shape = (spec.layers, sum(spec.seqlens), spec.kv_heads, spec.head_dim)
-    assert k.shape == shape and v.shape == shape
+    units, d = spec.units, spec.head_dim
+    assert k.dtype == v.dtype == spec.dtype
+    assert k.shape == v.shape == (spec.layers, sum(spec.seqlens), spec.kv_heads, d)
+    assert v.device == kept_offsets.device == kept_idx.device == cache.k.device == dev
     assert kept_offsets.dtype == torch.int64 and kept_idx.dtype == torch.int32
     assert kept_offsets.is_contiguous() and kept_idx.is_contiguous()
-    assert v.device == kept_offsets.device == kept_idx.device == dev
-    assert cache.offsets.numel() == kept_offsets.numel() == spec.units + 1
-    assert cache.format == fmt and cache.pos is not None and cache.head_dim == spec.head_dim
-    for t in (k_star, v_star):
-        if t is not None:
-            assert t.dtype == torch.float32 and t.is_contiguous() and t.device == dev
-            assert t.numel() == spec.units * spec.head_dim
-    c = cache.c_cache()
-    _run(dev, "certkv_compact_mx", ctypes.byref(spec.c_problem()), c.format, _tensor(k),
-         _tensor(v), kept_offsets.data_ptr(), kept_idx.data_ptr(), _ptr(k_star), _ptr(v_star), c.k,
-         c.k_scales, c.v, c.v_scales, cache.pos.data_ptr(), c.offsets)
+    assert cache.offsets.numel() == kept_offsets.numel() == units + 1
+    assert cache.format == fmt and cache.pos is not None and cache.head_dim == d
+    if k_star is not None and v_star is not None:
+        assert k_star.dtype == v_star.dtype == torch.float32 and k_star.device == v_star.device == dev
+        assert k_star.numel() == v_star.numel() == units * d
+        assert k_star.is_contiguous() and v_star.is_contiguous()
+    if not cache._checked:
+        cache._check_tensors()
+    _run(dev, "certkv_compact_mx", ctypes.byref(spec.c_problem()), _format_code(fmt), _tensor(k),
+         _tensor(v), kept_offsets.data_ptr(), kept_idx.data_ptr(), _ptr(k_star), _ptr(v_star),
+         cache.k.data_ptr(), cache.k_scales.data_ptr(), cache.v.data_ptr(),
+         cache.v_scales.data_ptr(), cache.pos.data_ptr(), cache.offsets.data_ptr())
     return cache
 
 

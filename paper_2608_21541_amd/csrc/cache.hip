@@ -105,14 +105,20 @@ __global__ __launch_bounds__(kMxThreads) void compact_mx_kernel(
   auto seg = [&](uint32_t u) { return kept_offsets[u] + (int64_t)g.slot * u; };  // first packed row
   for (uint32_t u = blockIdx.x * kMxThreads + threadIdx.x; u <= U; u += gridDim.x * kMxThreads)
     packed_offsets[u] = seg(u);
-  const int64_t base = seg(0), rows = seg(U) - base;
+  // (up to 63 units: their ends, the rows in all and the unit of the first from one load)
+  const bool few = U < 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t s0 = few ? seg(min((uint32_t)lane, U)) : 0;
+  const int64_t base = few ? __shfl(s0, 0, 64) : seg(0);
+  const int64_t rows = (few ? __shfl(s0, (int)U, 64) : seg(U)) - base;
   const int64_t per = ((rows + gridDim.x - 1) / gridDim.x + RPS - 1) / RPS * RPS;
   const int64_t r0 = base + blockIdx.x * per, r1 = min(base + rows, r0 + per);
   if (r0 >= r1) return;
   // the unit of row r0, 64 units' ends per step
   uint32_t u = 0;
-  for (uint32_t n = U; n > 0;) {
-    const uint32_t step = (n + 63) / 64, i = u + (threadIdx.x & 63) * step + step - 1;
+  if (few) u = (uint32_t)__popcll(__ballot(lane > 0 && lane <= (int)U && s0 <= r0));
+  for (uint32_t n = few ? 0 : U; n > 0;) {
+    const uint32_t step = (n + 63) / 64, i = u + lane * step + step - 1;
     const bool past = i >= U || seg(i + 1) > r0;
     u += (uint32_t)__popcll(__ballot(!past)) * step;
     if (step == 1) break;
@@ -124,8 +130,8 @@ __global__ __launch_bounds__(kMxThreads) void compact_mx_kernel(
   // (Worked out when the unit changes: its divisions would be the time of a row.)
   int64_t end = 0, k_at = 0, v_at = 0;
   int32_t n = 0;  // source rows; 0: another launch's sequence
-  auto enter = [&]() {
-    end = seg(u + 1);
+  auto enter = [&](int64_t unit_end) {
+    end = unit_end;
     const uint32_t h = u % (uint32_t)g.H, lb = u / (uint32_t)g.H;
     const uint32_t l = lb / (uint32_t)g.B;
     const int b = (int)(lb - l * (uint32_t)g.B) - st.first;
@@ -135,7 +141,7 @@ __global__ __launch_bounds__(kMxThreads) void compact_mx_kernel(
     k_at = l * k_sl + tok * k_st + h * k_sh + ci * 8;
     v_at = l * v_sl + tok * v_st + h * v_sh + ci * 8;
   };
-  enter();
+  enter(few ? __shfl(s0, (int)u + 1, 64) : seg(u + 1));
   for (int64_t r = r0 + ri; r < r1; r += RPS * UR) {
     // The rows' sources, then the rows, in flight together; rows past the run and other
     // launches' fetch the unit's first row (or the tensor's), unused.
@@ -148,7 +154,7 @@ __global__ __launch_bounds__(kMxThreads) void compact_mx_kernel(
       const int64_t x = r + q * RPS;
       while (x >= end && u + 1 < U) {
         ++u;
-        enter();
+        enter(seg(u + 1));
       }
       unit[q] = u;
       mine[q] = x < r1 && n > 0;
