@@ -5,7 +5,7 @@
 // as mx.h says, from the source's own precision (bf16, fp32, the slot's fp32).
 // Bound by memory: 2 d values of a row are read, 2 d codes, d/16 scales and a
 // position written (1.15M rows of 16 layers, bf16 to mxfp4: 0.75 GB in 165 us,
-// 4.6 TB/s, where a large copy reaches 5.2; 13k rows of one layer 9 us, latency).
+// 4.6 TB/s, where a large copy reaches 5.2; 13k rows of one layer 8.5 us, latency).
 // D / 8 lanes take a row, eight dims each, so that a wave reads whole rows in
 // 16-byte pieces (32 for fp32) and a block's largest magnitude is two exchanges
 // within four lanes.  The packed rows of all units, one after another, are cut into
