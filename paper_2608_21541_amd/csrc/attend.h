@@ -176,11 +176,12 @@ struct AtAcc {
   at_f32x4 o[QT][D / 16];
 };
 
-// The largest of a lane's eight scores.
+// The largest of a lane's eight scores; NaN where one is (as the row's sum will be), which
+// is one instruction for three where fmaxf first has to quiet each.
 __device__ __forceinline__ float at_max8(const at_f32x4 s[2]) {
   float m = s[0][0];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i >> 2][i & 3]);
+  for (int i = 1; i < 8; ++i) m = __builtin_elementwise_maximum(m, s[i >> 2][i & 3]);
   return m;
 }
 // Before the scores become weights: where a score (raw products; c2 > 0 turns them into
@@ -722,6 +723,10 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                 }
                 const int qt = pr / 4;
                 at_weights2<D, QT, PARTS>(acc, qt, 2 * (pr % 4), s[qt], c2, w[qt]);
+                // (here, not behind the mask's branch)
+                asm volatile("" : "+v"(acc.l[qt]));
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) asm volatile("" : "+v"((&w[qt].p[k].x)[pr % 4]));
                 if (pr >= 4 * QT - 2)
                   vf[pr - (4 * QT - 2)] = at_value_block<D>(value_tile(t & 1, j), pr - (4 * QT - 2), lane);
                 __builtin_amdgcn_sched_barrier(0);
