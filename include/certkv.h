@@ -358,7 +358,8 @@ certkv_status certkv_compress(const certkv_problem* p, certkv_tensor q_win,
  *   z_i = scale <q, k_i>, out = sum_i softmax(z)_i v_i, lse = log sum_i e^z_i.
  *   q_new          [L][B*tq][Hq][d] in (kv_dtype), same stride rules as q_win
  *   max_rows       bound on the rows of any head's segment (b_h + 1), or 0 for
- *                  n_b of the longest sequence; it sizes the workspace. A
+ *                  n_b + 1 of the longest sequence (n_b under CERTKV_NO_SLOT),
+ *                  the most that a segment can have; it sizes the workspace. A
  *                  longer segment stores CERTKV_ERANGE in *dev_status and its
  *                  rows past the next multiple of 4096 are left out. The
  *                  output's bits do not depend on it

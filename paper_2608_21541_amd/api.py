@@ -324,7 +324,7 @@ def decode(spec: ProblemSpec, q_new, k_packed, v_packed, packed_offsets, tq, wit
            bufs=None, max_rows=0):
     """Attention of tq new queries per sequence (q_new [L][B*tq][Hq][d]) over the packed
     cache: out [L][B*tq][Hq][d] fp32 (and the natural-log lse [L][B*tq][Hq] with_lse).
-    max_rows bounds the rows of any head's segment (0: the longest sequence)."""
+    max_rows bounds the rows of any head's segment (0: what the longest sequence can have)."""
     L = _lib.lib()
     dev = q_new.device
     if bufs is None:

@@ -853,9 +853,11 @@ certkv_status certkv_compact(const certkv_problem* p, certkv_tensor k, certkv_te
 
 // Decode partials: [rows][d] fp32 outputs, then (on a 256-byte boundary) the
 // rows' (max, sum) pairs.
-// A segment holds b_h <= n_b - 1 kept rows plus the slot row.
+// A segment holds b_h <= n_b kept rows (the pass keeps n_b - 1 at most; given budgets
+// and the coverage mode may keep all) plus the slot row.
 static int decode_rows_bound(const Plan& P, int32_t max_rows) {
-  return (max_rows > 0 && max_rows < P.max_len) ? max_rows : P.max_len;
+  const int most = P.max_len + P.g.slot;
+  return (max_rows > 0 && max_rows < most) ? max_rows : most;
 }
 
 // Decode workspace: partials (output rows, then (max, sum) pairs), each 256-byte
