@@ -420,6 +420,19 @@ certkv_status certkv_compact_mx(const certkv_problem* p, int32_t format, certkv_
                                 void* v_codes, uint8_t* v_scales, int32_t* pos_packed,
                                 int64_t* packed_offsets, void* stream);
 
+/* certkv_compact_mx into buffers of row_capacity rows, from a kept_idx of
+ * kept_capacity entries (the kept sets' sizes are known on the device alone).
+ * Kept rows past the one and packed rows past the other are left out, neither
+ * read nor written: packed_offsets ends with the rows that are there, and
+ * CERTKV_ERANGE is stored in *dev_status. */
+certkv_status certkv_compact_mx_bounded(const certkv_problem* p, int32_t format, certkv_tensor k,
+                                        certkv_tensor v, const int64_t* kept_offsets,
+                                        const int32_t* kept_idx, int64_t kept_capacity,
+                                        const float* k_star, const float* v_star, void* k_codes,
+                                        uint8_t* k_scales, void* v_codes, uint8_t* v_scales,
+                                        int32_t* pos_packed, int64_t row_capacity,
+                                        int64_t* packed_offsets, void* stream);
+
 /* certkv_compress with a packed cache in microscaled codes, written as
  * certkv_compact_mx does.  out->k_packed and out->v_packed are not written and
  * may be NULL, out->k_star and out->v_star are 16-byte aligned; everything else

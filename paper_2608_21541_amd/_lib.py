@@ -49,7 +49,7 @@ EXPORTS = [
     "certkv_decode_clustered", "certkv_profile_enable",
     "certkv_profile_read", "certkv_profile_reset",
     "certkv_score_noalloc", "certkv_score_noalloc_max_bytes",
-    "certkv_compact_mx", "certkv_compress_mx", "certkv_read_mx",
+    "certkv_compact_mx", "certkv_compact_mx_bounded", "certkv_compress_mx", "certkv_read_mx",
     "certkv_decode_cache_workspace_size", "certkv_decode_mx", "certkv_decode_tree",
 ]
 
@@ -142,6 +142,8 @@ def lib():
     L.certkv_decode_clustered.argtypes = [P, Tensor, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp,
                                           vp, vp, vp, vp, vp, vp, sz, vp]
     L.certkv_compact_mx.argtypes = [P, i32, Tensor, Tensor] + [vp] * 11
+    L.certkv_compact_mx_bounded.argtypes = ([P, i32, Tensor, Tensor, vp, vp, i64] + [vp] * 7 +
+                                            [i64, vp, vp])
     L.certkv_compress_mx.argtypes = [P, i32, Tensor, Tensor, Tensor, vp, vp, dbl, i32,
                                      ctypes.POINTER(Outputs), vp, vp, vp, vp, vp, sz, vp]
     L.certkv_read_mx.argtypes = [P, Cache, i64, i64, i32, vp, vp, vp]

@@ -455,7 +455,7 @@ _READ_SPECS = {}
 def compact_mx(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star, fmt, cache=None):
     """compact with the packed rows quantised as they are written: an MxCache of format fmt
     ("mxfp8" or "mxfp4"), `cache` if one is given (its rows past the last packed one are left
-    as they are)."""
+    as they are; rows that it has no room for are left out, and reported in spec.status)."""
     dev = k.device
     if cache is None:
         rows = int(kept_offsets[-1].item()) + (spec.units if spec.slot else 0)
@@ -474,10 +474,11 @@ def compact_mx(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star, 
         assert k_star.is_contiguous() and v_star.is_contiguous()
     if not cache._checked:
         cache._check_tensors()
-    _run(dev, "certkv_compact_mx", ctypes.byref(spec.c_problem()), _format_code(fmt), _tensor(k),
-         _tensor(v), kept_offsets.data_ptr(), kept_idx.data_ptr(), _ptr(k_star), _ptr(v_star),
-         cache.k.data_ptr(), cache.k_scales.data_ptr(), cache.v.data_ptr(),
-         cache.v_scales.data_ptr(), cache.pos.data_ptr(), cache.offsets.data_ptr())
+    _run(dev, "certkv_compact_mx_bounded", ctypes.byref(spec.c_problem()), _format_code(fmt),
+         _tensor(k), _tensor(v), kept_offsets.data_ptr(), kept_idx.data_ptr(), kept_idx.numel(),
+         _ptr(k_star), _ptr(v_star), cache.k.data_ptr(), cache.k_scales.data_ptr(),
+         cache.v.data_ptr(), cache.v_scales.data_ptr(), cache.pos.data_ptr(), cache.rows,
+         cache.offsets.data_ptr())
     return cache
 
 
@@ -592,6 +593,7 @@ class CompressBuffers:
         slot = 1 if spec.slot else 0
         kept = spec.layers * sum(H * nk - slot * H for nk in self.n_keep)
         rows = kept + slot * U
+        self.rows = rows
         shape = (spec.layers, H, spec.total_tokens)
         dt = spec.dtype
         self.scores = torch.empty(shape, dtype=torch.float32, device=device)
@@ -650,6 +652,7 @@ def compress(spec: ProblemSpec, q_win, k, v, n_keep, alpha=0.2, steps=40, bufs=N
     if fmt is not None:
         assert bufs.mx is not None and bufs.mx.format == fmt
     if bufs.mx is not None:
+        assert bufs.mx.rows >= bufs.rows and bufs.mx.head_dim == spec.head_dim
         c = bufs.mx.c_cache()
         _run(dev, "certkv_compress_mx", ctypes.byref(bufs._p), c.format, _tensor(q_win),
              _tensor(k), _tensor(v), _ptr(lse_in), bufs._nk, float(alpha), int(steps),

@@ -1016,7 +1016,8 @@ static certkv_status check_mx_out(const MxOut& o) {
 }
 static certkv_status do_compact_mx(const Plan& P, const MxOut& o, certkv_tensor k, certkv_tensor v,
                                    const int64_t* kept_offsets, const int32_t* kept_idx,
-                                   const float* k_star, const float* v_star, int32_t* pos_packed,
+                                   int64_t kept_cap, int64_t row_cap, const float* k_star,
+                                   const float* v_star, int32_t* pos_packed,
                                    int64_t* packed_offsets, hipStream_t s) {
   CompactMxArgs a;
   a.g = P.g;
@@ -1026,6 +1027,8 @@ static certkv_status do_compact_mx(const Plan& P, const MxOut& o, certkv_tensor 
   a.v = v;
   a.kept_offsets = kept_offsets;
   a.kept_idx = kept_idx;
+  a.kept_cap = kept_cap;
+  a.row_cap = row_cap;
   a.k_star = k_star;
   a.v_star = v_star;
   a.k_codes = static_cast<uint8_t*>(o.k_codes);
@@ -1048,12 +1051,13 @@ static certkv_status do_compact_mx(const Plan& P, const MxOut& o, certkv_tensor 
   return CERTKV_OK;
 }
 
-certkv_status certkv_compact_mx(const certkv_problem* p, int32_t format, certkv_tensor k,
-                                certkv_tensor v, const int64_t* kept_offsets,
-                                const int32_t* kept_idx, const float* k_star,
-                                const float* v_star, void* k_codes, uint8_t* k_scales,
-                                void* v_codes, uint8_t* v_scales, int32_t* pos_packed,
-                                int64_t* packed_offsets, void* stream) {
+certkv_status certkv_compact_mx_bounded(const certkv_problem* p, int32_t format, certkv_tensor k,
+                                        certkv_tensor v, const int64_t* kept_offsets,
+                                        const int32_t* kept_idx, int64_t kept_capacity,
+                                        const float* k_star, const float* v_star, void* k_codes,
+                                        uint8_t* k_scales, void* v_codes, uint8_t* v_scales,
+                                        int32_t* pos_packed, int64_t row_capacity,
+                                        int64_t* packed_offsets, void* stream) {
   Plan P;
   TRY(make_plan(p, &P));
   TRY(check_tensor(k, P));
@@ -1061,11 +1065,23 @@ certkv_status certkv_compact_mx(const certkv_problem* p, int32_t format, certkv_
   const MxOut o{format, k_codes, k_scales, v_codes, v_scales};
   TRY(check_mx_out(o));
   if (!kept_offsets || !kept_idx || !pos_packed || !packed_offsets) return CERTKV_EINVAL;
+  if (kept_capacity < 0 || row_capacity < 0) return CERTKV_EINVAL;
   if (P.g.slot && (!k_star || !v_star)) return CERTKV_EINVAL;
   if (((uintptr_t)k_star & 15u) || ((uintptr_t)v_star & 15u)) return CERTKV_EINVAL;
   if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
-  return do_compact_mx(P, o, k, v, kept_offsets, kept_idx, k_star, v_star, pos_packed,
-                       packed_offsets, (hipStream_t)stream);
+  return do_compact_mx(P, o, k, v, kept_offsets, kept_idx, kept_capacity, row_capacity, k_star,
+                       v_star, pos_packed, packed_offsets, (hipStream_t)stream);
+}
+
+certkv_status certkv_compact_mx(const certkv_problem* p, int32_t format, certkv_tensor k,
+                                certkv_tensor v, const int64_t* kept_offsets,
+                                const int32_t* kept_idx, const float* k_star,
+                                const float* v_star, void* k_codes, uint8_t* k_scales,
+                                void* v_codes, uint8_t* v_scales, int32_t* pos_packed,
+                                int64_t* packed_offsets, void* stream) {
+  return certkv_compact_mx_bounded(p, format, k, v, kept_offsets, kept_idx, INT64_MAX, k_star,
+                                   v_star, k_codes, k_scales, v_codes, v_scales, pos_packed,
+                                   INT64_MAX, packed_offsets, stream);
 }
 
 static certkv_status check_cache(const certkv_cache& c, bool scales_only) {
@@ -1252,8 +1268,8 @@ static certkv_status compress_impl(const certkv_problem* p, certkv_tensor q_win,
               out->v_star, out->tail_mass, out->k_packed, out->v_packed, out->pos_packed, true, !mx,
               true, w, s));
   if (mx)
-    TRY(do_compact_mx(P, *mx, k, v, out->kept_offsets, out->kept_idx, out->k_star, out->v_star,
-                      out->pos_packed, out->packed_offsets, s));
+    TRY(do_compact_mx(P, *mx, k, v, out->kept_offsets, out->kept_idx, cap, cap + P.U * P.g.slot,
+                      out->k_star, out->v_star, out->pos_packed, out->packed_offsets, s));
   return CERTKV_OK;
 }
 

@@ -91,7 +91,7 @@ __global__ __launch_bounds__(kMxThreads) void compact_mx_kernel(
     Geo g, SeqTab st, const T* __restrict__ kc, int64_t k_sl, int64_t k_st, int64_t k_sh,
     const T* __restrict__ vc, int64_t v_sl, int64_t v_st, int64_t v_sh,
     const int64_t* __restrict__ kept_offsets, const int32_t* __restrict__ kept_idx,
-    const float* __restrict__ k_star, const float* __restrict__ v_star,
+    int64_t kept_cap, int64_t row_cap, const float* __restrict__ k_star, const float* __restrict__ v_star,
     uint8_t* __restrict__ k_codes, uint8_t* __restrict__ k_scales, uint8_t* __restrict__ v_codes,
     uint8_t* __restrict__ v_scales, int32_t* __restrict__ pos_packed,
     int64_t* __restrict__ packed_offsets) {
@@ -102,15 +102,19 @@ __global__ __launch_bounds__(kMxThreads) void compact_mx_kernel(
   // 3.4 TB/s at most.)
   constexpr int UR = 2;
   const uint32_t U = (uint32_t)(g.L * g.B * g.H);
-  auto seg = [&](uint32_t u) { return kept_offsets[u] + (int64_t)g.slot * u; };  // first packed row
-  for (uint32_t u = blockIdx.x * kMxThreads + threadIdx.x; u <= U; u += gridDim.x * kMxThreads)
-    packed_offsets[u] = seg(u);
+  // a unit's first packed row; the offsets are the caller's on the device, so kept rows
+  // past the positions given, and packed rows past the buffers, are left out and reported
+  auto seg = [&](uint32_t u) { return min(kept_offsets[u], kept_cap) + (int64_t)g.slot * u; };
+  for (uint32_t u = blockIdx.x * kMxThreads + threadIdx.x; u <= U; u += gridDim.x * kMxThreads) {
+    packed_offsets[u] = min(seg(u), row_cap);
+    if (u == U && (kept_offsets[U] > kept_cap || seg(U) > row_cap)) report_range(g);
+  }
   // (up to 63 units: their ends, the rows in all and the unit of the first from one load)
   const bool few = U < 64;
   const int lane = threadIdx.x & 63;
   const int64_t s0 = few ? seg(min((uint32_t)lane, U)) : 0;
   const int64_t base = few ? __shfl(s0, 0, 64) : seg(0);
-  const int64_t rows = (few ? __shfl(s0, (int)U, 64) : seg(U)) - base;
+  const int64_t rows = min(few ? __shfl(s0, (int)U, 64) : seg(U), row_cap) - base;
   const int64_t per = ((rows + gridDim.x - 1) / gridDim.x + RPS - 1) / RPS * RPS;
   const int64_t r0 = base + blockIdx.x * per, r1 = min(base + rows, r0 + per);
   if (r0 >= r1) return;
@@ -197,7 +201,7 @@ static certkv_status launch_compact_mx(const CompactMxArgs& a, const SeqTab& st,
   CERTKV_LAUNCH("compact_mx", (compact_mx_kernel<D, T, F>), dim3(8 * 256), dim3(kMxThreads), 0, s,
                 a.g, st, static_cast<const T*>(a.k.ptr), a.k.s_layer, a.k.s_token, a.k.s_head,
                 static_cast<const T*>(a.v.ptr), a.v.s_layer, a.v.s_token, a.v.s_head,
-                a.kept_offsets, a.kept_idx, a.k_star, a.v_star, a.k_codes, a.k_scales, a.v_codes,
+                a.kept_offsets, a.kept_idx, a.kept_cap, a.row_cap, a.k_star, a.v_star, a.k_codes, a.k_scales, a.v_codes,
                 a.v_scales, a.pos_packed, a.packed_offsets);
   return CERTKV_OK;
 }

@@ -231,6 +231,8 @@ struct CompactMxArgs {
   certkv_tensor k, v;
   const int64_t* kept_offsets;
   const int32_t* kept_idx;
+  int64_t kept_cap;             // entries of kept_idx
+  int64_t row_cap;              // rows of the outputs
   const float* k_star;          // [U][d] (not read without slot rows)
   const float* v_star;
   uint8_t* k_codes;             // [rows][d or d/2]
