@@ -457,8 +457,9 @@ certkv_status certkv_read_mx(const certkv_problem* p, certkv_cache cache, int64_
  * than its bound of max_rows stores CERTKV_ERANGE in *dev_status and its rows
  * past the bound are left out.  A row with no packed row to see is out = 0, lse =
  * -infinity.  The rows of all segments by their bounds, and 256 for each unit, must
- * be fewer than 2^31 (else CERTKV_EUNSUPPORTED; max_rows bounds them).  The
- * workspace is certkv_decode_cache_workspace_size(p, format, tq, 0, max_rows)
+ * be fewer than 2^31 (else CERTKV_EUNSUPPORTED; max_rows bounds them).  Scores
+ * may be as large as fp32 holds: <q, k_i> and scale <q, k_i> log2 e up to 2^126.
+ * The workspace is certkv_decode_cache_workspace_size(p, format, tq, 0, max_rows)
  * bytes, 256-byte aligned. */
 size_t certkv_decode_cache_workspace_size(const certkv_problem* p, int32_t format, int32_t tq,
                                           int32_t tn, int32_t max_rows);

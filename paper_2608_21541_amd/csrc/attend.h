@@ -184,22 +184,24 @@ __device__ __forceinline__ float at_max8(const at_f32x4 s[2]) {
   for (int i = 1; i < 8; ++i) m = __builtin_elementwise_maximum(m, s[i >> 2][i & 3]);
   return m;
 }
-// Before the scores become weights: where a score (raw products; c2 > 0 turns them into
-// log2 units) is more than 8 above its row's reference, as in a row's first tile, the
-// references move to the maxima and the sums are rescaled.  Rows that have seen nothing
-// keep kAtNone, under which a masked score's weight is zero.
+// Before the scores become weights: where a score (raw products; a row's factor, c2 but for
+// huge scores (ref_factor), turns them into log2 units) is more than 8 above its row's
+// reference, as in a row's first tile, the references move to the maxima and the sums are
+// rescaled.  Rows that have seen nothing keep kAtNone, under which a masked score's weight is
+// zero.
 template <int D, int QT>
 __device__ __forceinline__ void at_reference(AtAcc<D, QT>& a, const float most[QT], float c2) {
   bool above = false;
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) above |= most[qt] * c2 > a.m[qt] + kAtSlack;
+  for (int qt = 0; qt < QT; ++qt)
+    above |= most[qt] * ref_factor(a.m[qt], c2) > a.m[qt] + kAtSlack;
   if (__builtin_amdgcn_ballot_w64(above) == 0) return;
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
-    float mt = most[qt] * c2;
+    float mt = most[qt];
     mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
     mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-    const float mnew = fmaxf(a.m[qt], mt);
+    const float mnew = fmaxf(a.m[qt], ref_of(mt, c2));
     const float alpha = __builtin_amdgcn_exp2f(a.m[qt] - mnew);
     a.m[qt] = mnew;
     a.l[qt] *= alpha;
@@ -213,12 +215,12 @@ template <int PARTS>
 struct AtParts {
   uint4 p[PARTS];
 };
-// Two weights (i even) of one query tile's scores s.
+// Two weights (i even) of one query tile's scores s; c: the row's factor.
 template <int D, int QT, int PARTS>
 __device__ __forceinline__ void at_weights2(AtAcc<D, QT>& a, int qt, int i, const at_f32x4 s[2],
-                                            float c2, AtParts<PARTS>& w) {
-  float p0 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -a.m[qt]));
-  float p1 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][(i + 1) & 3], c2, -a.m[qt]));
+                                            float c, AtParts<PARTS>& w) {
+  float p0 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c, -a.m[qt]));
+  float p1 = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][(i + 1) & 3], c, -a.m[qt]));
   a.l[qt] += p0 + p1;
 #pragma unroll
   for (int k = 0; k < PARTS; ++k) {
@@ -590,10 +592,12 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
           for (int qt = 0; qt < QT; ++qt) most[qt] = at_max8(s[qt]);
           at_reference<D, QT>(acc, most, c2);
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt)
+          for (int qt = 0; qt < QT; ++qt) {
+            const float cq = ref_factor(acc.m[qt], c2);
 #pragma unroll
             for (int i = 0; i < 8; i += 2)
-              at_weights2<D, QT, PARTS>(acc, qt, i, s[qt], c2, w[qt]);
+              at_weights2<D, QT, PARTS>(acc, qt, i, s[qt], cq, w[qt]);
+          }
           at_values<D, QT, PARTS>(acc, vt, w, lane);
           if constexpr (NEW) add_bad(bad, t, w, seen);
           __builtin_amdgcn_wave_barrier();
@@ -722,7 +726,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, uint16_t* lds, 
                       __builtin_bit_cast(at_bf16x8, q[qt][ks]), next[qt][kb], 0, 0, 0);
                 }
                 const int qt = pr / 4;
-                at_weights2<D, QT, PARTS>(acc, qt, 2 * (pr % 4), s[qt], c2, w[qt]);
+                at_weights2<D, QT, PARTS>(acc, qt, 2 * (pr % 4), s[qt],
+                                          ref_factor(acc.m[qt], c2), w[qt]);
                 // (here, not behind the mask's branch)
                 asm volatile("" : "+v"(acc.l[qt]));
 #pragma unroll

@@ -136,7 +136,8 @@ __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs 
   }
   if (!fine) report_nonfinite(g);
   if (a.lse && c4 == 0)
-    a.lse[orow] = L == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(L)) * kAtLn2;
+    a.lse[orow] = L == 0.f ? -INFINITY
+                           : (ref_log2(m, g.scale * kAtLog2e) + __builtin_amdgcn_logf(L)) * kAtLn2;
 }
 
 template <int D>

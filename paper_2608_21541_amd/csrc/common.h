@@ -61,6 +61,31 @@ __device__ __forceinline__ void report_range(const Geo& g) {
   if (g.status) *g.status = CERTKV_ERANGE;
 }
 
+// The reference of a row's running softmax and its units.  A weight is 2^(c s - m) for a raw
+// product s, the row's reference m = c t for the t that was the largest when m moved last, and
+// c2 = scale log2 e for c: one fused operation, whose error at s = t is the rounding of c2 t,
+// up to |m| 2^-24.  The weights of a row share it, and it cancels with their sum, up to
+// |m| = 2^29, where it is 2^16 at most in a weight.  Beyond, it would leave fp32's range, and
+// c is the next power of two instead, whose products are exact: two different fp32 scores are
+// then 2^29 2^-24 = 32 apart or more in log2 units, so the largest ones have equal weights and
+// the others none that counts, as with c2.  The larger c keeps references in order, and their
+// magnitude tells which c they have.  (-infinity or a start value below -2^29: a row that has
+// seen nothing; any c will do.)
+constexpr float kRefLarge = 0x1p29f;
+__device__ __forceinline__ float ref_pow2(float c2) {
+  return __uint_as_float((__float_as_uint(c2) + 0x7fffffu) & 0xff800000u);
+}
+// The factor of a row whose reference is m.
+__device__ __forceinline__ float ref_factor(float m, float c2) {
+  return fabsf(m) >= kRefLarge ? ref_pow2(c2) : c2;
+}
+// The reference for the largest product t.
+__device__ __forceinline__ float ref_of(float t, float c2) { return t * ref_factor(t * c2, c2); }
+// m in log2 units.
+__device__ __forceinline__ float ref_log2(float m, float c2) {
+  return fabsf(m) >= kRefLarge ? m * (c2 / ref_pow2(c2)) : m;
+}
+
 __device__ __forceinline__ int64_t unit_index(const Geo& g, int l, int b, int h) {
   return ((int64_t)l * g.B + b) * g.H + h;
 }
