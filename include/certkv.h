@@ -371,7 +371,9 @@ certkv_status certkv_compress(const certkv_problem* p, certkv_tensor q_win,
  * sums are grouped differently beside other units: its output differs by the
  * rounding of the sums (a few 1e-6 of a row's norm), in no other way.
  * Every packed row is visible to every new query (they follow the whole
- * cache).  bf16 caches only (CERTKV_EUNSUPPORTED for fp32); tq * G <= 512.
+ * cache).  Scores may be as large as fp32 holds: <q, k_i> and
+ * scale <q, k_i> log2 e up to 2^126.
+ * bf16 caches only (CERTKV_EUNSUPPORTED for fp32); tq * G <= 512.
  * The workspace is certkv_decode_workspace_size(p, tq, max_rows) bytes,
  * 256-byte aligned; a non-finite output sets the status word. */
 size_t certkv_decode_workspace_size(const certkv_problem* p, int32_t tq,

@@ -362,8 +362,8 @@ __device__ __forceinline__ void decode_body(
   auto finish_tile = [&](int sb, int t0, dec_f32x16 s) {
     const uint16_t* vt = lds[sb][1];
     // Online softmax of the row in log2 units (z = c2 * s, c2 > 0, so the
-    // maximum is taken on the raw products).  Keys past the chunk occur only
-    // in its last tile.
+    // maximum is taken on the raw products; huge ones have another factor,
+    // ref_factor).  Keys past the chunk occur only in its last tile.
     if (t0 + kDecTile > c1) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
@@ -377,14 +377,14 @@ __device__ __forceinline__ void decode_body(
     {
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt),
                                                        false, false);
-      mt = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2;
+      mt = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
     }
     // Lazy rescaling: the reference maximum m_run moves only when some row of
     // the wave would otherwise see a weight above 2^kDecSlack; the weights
     // exp2(z - m_run) then stay below 2^kDecSlack and the partial (m_run,
     // l_run, O) is the same quantity for any reference.
-    if (__builtin_amdgcn_ballot_w64(mt > m_run + kDecSlack) != 0) {
-      const float mnew = fmaxf(m_run, mt);
+    if (__builtin_amdgcn_ballot_w64(mt * ref_factor(m_run, c2) > m_run + kDecSlack) != 0) {
+      const float mnew = fmaxf(m_run, ref_of(mt, c2));
       const float alpha = __builtin_amdgcn_exp2f(m_run - mnew);
       m_run = mnew;
       l_run *= alpha;
@@ -396,11 +396,12 @@ __device__ __forceinline__ void decode_body(
     // P^T fragments: k-step kk takes the lane's values v = 8 kk .. 8 kk + 7,
     // i.e. keys 16 kk + 8 (i/4) + 4 hh + i%4 for k-slot 8 hh + i; each weight
     // is the bf16 (round to nearest even) of p plus the bf16 of p - hi.
+    const float c = ref_factor(m_run, c2);
     DecFrag ph[2], pl[2];
 #pragma unroll
     for (int v = 0; v < 16; v += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[v], c2, -m_run));
-      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[v + 1], c2, -m_run));
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[v], c, -m_run));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[v + 1], c, -m_run));
       l_run += p0 + p1;
       const uint32_t hi = dec_pack_bf16(p0, p1);
       const float r0 = p0 - __uint_as_float(hi << 16);
@@ -649,6 +650,7 @@ __global__ __launch_bounds__(kCombThreads) void decode_combine_kernel(
     if (dd < D) at += reinterpret_cast<const float*>(&acc_s[k][0])[dd] * w;
   }
   if (CL) {
+    mx = ref_log2(mx, c2);  // (as the clusters' logits)
     float mc = mx;
     for (int gi = 0; gi < cl.m; ++gi) mc = fmaxf(mc, zc_s[gi]);
     const float a = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - mc);
@@ -687,7 +689,8 @@ __global__ __launch_bounds__(kCombThreads) void decode_combine_kernel(
   const float o = at / Lt;
   if (!isfinite(o)) report_nonfinite(g);
   out[orow * D + dd] = o;
-  if (lse && dd == 0) lse[orow] = (mx + __builtin_amdgcn_logf(Lt)) * kDecLn2;
+  if (lse && dd == 0)
+    lse[orow] = ((CL ? mx : ref_log2(mx, c2)) + __builtin_amdgcn_logf(Lt)) * kDecLn2;
 }
 
 // The combine for many rows: D / 4 threads take a row, so that a workgroup has
@@ -752,7 +755,8 @@ __global__ __launch_bounds__(kCombThreads) void decode_combine_rows_kernel(
     report_nonfinite(g);
   *reinterpret_cast<dec_f32x4_any*>(out + orow * D + 4 * c4) =
       (dec_f32x4_any){acc.x, acc.y, acc.z, acc.w};
-  if (lse && c4 == 0) lse[orow] = (m + __builtin_amdgcn_logf(L)) * kDecLn2;
+  if (lse && c4 == 0)
+    lse[orow] = (ref_log2(m, g.scale * kDecLog2e) + __builtin_amdgcn_logf(L)) * kDecLn2;
 }
 
 template <int D, int NQT>

@@ -113,3 +113,21 @@ def test_attention_over_a_cache(fmt, M, sign):
             r = slice(off[h], off[h + 1])
             compare(head(out, h), head(lse, h), q, exps, torch.cat([k[r], kn[0, :, h]]),
                     torch.cat([v[r], vn[0, :, h]]), d, ("tree", d, h))
+
+
+@pytest.mark.parametrize("M", [4, 64, 200, 512])
+@pytest.mark.parametrize("sign", [0, 1, -1])
+def test_decode_over_bf16_rows(M, sign):
+    # (its weights are two bf16, which leave 2^-18 of each)
+    for d, segs in ((128, [700, 33, 5000]), (64, [1, 257, 300])):
+        H = len(segs)
+        cache, k, v, q, exps, off = inputs("bf16", segs, d, M, BIG, sign, gen(M + d + sign))
+        spec = ck.ProblemSpec(1, H, 4, d, 1, [8000])
+        tq = M // 4
+        qd = q.view(tq, 1, 4, d).expand(tq, H, 4, d).reshape(1, tq, H * 4, d).bfloat16().to(dev())
+        out, lse = ck.decode(spec, qd, *cache, tq, with_lse=True)
+        out, lse = out[0].view(tq, H, 4, d), lse[0].view(tq, H, 4)
+        for h in range(H):
+            r = slice(off[h], off[h + 1])
+            compare(out[:, h].reshape(M, d), lse[:, h].reshape(M), q, exps, k[r], v[r], d, (d, h),
+                    2.0 ** -18)
