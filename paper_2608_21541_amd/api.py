@@ -428,6 +428,8 @@ class MxCache:
         object.__setattr__(self, name, value)
 
     def _check_tensors(self):
+        if self.format not in ("mxfp8", "mxfp4"):
+            raise ValueError(f"a microscaled cache is mxfp8 or mxfp4, not {self.format!r}")
         k, ks, v, vs = self.k, self.k_scales, self.v, self.v_scales
         rows, wide = k.shape
         scales = (rows, wide // (32 if self.format == "mxfp8" else 16))

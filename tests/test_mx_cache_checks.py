@@ -1,0 +1,28 @@
+"""What the Python binding refuses of a microscaled cache's description before any call."""
+import pytest
+import torch
+
+import paper_2608_21541_amd as ck
+
+
+def spec_and_cache(fmt, d=128, rows=30):
+    spec = ck.ProblemSpec(1, 2, 2, d, 4, [40])
+    return spec, ck.MxCache.empty(spec, rows, fmt, "cpu")
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8", None])
+@pytest.mark.parametrize("made", [False, True])
+def test_a_cache_of_another_format_is_refused(fmt, made):
+    # codes of 4 bits with the scales of their rows: as bf16 rows they would be four times as long
+    spec, c = spec_and_cache("mxfp4")
+    if made:
+        c = ck.MxCache(fmt, c.k, c.k_scales, c.v, c.v_scales, c.offsets, c.pos)
+    else:
+        c.format = fmt
+    q = torch.zeros((1, 2, 4, 128), dtype=torch.bfloat16)
+    new = torch.zeros((1, 2, 2, 128), dtype=torch.bfloat16)
+    for call in (c.c_cache, lambda: ck.decode_tree(spec, q, c, 2, new, new),
+                 lambda: ck.decode_mx(spec, q, c, 2), lambda: ck.read_mx(c)):
+        with pytest.raises((AssertionError, ValueError)) as e:
+            call()
+        assert "expected tensors on a GPU" not in str(e.value)  # (refused before that)
