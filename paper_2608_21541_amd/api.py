@@ -57,15 +57,7 @@ class ProblemSpec:
         return cu
 
     def c_problem(self):
-        # built anew when a field has changed (a call of a small problem would take longer
-        # to describe than to run)
-        key = (self.layers, self.kv_heads, self.group, self.head_dim, self.window,
-               tuple(self.seqlens), self.dtype, self.softmax_scale, self.causal, self.dry_run,
-               self.keep_window, self.statistic, self.allocator, self.slot,
-               self.status.data_ptr() if self.status is not None else None)
-        kept = self.__dict__.get("_c")
-        if kept is not None and kept[0] == key:
-            return kept[1]
+        """The problem as the C entry points take it, the caller's own to change."""
         cu = self.cu_seqlens()
         self._cu = (ctypes.c_int64 * len(cu))(*cu)  # kept alive with the spec
         dt = _dtype_code(self.dtype)
@@ -77,9 +69,22 @@ class ProblemSpec:
             "lagrangian": 0, "uniform": _lib.CERTKV_ALLOC_UNIFORM,
             "greedy": _lib.CERTKV_ALLOC_GREEDY}[self.allocator] | (
             0 if self.slot else _lib.CERTKV_NO_SLOT)
-        p = _lib.Problem(self.layers, self.batch, self.kv_heads, self.group, self.head_dim,
-                         self.window, ctypes.cast(self._cu, ctypes.POINTER(ctypes.c_int64)),
-                         dt, dt, float(self.softmax_scale), flags, key[-1])
+        return _lib.Problem(self.layers, self.batch, self.kv_heads, self.group, self.head_dim,
+                            self.window, ctypes.cast(self._cu, ctypes.POINTER(ctypes.c_int64)),
+                            dt, dt, float(self.softmax_scale), flags,
+                            self.status.data_ptr() if self.status is not None else None)
+
+    def _problem(self):
+        # c_problem for this module's calls, which do not change it: made anew when a field
+        # has changed (a call of a small problem would take longer to describe than to run)
+        key = (self.layers, self.kv_heads, self.group, self.head_dim, self.window,
+               tuple(self.seqlens), self.dtype, self.softmax_scale, self.causal, self.dry_run,
+               self.keep_window, self.statistic, self.allocator, self.slot,
+               self.status.data_ptr() if self.status is not None else None)
+        kept = self.__dict__.get("_c")
+        if kept is not None and kept[0] == key:
+            return kept[1]
+        p = self.c_problem()
         self.__dict__["_c"] = (key, p)
         return p
 
@@ -129,7 +134,7 @@ def _check(st, what):
 
 
 def workspace_size(spec: ProblemSpec, stage: int) -> int:
-    p = spec.c_problem()
+    p = spec._problem()
     return int(_lib.lib().certkv_workspace_size(ctypes.byref(p), stage))
 
 
@@ -161,7 +166,7 @@ def score(spec: ProblemSpec, q_win, k, with_ksum=False, lse_in=None, with_lse=Fa
         assert lse_in.dtype == torch.float32 and lse_in.is_contiguous()
         assert tuple(lse_in.shape) == _lse_shape(spec)
     ws, n = _workspace(spec, _lib.STAGE_SCORE, dev)
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_score(ctypes.byref(p), _tensor(q_win), _tensor(k), _ptr(lse_in), _ptr(scores),
                           _ptr(ksum), _ptr(lse), _ptr(ws), n, _stream(dev)), "certkv_score")
     out = [scores] + ([ksum] if with_ksum else []) + ([lse] if with_lse else [])
@@ -182,7 +187,7 @@ def score_noalloc(spec: ProblemSpec, q_win, k, scores, ksum=None, lse_out=None, 
         if t is not None:
             assert t.dtype == torch.float32 and t.is_contiguous()
             assert tuple(t.shape) == _lse_shape(spec)
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_score_noalloc(ctypes.byref(p), _tensor(q_win), _tensor(k), _ptr(lse_in),
                                   _ptr(scores), _ptr(ksum), _ptr(lse_out), _stream(dev)),
            "certkv_score_noalloc")
@@ -202,7 +207,7 @@ def allocate(spec: ProblemSpec, scores, v, n_keep, alpha=0.2, steps=40, with_per
         if with_vsum else None
     nk = (ctypes.c_int32 * spec.batch)(*[int(x) for x in n_keep])
     ws, n = _workspace(spec, _lib.STAGE_ALLOCATE, dev)
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_allocate(ctypes.byref(p), _ptr(scores), _tensor(v), nk, float(alpha),
                              int(steps), _ptr(budgets), _ptr(perm), _ptr(curves), _ptr(vsum),
                              _ptr(ws), n, _stream(dev)), "certkv_allocate")
@@ -224,7 +229,7 @@ def allocate_curves(spec: ProblemSpec, curves, n_keep, alpha=0.2, steps=40):
     nk = (ctypes.c_int32 * spec.batch)(*[int(x) for x in n_keep])
     # min/max scratch: same layout as the allocation stage's
     ws, n = _workspace(spec, _lib.STAGE_ALLOCATE, dev)
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_allocate_curves(ctypes.byref(p), _ptr(curves), nk, float(alpha), int(steps),
                                     _ptr(budgets), _ptr(ws), n, _stream(dev)),
            "certkv_allocate_curves")
@@ -250,7 +255,7 @@ def select(spec: ProblemSpec, scores, budgets=None, mode="budget", retain_mass=0
     mask = torch.empty((spec.layers, spec.kv_heads, spec.total_tokens), dtype=torch.uint8,
                        device=dev) if with_mask else None
     ws, n = _workspace(spec, _lib.STAGE_SELECT, dev)
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_select(ctypes.byref(p), _ptr(scores), _ptr(b), m, float(retain_mass),
                            _ptr(kept_offsets), _ptr(kept_idx), cap, _ptr(mask), _ptr(ws), n,
                            _stream(dev)), "certkv_select")
@@ -265,7 +270,7 @@ def tail_summary(spec: ProblemSpec, scores, k, v, kept_offsets, kept_idx, ksum=N
     v_star = torch.empty_like(k_star)
     tail_mass = torch.empty(spec.units, dtype=torch.float64, device=dev)
     ws, n = _workspace(spec, _lib.STAGE_TAIL, dev)
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_tail_summary(ctypes.byref(p), _ptr(scores), _tensor(k), _tensor(v),
                                  _ptr(kept_offsets), _ptr(kept_idx), _ptr(ksum), _ptr(vsum),
                                  _ptr(k_star), _ptr(v_star), _ptr(tail_mass), _ptr(ws), n,
@@ -282,7 +287,7 @@ def compact(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star):
     v_packed = torch.empty_like(k_packed)
     pos_packed = torch.empty(rows, dtype=torch.int32, device=dev)
     packed_offsets = torch.empty(spec.units + 1, dtype=torch.int64, device=dev)
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_compact(ctypes.byref(p), _tensor(k), _tensor(v), _ptr(kept_offsets),
                             _ptr(kept_idx), _ptr(k_star), _ptr(v_star), _ptr(k_packed),
                             _ptr(v_packed), _ptr(pos_packed), _ptr(packed_offsets), _stream(dev)),
@@ -291,7 +296,7 @@ def compact(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star):
 
 
 def decode_workspace_size(spec: ProblemSpec, tq: int, max_rows: int = 0) -> int:
-    p = spec.c_problem()
+    p = spec._problem()
     return int(_lib.lib().certkv_decode_workspace_size(ctypes.byref(p), int(tq), int(max_rows)))
 
 
@@ -330,7 +335,7 @@ def decode(spec: ProblemSpec, q_new, k_packed, v_packed, packed_offsets, tq, wit
     if bufs is None:
         bufs = DecodeBuffers(spec, tq, dev, with_lse=with_lse, max_rows=max_rows)
     assert k_packed.is_contiguous() and v_packed.is_contiguous()
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_decode(ctypes.byref(p), _tensor(q_new), int(tq), bufs.max_rows, _ptr(k_packed),
                            _ptr(v_packed), _ptr(packed_offsets), _ptr(bufs.out), _ptr(bufs.lse),
                            _ptr(bufs.ws), bufs.ws_bytes, _stream(dev)), "certkv_decode")
@@ -350,7 +355,7 @@ def cluster_tail(spec: ProblemSpec, k, v, perm, budgets, m):
                rk=torch.empty((U, m), dtype=torch.float32, device=dev),
                rv=torch.empty((U, m), dtype=torch.float32, device=dev),
                vmax_kept=torch.empty(U, dtype=torch.float32, device=dev))
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_cluster_tail(ctypes.byref(p), _tensor(k), _tensor(v), _ptr(perm),
                                  _ptr(budgets), int(m), _ptr(out["kbar"]), _ptr(out["vbar"]),
                                  _ptr(out["count"]), _ptr(out["rk"]), _ptr(out["rv"]),
@@ -368,7 +373,7 @@ def decode_clustered(spec: ProblemSpec, q_new, k_packed, v_packed, packed_offset
     bufs = DecodeBuffers(spec, tq, dev, with_lse=True, max_rows=max_rows)
     bound = torch.empty_like(bufs.lse)
     m = clusters["count"].shape[1]
-    p = spec.c_problem()
+    p = spec._problem()
     _check(L.certkv_decode_clustered(
         ctypes.byref(p), _tensor(q_new), int(tq), bufs.max_rows, _ptr(k_packed), _ptr(v_packed),
         _ptr(packed_offsets), int(m), _ptr(clusters["kbar"]), _ptr(clusters["vbar"]),
@@ -476,7 +481,7 @@ def compact_mx(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star, 
         assert k_star.is_contiguous() and v_star.is_contiguous()
     if not cache._checked:
         cache._check_tensors()
-    _run(dev, "certkv_compact_mx_bounded", ctypes.byref(spec.c_problem()), _format_code(fmt),
+    _run(dev, "certkv_compact_mx_bounded", ctypes.byref(spec._problem()), _format_code(fmt),
          _tensor(k), _tensor(v), kept_offsets.data_ptr(), kept_idx.data_ptr(), kept_idx.numel(),
          _ptr(k_star), _ptr(v_star), cache.k.data_ptr(), cache.k_scales.data_ptr(),
          cache.v.data_ptr(), cache.v_scales.data_ptr(), cache.pos.data_ptr(), cache.rows,
@@ -499,14 +504,14 @@ def read_mx(cache: MxCache, dtype=torch.bfloat16, first_row=0, rows=None, out=No
     assert ko.is_contiguous() and vo.is_contiguous() and ko.device == vo.device == cache.k.device
     if d not in _READ_SPECS:  # (of the problem only the row length is read)
         _READ_SPECS[d] = ProblemSpec(1, 1, 1, d, 1, [1])
-    _run(cache.k.device, "certkv_read_mx", ctypes.byref(_READ_SPECS[d].c_problem()), c,
+    _run(cache.k.device, "certkv_read_mx", ctypes.byref(_READ_SPECS[d]._problem()), c,
          int(first_row), n, _dtype_code(ko.dtype), ko.data_ptr(), vo.data_ptr())
     return ko, vo
 
 
 def decode_cache_workspace_size(spec: ProblemSpec, fmt: str, tq: int, tn: int = 0,
                                 max_rows: int = 0) -> int:
-    p = spec.c_problem()
+    p = spec._problem()
     return int(_lib.lib().certkv_decode_cache_workspace_size(
         ctypes.byref(p), _format_code(fmt), int(tq), int(tn), int(max_rows)))
 
@@ -535,7 +540,7 @@ def decode_mx(spec: ProblemSpec, q_new, cache: MxCache, tq, with_lse=False, bufs
     assert cache.head_dim == spec.head_dim and cache.offsets.numel() == spec.units + 1
     assert cache.k.device == dev
     bufs = _cache_buffers(spec, cache.format, tq, 0, dev, with_lse, bufs, max_rows)
-    _run(dev, "certkv_decode_mx", ctypes.byref(spec.c_problem()), _tensor(q_new), bufs.tq,
+    _run(dev, "certkv_decode_mx", ctypes.byref(spec._problem()), _tensor(q_new), bufs.tq,
          bufs.max_rows, cache.c_cache(), bufs.out.data_ptr(), _ptr(bufs.lse), bufs.ws.data_ptr(),
          bufs.ws_bytes)
     return (bufs.out, bufs.lse) if with_lse else bufs.out
@@ -575,7 +580,7 @@ def decode_tree(spec: ProblemSpec, q_new, cache, tq, k_new, v_new, mask=None, wi
     assert offsets.dtype == torch.int64 and offsets.numel() == spec.units + 1
     assert offsets.device == dev
     bufs = _cache_buffers(spec, fmt, tq, tn, dev, with_lse, bufs, max_rows)
-    _run(dev, "certkv_decode_tree", ctypes.byref(spec.c_problem()), _tensor(q_new), bufs.tq,
+    _run(dev, "certkv_decode_tree", ctypes.byref(spec._problem()), _tensor(q_new), bufs.tq,
          bufs.max_rows, c, _tensor(k_new), _tensor(v_new), tn, _ptr(mask), bufs.out.data_ptr(),
          _ptr(bufs.lse), bufs.ws.data_ptr(), bufs.ws_bytes)
     return (bufs.out, bufs.lse) if with_lse else bufs.out

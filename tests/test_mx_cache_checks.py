@@ -26,3 +26,19 @@ def test_a_cache_of_another_format_is_refused(fmt, made):
         with pytest.raises((AssertionError, ValueError)) as e:
             call()
         assert "expected tensors on a GPU" not in str(e.value)  # (refused before that)
+
+
+def test_a_problem_that_its_caller_changes_is_the_callers_own():
+    spec, _ = spec_and_cache("mxfp8")
+    size = lambda: ck.decode_cache_workspace_size(spec, "mxfp8", 1)  # noqa: E731
+    want = size()
+    for p in (spec.c_problem(), spec.c_problem(), ck.CompressBuffers(spec, [10], "meta")._p):
+        p.head_dim, p.cu_seqlens_host[1] = 96, 7
+        assert size() == want
+        q = spec.c_problem()
+        assert (q.head_dim, q.cu_seqlens_host[1]) == (128, 40)
+    # and a changed field is seen
+    spec.seqlens[0] = 70000
+    assert size() > want
+    spec.seqlens[0], spec.layers = 40, 3
+    assert size() > want
