@@ -108,7 +108,7 @@ def _tensor(t: torch.Tensor) -> _lib.Tensor:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(device):
@@ -429,7 +429,7 @@ class MxCache:
         return self.k.shape[1] * (1 if self.format == "mxfp8" else 2)
 
     def __setattr__(self, name, value):
-        object.__setattr__(self, "_checked", False)
+        object.__setattr__(self, "_seen", None)
         object.__setattr__(self, name, value)
 
     def _check_tensors(self):
@@ -446,14 +446,23 @@ class MxCache:
         if self.pos is not None:
             assert self.pos.dtype == torch.int32 and self.pos.is_contiguous()
             assert self.pos.numel() >= rows and self.pos.device == k.device
-        object.__setattr__(self, "_checked", True)
+
+    def _addresses(self):
+        """Of k, k_scales, v, v_scales, offsets, pos, whose shapes and types are checked when a
+        field has changed, or one of them in place: its address, or the rows that k says there
+        are (others keep the memory that they had under the same address)."""
+        k, pos = self.k, self.pos
+        seen = (k.data_ptr(), self.k_scales.data_ptr(), self.v.data_ptr(),
+                self.v_scales.data_ptr(), self.offsets.data_ptr(),
+                None if pos is None else pos.data_ptr(), k.numel())
+        if seen != self._seen:
+            self._check_tensors()
+            object.__setattr__(self, "_seen", seen)
+        return seen
 
     def c_cache(self):
-        if not self._checked:  # (again when a field has changed)
-            self._check_tensors()
-        return _lib.Cache(_format_code(self.format), self.k.data_ptr(), self.v.data_ptr(),
-                          self.k_scales.data_ptr(), self.v_scales.data_ptr(),
-                          self.offsets.data_ptr())
+        k, ks, v, vs, off, _, _ = self._addresses()
+        return _lib.Cache(_FORMATS[self.format], k, v, ks, vs, off)
 
 
 _READ_SPECS = {}
@@ -474,18 +483,16 @@ def compact_mx(spec: ProblemSpec, k, v, kept_offsets, kept_idx, k_star, v_star, 
     assert kept_offsets.dtype == torch.int64 and kept_idx.dtype == torch.int32
     assert kept_offsets.is_contiguous() and kept_idx.is_contiguous()
     assert cache.offsets.numel() == kept_offsets.numel() == units + 1
-    assert cache.format == fmt and cache.pos is not None and cache.head_dim == d
+    assert cache.format == fmt and cache.pos is not None
+    assert cache.k.shape[1] == (d if fmt == "mxfp8" else d // 2)
     if k_star is not None and v_star is not None:
         assert k_star.dtype == v_star.dtype == torch.float32 and k_star.device == v_star.device == dev
         assert k_star.numel() == v_star.numel() == units * d
         assert k_star.is_contiguous() and v_star.is_contiguous()
-    if not cache._checked:
-        cache._check_tensors()
+    c_k, c_ks, c_v, c_vs, c_off, c_pos, _ = cache._addresses()
     _run(dev, "certkv_compact_mx_bounded", ctypes.byref(spec._problem()), _format_code(fmt),
          _tensor(k), _tensor(v), kept_offsets.data_ptr(), kept_idx.data_ptr(), kept_idx.numel(),
-         _ptr(k_star), _ptr(v_star), cache.k.data_ptr(), cache.k_scales.data_ptr(),
-         cache.v.data_ptr(), cache.v_scales.data_ptr(), cache.pos.data_ptr(), cache.rows,
-         cache.offsets.data_ptr())
+         _ptr(k_star), _ptr(v_star), c_k, c_ks, c_v, c_vs, c_pos, cache.k.shape[0], c_off)
     return cache
 
 
@@ -493,10 +500,10 @@ def read_mx(cache: MxCache, dtype=torch.bfloat16, first_row=0, rows=None, out=No
     """The values (k, v) [rows][d] of a cache's rows first_row .. first_row + rows - 1 (all
     from first_row on by default), exact in bf16 and fp32; out: the two tensors to write."""
     c = cache.c_cache()
-    n, d = cache.k.shape
+    rows_all, d = cache.k.shape
     d = d if cache.format == "mxfp8" else 2 * d
-    n = n - first_row if rows is None else int(rows)
-    assert 0 <= first_row and 0 <= n and first_row + n <= cache.rows
+    n = rows_all - first_row if rows is None else int(rows)
+    assert 0 <= first_row and 0 <= n and first_row + n <= rows_all
     if out is None:
         out = [torch.empty((n, d), dtype=dtype, device=cache.k.device) for _ in range(2)]
     ko, vo = out
@@ -522,12 +529,11 @@ def _check_queries(spec, q_new, tq):
                            spec.head_dim)
 
 
-def _cache_buffers(spec, fmt, tq, tn, dev, with_lse, bufs, max_rows):
+def _cache_buffers(spec, q_new, fmt, tq, tn, dev, with_lse, bufs, max_rows):
     if bufs is None:
         bufs = DecodeBuffers(spec, tq, dev, with_lse=with_lse, max_rows=max_rows, tn=tn, fmt=fmt)
     assert bufs.fmt == fmt and bufs.tq == int(tq) and bufs.tn == int(tn)
-    assert bufs.out.shape == (spec.layers, spec.batch * bufs.tq, spec.kv_heads * spec.group,
-                              spec.head_dim) and bufs.out.device == dev
+    assert bufs.out.shape == q_new.shape and bufs.out.device == dev  # (as the queries, checked)
     assert bufs.lse is not None or not with_lse
     return bufs
 
@@ -539,7 +545,7 @@ def decode_mx(spec: ProblemSpec, q_new, cache: MxCache, tq, with_lse=False, bufs
     _check_queries(spec, q_new, tq)
     assert cache.head_dim == spec.head_dim and cache.offsets.numel() == spec.units + 1
     assert cache.k.device == dev
-    bufs = _cache_buffers(spec, cache.format, tq, 0, dev, with_lse, bufs, max_rows)
+    bufs = _cache_buffers(spec, q_new, cache.format, tq, 0, dev, with_lse, bufs, max_rows)
     _run(dev, "certkv_decode_mx", ctypes.byref(spec._problem()), _tensor(q_new), bufs.tq,
          bufs.max_rows, cache.c_cache(), bufs.out.data_ptr(), _ptr(bufs.lse), bufs.ws.data_ptr(),
          bufs.ws_bytes)
@@ -579,7 +585,7 @@ def decode_tree(spec: ProblemSpec, q_new, cache, tq, k_new, v_new, mask=None, wi
                        offsets.data_ptr())
     assert offsets.dtype == torch.int64 and offsets.numel() == spec.units + 1
     assert offsets.device == dev
-    bufs = _cache_buffers(spec, fmt, tq, tn, dev, with_lse, bufs, max_rows)
+    bufs = _cache_buffers(spec, q_new, fmt, tq, tn, dev, with_lse, bufs, max_rows)
     _run(dev, "certkv_decode_tree", ctypes.byref(spec._problem()), _tensor(q_new), bufs.tq,
          bufs.max_rows, c, _tensor(k_new), _tensor(v_new), tn, _ptr(mask), bufs.out.data_ptr(),
          _ptr(bufs.lse), bufs.ws.data_ptr(), bufs.ws_bytes)

@@ -42,3 +42,33 @@ def test_a_problem_that_its_caller_changes_is_the_callers_own():
     assert size() > want
     spec.seqlens[0], spec.layers = 40, 3
     assert size() > want
+
+
+@pytest.mark.parametrize("name", ["k", "k_scales", "v", "v_scales", "pos"])
+@pytest.mark.parametrize("how", ["data", "set"])
+def test_a_tensor_changed_in_place_is_checked_again(name, how):
+    spec, c = spec_and_cache("mxfp8")
+    c.c_cache()
+    t = getattr(c, name)
+    less = t[:29].clone()
+    if how == "data":
+        t.data = less
+    else:
+        t.set_(less.untyped_storage(), 0, less.shape, less.stride())
+    assert len(getattr(c, name)) == 29
+    with pytest.raises(AssertionError):
+        c.c_cache()
+    for other in ("k", "k_scales", "v", "v_scales"):  # and all of one size will do
+        setattr(c, other, getattr(c, other)[:29])
+    c.c_cache()
+
+
+@pytest.mark.parametrize("rows", [29, 31, 3000])
+def test_keys_resized_in_place_are_checked_again(rows):
+    spec, c = spec_and_cache("mxfp4", rows=3000)  # (room for what it grows to)
+    c = ck.MxCache("mxfp4", c.k[:30], c.k_scales[:30].clone(), c.v[:30].clone(),
+                   c.v_scales[:30].clone(), c.offsets, c.pos[:30].clone())
+    c.c_cache()
+    c.k.resize_((rows, 64))
+    with pytest.raises(AssertionError):
+        c.c_cache()
