@@ -1174,10 +1174,10 @@ static certkv_status attend_impl(const certkv_problem* p, certkv_tensor q_new, i
   if ((int64_t)tq * P.g.G > 512) return CERTKV_EUNSUPPORTED;
   TRY(check_rows(q_new));
   if (!cache.offsets || !out) return CERTKV_EINVAL;
+  AttendWs W;  // (first: such a call has no workspace that would do, its size is given as 0)
+  if (!attend_ws_layout(P, tq, tn, max_rows, &W)) return CERTKV_EUNSUPPORTED;
   if (!ws) return CERTKV_EWORKSPACE;
   if (((uintptr_t)ws & 255u) != 0) return CERTKV_EINVAL;
-  AttendWs W;
-  if (!attend_ws_layout(P, tq, tn, max_rows, &W)) return CERTKV_EUNSUPPORTED;
   if (ws_bytes < W.total) return CERTKV_EWORKSPACE;
   if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
   AttendArgs a;
