@@ -461,6 +461,10 @@ certkv_status certkv_read_mx(const certkv_problem* p, certkv_cache cache, int64_
  * -infinity.  The rows of all segments by their bounds, and 256 for each unit, must
  * be fewer than 2^31 (else CERTKV_EUNSUPPORTED; max_rows bounds them).  Scores
  * may be as large as fp32 holds: <q, k_i> and scale <q, k_i> log2 e up to 2^126.
+ * Values are summed with weights of 2^8 at most (2^24 where log2 scores are beyond
+ * 2^24) before the division, which fp32 has to hold.  The problem's dtypes are
+ * CERTKV_BF16, the queries' (else CERTKV_EUNSUPPORTED): a cache that was written
+ * from fp32 rows is attended under the same problem but for them.
  * The workspace is certkv_decode_cache_workspace_size(p, format, tq, 0, max_rows)
  * bytes, 256-byte aligned. */
 size_t certkv_decode_cache_workspace_size(const certkv_problem* p, int32_t format, int32_t tq,

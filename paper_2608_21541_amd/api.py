@@ -540,7 +540,9 @@ def _cache_buffers(spec, q_new, fmt, tq, tn, dev, with_lse, bufs, max_rows):
 
 def decode_mx(spec: ProblemSpec, q_new, cache: MxCache, tq, with_lse=False, bufs=None, max_rows=0):
     """decode over a microscaled packed cache: out [L][B*tq][Hq][d] fp32 (and the natural-log
-    lse [L][B*tq][Hq] with_lse).  bufs: DecodeBuffers(..., fmt=cache.format)."""
+    lse [L][B*tq][Hq] with_lse).  bufs: DecodeBuffers(..., fmt=cache.format).  spec.dtype is
+    bfloat16, the queries': a cache written from fp32 rows is attended under
+    dataclasses.replace(spec, dtype=torch.bfloat16)."""
     dev = q_new.device
     _check_queries(spec, q_new, tq)
     assert cache.head_dim == spec.head_dim and cache.offsets.numel() == spec.units + 1
