@@ -16,8 +16,8 @@
 //     row-major value tile along the same key order.
 // A weight is three bf16 whose sum it is exactly, eight of its 24 bits in each.  (Two,
 // rounded, leave an error of 2e-6 against 64 bits where fp32 sums leave 4e-7, and one
-// 1e-3; 128 query rows over 3.36M rows of mxfp8 take 433 us with three, 356 with two, and
-// 4 query rows of mxfp4 76 and 72.)
+// 1e-3; a call of 128 query rows over 3.36M rows of mxfp8 takes 420 us with three, 353 with
+// two, and of 4 query rows over mxfp4 87 and 83.)
 // Codes become bf16 values, exactly, on the way from memory to the matrix unit: a
 // conversion takes the block's scale as its operand (one instruction for two codes).
 //
@@ -29,12 +29,12 @@
 // its share, two tiles to a stage, into LDS buffers ahead of those that they multiply, with
 // one barrier for a stage.
 //
-// Bounds: one to sixteen query rows, the reads (3.36M rows of 128 dims, mxfp4, 4 query rows
-// of each: 459 MB in 76 us, 6.0 TB/s; mxfp8: 144); many, the issue of matrix and vector
-// instructions, with little of either under the other (the same rows of mxfp8, 128 query
-// rows: 433 us; 256 and as many new rows: 795 us, 1.1 PFLOP/s with the weights' three parts
-// counted, where a library's plain product of 8192^3 reaches 1.2).  One layer's call is
-// latency: 6.5 us for 13.1k rows.
+// Bounds (calls, the join of partials included): one to sixteen query rows, the reads (3.36M
+// rows of 128 dims, mxfp4, 4 query rows of each: 459 MB in 86 us, 5.3 TB/s; mxfp8: 890 MB in
+// 143, 6.2 TB/s); many, the issue of matrix and vector instructions, with little of either
+// under the other (the same rows of mxfp8, 128 query rows: 413 us; 256, with 64 new rows to
+// a unit: 755 us, 1.2 PFLOP/s with the weights' three parts counted, which is what a library's
+// plain product of 8192^3 reaches).  One layer's kernel is latency: 6.3 us for 13.1k rows.
 #pragma once
 
 #include "mx.h"

@@ -42,8 +42,8 @@ constexpr int kAtJoinThreads = 256;
 // maxima m_k, out = sum_k 2^(m_k - m) o_k / sum_k 2^(m_k - m) l_k.  D / 4 threads fold one
 // row's, four in flight; S groups of them share the partials of a row (with few rows),
 // or take a row each (S = 1).  Bound by the reads of the partials (256 units, 256 query rows:
-// 135 MB read and written in 27 us, 5.0 TB/s; of 192 rows and three pieces to a unit 97 MB in
-// 20 us); for one layer by their latency (5 us).
+// 135 MB read and written in 25 us, 5.5 TB/s; of 192 rows and three pieces to a unit 97 MB in
+// 21 us); for one layer by their latency (5 us).
 template <int D, int S>
 __global__ __launch_bounds__(kAtJoinThreads) void attend_join_kernel(AttendArgs a) {
   constexpr int C4 = D / 4, GR = kAtJoinThreads / C4, RW = GR / S;

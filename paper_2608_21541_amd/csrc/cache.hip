@@ -4,8 +4,9 @@
 // kept_idx[i], its last one the slot (k*, v*); each block of 32 dims is quantised
 // as mx.h says, from the source's own precision (bf16, fp32, the slot's fp32).
 // Bound by memory: 2 d values of a row are read, 2 d codes, d/16 scales and a
-// position written (1.15M rows of 16 layers, bf16 to mxfp4: 0.75 GB in 165 us,
-// 4.6 TB/s, where a large copy reaches 5.2; 13k rows of one layer 8.5 us, latency).
+// position written (1.15M rows of 16 layers, bf16 to mxfp4: 0.75 GB in 162 us,
+// 4.6 TB/s, where a large copy reaches 5.1; 173 us with other inputs each time; as many
+// rows of 64 dims from fp32 0.67 GB in 162 us; 13k rows of one layer 8.2 us, latency).
 // D / 8 lanes take a row, eight dims each, so that a wave reads whole rows in
 // 16-byte pieces (32 for fp32) and a block's largest magnitude is two exchanges
 // within four lanes.  The packed rows of all units, one after another, are cut into
@@ -223,8 +224,8 @@ certkv_status run_compact_mx(const CompactMxArgs& a, const SeqTab& st, hipStream
 // Codes back to values, eight dims a lane: the rows of both arrays are contiguous,
 // so an item is eight dims of either and its scale byte the item's quarter.  Bound
 // by the writes (mxfp8: 1.03 bytes read for 2 written as bf16), which are made
-// non-temporally (1.15M rows of mxfp4 after they were written 153 us without, 113
-// with; 3.36M of mxfp8 by themselves 510 and 504, 5.2 TB/s).  blockIdx.y: keys or values.
+// non-temporally (1.15M rows of mxfp4 after they were written 153 us without, 111
+// with; 3.36M of mxfp8 by themselves 510 and 496, 5.3 TB/s).  blockIdx.y: keys or values.
 template <int F, bool F32>
 __global__ __launch_bounds__(kMxThreads) void read_mx_kernel(
     int64_t items, const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_scales,
