@@ -334,6 +334,7 @@ def decode(spec: ProblemSpec, q_new, k_packed, v_packed, packed_offsets, tq, wit
     dev = q_new.device
     if bufs is None:
         bufs = DecodeBuffers(spec, tq, dev, with_lse=with_lse, max_rows=max_rows)
+    assert bufs.tq >= int(tq)  # (the outputs' room)
     assert k_packed.is_contiguous() and v_packed.is_contiguous()
     p = spec._problem()
     _check(L.certkv_decode(ctypes.byref(p), _tensor(q_new), int(tq), bufs.max_rows, _ptr(k_packed),

@@ -72,3 +72,12 @@ def test_keys_resized_in_place_are_checked_again(rows):
     c.k.resize_((rows, 64))
     with pytest.raises(AssertionError):
         c.c_cache()
+
+
+def test_decode_refuses_outputs_of_fewer_queries():
+    spec, _ = spec_and_cache("mxfp8")
+    packed = torch.zeros((30, 128), dtype=torch.bfloat16)
+    q = torch.zeros((1, 2, 4, 128), dtype=torch.bfloat16)
+    bufs = ck.DecodeBuffers(spec, 1, "meta")
+    with pytest.raises(AssertionError):
+        ck.decode(spec, q, packed, packed, torch.zeros(3, dtype=torch.int64), 2, bufs=bufs)
