@@ -493,6 +493,134 @@ certkv_status certkv_decode_tree(const certkv_problem* p, certkv_tensor q_new, i
                                  certkv_tensor v_new, int32_t tn, const uint8_t* mask, float* out,
                                  float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- The paged cache -------------------------------------------------------
+ * Rows of K and V in pages of a pool, `page` consecutive rows of one list to a
+ * page, so that caches grow and shrink in place: a list is a sequence, whose
+ * pages hold the rows of every layer and KV head (a prefill's cache), or one
+ * (layer, sequence, KV head) unit (after a compression every head has a length
+ * of its own).  Row r of page p for layer l and head h is the pool's row
+ *   l s_layer + p s_page + r s_row + h s_head,
+ * held as in a certkv_cache of the format: k, v [rows][d] bf16, or codes and
+ * scales.  Strides are in rows, >= 0, s_row >= 1, and s_layer = s_head = 0 for
+ * units' lists; rows that two places share are the caller's.
+ *   page         16, 32, ... or 1024 rows; num_pages * page and max_pages * page
+ *                at most 2^31 - 1024, 16 s_row rows of k below 2^31 bytes
+ *   table        [lists][max_pages] int32: the page of row i of a list is
+ *                table[list][i / page]; entries behind its last page are not read
+ *   offsets      [lists+1] int64: list r holds offsets[r+1] - offsets[r] rows
+ *                (offsets[0] may be any)
+ *   ring, free   [num_pages] int32 and [2] int64: the pages that no list has are
+ *                ring[(free[0] + i) mod num_pages], i < free[1]
+ * Lists are numbered as sequences (B) or units (L*B*H).  Of the problem the calls
+ * below read L, B, H, G, d, the dtype, the scale, CERTKV_DRY_RUN and dev_status;
+ * cu_seqlens_host and window are not read.  Page numbers, lengths and slots are
+ * the caller's on the device: what none of the pool's or the table's stands for
+ * is neither read nor written, and stores CERTKV_ERANGE in *dev_status. */
+typedef struct certkv_pages {
+  int32_t format;    /* CERTKV_CACHE_                                          */
+  int32_t page;
+  int32_t num_pages;
+  int32_t max_pages;
+  int32_t per_head;  /* 0: a list for each sequence, 1: for each unit          */
+  int64_t s_layer;
+  int64_t s_page;
+  int64_t s_row;
+  int64_t s_head;
+  void* k;           /* 16-byte aligned                                        */
+  void* v;
+  uint8_t* k_scales; /* 4-byte aligned; NULL for bf16                          */
+  uint8_t* v_scales;
+  int32_t* table;
+  int64_t* offsets;
+  int32_t* ring;
+  int64_t* free;
+} certkv_pages;
+
+/* Block table and slots of a step.  change[r] > 0 appends rows to list r, < 0
+ * drops its last rows (all of them, if it has fewer), 0 leaves it.  New pages are
+ * taken from the ring's begin, list after list; pages that hold no row any more go
+ * to its end, list after list, and are free from the next call on.
+ *   change       [lists] int32
+ *   offsets_out, free_out  [lists+1], [2] out: the lists' new offsets and the
+ *                ring's new state.  May be pages->offsets and pages->free (in
+ *                place); or others, which leaves those as they are (a step planned
+ *                beside the present one's attention)
+ *   slots        [slot_capacity] int32 out: for each appended row, lists one after
+ *                another, its slot, page number * page + row of the page.  Entries
+ *                behind the last appended row are not written
+ *   slot_offsets [lists+1] int64 out: first slot of each list's
+ * pages->table and pages->ring are written in place: entries of new pages, and the
+ * ring's behind its end.  A list whose pages would be more than max_pages, whose
+ * slots end behind slot_capacity, or whose new pages, with those of all lists
+ * before it, are more than were free, is refused: it stays as it was, its slots are
+ * -1, and CERTKV_ERANGE is stored in *dev_status.  Of pages k, v, the scales, the
+ * format and the strides are not read.  The workspace is
+ * certkv_page_workspace_size(p, pages) bytes, 256-byte aligned. */
+size_t certkv_page_workspace_size(const certkv_problem* p, const certkv_pages* pages);
+certkv_status certkv_page_resize(const certkv_problem* p, const certkv_pages* pages,
+                                 const int32_t* change, int64_t* offsets_out, int64_t* free_out,
+                                 int32_t* slots, int64_t slot_capacity, int64_t* slot_offsets,
+                                 void* ws, size_t ws_bytes, void* stream);
+
+/* Rows of new tokens written to their slots.
+ *   k, v         [L][tokens][H][d] in kv_dtype (bf16 or fp32), stride rules as for
+ *                certkv_score
+ *   tokens, tn   tn = 0 (sequences' lists): sequence after sequence, token j of
+ *                all has slots[j]; tokens behind the last slot are left out.
+ *                tn >= 1: tokens = B * tn, tn of each sequence (decode's layout),
+ *                of which list r takes its slots' number from the first on
+ *   slots, slot_offsets  as certkv_page_resize writes them, slot_count entries; a
+ *                slot of -1 leaves its row out.  Slots must differ
+ * bf16 pages: rows copied (from fp32 rounded to nearest, ties to even); mxfp8 and
+ * mxfp4: quantised as certkv_compact_mx does, a non-finite value setting the
+ * status word.  Reads of the pages nothing but their geometry. */
+certkv_status certkv_page_write(const certkv_problem* p, const certkv_pages* pages,
+                                certkv_tensor k, certkv_tensor v, int64_t tokens, int32_t tn,
+                                const int32_t* slots, int64_t slot_count,
+                                const int64_t* slot_offsets, void* stream);
+
+/* A packed cache (of certkv_compact, certkv_compact_mx or the fused passes) copied
+ * into pages of its format, units' lists: its row j, j < rows, to slots[j], as they
+ * are held.  cache.offsets is not read: the rows' order is that of slots written for
+ * lists that were empty and take packed_offsets[u+1] - packed_offsets[u] rows each.
+ * Rows behind the last slot are left out. */
+certkv_status certkv_page_adopt(const certkv_problem* p, const certkv_pages* pages,
+                                certkv_cache cache, int64_t rows, const int32_t* slots,
+                                int64_t slot_count, const int64_t* slot_offsets, void* stream);
+
+/* The rows of all lists in order, out of their pages: what certkv_compress takes
+ * (sequences' lists: k_out, v_out [L][rows][H][d], sequence after sequence) or a
+ * packed cache whose offsets are the lists' (units' lists: [rows][d]), contiguous, in
+ * out_dtype (CERTKV_BF16 or CERTKV_F32; microscaled rows are exact in both),
+ * 16-byte aligned; either may be NULL.  rows: the outputs' room; rows behind it are
+ * left out and store CERTKV_ERANGE in *dev_status, and what the lists do not fill is
+ * not written. */
+certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* pages, int64_t rows,
+                               int32_t out_dtype, void* k_out, void* v_out, void* stream);
+
+/* certkv_decode over a paged cache of any format: tq new queries per sequence, of
+ * which q_lens[b] are sequence b's own (NULL: tq), its list's last rows being the
+ * queries' own tokens: query t < n sees rows j <= len - n + t, len the rows of the
+ * unit's list.  A row that a query does not see has no part in its output, whatever
+ * it holds, and what lies behind a list's last row is not read.  A query that sees
+ * nothing (t >= n, or len - n + t < 0) is out = 0, lse = -infinity.
+ *   q_new, out, lse  as certkv_decode; tq * G <= 512
+ *   q_lens           optional [B] int32, device
+ *   max_rows         bound on the rows of any list, or 0 for max_pages * page; it
+ *                    sizes the workspace.  A longer list stores CERTKV_ERANGE in
+ *                    *dev_status and its rows past the bound are left out
+ * Rows are summed in chunks as in certkv_decode; the problem's dtypes are
+ * CERTKV_BF16, the queries'.  Tiles of 32 rows of all units, by the lists' bounds or
+ * the pool's pages, must be fewer than 2^31 (else CERTKV_EUNSUPPORTED).  The workspace
+ * is certkv_decode_paged_workspace_size(p, pages, tq, max_rows) bytes, 256-byte
+ * aligned. */
+size_t certkv_decode_paged_workspace_size(const certkv_problem* p, const certkv_pages* pages,
+                                          int32_t tq, int32_t max_rows);
+certkv_status certkv_decode_paged(const certkv_problem* p, certkv_tensor q_new, int32_t tq,
+                                  const int32_t* q_lens, int32_t max_rows,
+                                  const certkv_pages* pages, float* out, float* lse, void* ws,
+                                  size_t ws_bytes, void* stream);
+
 /* Clustered tail summaries (appendix, deterministic output-error bound for
  * clustered tail summaries): per head, the evicted ranks b_h..n-1 in the
  * pass's rank order are cut into m contiguous groups of ceil((n - b_h) / m)

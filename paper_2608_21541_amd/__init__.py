@@ -8,5 +8,6 @@ from .api import (ProblemSpec, CompressBuffers, score, score_noalloc, allocate, 
                   tail_summary, compact, compress, workspace_size, decode, DecodeBuffers,
                   decode_workspace_size, cluster_tail, decode_clustered, profile_enable, profile_reset, profile_read,
                   MxCache, compact_mx, read_mx, decode_mx, decode_tree,
-                  decode_cache_workspace_size)
+                  decode_cache_workspace_size, PagedCache, ResizeBuffers, page_resize, page_write,
+                  page_adopt, page_read, decode_paged, decode_paged_workspace_size)
 from ._lib import CertKVError, CERTKV_OK, CERTKV_ENONFINITE, CERTKV_ERANGE  # noqa: F401

@@ -51,6 +51,8 @@ EXPORTS = [
     "certkv_score_noalloc", "certkv_score_noalloc_max_bytes",
     "certkv_compact_mx", "certkv_compact_mx_bounded", "certkv_compress_mx", "certkv_read_mx",
     "certkv_decode_cache_workspace_size", "certkv_decode_mx", "certkv_decode_tree",
+    "certkv_page_workspace_size", "certkv_page_resize", "certkv_page_write", "certkv_page_adopt",
+    "certkv_page_read", "certkv_decode_paged_workspace_size", "certkv_decode_paged",
 ]
 
 
@@ -88,6 +90,28 @@ class Cache(ctypes.Structure):
         ("k_scales", ctypes.c_void_p),
         ("v_scales", ctypes.c_void_p),
         ("offsets", ctypes.c_void_p),
+    ]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [
+        ("format", ctypes.c_int32),
+        ("page", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("per_head", ctypes.c_int32),
+        ("s_layer", ctypes.c_int64),
+        ("s_page", ctypes.c_int64),
+        ("s_row", ctypes.c_int64),
+        ("s_head", ctypes.c_int64),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p),
+        ("v_scales", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+        ("offsets", ctypes.c_void_p),
+        ("ring", ctypes.c_void_p),
+        ("free", ctypes.c_void_p),
     ]
 
 
@@ -152,6 +176,16 @@ def lib():
     L.certkv_decode_mx.argtypes = [P, Tensor, i32, i32, Cache, vp, vp, vp, sz, vp]
     L.certkv_decode_tree.argtypes = [P, Tensor, i32, i32, Cache, Tensor, Tensor, i32, vp, vp, vp,
                                      vp, sz, vp]
+    G = ctypes.POINTER(Pages)
+    L.certkv_page_workspace_size.argtypes = [P, G]
+    L.certkv_page_workspace_size.restype = sz
+    L.certkv_page_resize.argtypes = [P, G, vp, vp, vp, vp, i64, vp, vp, sz, vp]
+    L.certkv_page_write.argtypes = [P, G, Tensor, Tensor, i64, i32, vp, i64, vp, vp]
+    L.certkv_page_adopt.argtypes = [P, G, Cache, i64, vp, i64, vp, vp]
+    L.certkv_page_read.argtypes = [P, G, i64, i32, vp, vp, vp]
+    L.certkv_decode_paged_workspace_size.argtypes = [P, G, i32, i32]
+    L.certkv_decode_paged_workspace_size.restype = sz
+    L.certkv_decode_paged.argtypes = [P, Tensor, i32, vp, i32, G, vp, vp, vp, sz, vp]
     L.certkv_profile_enable.argtypes = [i32]
     L.certkv_profile_read.argtypes = [vp, vp, vp, i32]
     L.certkv_profile_read.restype = i32
@@ -161,7 +195,8 @@ def lib():
         if name not in ("certkv_status_string", "certkv_workspace_size",
                         "certkv_decode_workspace_size", "certkv_profile_read",
                         "certkv_profile_reset", "certkv_score_noalloc_max_bytes",
-                        "certkv_decode_cache_workspace_size"):
+                        "certkv_decode_cache_workspace_size", "certkv_page_workspace_size",
+                        "certkv_decode_paged_workspace_size"):
             getattr(L, name).restype = i32
     _LIB = L
     return L

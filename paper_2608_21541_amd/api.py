@@ -303,10 +303,11 @@ def decode_workspace_size(spec: ProblemSpec, tq: int, max_rows: int = 0) -> int:
 class DecodeBuffers:
     """Preallocated outputs and workspace of certkv_decode (reusable); with fmt
     ("bf16", "mxfp8" or "mxfp4") those of certkv_decode_mx and certkv_decode_tree
-    over a cache of that format and tn new rows per sequence."""
+    over a cache of that format and tn new rows per sequence, with pages (a PagedCache)
+    those of certkv_decode_paged over it."""
 
     def __init__(self, spec: ProblemSpec, tq: int, device, with_lse=False, max_rows=0, tn=0,
-                 fmt=None):
+                 fmt=None, pages=None):
         self.tq = int(tq)
         self.max_rows = int(max_rows)
         rows = spec.layers * spec.batch * self.tq
@@ -317,7 +318,10 @@ class DecodeBuffers:
                                device=device) if with_lse else None
         self.tn = int(tn)
         self.fmt = fmt
-        if fmt is None:
+        self.paged = pages is not None
+        if pages is not None:
+            self.ws_bytes = decode_paged_workspace_size(spec, pages, self.tq, self.max_rows)
+        elif fmt is None:
             self.ws_bytes = decode_workspace_size(spec, self.tq, self.max_rows)
         else:
             self.ws_bytes = decode_cache_workspace_size(spec, fmt, self.tq, self.tn, self.max_rows)
@@ -592,6 +596,285 @@ def decode_tree(spec: ProblemSpec, q_new, cache, tq, k_new, v_new, mask=None, wi
     _run(dev, "certkv_decode_tree", ctypes.byref(spec._problem()), _tensor(q_new), bufs.tq,
          bufs.max_rows, c, _tensor(k_new), _tensor(v_new), tn, _ptr(mask), bufs.out.data_ptr(),
          _ptr(bufs.lse), bufs.ws.data_ptr(), bufs.ws_bytes)
+    return (bufs.out, bufs.lse) if with_lse else bufs.out
+
+
+@dataclass
+class PagedCache:
+    """Rows of K and V in pages of a pool, `page` rows of one list to a page.  Lists are
+    sequences (k, v [L][pages][page][H][d], any order of the axes in memory but for d, whose rows
+    are consecutive), or, per_head, the (layer, sequence, head) units ([pages][page][d]).  format
+    "bf16", or "mxfp8" and "mxfp4": k, v uint8 codes (of d or d/2 bytes), k_scales and v_scales
+    as them with d/32 bytes.  table [lists][max_pages] int32, offsets [lists+1] int64, ring
+    [pages] int32 and free [2] int64 (first place and number of the ring's free pages).  k and v
+    may be None where only tables are planned."""
+    format: str
+    page: int
+    k: Optional[torch.Tensor]
+    v: Optional[torch.Tensor]
+    table: torch.Tensor
+    offsets: torch.Tensor
+    k_scales: Optional[torch.Tensor] = None
+    v_scales: Optional[torch.Tensor] = None
+    ring: Optional[torch.Tensor] = None
+    free: Optional[torch.Tensor] = None
+    per_head: bool = False
+
+    @staticmethod
+    def empty(spec: ProblemSpec, num_pages: int, page: int, max_pages: int, device, fmt="bf16",
+              per_head=False, head_major=False):
+        """A pool of num_pages free pages and empty lists of max_pages pages at most.  head_major:
+        the rows of one head of a page are consecutive, not the heads of one row."""
+        code = _format_code(fmt)
+        d = spec.head_dim
+        wide, dt = {_lib.CERTKV_CACHE_BF16: (d, torch.bfloat16), _lib.CERTKV_CACHE_MXFP8:
+                    (d, torch.uint8), _lib.CERTKV_CACHE_MXFP4: (d // 2, torch.uint8)}[code]
+        L, H = spec.layers, spec.kv_heads
+
+        def pool(width, dtype):
+            if per_head:
+                return torch.empty((num_pages, page, width), dtype=dtype, device=device)
+            if head_major:
+                return torch.empty((L, num_pages, H, page, width), dtype=dtype,
+                                   device=device).transpose(2, 3)
+            return torch.empty((L, num_pages, page, H, width), dtype=dtype, device=device)
+
+        lists = spec.units if per_head else spec.batch
+        scales = [pool(d // 32, torch.uint8) if fmt != "bf16" else None for _ in range(2)]
+        return PagedCache(fmt, page, pool(wide, dt), pool(wide, dt),
+                          torch.full((lists, max_pages), -1, dtype=torch.int32, device=device),
+                          torch.zeros(lists + 1, dtype=torch.int64, device=device), *scales,
+                          ring=torch.arange(num_pages, dtype=torch.int32, device=device),
+                          free=torch.tensor([0, num_pages], device=device), per_head=per_head)
+
+    @property
+    def lists(self):
+        return self.offsets.numel() - 1
+
+    @property
+    def num_pages(self):
+        if self.k is None:
+            return self.ring.numel()
+        return self.k.shape[0 if self.per_head else 1]
+
+    def layer(self, layer: int, layers: int):
+        """Layer `layer` of `layers` as a cache of its own, of the same tensors, for calls whose
+        spec has one layer (not to be resized: its lists are the whole cache's)."""
+        assert 0 <= layer < layers
+        if self.per_head:
+            assert self.lists % layers == 0
+            n = self.lists // layers
+            rows, at = (self.k, self.v, self.k_scales, self.v_scales), slice(layer * n, layer * n + n)
+            table, offsets = self.table[at], self.offsets[layer * n:layer * n + n + 1]
+        else:
+            assert self.k.shape[0] == layers
+            rows = [t if t is None else t[layer:layer + 1]
+                    for t in (self.k, self.v, self.k_scales, self.v_scales)]
+            table, offsets = self.table, self.offsets
+        return PagedCache(self.format, self.page, rows[0], rows[1], table, offsets, rows[2], rows[3],
+                          per_head=self.per_head)
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, "_seen", None)
+        object.__setattr__(self, name, value)
+
+    def _strides(self, t, width):
+        # in rows: of layer, page, row and head
+        s = t.stride()
+        assert s[-1] == 1 and t.shape[-1] == width
+        n = len(s) - 1
+        # (an axis of one element may have any stride)
+        rows = [0 if t.shape[i] == 1 and i != n - (1 if self.per_head else 2) else s[i]
+                for i in range(n)]
+        assert all(x % width == 0 for x in rows), "rows of a page's pool are consecutive"
+        rows = [x // width for x in rows]
+        return [0, rows[0], rows[1], 0] if self.per_head else rows
+
+    def _c_pages(self, spec):
+        """The cache as the C entry points take it.  Shapes and types are checked when a field has
+        changed, or a tensor's address, or the lists and heads that the spec says there are."""
+        k, v, ks, vs, ring = self.k, self.v, self.k_scales, self.v_scales, self.ring
+        seen = (None if k is None else (k.data_ptr(), k.shape, k.stride(), v.data_ptr(), v.stride()),
+                None if ks is None else (ks.data_ptr(), ks.stride(), vs.data_ptr(), vs.stride()),
+                self.table.data_ptr(), self.table.shape, self.offsets.data_ptr(),
+                None if ring is None else (ring.data_ptr(), self.free.data_ptr()),
+                spec.layers, len(spec.seqlens), spec.kv_heads, spec.head_dim)
+        kept = self._seen
+        if kept is not None and kept[0] == seen:
+            return kept[1]
+        dev = self.table.device
+        strides = [0, 0, 1, 0]
+        if k is not None:
+            d = spec.head_dim
+            width = {"bf16": d, "mxfp8": d, "mxfp4": d // 2}.get(self.format)
+            if width is None:
+                raise ValueError(f"unsupported cache format {self.format!r}")
+            shape = (k.shape[0], self.page) if self.per_head else \
+                (spec.layers, k.shape[1], self.page, spec.kv_heads)
+            dt = torch.bfloat16 if self.format == "bf16" else torch.uint8
+            strides = self._strides(k, width)
+            for t in (k, self.v):
+                assert t.shape == shape + (width,) and t.dtype == dt and t.device == dev
+                assert self._strides(t, width) == strides
+            if self.format != "bf16":
+                for t in (self.k_scales, self.v_scales):
+                    assert t.shape == shape + (d // 32,) and t.dtype == torch.uint8
+                    assert t.device == dev and self._strides(t, d // 32) == strides
+        lists = spec.units if self.per_head else spec.batch
+        assert self.table.dtype == torch.int32 and self.table.is_contiguous()
+        assert self.table.dim() == 2 and self.table.shape[0] == lists
+        assert self.offsets.dtype == torch.int64 and self.offsets.is_contiguous()
+        assert self.offsets.numel() == lists + 1 and self.offsets.device == dev
+        if ring is not None:
+            assert ring.dtype == torch.int32 and ring.is_contiguous()
+            assert ring.numel() == self.num_pages and ring.device == dev
+            assert self.free.dtype == torch.int64 and self.free.is_contiguous()
+            assert self.free.numel() == 2 and self.free.device == dev
+        mx = k is not None and self.format != "bf16"
+        c = _lib.Pages(_format_code(self.format), int(self.page), self.num_pages,
+                       self.table.shape[1], int(self.per_head), *strides, _ptr(k), _ptr(self.v),
+                       self.k_scales.data_ptr() if mx else None,
+                       self.v_scales.data_ptr() if mx else None, self.table.data_ptr(),
+                       self.offsets.data_ptr(), _ptr(ring), _ptr(self.free))
+        object.__setattr__(self, "_seen", (seen, c))
+        return c
+
+
+class ResizeBuffers:
+    """Preallocated outputs and workspace of page_resize (reusable): slots for `capacity` appended
+    rows, and each list's first of them."""
+
+    def __init__(self, cache: PagedCache, capacity: int, device):
+        lists = cache.lists
+        self.slots = torch.empty(int(capacity), dtype=torch.int32, device=device)
+        self.slot_offsets = torch.empty(lists + 1, dtype=torch.int64, device=device)
+        one = _lib.Problem(1, lists, 1, 1, 64, 1, None, _lib.CERTKV_BF16, _lib.CERTKV_BF16, 0.0, 0,
+                           None)
+        c = _lib.Pages(0, int(cache.page), cache.num_pages, cache.table.shape[1], 0, 0, 0, 1, 0,
+                       None, None, None, None, cache.table.data_ptr(), cache.offsets.data_ptr(),
+                       None, None)
+        self.ws_bytes = int(_lib.lib().certkv_page_workspace_size(ctypes.byref(one),
+                                                                  ctypes.byref(c)))
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+
+
+def page_resize(spec: ProblemSpec, cache: PagedCache, change, bufs=None, into=None):
+    """Block table and slots of a step: change [lists] int32, the rows that each list gains (> 0:
+    pages come from the ring) or loses (< 0: its last ones; their pages go back).  Returns (slots
+    int32, one for each appended row, lists one after another, slot_offsets [lists+1] int64).  The
+    cache's offsets and free are updated in place, or, where `into` is two tensors like them, left
+    as they are and the new ones written there.  A list that does not fit is refused: its slots are
+    -1, it stays as it was, and spec.status says CERTKV_ERANGE.  bufs: ResizeBuffers (without, the
+    rows to append are counted on the device first)."""
+    dev = change.device
+    c = cache._c_pages(spec)
+    assert change.dtype == torch.int32 and change.is_contiguous()
+    assert change.numel() == cache.lists and cache.table.device == dev
+    assert cache.ring is not None and cache.free is not None
+    if bufs is None:
+        bufs = ResizeBuffers(cache, int(change.clamp(min=0).sum().item()), dev)
+    offsets, free = (cache.offsets, cache.free) if into is None else into
+    if into is not None:
+        assert offsets.dtype == free.dtype == torch.int64
+        assert offsets.shape == cache.offsets.shape and free.shape == cache.free.shape
+        assert offsets.is_contiguous() and free.is_contiguous()
+        assert offsets.device == free.device == dev
+    assert bufs.slot_offsets.numel() == cache.lists + 1 and bufs.slots.device == dev
+    slots = bufs.slots
+    _run(dev, "certkv_page_resize", ctypes.byref(spec._problem()), ctypes.byref(c),
+         change.data_ptr(), offsets.data_ptr(), free.data_ptr(), slots.data_ptr(), slots.numel(),
+         bufs.slot_offsets.data_ptr(), bufs.ws.data_ptr(), bufs.ws_bytes)
+    return slots, bufs.slot_offsets
+
+
+def _check_slots(cache, slots, slot_offsets, dev):
+    assert slots.dtype == torch.int32 and slots.is_contiguous() and slots.device == dev
+    assert slot_offsets.dtype == torch.int64 and slot_offsets.is_contiguous()
+    assert slot_offsets.numel() == cache.lists + 1 and slot_offsets.device == dev
+
+
+def page_write(spec: ProblemSpec, cache: PagedCache, k, v, slots, slot_offsets, tn=0):
+    """Rows of new tokens to their slots (of page_resize): k, v [L][tokens][H][d] in spec.dtype,
+    sequence after sequence, or, with tn, tn tokens of each sequence, of which a list takes as many
+    as it has slots."""
+    dev = k.device
+    c = cache._c_pages(spec)
+    tokens = k.shape[1]
+    assert k.shape == v.shape == (spec.layers, tokens, spec.kv_heads, spec.head_dim)
+    assert k.dtype == v.dtype == spec.dtype and v.device == dev and cache.k.device == dev
+    _check_slots(cache, slots, slot_offsets, dev)
+    _run(dev, "certkv_page_write", ctypes.byref(spec._problem()), ctypes.byref(c), _tensor(k),
+         _tensor(v), tokens, int(tn), slots.data_ptr(), slots.numel(), slot_offsets.data_ptr())
+
+
+def page_adopt(spec: ProblemSpec, cache: PagedCache, packed, slots, slot_offsets):
+    """A packed cache's rows to the slots of lists (units') that take them whole: an MxCache, or
+    (k_packed, v_packed, packed_offsets) of a bf16 one, of the pages' format."""
+    c = cache._c_pages(spec)
+    if isinstance(packed, MxCache):
+        src, rows, d, dev = packed.c_cache(), packed.rows, packed.head_dim, packed.k.device
+        assert packed.format == cache.format
+    else:
+        k, v = packed[0], packed[1]
+        assert k.is_contiguous() and v.is_contiguous() and k.shape == v.shape
+        assert k.dtype == v.dtype == torch.bfloat16 and v.device == k.device
+        assert cache.format == "bf16"
+        (rows, d), dev = k.shape, k.device
+        src = _lib.Cache(_lib.CERTKV_CACHE_BF16, k.data_ptr(), v.data_ptr(), None, None, None)
+    assert d == spec.head_dim and cache.k.device == dev
+    _check_slots(cache, slots, slot_offsets, dev)
+    _run(dev, "certkv_page_adopt", ctypes.byref(spec._problem()), ctypes.byref(c), src, rows,
+         slots.data_ptr(), slots.numel(), slot_offsets.data_ptr())
+
+
+def page_read(spec: ProblemSpec, cache: PagedCache, dtype=torch.bfloat16, rows=None, out=None):
+    """The rows of all lists, out of their pages: (k, v) [L][rows][H][d], as compress takes them, or
+    of units' lists [rows][d], a packed cache.  rows: their number (None: asked of the device);
+    out: the two tensors to write, whose rows past the lists' last are left as they are."""
+    c = cache._c_pages(spec)
+    dev = cache.k.device
+    if out is None:
+        n = int((cache.offsets[-1] - cache.offsets[0]).item()) if rows is None else int(rows)
+        shape = (n, spec.head_dim) if cache.per_head else \
+            (spec.layers, n, spec.kv_heads, spec.head_dim)
+        out = [torch.empty(shape, dtype=dtype, device=dev) for _ in range(2)]
+    ko, vo = out
+    n = ko.shape[0 if cache.per_head else 1]
+    shape = (n, spec.head_dim) if cache.per_head else (spec.layers, n, spec.kv_heads, spec.head_dim)
+    assert ko.shape == vo.shape == shape and ko.dtype == vo.dtype
+    assert ko.is_contiguous() and vo.is_contiguous() and ko.device == vo.device == dev
+    _run(dev, "certkv_page_read", ctypes.byref(spec._problem()), ctypes.byref(c), n,
+         _dtype_code(ko.dtype), ko.data_ptr(), vo.data_ptr())
+    return ko, vo
+
+
+def decode_paged_workspace_size(spec: ProblemSpec, cache: PagedCache, tq: int,
+                                max_rows: int = 0) -> int:
+    return int(_lib.lib().certkv_decode_paged_workspace_size(
+        ctypes.byref(spec._problem()), ctypes.byref(cache._c_pages(spec)), int(tq), int(max_rows)))
+
+
+def decode_paged(spec: ProblemSpec, q_new, cache: PagedCache, tq, q_lens=None, with_lse=False,
+                 bufs=None, max_rows=0):
+    """decode over a paged cache, whose lists' last rows are the new tokens' own: query t of
+    sequence b's n = q_lens[b] (int32 [B]; None: tq) sees the rows up to len - n + t.  Returns out
+    [L][B*tq][Hq][d] fp32 (and the natural-log lse [L][B*tq][Hq] with_lse); a query that sees
+    nothing (t >= n, an empty list) is out 0, lse -inf.  bufs: DecodeBuffers(..., pages=cache)."""
+    dev = q_new.device
+    _check_queries(spec, q_new, tq)
+    c = cache._c_pages(spec)
+    assert cache.k.device == dev
+    if q_lens is not None:
+        assert q_lens.dtype == torch.int32 and q_lens.is_contiguous()
+        assert q_lens.shape == (spec.batch,) and q_lens.device == dev
+    if bufs is None:
+        bufs = DecodeBuffers(spec, tq, dev, with_lse=with_lse, max_rows=max_rows, pages=cache)
+    assert bufs.paged and bufs.tq == int(tq)
+    assert bufs.out.shape == q_new.shape and bufs.out.device == dev
+    assert bufs.lse is not None or not with_lse
+    _run(dev, "certkv_decode_paged", ctypes.byref(spec._problem()), _tensor(q_new), bufs.tq,
+         _ptr(q_lens), bufs.max_rows, ctypes.byref(c), bufs.out.data_ptr(), _ptr(bufs.lse),
+         bufs.ws.data_ptr(), bufs.ws_bytes)
     return (bufs.out, bufs.lse) if with_lse else bufs.out
 
 

@@ -6,7 +6,7 @@
 #include <string>
 #include <vector>
 
-#include "mx.h"
+#include "paged.h"
 #include "stages.h"
 
 namespace certkv {
@@ -1222,6 +1222,259 @@ certkv_status certkv_decode_tree(const certkv_problem* p, certkv_tensor q_new, i
     if (st > (int64_t)0x7FFFFF00 / tn) return CERTKV_EUNSUPPORTED;
   return attend_impl(p, q_new, tq, max_rows, cache, k_new, v_new, tn, mask, out, lse, ws, ws_bytes,
                      stream);
+}
+
+// ---- the paged cache ----------------------------------------------------------
+
+// Rows of a pool or a list at most: slots and rows are counted in 31 bits.
+constexpr int64_t kPgMostRows = ((int64_t)1 << 31) - 1024;
+
+// What the paged calls read of a problem.  (make_plan works out the pass's launches, by sequence.)
+static certkv_status page_problem(const certkv_problem* p, Geo* g) {
+  if (!p) return CERTKV_EINVAL;
+  if (p->num_layers < 1 || p->batch < 1 || p->num_kv_heads < 1 || p->group < 1)
+    return CERTKV_EINVAL;
+  if (p->num_kv_heads > 64 || p->num_layers > 65535) return CERTKV_EUNSUPPORTED;
+  if (p->head_dim != 64 && p->head_dim != 128) return CERTKV_EUNSUPPORTED;
+  if (p->q_dtype != p->kv_dtype) return CERTKV_EUNSUPPORTED;
+  if (p->kv_dtype != CERTKV_F32 && p->kv_dtype != CERTKV_BF16) return CERTKV_EUNSUPPORTED;
+  if (p->flags & ~(uint32_t)(2 * CERTKV_NO_SLOT - 1)) return CERTKV_EINVAL;
+  if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale)) return CERTKV_EINVAL;
+  if ((int64_t)p->num_layers * p->batch > (int64_t)INT32_MAX / 64 / p->num_kv_heads)
+    return CERTKV_EUNSUPPORTED;
+  memset(g, 0, sizeof(*g));
+  g->L = p->num_layers;
+  g->B = p->batch;
+  g->H = p->num_kv_heads;
+  g->G = p->group;
+  g->D = p->head_dim;
+  g->scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
+  g->status = p->dev_status;
+  return CERTKV_OK;
+}
+
+// Tables and pool sizes, and (rows) the pool's rows too.
+static certkv_status page_args(const certkv_problem* p, const certkv_pages* x, bool rows,
+                               PageArgs* a) {
+  memset(a, 0, sizeof(*a));
+  TRY(page_problem(p, &a->g));
+  if (!x || x->num_pages < 1 || x->max_pages < 1) return CERTKV_EINVAL;
+  if (x->page < 16 || x->page > 1024 || (x->page & (x->page - 1))) return CERTKV_EINVAL;
+  if (x->per_head != 0 && x->per_head != 1) return CERTKV_EINVAL;
+  if ((int64_t)x->num_pages * x->page > kPgMostRows || (int64_t)x->max_pages * x->page > kPgMostRows)
+    return CERTKV_EUNSUPPORTED;
+  if (!x->table || !x->offsets) return CERTKV_EINVAL;
+  a->lp = __builtin_ctz((unsigned)x->page);
+  a->num_pages = x->num_pages;
+  a->max_pages = x->max_pages;
+  a->per_head = x->per_head;
+  a->lists = x->per_head ? a->g.L * a->g.B * a->g.H : a->g.B;
+  a->table = x->table;
+  a->offsets = x->offsets;
+  if (!rows) return CERTKV_OK;
+  const bool mx = x->format == CERTKV_CACHE_MXFP8 || x->format == CERTKV_CACHE_MXFP4;
+  if (!mx && x->format != CERTKV_CACHE_BF16) return CERTKV_EINVAL;
+  if (!x->k || !x->v || ((uintptr_t)x->k & 15u) || ((uintptr_t)x->v & 15u)) return CERTKV_EINVAL;
+  if (mx && (!x->k_scales || !x->v_scales || ((uintptr_t)x->k_scales & 3u) ||
+             ((uintptr_t)x->v_scales & 3u)))
+    return CERTKV_EINVAL;
+  if (x->s_layer < 0 || x->s_page < 0 || x->s_row < 1 || x->s_head < 0) return CERTKV_EINVAL;
+  if (x->per_head && (x->s_layer || x->s_head)) return CERTKV_EINVAL;
+  // half a tile's rows are addressed with 31-bit byte offsets, the pool's with 63-bit ones
+  if (x->s_row > (int64_t)INT32_MAX / 16 / mx_row_bytes(x->format, a->g.D))
+    return CERTKV_EUNSUPPORTED;
+  const int64_t far = (int64_t)1 << 52;
+  if (x->s_layer > far / a->g.L || x->s_page > far / x->num_pages || x->s_head > far / a->g.H)
+    return CERTKV_EUNSUPPORTED;
+  a->format = x->format;
+  a->s_layer = x->s_layer;
+  a->s_page = x->s_page;
+  a->s_row = x->s_row;
+  a->s_head = x->s_head;
+  a->k = static_cast<uint8_t*>(x->k);
+  a->v = static_cast<uint8_t*>(x->v);
+  a->k_scales = x->k_scales;
+  a->v_scales = x->v_scales;
+  return CERTKV_OK;
+}
+
+size_t certkv_page_workspace_size(const certkv_problem* p, const certkv_pages* pages) {
+  PageArgs a;
+  if (page_args(p, pages, false, &a) != CERTKV_OK) return 0;
+  return (page_resize_ws(a.lists) + 255) & ~(size_t)255;
+}
+
+certkv_status certkv_page_resize(const certkv_problem* p, const certkv_pages* pages,
+                                 const int32_t* change, int64_t* offsets_out, int64_t* free_out,
+                                 int32_t* slots, int64_t slot_capacity, int64_t* slot_offsets,
+                                 void* ws, size_t ws_bytes, void* stream) {
+  PageArgs x;
+  TRY(page_args(p, pages, false, &x));
+  if (!pages->ring || !pages->free || !change || !offsets_out || !free_out || !slot_offsets)
+    return CERTKV_EINVAL;
+  if (slot_capacity < 0 || (slot_capacity > 0 && !slots)) return CERTKV_EINVAL;
+  if (!ws) return CERTKV_EWORKSPACE;
+  if (((uintptr_t)ws & 255u) != 0) return CERTKV_EINVAL;
+  if (ws_bytes < page_resize_ws(x.lists)) return CERTKV_EWORKSPACE;
+  if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
+  PageResizeArgs a;
+  a.g = x.g;
+  a.lp = x.lp;
+  a.num_pages = x.num_pages;
+  a.max_pages = x.max_pages;
+  a.lists = x.lists;
+  a.table = pages->table;
+  a.offsets = pages->offsets;
+  a.ring = pages->ring;
+  a.free = pages->free;
+  a.change = change;
+  a.offsets_out = offsets_out;
+  a.free_out = free_out;
+  a.slots = slots;
+  a.slot_capacity = slot_capacity;
+  a.slot_offsets = slot_offsets;
+  a.ws = static_cast<int32_t*>(ws);
+  return run_page_resize(a, (hipStream_t)stream);
+}
+
+certkv_status certkv_page_write(const certkv_problem* p, const certkv_pages* pages,
+                                certkv_tensor k, certkv_tensor v, int64_t tokens, int32_t tn,
+                                const int32_t* slots, int64_t slot_count,
+                                const int64_t* slot_offsets, void* stream) {
+  PageWriteArgs a;
+  TRY(page_args(p, pages, true, &a.p));
+  if (tokens != 0) {
+    TRY(check_rows(k));
+    TRY(check_rows(v));
+  }
+  if (tokens < 0 || tn < 0 || slot_count < 0 || !slot_offsets) return CERTKV_EINVAL;
+  if (slot_count > 0 && !slots) return CERTKV_EINVAL;
+  if (tn ? tokens != (int64_t)tn * a.p.g.B : a.p.per_head != 0) return CERTKV_EINVAL;
+  if (tokens > kPgMostRows / a.p.g.H) return CERTKV_EUNSUPPORTED;
+  if ((p->flags & CERTKV_DRY_RUN) || tokens == 0) return CERTKV_OK;
+  a.dtype = p->kv_dtype;
+  a.k = k;
+  a.v = v;
+  a.tokens = tokens;
+  a.tn = tn;
+  a.slots = slots;
+  a.slot_count = slot_count;
+  a.slot_offsets = slot_offsets;
+  return run_page_write(a, (hipStream_t)stream);
+}
+
+certkv_status certkv_page_adopt(const certkv_problem* p, const certkv_pages* pages,
+                                certkv_cache cache, int64_t rows, const int32_t* slots,
+                                int64_t slot_count, const int64_t* slot_offsets, void* stream) {
+  PageAdoptArgs a;
+  TRY(page_args(p, pages, true, &a.p));
+  if (rows != 0) TRY(check_cache(cache, false));
+  if (!a.p.per_head || cache.format != pages->format) return CERTKV_EINVAL;
+  if (rows < 0 || slot_count < 0 || !slot_offsets || (slot_count > 0 && !slots))
+    return CERTKV_EINVAL;
+  if ((p->flags & CERTKV_DRY_RUN) || rows == 0) return CERTKV_OK;
+  a.k = static_cast<const uint8_t*>(cache.k);
+  a.v = static_cast<const uint8_t*>(cache.v);
+  a.k_scales = cache.k_scales;
+  a.v_scales = cache.v_scales;
+  a.rows = rows;
+  a.slots = slots;
+  a.slot_count = slot_count;
+  a.slot_offsets = slot_offsets;
+  return run_page_adopt(a, (hipStream_t)stream);
+}
+
+certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* pages, int64_t rows,
+                               int32_t out_dtype, void* k_out, void* v_out, void* stream) {
+  PageReadArgs a;
+  TRY(page_args(p, pages, true, &a.p));
+  if (out_dtype != CERTKV_BF16 && out_dtype != CERTKV_F32) return CERTKV_EUNSUPPORTED;
+  if (rows < 0) return CERTKV_EINVAL;
+  if (rows > ((int64_t)1 << 44) / a.p.g.L / a.p.g.H) return CERTKV_EUNSUPPORTED;
+  if ((rows > 0 && !k_out && !v_out) || ((uintptr_t)k_out & 15u) || ((uintptr_t)v_out & 15u))
+    return CERTKV_EINVAL;
+  if ((p->flags & CERTKV_DRY_RUN) || rows == 0) return CERTKV_OK;
+  a.f32 = out_dtype == CERTKV_F32;
+  a.rows = rows;
+  a.k = k_out;
+  a.v = v_out;
+  return run_page_read(a, (hipStream_t)stream);
+}
+
+// Chunks of paged attention and its workspace: partials (output rows, then (max, sum) pairs), each
+// 256-byte aligned.
+struct PagedWs {
+  int shape;
+  int32_t copies, cover, qgroups, mp, parts, most;
+  size_t ml_off, total;
+};
+static bool paged_ws_layout(const PageArgs& x, int32_t tq, int32_t max_rows, PagedWs* w) {
+  auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  const int64_t M = (int64_t)tq * x.g.G;
+  if (M > 512) return false;
+  w->shape = M <= 16 ? kAtOne : kAtTwo;
+  const int held = w->shape == kAtOne ? 16 : 32;
+  w->qgroups = (int32_t)((M + held - 1) / held);
+  w->mp = (int32_t)M;
+  // as many chunks as their workgroups stay resident: 256 compute units of four SIMDs
+  w->parts = 256 * 4 * attend_waves(x.g.D, w->shape) / attend_wg_waves(w->shape);
+  w->parts = (w->parts + w->qgroups - 1) / w->qgroups;
+  w->copies = x.per_head ? 1 : x.g.L * x.g.H;
+  const int64_t list = (int64_t)x.max_pages << x.lp;
+  w->cover = (int32_t)(max_rows > 0 && max_rows < list ? max_rows : list);
+  const int64_t by_lists = (int64_t)x.lists * ((w->cover + 31) / 32 + kPgGap);
+  const int64_t by_pool = ((int64_t)x.num_pages << x.lp) / 32 + (int64_t)x.lists * (1 + kPgGap);
+  const int64_t tiles = w->copies * (1 + (by_lists < by_pool ? by_lists : by_pool));
+  if (by_lists > INT32_MAX || tiles > INT32_MAX) return false;
+  int64_t most = (tiles + kPgMaxTiles - 1) / kPgMaxTiles;
+  const int64_t shortest = (tiles + kPgMinTiles - 1) / kPgMinTiles;
+  if (most < w->parts) most = w->parts;
+  if (most > shortest) most = shortest;
+  w->most = (int32_t)most;
+  const size_t part = (size_t)(most + (int64_t)x.lists * w->copies) * w->mp;
+  w->ml_off = up(part * (size_t)x.g.D * sizeof(float));
+  w->total = up(w->ml_off + part * sizeof(float2));
+  return true;
+}
+
+size_t certkv_decode_paged_workspace_size(const certkv_problem* p, const certkv_pages* pages,
+                                          int32_t tq, int32_t max_rows) {
+  PageArgs a;
+  if (page_args(p, pages, true, &a) != CERTKV_OK || tq < 1 || max_rows < 0) return 0;
+  PagedWs w;
+  return paged_ws_layout(a, tq, max_rows, &w) ? w.total : 0;
+}
+
+certkv_status certkv_decode_paged(const certkv_problem* p, certkv_tensor q_new, int32_t tq,
+                                  const int32_t* q_lens, int32_t max_rows,
+                                  const certkv_pages* pages, float* out, float* lse, void* ws,
+                                  size_t ws_bytes, void* stream) {
+  PagedArgs a;
+  TRY(page_args(p, pages, true, &a.p));
+  if (tq < 1 || max_rows < 0) return CERTKV_EINVAL;
+  if (p->kv_dtype != CERTKV_BF16) return CERTKV_EUNSUPPORTED;
+  TRY(check_rows(q_new));
+  if (!out) return CERTKV_EINVAL;
+  PagedWs W;  // (first: such a call has no workspace that would do, its size is given as 0)
+  if (!paged_ws_layout(a.p, tq, max_rows, &W)) return CERTKV_EUNSUPPORTED;
+  if (!ws) return CERTKV_EWORKSPACE;
+  if (((uintptr_t)ws & 255u) != 0) return CERTKV_EINVAL;
+  if (ws_bytes < W.total) return CERTKV_EWORKSPACE;
+  if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
+  a.tq = tq;
+  a.copies = W.copies;
+  a.cover = W.cover;
+  a.qgroups = W.qgroups;
+  a.mp = W.mp;
+  a.parts = W.parts;
+  a.most = W.most;
+  a.q_lens = q_lens;
+  a.q = q_new;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + W.ml_off);
+  a.out = out;
+  a.lse = lse;
+  return run_paged(a, W.shape, (hipStream_t)stream);
 }
 
 // The whole pass; mx: the packed cache in microscaled codes, or NULL.

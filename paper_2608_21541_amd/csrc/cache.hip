@@ -20,73 +20,6 @@ namespace certkv {
 
 constexpr int kMxThreads = 256;
 
-// The block maximum over its four lanes (bits of magnitudes order as numbers do).
-__device__ __forceinline__ uint32_t mx_max4(uint32_t x) {
-  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, true));  // lanes 1 0 3 2
-  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true));  // lanes 2 3 0 1
-  return x;
-}
-
-// A lane's eight dims of a row to codes and, from the first of the block's four
-// lanes, the scale byte.
-template <int F>
-__device__ __forceinline__ void mx_store8(const Geo& g, const float x[8], int64_t at,
-                                          uint8_t* __restrict__ codes,
-                                          uint8_t* __restrict__ scales) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
-  m = mx_max4(m);
-  const bool bad = m >= 0x7f800000u;
-  const int e = bad ? 0 : mx_exponent<F>(m);
-  const float inv = mx_pow2(-e);
-  float y[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = bad ? 0.f : x[i] * inv;  // (exact, or far below a code)
-  const uint2 c = mx_encode8<F>(y);
-  if constexpr (F == CERTKV_CACHE_MXFP8)
-    *reinterpret_cast<uint2*>(codes + at) = c;
-  else
-    *reinterpret_cast<uint32_t*>(codes + at / 2) = c.x;
-  if ((threadIdx.x & 3) == 0) scales[at / kMxBlock] = bad ? 255u : (uint8_t)(e + 127);
-  if (bad) report_nonfinite(g);
-}
-
-typedef uint32_t MxU4 __attribute__((ext_vector_type(4)));
-typedef float MxF4 __attribute__((ext_vector_type(4)));
-template <typename T>
-struct MxRaw;  // eight values as they are loaded
-template <>
-struct MxRaw<uint16_t> {
-  uint4 a;
-  __device__ __forceinline__ void load(const uint16_t* p) {
-    const MxU4 v = __builtin_nontemporal_load(reinterpret_cast<const MxU4*>(p));
-    a = make_uint4(v[0], v[1], v[2], v[3]);
-  }
-  __device__ __forceinline__ void values(float x[8]) const {
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = bf16_lo(w[i]);
-      x[2 * i + 1] = bf16_hi(w[i]);
-    }
-  }
-};
-template <>
-struct MxRaw<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p) {
-    const MxF4 v = __builtin_nontemporal_load(reinterpret_cast<const MxF4*>(p));
-    const MxF4 w = __builtin_nontemporal_load(reinterpret_cast<const MxF4*>(p) + 1);
-    a = make_float4(v[0], v[1], v[2], v[3]);
-    b = make_float4(w[0], w[1], w[2], w[3]);
-  }
-  __device__ __forceinline__ void values(float x[8]) const {
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-    x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-  }
-};
-
 template <int D, typename T, int F>
 __global__ __launch_bounds__(kMxThreads) void compact_mx_kernel(
     Geo g, SeqTab st, const T* __restrict__ kc, int64_t k_sl, int64_t k_st, int64_t k_sh,

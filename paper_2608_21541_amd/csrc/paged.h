@@ -1,0 +1,447 @@
+// Attention of new queries over a paged cache: the kernel.
+//
+// For query row (t, head h G + g) of sequence b, whose unit's list holds len rows, n of the tq
+// queries being the sequence's own:
+//   z_j = scale <q, k_j> for j <= len - n + t (t < n; none for t >= n),
+//   out = sum_j softmax(z)_j v_j,  lse = log sum_j e^z_j,
+// with out = 0 and lse = -inf where no row is visible.
+//
+// Tiles of 32 rows, products and weights are those of attend.h: S^T = K Q^T and O^T += V^T P^T on
+// v_mfma_f32_16x16x32_bf16, weights in three bf16 parts against a reference that moves only on
+// overflow.  A workgroup has 16 or 32 query rows and four waves, which take a piece's tiles in
+// turn, each by itself, and are joined at the piece's end.
+//
+// A page is a power of two of 16 rows or more, so that the 16 rows of half a tile are consecutive
+// rows of one page: their place is scalar arithmetic, and each half has buffer resources of its
+// own, which end with the list's last row (rows behind it, which may hold anything, are zero).
+// The table's entries of 32 tiles of a wave are one load, half a tile's to each lane.
+#pragma once
+
+#include "attend.h"
+#include "pages.h"
+
+namespace certkv {
+
+constexpr int kPgGap = 8;         // tiles between lists' places beside their rows': a piece's cost
+constexpr int kPgMinTiles = 4;    // shortest chunk, and the unit of its length
+constexpr int kPgMaxTiles = kAtMaxKeys / kAtTile;  // longest, unless partials are short
+
+struct PagedArgs {
+  PageArgs p;
+  int32_t tq;
+  int32_t copies;               // units of a list: L H of a sequence's, 1 of a head's
+  int32_t cover;                // rows of a list that are attended
+  int32_t qgroups, mp;          // workgroups of a chunk, query rows of a partial
+  int32_t parts, most;          // chunks taken at once, and that the workspace has room for
+  const int32_t* q_lens;        // [B], or NULL: tq
+  certkv_tensor q;
+  float* part_o;                // [most + U][mp][d]
+  float2* part_ml;
+  float* out;
+  float* lse;
+};
+certkv_status run_paged(const PagedArgs& a, int shape, hipStream_t s);
+certkv_status run_paged_bf16(const PagedArgs& a, int shape, hipStream_t s);   // by format
+certkv_status run_paged_mxfp8(const PagedArgs& a, int shape, hipStream_t s);
+certkv_status run_paged_mxfp4(const PagedArgs& a, int shape, hipStream_t s);
+
+// The units in one order (a list's copies one after another), each at a place, in tiles, that
+// follows from its list's first row alone; chunks of equal length are cut from it.
+struct PgCut {
+  uint32_t tiles, total;        // of a chunk, of all
+};
+__device__ __forceinline__ uint32_t pg_up(int64_t rows) { return (uint32_t)((uint64_t)(rows + 31) >> 5); }
+// The first tile of list r, for copies = 1.
+__device__ __forceinline__ uint32_t pg_place(int64_t rows_before, uint32_t r) {
+  return pg_up(rows_before) + r * (uint32_t)kPgGap;
+}
+__device__ __forceinline__ PgCut pg_cut(const PagedArgs& a, int64_t rows) {
+  const uint32_t total = (uint32_t)a.copies * pg_place(rows, (uint32_t)a.p.lists);
+  uint32_t k = (total + (uint32_t)a.parts - 1u) / (uint32_t)a.parts;
+  k = min(max(k, (uint32_t)kPgMinTiles), (uint32_t)kPgMaxTiles);
+  // (more rows than the caller's bound or the pool allow for, as with pages that lists share:
+  // longer chunks, so that the partials stay within the workspace)
+  if (total > (uint64_t)a.most * k) k = (total + (uint32_t)a.most - 1u) / (uint32_t)a.most;
+  return PgCut{(k + kPgMinTiles - 1u) / kPgMinTiles * kPgMinTiles, total};
+}
+
+// The lists' offsets, as a wave reads them: those of 64 lists at a time in its lanes.
+struct PgOffsets {
+  const int64_t* __restrict__ off;
+  uint32_t R, at;
+  int64_t base, rows, first, end;
+  __device__ __forceinline__ PgOffsets(const int64_t* o, int32_t lists, int lane)
+      : off(o), R((uint32_t)lists) {
+    window(0, lane);
+    base = AtOffsets::lane64(first, 0);
+    rows = (lists <= 64 ? AtOffsets::lane64(end, R - 1) : off[R]) - base;
+  }
+  __device__ __forceinline__ void window(uint32_t r, int lane) {
+    at = r;
+    first = off[min(r + lane, R)];
+    end = off[min(r + lane + 1, R)];
+  }
+  // a list's first row and the one behind its last
+  __device__ __forceinline__ void list(uint32_t r, int lane, int64_t& p0, int64_t& p1) {
+    if (r - at >= 64) window(r, lane);
+    p0 = AtOffsets::lane64(first, r - at) - base;
+    p1 = AtOffsets::lane64(end, r - at) - base;
+  }
+  // The list whose place holds tile x (of one copy): 64 lists' ends per step.
+  __device__ __forceinline__ uint32_t find(uint32_t x, int lane) {
+    uint32_t lo = 0, n = R;  // the answer is one of [lo, lo + n]
+    while (n > 64) {
+      const uint32_t step = (n + 63) / 64, i = lo + lane * step + step - 1;
+      const bool past = i >= R || pg_place(off[min(i + 1, R)] - base, i + 1) > x;
+      lo += (uint32_t)__popcll(__ballot(!past)) * step;
+      n = step;
+    }
+    if (lo != at) window(lo, lane);
+    const uint32_t i = lo + lane;
+    const uint64_t past = __ballot(i >= R || pg_place(end - base, i + 1) > x);
+    return past ? min(lo + (uint32_t)__builtin_ctzll(past), R) : R;
+  }
+};
+
+template <int F, int D, int QT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(attend_waves(D, QT - 1)))) void
+paged_kernel(PagedArgs a) {
+  using Shape = AtShape<D, 1, QT>;
+  constexpr int KS = Shape::KS, NT = Shape::NT, PARTS = Shape::PARTS;
+  constexpr int BITS = F == CERTKV_CACHE_BF16 ? 16 : F == CERTKV_CACHE_MXFP8 ? 8 : 4;
+  constexpr bool MX = F != CERTKV_CACHE_BF16;
+  constexpr int RB = mx_row_bytes(F, D);
+  constexpr int KSTEP = D / 32;
+  // keys: lane (g, c) holds WK bytes of row c at a time, EK dims
+  constexpr int WK = RB >= 64 ? 16 : 8, EK = WK * 8 / BITS, SK = EK / 8, NLK = KSTEP / SK;
+  // values: W bytes of a lane, so that a load is at most 16 rows; a tile is NLT loads
+  constexpr int W = RB >= 64 ? 16 : 8, EV = W * 8 / BITS, LPR = RB / W, RPL = 64 / LPR;
+  constexpr int NLT = kAtTile / RPL;
+  static_assert(RPL <= 16 && SK * NLK == KSTEP && NT == 256, "a load's rows are in one half");
+  __shared__ __align__(16) uint16_t lds[Shape::LDS];
+  __shared__ float2 ml_s[KS * 16];
+
+  const PageArgs& p = a.p;
+  const Geo& gm = p.g;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, c = lane & 15;
+  const int M = a.tq * gm.G, mp = a.mp;
+  const float c2 = gm.scale * kAtLog2e;
+  const uint32_t copies = (uint32_t)a.copies;
+  // Query groups of a chunk: eight workgroups apart, on the same XCD, whose L2 then serves all
+  // but the first.
+  const int wgx = blockIdx.x;
+  const int qg = (wgx >> 3) % a.qgroups;
+  const uint32_t x0 = a.qgroups == 1 ? wgx : (wgx >> 3) / a.qgroups * 8 + (wgx & 7);
+  const uint32_t xstep = gridDim.x / a.qgroups;
+  const int row0 = qg * QT * 16;  // the first query row
+  auto kdim = [&](int ks) { return (ks / SK) * 4 * EK + g * EK + 8 * (ks % SK); };
+  uint16_t* const vt = lds + wave * Shape::GROUP;
+
+  PgOffsets off(p.offsets, p.lists, lane);
+  const PgCut cut = pg_cut(a, off.rows);
+  const uint32_t nch = (cut.total + cut.tiles - 1) / cut.tiles;
+  for (uint32_t x = x0; x < nch; x += xstep) {
+    const uint32_t r0 = x * cut.tiles, r1 = min(cut.total, r0 + cut.tiles);
+    uint32_t r = off.find(r0 / copies, lane), copy = 0;
+    bool begun = false;
+    while (r < off.R) {
+      int64_t p0, p1;
+      off.list(r, lane, p0, p1);
+      const uint32_t place = copies * pg_place(p0, r);
+      const uint32_t span = pg_place(p1, r + 1) - pg_place(p0, r);
+      if (!begun) copy = r0 > place ? (r0 - place) / span : 0;
+      begun = true;
+      if (copy >= copies) {
+        ++r, copy = 0;
+        continue;
+      }
+      const uint32_t vs = place + copy * span, u = r * copies + copy;
+      if (vs >= r1) break;
+      // the piece: tiles [lo, lo + ntp) of the unit's
+      const int len = min(page_rows(p, p0, p1), a.cover);
+      const uint32_t lo = max(r0, vs) - vs;
+      const int ntp = (int)min(r1 - vs, pg_up(len)) - (int)lo;
+      const uint32_t mine = copy++;
+      if (ntp <= 0) continue;  // (only what lies between units)
+      int l, b, h;
+      if (p.per_head) {
+        h = (int)(r % (uint32_t)gm.H), b = (int)(r / gm.H % (uint32_t)gm.B);
+        l = (int)(r / gm.H / gm.B);
+      } else {
+        b = (int)r, l = (int)(mine / (uint32_t)gm.H), h = (int)(mine % (uint32_t)gm.H);
+      }
+      const int own = a.q_lens ? min(max(a.q_lens[b], 0), a.tq) : a.tq;
+      const int64_t at0 = p.per_head ? 0 : l * p.s_layer + h * p.s_head;
+      const uint32_t st = (uint32_t)p.s_row * RB;  // bytes from row to row
+      // the last row that a lane's queries see, and the first of these
+      int last[QT];
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        const int row = row0 + qt * 16 + c, t = min(row, M - 1) / gm.G;
+        last[qt] = row < M && t < own ? len - own + t : -1;
+      }
+      const int t0 = row0 / gm.G;  // the first token; rows up to `whole` are seen by all
+      const int whole = len - own + t0;
+
+      // The pages of the wave's tiles lo + wave + 4 n, 32 at a time: half i % 2 of the one of
+      // n = i / 2 in lane i.
+      int32_t ids = 0, window = -1;
+      auto pages = [&](int n) {
+        if ((n >> 5) == window) return;
+        window = n >> 5;
+        const int row = (int)(lo + wave + KS * ((n & ~31) + (lane >> 1))) * kAtTile + (lane & 1) * 16;
+        ids = -1;
+        if (row < len) {
+          const int32_t id = p.table[(int64_t)r * p.max_pages + (row >> p.lp)];
+          if ((uint32_t)id < (uint32_t)p.num_pages)
+            ids = id;
+          else
+            report_range(gm);  // (the caller's numbers)
+        }
+      };
+      // rows of half kb of the wave's tile n that are there, and their place in the pool
+      auto half = [&](int n, int kb, int& there) {
+        const int row = (int)(lo + wave + KS * n) * kAtTile + kb * 16;
+        const int32_t id = __builtin_amdgcn_readlane(ids, 2 * (n & 31) + kb);
+        there = id < 0 ? 0 : min(max(len - row, 0), 16);
+        return at0 + (int64_t)max(id, 0) * p.s_page + (row & ((1 << p.lp) - 1)) * p.s_row;
+      };
+
+      AtAcc<D, QT> acc;
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        acc.m[qt] = kAtNone;
+        acc.l[qt] = 0.f;
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) acc.o[qt][db] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
+      }
+      uint4 q[QT][KSTEP];
+      AtRaw<F, WK> kx[2][NLK];
+      AtRaw<F, W> vx[NLT];
+      uint32_t ksc[2] = {}, vsc[NLT] = {};
+      int kthere[2] = {};
+      auto load_keys = [&](int n) {
+        pages(n);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const int64_t row = half(n, kb, kthere[kb]);
+          const uint32_t bytes = kthere[kb] ? (kthere[kb] - 1) * st + RB : 0;
+          const BufRsrc kr = make_rsrc(p.k + row * RB, bytes);
+#pragma unroll
+          for (int i = 0; i < NLK; ++i) kx[kb][i].template load<false>(kr, c * st + g * WK + i * 4 * WK);
+          if constexpr (MX) {
+            const BufRsrc sr = make_rsrc(p.k_scales + row * (D / 32), bytes / RB * (D / 32));
+            const uint32_t so = c * (uint32_t)p.s_row * (D / 32);
+            ksc[kb] = D == 128 ? buf_load_u32(sr, so) : buf_load_u16(sr, so);
+          }
+        }
+      };
+      auto load_values = [&](int n) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          int there;
+          const int64_t row = half(n, kb, there);
+          const uint32_t bytes = there ? (there - 1) * st + RB : 0;
+          const BufRsrc vr = make_rsrc(p.v + row * RB, bytes);
+          const BufRsrc sr = make_rsrc(p.v_scales + (MX ? row * (D / 32) : 0),
+                                       MX ? bytes / RB * (D / 32) : 0);
+#pragma unroll
+          for (int i = 0; i < NLT / 2; ++i) {
+            const uint32_t rr = i * RPL + lane / LPR;
+            vx[kb * (NLT / 2) + i].template load<true>(vr, rr * st + (lane % LPR) * W);
+            if constexpr (MX)
+              vsc[kb * (NLT / 2) + i] = __builtin_amdgcn_raw_buffer_load_b8(
+                  sr, (int)(rr * (uint32_t)p.s_row * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
+          }
+        }
+      };
+      const int own_tiles = t0 < own ? (ntp - wave + KS - 1) / KS : 0;  // of the wave
+      if (own_tiles > 0) {
+        load_keys(0);
+        load_values(0);
+      }
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        const int row = row0 + qt * 16 + c, rc = min(row, M - 1);
+        const uint16_t* src = static_cast<const uint16_t*>(a.q.ptr) + l * a.q.s_layer +
+                              (int64_t)(b * a.tq + rc / gm.G) * a.q.s_token +
+                              (int64_t)(h * gm.G + rc % gm.G) * a.q.s_head;
+#pragma unroll
+        for (int ks = 0; ks < KSTEP; ++ks) {
+          q[qt][ks] = *reinterpret_cast<const uint4*>(src + kdim(ks));
+          if (row >= M) q[qt][ks] = make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
+      for (int n = 0; n < own_tiles; ++n) {
+        const int trow = (int)(lo + wave + KS * n) * kAtTile;
+        at_f32x4 s[QT][2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) s[qt][kb] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < KSTEP; ++ks) {
+            const int i = ks / SK;
+            float f = 1.f;
+            if constexpr (MX) f = mx_scale((ksc[kb] >> (8 * ((i * 4 + g) * EK / 32))) & 255u);
+            const at_bf16x8 k = __builtin_bit_cast(at_bf16x8, at_bf16<F, WK>(kx[kb][i], ks % SK, f));
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt)
+              s[qt][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  k, __builtin_bit_cast(at_bf16x8, q[qt][ks]), s[qt][kb], 0, 0, 0);
+          }
+        }
+        const int there[2] = {kthere[0], kthere[1]};
+        if (n + 1 < own_tiles) load_keys(n + 1);
+        // Some row of the tile is not there, or some query does not see one.
+        const bool part = there[0] < 16 || there[1] < 16 || trow + kAtTile - 1 > whole;
+        uint32_t bad = 0;  // rows with a value that is not finite, of such a tile
+#pragma unroll
+        for (int i = 0; i < NLT; ++i) {
+          const int rr = i * RPL + lane / LPR;
+          const float f = MX ? mx_scale(vsc[i]) : 1.f;
+#pragma unroll
+          for (int e = 0; e < EV / 8; ++e) {
+            const uint4 v = at_bf16<F, W>(vx[i], e, f);
+            if (part) bad |= at_bad8(v);
+            reinterpret_cast<uint4*>(vt)[at_value_chunk<D>(rr, (lane % LPR) * (EV / 8) + e)] = v;
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (n + 1 < own_tiles) load_values(n + 1);
+        if (part) {
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int j = 4 * g + (i & 3);
+              if (j >= there[i >> 2] || trow + 16 * (i >> 2) + j > last[qt])
+                s[qt][i >> 2][i & 3] = -INFINITY;
+            }
+        }
+        float most[QT];
+        AtParts<PARTS> w[QT];
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) most[qt] = at_max8(s[qt]);
+        at_reference<D, QT>(acc, most, c2);
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          const float cq = ref_factor(acc.m[qt], c2);
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) at_weights2<D, QT, PARTS>(acc, qt, i, s[qt], cq, w[qt]);
+        }
+        if (__ballot(bad) == 0) {
+          at_values<D, QT, PARTS>(acc, vt, w, lane);
+        } else {
+          // A row that a query does not see has no part in its output, whatever it holds: token
+          // by token from the last, the rows behind what it sees are zero, and the products
+          // count for its own queries alone.
+          for (int t = min(min(row0 + QT * 16 - 1, M - 1) / gm.G, own - 1); t >= t0; --t) {
+            const int sees = len - own + t - trow;  // the last row of the tile
+            for (int rr = max(sees + 1, 0) + (lane >> 4); rr < kAtTile; rr += 4)
+              for (int ch = lane & 15; ch < D / 8; ch += 16)
+                reinterpret_cast<uint4*>(vt)[at_value_chunk<D>(rr, ch)] = make_uint4(0u, 0u, 0u, 0u);
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db) {
+              const at_bf16x8 vf = at_value_block<D>(vt, db, lane);
+#pragma unroll
+              for (int qt = 0; qt < QT; ++qt) {
+                at_f32x4 o = acc.o[qt][db];
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k)
+                  o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                      vf, __builtin_bit_cast(at_bf16x8, w[qt].p[k]), o, 0, 0, 0);
+                const int row = row0 + qt * 16 + c;
+                const bool its = min(row, M - 1) / gm.G == t && sees >= 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc.o[qt][db][k] = its ? o[k] : acc.o[qt][db][k];
+              }
+            }
+            __builtin_amdgcn_wave_barrier();
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+
+      // The piece's partial: (maximum, sum, unnormalized output) of each query row, the waves
+      // joined in LDS.
+      const int64_t slot = (int64_t)x + u;
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        if (last[qt] < 0) {  // (a query that is not there has seen what is seen by all)
+          acc.m[qt] = kAtNone;
+          acc.l[qt] = 0.f;
+#pragma unroll
+          for (int db = 0; db < D / 16; ++db) acc.o[qt][db] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+        float l_row = acc.l[qt];
+        l_row += __shfl_xor(l_row, 16, 64);
+        l_row += __shfl_xor(l_row, 32, 64);
+        constexpr int ROW = Shape::ROW;
+        float* join = reinterpret_cast<float*>(lds);
+        __syncthreads();  // every wave is done with its tiles (and with the tile before)
+        if (g == 0) ml_s[wave * 16 + c] = make_float2(acc.m[qt], l_row);
+        __syncthreads();
+        float mx = kAtNone;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) mx = fmaxf(mx, ml_s[k * 16 + c].x);
+        const float w = __builtin_amdgcn_exp2f(acc.m[qt] - mx);
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) {
+          const at_f32x4 o = acc.o[qt][db];
+          *reinterpret_cast<float4*>(join + (wave * 16 + c) * ROW + 16 * db + 4 * g) =
+              make_float4(o[0] * w, o[1] * w, o[2] * w, o[3] * w);
+        }
+        __syncthreads();
+        for (int i = tid; i < 16 * (D / 4); i += NT) {
+          const int rr = i / (D / 4), d4 = i % (D / 4);
+          const int row = row0 + qt * 16 + rr;
+          if (row >= M) continue;
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            const float4 y = *reinterpret_cast<const float4*>(join + (k * 16 + rr) * ROW + 4 * d4);
+            o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
+          }
+          const int64_t pr = slot * mp + row;
+          reinterpret_cast<float4*>(a.part_o + pr * D)[d4] = o;
+          if (d4 == 0) {
+            float mm = kAtNone, sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) mm = fmaxf(mm, ml_s[k * 16 + rr].x);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              const float2 ml = ml_s[k * 16 + rr];
+              sum += ml.y * __builtin_amdgcn_exp2f(ml.x - mm);
+            }
+            a.part_ml[pr] = make_float2(mm, sum);
+          }
+        }
+      }
+      __syncthreads();  // the joined tiles are read before the next piece overwrites them
+    }
+  }
+}
+
+template <int F>
+static certkv_status launch_paged(const PagedArgs& a, int shape, hipStream_t s) {
+  const int wgs = a.most < a.parts ? a.most : a.parts;
+  const dim3 grid(a.qgroups == 1 ? wgs : (wgs + 7) / 8 * 8 * a.qgroups);
+  if (a.p.g.D == 128) {
+    if (shape == kAtOne)
+      CERTKV_LAUNCH("paged", (paged_kernel<F, 128, 1>), grid, dim3(256), 0, s, a);
+    else
+      CERTKV_LAUNCH("paged", (paged_kernel<F, 128, 2>), grid, dim3(256), 0, s, a);
+  } else {
+    if (shape == kAtOne)
+      CERTKV_LAUNCH("paged", (paged_kernel<F, 64, 1>), grid, dim3(256), 0, s, a);
+    else
+      CERTKV_LAUNCH("paged", (paged_kernel<F, 64, 2>), grid, dim3(256), 0, s, a);
+  }
+  return CERTKV_OK;
+}
+
+}  // namespace certkv
