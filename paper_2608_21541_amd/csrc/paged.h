@@ -17,6 +17,8 @@
 // The table's entries of 32 tiles of a wave are one load, half a tile's to each lane.
 #pragma once
 
+#include <type_traits>
+
 #include "attend.h"
 #include "pages.h"
 
@@ -103,6 +105,20 @@ struct PgOffsets {
   }
 };
 
+// A lane's part of a row, from a place that is the wave's.  NT: non-temporally.
+template <bool NT, typename T>
+__device__ __forceinline__ void pg_load(T& x, const uint8_t* at, uint32_t off) {
+  typedef uint32_t V __attribute__((ext_vector_type(sizeof(T) / 4)));
+  const V* src = reinterpret_cast<const V*>(at + off);
+  x = __builtin_bit_cast(T, NT ? __builtin_nontemporal_load(src) : *src);
+}
+// Two bf16, those that are not finite as zero.
+__device__ __forceinline__ uint32_t pg_finite(uint32_t x) {
+  if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+  if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+  return x;
+}
+
 template <int F, int D, int QT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(attend_waves(D, QT - 1)))) void
 paged_kernel(PagedArgs a) {
@@ -138,6 +154,12 @@ paged_kernel(PagedArgs a) {
   const int row0 = qg * QT * 16;  // the first query row
   auto kdim = [&](int ks) { return (ks / SK) * 4 * EK + g * EK + 8 * (ks % SK); };
   uint16_t* const vt = lds + wave * Shape::GROUP;
+  // bytes from row to row and from page to page, and a lane's share of a load
+  const uint32_t st = (uint32_t)p.s_row * RB;
+  const uint64_t page_bytes = (uint64_t)p.s_page * RB;
+  const uint32_t k_off = c * st + g * WK, v_off = (lane / LPR) * st + (lane % LPR) * W;
+  const uint32_t ks_off = c * (uint32_t)p.s_row * (D / 32);
+  const uint32_t vs_off = (lane / LPR) * (uint32_t)p.s_row * (D / 32) + (lane % LPR) * EV / 32;
 
   PgOffsets off(p.offsets, p.lists, lane);
   const PgCut cut = pg_cut(a, off.rows);
@@ -174,7 +196,10 @@ paged_kernel(PagedArgs a) {
       }
       const int own = a.q_lens ? min(max(a.q_lens[b], 0), a.tq) : a.tq;
       const int64_t at0 = p.per_head ? 0 : l * p.s_layer + h * p.s_head;
-      const uint32_t st = (uint32_t)p.s_row * RB;  // bytes from row to row
+      const uint8_t* const kp = p.k + at0 * RB;
+      const uint8_t* const vp = p.v + at0 * RB;
+      const uint8_t* const ksp = p.k_scales + (MX ? at0 * (D / 32) : 0);
+      const uint8_t* const vsp = p.v_scales + (MX ? at0 * (D / 32) : 0);
       // the last row that a lane's queries see, and the first of these
       int last[QT];
 #pragma unroll
@@ -201,12 +226,12 @@ paged_kernel(PagedArgs a) {
             report_range(gm);  // (the caller's numbers)
         }
       };
-      // rows of half kb of the wave's tile n that are there, and their place in the pool
+      // rows of half kb of the wave's tile n that are there, and their first byte behind kp and vp
       auto half = [&](int n, int kb, int& there) {
         const int row = (int)(lo + wave + KS * n) * kAtTile + kb * 16;
         const int32_t id = __builtin_amdgcn_readlane(ids, 2 * (n & 31) + kb);
         there = id < 0 ? 0 : min(max(len - row, 0), 16);
-        return at0 + (int64_t)max(id, 0) * p.s_page + (row & ((1 << p.lp) - 1)) * p.s_row;
+        return (uint32_t)max(id, 0) * page_bytes + (uint32_t)(row & ((1 << p.lp) - 1)) * (uint64_t)st;
       };
 
       AtAcc<D, QT> acc;
@@ -222,19 +247,21 @@ paged_kernel(PagedArgs a) {
       AtRaw<F, W> vx[NLT];
       uint32_t ksc[2] = {}, vsc[NLT] = {};
       int kthere[2] = {};
+      // (rows that are not there are read as well, of the same page: their scores are replaced and
+      // their values zero)
       auto load_keys = [&](int n) {
         pages(n);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-          const int64_t row = half(n, kb, kthere[kb]);
-          const uint32_t bytes = kthere[kb] ? (kthere[kb] - 1) * st + RB : 0;
-          const BufRsrc kr = make_rsrc(p.k + row * RB, bytes);
+          const uint64_t at = half(n, kb, kthere[kb]);
 #pragma unroll
-          for (int i = 0; i < NLK; ++i) kx[kb][i].template load<false>(kr, c * st + g * WK + i * 4 * WK);
+          for (int i = 0; i < NLK; ++i) pg_load<false>(kx[kb][i].x, kp + at + i * 4 * WK, k_off);
           if constexpr (MX) {
-            const BufRsrc sr = make_rsrc(p.k_scales + row * (D / 32), bytes / RB * (D / 32));
-            const uint32_t so = c * (uint32_t)p.s_row * (D / 32);
-            ksc[kb] = D == 128 ? buf_load_u32(sr, so) : buf_load_u16(sr, so);
+            const uint8_t* sp = ksp + at / (RB / (D / 32));
+            if constexpr (D == 128)
+              ksc[kb] = *reinterpret_cast<const uint32_t*>(sp + ks_off);
+            else
+              ksc[kb] = *reinterpret_cast<const uint16_t*>(sp + ks_off);
           }
         }
       };
@@ -242,18 +269,12 @@ paged_kernel(PagedArgs a) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
           int there;
-          const int64_t row = half(n, kb, there);
-          const uint32_t bytes = there ? (there - 1) * st + RB : 0;
-          const BufRsrc vr = make_rsrc(p.v + row * RB, bytes);
-          const BufRsrc sr = make_rsrc(p.v_scales + (MX ? row * (D / 32) : 0),
-                                       MX ? bytes / RB * (D / 32) : 0);
+          const uint64_t at = half(n, kb, there);
 #pragma unroll
           for (int i = 0; i < NLT / 2; ++i) {
-            const uint32_t rr = i * RPL + lane / LPR;
-            vx[kb * (NLT / 2) + i].template load<true>(vr, rr * st + (lane % LPR) * W);
-            if constexpr (MX)
-              vsc[kb * (NLT / 2) + i] = __builtin_amdgcn_raw_buffer_load_b8(
-                  sr, (int)(rr * (uint32_t)p.s_row * (D / 32) + (lane % LPR) * EV / 32), 0, 0);
+            const uint64_t ati = at + (uint32_t)(i * RPL) * (uint64_t)st;
+            pg_load<true>(vx[kb * (NLT / 2) + i].x, vp + ati, v_off);
+            if constexpr (MX) vsc[kb * (NLT / 2) + i] = vsp[ati / (RB / (D / 32)) + vs_off];
           }
         }
       };
@@ -274,8 +295,16 @@ paged_kernel(PagedArgs a) {
           if (row >= M) q[qt][ks] = make_uint4(0u, 0u, 0u, 0u);
         }
       }
-      for (int n = 0; n < own_tiles; ++n) {
+      // One tile, whose keys and values have been asked for; TAIL: some row of it may not be seen by
+      // some query.  (Apart, so that what the few last tiles need takes no registers from the
+      // others' loads in flight.)
+      auto tile = [&](int n, auto tail_c) {
+        constexpr bool TAIL = decltype(tail_c)::value;
         const int trow = (int)(lo + wave + KS * n) * kAtTile;
+        // (its addresses by itself too)
+        int ln = lane;
+        if constexpr (TAIL) asm volatile("" : "+v"(ln));
+        const int g = ln >> 4;
         at_f32x4 s[QT][2];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -292,32 +321,40 @@ paged_kernel(PagedArgs a) {
               s[qt][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                   k, __builtin_bit_cast(at_bf16x8, q[qt][ks]), s[qt][kb], 0, 0, 0);
           }
+          __builtin_amdgcn_sched_barrier(0);
         }
         const int there[2] = {kthere[0], kthere[1]};
-        if (n + 1 < own_tiles) load_keys(n + 1);
-        // Some row of the tile is not there, or some query does not see one.
-        const bool part = there[0] < 16 || there[1] < 16 || trow + kAtTile - 1 > whole;
-        uint32_t bad = 0;  // rows with a value that is not finite, of such a tile
+        if (!TAIL && n + 1 < own_tiles) load_keys(n + 1);
+        // (of a tile of drafted tokens' rows: values that are not finite)
+        const bool guard = TAIL && a.tq > 1;
+        bool bad = false;
 #pragma unroll
         for (int i = 0; i < NLT; ++i) {
-          const int rr = i * RPL + lane / LPR;
+          const int rr = i * RPL + ln / LPR;
           const float f = MX ? mx_scale(vsc[i]) : 1.f;
 #pragma unroll
           for (int e = 0; e < EV / 8; ++e) {
-            const uint4 v = at_bf16<F, W>(vx[i], e, f);
-            if (part) bad |= at_bad8(v);
-            reinterpret_cast<uint4*>(vt)[at_value_chunk<D>(rr, (lane % LPR) * (EV / 8) + e)] = v;
+            uint4 v = at_bf16<F, W>(vx[i], e, f);
+            if (guard) {
+              bad |= at_bad8(v) && rr % 16 < there[rr / 16];
+              v = make_uint4(pg_finite(v.x), pg_finite(v.y), pg_finite(v.z), pg_finite(v.w));
+            }
+            reinterpret_cast<uint4*>(vt)[at_value_chunk<D>(rr, (ln % LPR) * (EV / 8) + e)] = v;
           }
         }
         __builtin_amdgcn_wave_barrier();
-        if (n + 1 < own_tiles) load_values(n + 1);
-        if (part) {
+        if (!TAIL && n + 1 < own_tiles) load_values(n + 1);
+        if (TAIL || there[0] < 16 || there[1] < 16) {
+          for (int rr = ln / (D / 8); rr < kAtTile; rr += 64 / (D / 8))
+            if (rr % 16 >= there[rr / 16])
+              reinterpret_cast<uint4*>(vt)[at_value_chunk<D>(rr, ln % (D / 8))] = make_uint4(0u, 0u, 0u, 0u);
+          __builtin_amdgcn_wave_barrier();
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int j = 4 * g + (i & 3);
-              if (j >= there[i >> 2] || trow + 16 * (i >> 2) + j > last[qt])
+              if (j >= there[i >> 2] || (TAIL && trow + 16 * (i >> 2) + j > last[qt]))
                 s[qt][i >> 2][i & 3] = -INFINITY;
             }
         }
@@ -332,43 +369,51 @@ paged_kernel(PagedArgs a) {
 #pragma unroll
           for (int i = 0; i < 8; i += 2) at_weights2<D, QT, PARTS>(acc, qt, i, s[qt], cq, w[qt]);
         }
-        if (__ballot(bad) == 0) {
-          at_values<D, QT, PARTS>(acc, vt, w, lane);
-        } else {
-          // A row that a query does not see has no part in its output, whatever it holds: token
-          // by token from the last, the rows behind what it sees are zero, and the products
-          // count for its own queries alone.
-          for (int t = min(min(row0 + QT * 16 - 1, M - 1) / gm.G, own - 1); t >= t0; --t) {
-            const int sees = len - own + t - trow;  // the last row of the tile
-            for (int rr = max(sees + 1, 0) + (lane >> 4); rr < kAtTile; rr += 4)
-              for (int ch = lane & 15; ch < D / 8; ch += 16)
-                reinterpret_cast<uint4*>(vt)[at_value_chunk<D>(rr, ch)] = make_uint4(0u, 0u, 0u, 0u);
-            __builtin_amdgcn_wave_barrier();
+        at_values<D, QT, PARTS>(acc, vt, w, ln);
+        if (guard && __ballot(bad)) {
+          // A row that a query does not see has no part in its output, whatever it holds: what is
+          // not finite was left out above, and is added for the queries that see it, row by row.
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int i = 0; i < NLT; ++i) {
+            const float f = MX ? mx_scale(vsc[i]) : 1.f;
+#pragma unroll
+            for (int e = 0; e < EV / 8; ++e)
+              reinterpret_cast<uint4*>(vt)[at_value_chunk<D>(i * RPL + ln / LPR, (ln % LPR) * (EV / 8) + e)] =
+                  at_bf16<F, W>(vx[i], e, f);
+          }
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+          for (int rr = 0; rr < kAtTile; ++rr) {
+            if (rr % 16 >= there[rr / 16]) continue;
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) {
-              const at_bf16x8 vf = at_value_block<D>(vt, db, lane);
+              const uint2 v = *reinterpret_cast<const uint2*>(vt + at_value_chunk<D>(rr, 2 * db) * 8 + 4 * g);
+              const float x[4] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y)};
 #pragma unroll
-              for (int qt = 0; qt < QT; ++qt) {
-                at_f32x4 o = acc.o[qt][db];
+              for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int k = 0; k < PARTS; ++k)
-                  o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                      vf, __builtin_bit_cast(at_bf16x8, w[qt].p[k]), o, 0, 0, 0);
-                const int row = row0 + qt * 16 + c;
-                const bool its = min(row, M - 1) / gm.G == t && sees >= 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) acc.o[qt][db][k] = its ? o[k] : acc.o[qt][db][k];
-              }
+                for (int qt = 0; qt < QT; ++qt)
+                  acc.o[qt][db][k] += !isfinite(x[k]) && trow + rr <= last[qt] ? x[k] : 0.f;
             }
-            __builtin_amdgcn_wave_barrier();
           }
         }
         __builtin_amdgcn_wave_barrier();
-      }
+        if (TAIL && n + 1 < own_tiles) {
+          load_keys(n + 1);
+          load_values(n + 1);
+        }
+      };
+      int n = 0;
+      for (; n < own_tiles && (int)(lo + wave + KS * n + 1) * kAtTile <= whole + 1; ++n)
+        tile(n, std::false_type{});
+      for (; n < own_tiles; ++n) tile(n, std::true_type{});
 
       // The piece's partial: (maximum, sum, unnormalized output) of each query row, the waves
       // joined in LDS.
       const int64_t slot = (int64_t)x + u;
+      int tid_j = tid;
+      asm volatile("" : "+v"(tid_j));
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
         if (last[qt] < 0) {  // (a query that is not there has seen what is seen by all)
@@ -380,6 +425,7 @@ paged_kernel(PagedArgs a) {
         float l_row = acc.l[qt];
         l_row += __shfl_xor(l_row, 16, 64);
         l_row += __shfl_xor(l_row, 32, 64);
+        const int g = (tid_j & 63) >> 4, c = tid_j & 15;
         constexpr int ROW = Shape::ROW;
         float* join = reinterpret_cast<float*>(lds);
         __syncthreads();  // every wave is done with its tiles (and with the tile before)
@@ -396,7 +442,7 @@ paged_kernel(PagedArgs a) {
               make_float4(o[0] * w, o[1] * w, o[2] * w, o[3] * w);
         }
         __syncthreads();
-        for (int i = tid; i < 16 * (D / 4); i += NT) {
+        for (int i = tid_j; i < 16 * (D / 4); i += NT) {
           const int rr = i / (D / 4), d4 = i % (D / 4);
           const int row = row0 + qt * 16 + rr;
           if (row >= M) continue;
