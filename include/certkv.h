@@ -504,7 +504,8 @@ certkv_status certkv_decode_tree(const certkv_problem* p, certkv_tensor q_new, i
  * scales.  Strides are in rows, >= 0, s_row >= 1, and s_layer = s_head = 0 for
  * units' lists; rows that two places share are the caller's.
  *   page         16, 32, ... or 1024 rows; num_pages * page and max_pages * page
- *                at most 2^31 - 1024, 16 s_row rows of k below 2^31 bytes
+ *                at most 2^31 - 1024, 16 s_row rows of k below 2^31 bytes, s_page
+ *                and s_head below 2^31
  *   table        [lists][max_pages] int32: the page of row i of a list is
  *                table[list][i / page]; entries behind its last page are not read
  *   offsets      [lists+1] int64: list r holds offsets[r+1] - offsets[r] rows

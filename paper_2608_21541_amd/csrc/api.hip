@@ -1284,7 +1284,7 @@ static certkv_status page_args(const certkv_problem* p, const certkv_pages* x, b
   if (x->s_row > (int64_t)INT32_MAX / 16 / mx_row_bytes(x->format, a->g.D))
     return CERTKV_EUNSUPPORTED;
   const int64_t far = (int64_t)1 << 52;
-  if (x->s_layer > far / a->g.L || x->s_page > far / x->num_pages || x->s_head > far / a->g.H)
+  if (x->s_layer > far / a->g.L || x->s_page > INT32_MAX || x->s_head > INT32_MAX)
     return CERTKV_EUNSUPPORTED;
   a->format = x->format;
   a->s_layer = x->s_layer;
@@ -1390,7 +1390,7 @@ certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* page
   TRY(page_args(p, pages, true, &a.p));
   if (out_dtype != CERTKV_BF16 && out_dtype != CERTKV_F32) return CERTKV_EUNSUPPORTED;
   if (rows < 0) return CERTKV_EINVAL;
-  if (rows > ((int64_t)1 << 44) / a.p.g.L / a.p.g.H) return CERTKV_EUNSUPPORTED;
+  if (rows > kPgMostRows / (a.p.per_head ? 1 : a.p.g.H)) return CERTKV_EUNSUPPORTED;
   if ((rows > 0 && !k_out && !v_out) || ((uintptr_t)k_out & 15u) || ((uintptr_t)v_out & 15u))
     return CERTKV_EINVAL;
   if ((p->flags & CERTKV_DRY_RUN) || rows == 0) return CERTKV_OK;
@@ -1430,8 +1430,9 @@ static bool paged_ws_layout(const PageArgs& x, int32_t tq, int32_t max_rows, Pag
   const int64_t shortest = (tiles + kPgMinTiles - 1) / kPgMinTiles;
   if (most < w->parts) most = w->parts;
   if (most > shortest) most = shortest;
+  if (pg_whole(w->cover, x.lists * (int64_t)w->copies)) most = 0;
   w->most = (int32_t)most;
-  const size_t part = (size_t)(most + (int64_t)x.lists * w->copies) * w->mp;
+  const size_t part = most ? (size_t)(most + (int64_t)x.lists * w->copies) * w->mp : 1;
   w->ml_off = up(part * (size_t)x.g.D * sizeof(float));
   w->total = up(w->ml_off + part * sizeof(float2));
   return true;

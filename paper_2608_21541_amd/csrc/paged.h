@@ -28,13 +28,23 @@ constexpr int kPgGap = 8;         // tiles between lists' places beside their ro
 constexpr int kPgMinTiles = 4;    // shortest chunk, and the unit of its length
 constexpr int kPgMaxTiles = kAtMaxKeys / kAtTile;  // longest, unless partials are short
 
+// Waves of a workgroup, by whether it has whole units.
+constexpr int pg_waves(bool whole) { return whole ? 8 : 4; }
+
+// Whether they have, by the most rows of a unit.
+#ifndef PG_WHOLE
+#define PG_WHOLE 1024
+#endif
+inline bool pg_whole(int64_t cover, int64_t) { return cover <= PG_WHOLE; }
+
 struct PagedArgs {
   PageArgs p;
   int32_t tq;
   int32_t copies;               // units of a list: L H of a sequence's, 1 of a head's
   int32_t cover;                // rows of a list that are attended
   int32_t qgroups, mp;          // workgroups of a chunk, query rows of a partial
-  int32_t parts, most;          // chunks taken at once, and that the workspace has room for
+  int32_t parts, most;          // chunks taken at once, and that the workspace has room for (0: a
+                                // workgroup has a whole unit)
   const int32_t* q_lens;        // [B], or NULL: tq
   certkv_tensor q;
   float* part_o;                // [most + U][mp][d]
@@ -73,7 +83,8 @@ struct PgOffsets {
   uint32_t R, at;
   int64_t base, rows, first, end;
   __device__ __forceinline__ PgOffsets(const int64_t* o, int32_t lists, int lane)
-      : off(o), R((uint32_t)lists) {
+      : off(o), R((uint32_t)lists), at(0), base(0), rows(0), first(0), end(0) {
+    if (lists == 0) return;  // (not asked for)
     window(0, lane);
     base = AtOffsets::lane64(first, 0);
     rows = (lists <= 64 ? AtOffsets::lane64(end, R - 1) : off[R]) - base;
@@ -105,6 +116,26 @@ struct PgOffsets {
   }
 };
 
+// Four dims of query row `row` of a unit: its unnormalized output o, sum L against reference m.
+__device__ __forceinline__ void pg_output(const PagedArgs& a, int l, int b, int h, int row, int d4,
+                                          int D, float4 o, float m, float L) {
+  const Geo& g = a.p.g;
+  const int t = row / g.G, gq = row % g.G;
+  const int64_t orow = ((int64_t)l * g.B * a.tq + (int64_t)b * a.tq + t) * (g.H * g.G) + h * g.G + gq;
+  const float inv = L == 0.f ? 0.f : 1.f / L;  // (nothing visible: out 0, lse -inf)
+  const float y[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+  bool fine = true;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    fine = fine && isfinite(y[i]);
+    a.out[orow * D + 4 * d4 + i] = y[i];
+  }
+  if (!fine) report_nonfinite(g);
+  if (a.lse && d4 == 0)
+    a.lse[orow] = L == 0.f ? -INFINITY
+                           : (ref_log2(m, g.scale * kAtLog2e) + __builtin_amdgcn_logf(L)) * kAtLn2;
+}
+
 // A lane's part of a row, from a place that is the wave's.  NT: non-temporally.
 template <bool NT, typename T>
 __device__ __forceinline__ void pg_load(T& x, const uint8_t* at, uint32_t off) {
@@ -119,11 +150,15 @@ __device__ __forceinline__ uint32_t pg_finite(uint32_t x) {
   return x;
 }
 
-template <int F, int D, int QT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(attend_waves(D, QT - 1)))) void
-paged_kernel(PagedArgs a) {
+// WHOLE: a workgroup of eight waves has a unit's rows from first to last, and writes its outputs
+// itself.
+template <int F, int D, int QT, bool WHOLE>
+__global__ __launch_bounds__(64 * pg_waves(WHOLE))
+__attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void paged_kernel(PagedArgs a) {
   using Shape = AtShape<D, 1, QT>;
-  constexpr int KS = Shape::KS, NT = Shape::NT, PARTS = Shape::PARTS;
+  constexpr int KS = pg_waves(WHOLE), NT = 64 * KS, PARTS = Shape::PARTS;
+  constexpr int ROW = D + 4;  // floats of a joined output row
+  constexpr int JOIN = 2 * KS * 16 * ROW, TILES = KS * AtTile<D>::V;  // bf16 elements
   constexpr int BITS = F == CERTKV_CACHE_BF16 ? 16 : F == CERTKV_CACHE_MXFP8 ? 8 : 4;
   constexpr bool MX = F != CERTKV_CACHE_BF16;
   constexpr int RB = mx_row_bytes(F, D);
@@ -133,15 +168,14 @@ paged_kernel(PagedArgs a) {
   // values: W bytes of a lane, so that a load is at most 16 rows; a tile is NLT loads
   constexpr int W = RB >= 64 ? 16 : 8, EV = W * 8 / BITS, LPR = RB / W, RPL = 64 / LPR;
   constexpr int NLT = kAtTile / RPL;
-  static_assert(RPL <= 16 && SK * NLK == KSTEP && NT == 256, "a load's rows are in one half");
-  __shared__ __align__(16) uint16_t lds[Shape::LDS];
+  static_assert(RPL <= 16 && SK * NLK == KSTEP, "a load's rows are in one half");
+  __shared__ __align__(16) uint16_t lds[TILES > JOIN ? TILES : JOIN];
   __shared__ float2 ml_s[KS * 16];
 
   const PageArgs& p = a.p;
   const Geo& gm = p.g;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 4, c = lane & 15;
   const int M = a.tq * gm.G, mp = a.mp;
   const float c2 = gm.scale * kAtLog2e;
   const uint32_t copies = (uint32_t)a.copies;
@@ -152,41 +186,57 @@ paged_kernel(PagedArgs a) {
   const uint32_t x0 = a.qgroups == 1 ? wgx : (wgx >> 3) / a.qgroups * 8 + (wgx & 7);
   const uint32_t xstep = gridDim.x / a.qgroups;
   const int row0 = qg * QT * 16;  // the first query row
-  auto kdim = [&](int ks) { return (ks / SK) * 4 * EK + g * EK + 8 * (ks % SK); };
-  uint16_t* const vt = lds + wave * Shape::GROUP;
-  // bytes from row to row and from page to page, and a lane's share of a load
-  const uint32_t st = (uint32_t)p.s_row * RB;
-  const uint64_t page_bytes = (uint64_t)p.s_page * RB;
-  const uint32_t k_off = c * st + g * WK, v_off = (lane / LPR) * st + (lane % LPR) * W;
-  const uint32_t ks_off = c * (uint32_t)p.s_row * (D / 32);
-  const uint32_t vs_off = (lane / LPR) * (uint32_t)p.s_row * (D / 32) + (lane % LPR) * EV / 32;
-
-  PgOffsets off(p.offsets, p.lists, lane);
-  const PgCut cut = pg_cut(a, off.rows);
-  const uint32_t nch = (cut.total + cut.tiles - 1) / cut.tiles;
-  for (uint32_t x = x0; x < nch; x += xstep) {
+  uint16_t* const vt = lds + wave * AtTile<D>::V;
+  // The units' pieces: of the chunks that the workgroup takes, or the whole units.
+  PgOffsets off(p.offsets, WHOLE ? 0 : p.lists, lane);
+  const PgCut cut = WHOLE ? PgCut{1, 0} : pg_cut(a, off.rows);
+  const uint32_t nch = WHOLE ? (uint32_t)p.lists * copies : (cut.total + cut.tiles - 1) / cut.tiles;
+  for (uint32_t x = x0; x < nch; x = WHOLE ? nch : x + xstep) {
     const uint32_t r0 = x * cut.tiles, r1 = min(cut.total, r0 + cut.tiles);
-    uint32_t r = off.find(r0 / copies, lane), copy = 0;
+    uint32_t r = WHOLE ? x / copies : off.find(r0 / copies, lane), copy = WHOLE ? x - r * copies : 0;
     bool begun = false;
-    while (r < off.R) {
+    while (WHOLE ? !begun : r < off.R) {
       int64_t p0, p1;
-      off.list(r, lane, p0, p1);
-      const uint32_t place = copies * pg_place(p0, r);
-      const uint32_t span = pg_place(p1, r + 1) - pg_place(p0, r);
-      if (!begun) copy = r0 > place ? (r0 - place) / span : 0;
-      begun = true;
-      if (copy >= copies) {
-        ++r, copy = 0;
-        continue;
+      uint32_t u = x, lo = 0, mine = copy;
+      int len, ntp;
+      if constexpr (WHOLE) {
+        begun = true;
+        p0 = p.offsets[r], p1 = p.offsets[r + 1];
+        len = min(page_rows(p, p0, p1), a.cover);
+        if (p1 - p0 != len && tid == 0) report_range(gm);
+        ntp = (int)pg_up(len);
+      } else {
+        off.list(r, lane, p0, p1);
+        const uint32_t place = copies * pg_place(p0, r);
+        const uint32_t span = pg_place(p1, r + 1) - pg_place(p0, r);
+        if (!begun) copy = r0 > place ? (r0 - place) / span : 0;
+        begun = true;
+        if (copy >= copies) {
+          ++r, copy = 0;
+          continue;
+        }
+        const uint32_t vs = place + copy * span;
+        u = r * copies + copy;
+        if (vs >= r1) break;
+        // the piece: tiles [lo, lo + ntp) of the unit's
+        len = min(page_rows(p, p0, p1), a.cover);
+        lo = max(r0, vs) - vs;
+        ntp = (int)min(r1 - vs, pg_up(len)) - (int)lo;
+        mine = copy++;
+        if (ntp <= 0) continue;  // (only what lies between units)
       }
-      const uint32_t vs = place + copy * span, u = r * copies + copy;
-      if (vs >= r1) break;
-      // the piece: tiles [lo, lo + ntp) of the unit's
-      const int len = min(page_rows(p, p0, p1), a.cover);
-      const uint32_t lo = max(r0, vs) - vs;
-      const int ntp = (int)min(r1 - vs, pg_up(len)) - (int)lo;
-      const uint32_t mine = copy++;
-      if (ntp <= 0) continue;  // (only what lies between units)
+      // (What follows from the lane is worked out for each piece: kept beyond it, it would take
+      // registers from the loads in flight.)
+      int lane = tid & 63;
+      if constexpr (!WHOLE) asm volatile("" : "+v"(lane));
+      const int g = lane >> 4, c = lane & 15;
+      auto kdim = [&](int ks) { return (ks / SK) * 4 * EK + g * EK + 8 * (ks % SK); };
+      // bytes from row to row and from page to page, and a lane's share of a load
+      const uint32_t st = (uint32_t)p.s_row * RB;
+      const uint64_t page_bytes = (uint64_t)p.s_page * RB;
+      const uint32_t k_off = c * st + g * WK, v_off = (lane / LPR) * st + (lane % LPR) * W;
+      const uint32_t ks_off = c * (uint32_t)p.s_row * (D / 32);
+      const uint32_t vs_off = (lane / LPR) * (uint32_t)p.s_row * (D / 32) + (lane % LPR) * EV / 32;
       int l, b, h;
       if (p.per_head) {
         h = (int)(r % (uint32_t)gm.H), b = (int)(r / gm.H % (uint32_t)gm.B);
@@ -426,13 +476,12 @@ paged_kernel(PagedArgs a) {
         l_row += __shfl_xor(l_row, 16, 64);
         l_row += __shfl_xor(l_row, 32, 64);
         const int g = (tid_j & 63) >> 4, c = tid_j & 15;
-        constexpr int ROW = Shape::ROW;
         float* join = reinterpret_cast<float*>(lds);
         __syncthreads();  // every wave is done with its tiles (and with the tile before)
         if (g == 0) ml_s[wave * 16 + c] = make_float2(acc.m[qt], l_row);
         __syncthreads();
         float mx = kAtNone;
-#pragma unroll
+#pragma unroll 4
         for (int k = 0; k < KS; ++k) mx = fmaxf(mx, ml_s[k * 16 + c].x);
         const float w = __builtin_amdgcn_exp2f(acc.m[qt] - mx);
 #pragma unroll
@@ -447,23 +496,27 @@ paged_kernel(PagedArgs a) {
           const int row = row0 + qt * 16 + rr;
           if (row >= M) continue;
           float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
+#pragma unroll 4
           for (int k = 0; k < KS; ++k) {
             const float4 y = *reinterpret_cast<const float4*>(join + (k * 16 + rr) * ROW + 4 * d4);
             o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
           }
-          const int64_t pr = slot * mp + row;
-          reinterpret_cast<float4*>(a.part_o + pr * D)[d4] = o;
-          if (d4 == 0) {
-            float mm = kAtNone, sum = 0.f;
-#pragma unroll
+          float mm = kAtNone, sum = 0.f;
+          if (WHOLE || d4 == 0) {
+#pragma unroll 4
             for (int k = 0; k < KS; ++k) mm = fmaxf(mm, ml_s[k * 16 + rr].x);
-#pragma unroll
+#pragma unroll 4
             for (int k = 0; k < KS; ++k) {
               const float2 ml = ml_s[k * 16 + rr];
               sum += ml.y * __builtin_amdgcn_exp2f(ml.x - mm);
             }
-            a.part_ml[pr] = make_float2(mm, sum);
+          }
+          if constexpr (WHOLE) {
+            pg_output(a, l, b, h, row, d4, D, o, mm, sum);
+          } else {
+            const int64_t pr = slot * mp + row;
+            reinterpret_cast<float4*>(a.part_o + pr * D)[d4] = o;
+            if (d4 == 0) a.part_ml[pr] = make_float2(mm, sum);
           }
         }
       }
@@ -472,22 +525,25 @@ paged_kernel(PagedArgs a) {
   }
 }
 
-template <int F>
-static certkv_status launch_paged(const PagedArgs& a, int shape, hipStream_t s) {
+template <int F, int D, int QT>
+static certkv_status launch_paged_d(const PagedArgs& a, hipStream_t s) {
+  if (a.most == 0) {
+    const int64_t U = (int64_t)a.p.lists * a.copies;
+    const dim3 grid((unsigned)(a.qgroups == 1 ? U : (U + 7) / 8 * 8 * a.qgroups));
+    CERTKV_LAUNCH("paged_whole", (paged_kernel<F, D, QT, true>), grid, dim3(64 * pg_waves(true)), 0, s, a);
+    return CERTKV_OK;
+  }
   const int wgs = a.most < a.parts ? a.most : a.parts;
   const dim3 grid(a.qgroups == 1 ? wgs : (wgs + 7) / 8 * 8 * a.qgroups);
-  if (a.p.g.D == 128) {
-    if (shape == kAtOne)
-      CERTKV_LAUNCH("paged", (paged_kernel<F, 128, 1>), grid, dim3(256), 0, s, a);
-    else
-      CERTKV_LAUNCH("paged", (paged_kernel<F, 128, 2>), grid, dim3(256), 0, s, a);
-  } else {
-    if (shape == kAtOne)
-      CERTKV_LAUNCH("paged", (paged_kernel<F, 64, 1>), grid, dim3(256), 0, s, a);
-    else
-      CERTKV_LAUNCH("paged", (paged_kernel<F, 64, 2>), grid, dim3(256), 0, s, a);
-  }
+  CERTKV_LAUNCH("paged", (paged_kernel<F, D, QT, false>), grid, dim3(64 * pg_waves(false)), 0, s, a);
   return CERTKV_OK;
+}
+
+template <int F>
+static certkv_status launch_paged(const PagedArgs& a, int shape, hipStream_t s) {
+  if (a.p.g.D == 128)
+    return shape == kAtOne ? launch_paged_d<F, 128, 1>(a, s) : launch_paged_d<F, 128, 2>(a, s);
+  return shape == kAtOne ? launch_paged_d<F, 64, 1>(a, s) : launch_paged_d<F, 64, 2>(a, s);
 }
 
 }  // namespace certkv

@@ -89,20 +89,7 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
   } else {
     b = (int)r, l = (int)(copy / (uint32_t)g.H), h = (int)(copy % (uint32_t)g.H);
   }
-  const int t = row / g.G, gq = row % g.G;
-  const int64_t orow = ((int64_t)l * g.B * a.tq + (int64_t)b * a.tq + t) * (g.H * g.G) + h * g.G + gq;
-  const float inv = L == 0.f ? 0.f : 1.f / L;  // (nothing visible: out 0, lse -inf)
-  const float y[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
-  bool fine = true;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    fine = fine && isfinite(y[i]);
-    a.out[orow * D + 4 * c4 + i] = y[i];
-  }
-  if (!fine) report_nonfinite(g);
-  if (a.lse && c4 == 0)
-    a.lse[orow] = L == 0.f ? -INFINITY
-                           : (ref_log2(m, g.scale * kAtLog2e) + __builtin_amdgcn_logf(L)) * kAtLn2;
+  pg_output(a, l, b, h, row, c4, D, o, m, L);
 }
 
 template <int D>
@@ -124,7 +111,7 @@ certkv_status run_paged(const PagedArgs& a, int shape, hipStream_t s) {
   const certkv_status st = a.p.format == CERTKV_CACHE_MXFP8   ? run_paged_mxfp8(a, shape, s)
                            : a.p.format == CERTKV_CACHE_MXFP4 ? run_paged_mxfp4(a, shape, s)
                                                               : run_paged_bf16(a, shape, s);
-  if (st != CERTKV_OK) return st;
+  if (st != CERTKV_OK || a.most == 0) return st;
   return a.p.g.D == 128 ? launch_paged_join<128>(a, s) : launch_paged_join<64>(a, s);
 }
 

@@ -15,8 +15,13 @@ constexpr int kPgSmallSlots = 16384;  // slots that the scan's own workgroup fil
 // behind the free ones, from sum_{i<r} give_i on; its slots stand from sum_{i<r} max(0, change_i)
 // on.  Lists are refused in order, so that a list that takes pages has none that is refused for
 // their number before it, and the places taken have no gap.  (Refused for its own length: need
-// counts as 0.)  A scan of the lists by one workgroup, 1024 at a time, then the slots and table
-// entries from the sums: by the same workgroup where they are few, else by a second launch.
+// counts as 0.)
+//
+// The sums are a scan of the lists, a workgroup's; the slots and table entries follow from them.
+// Up to 1024 lists one launch does both: few slots by the scan's own workgroup, many by workgroups
+// that each scan all lists and take a share of the slots.  More lists: a second launch.
+// Bound by latency: a launch, three loads in turn (offsets, then entries of the table or ring)
+// and the scan.
 
 // What the second part needs of each list, in the workspace or LDS.
 struct PgLists {
@@ -40,35 +45,55 @@ size_t page_resize_ws(int64_t lists) {
   return (size_t)(64 + 3 * pg_pad(lists) + pg_pad(lists + 1)) * sizeof(int32_t);
 }
 
+// x of the lane that a data-parallel step takes it from, 0 where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int32_t pg_dpp(int32_t x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t pg_dpp(int64_t x) {
+  const uint32_t lo = (uint32_t)pg_dpp<CTRL, ROWS>((int32_t)x);
+  return (int64_t)((uint64_t)(uint32_t)pg_dpp<CTRL, ROWS>((int32_t)(x >> 32)) << 32 | lo);
+}
+// Sums up to and with the lane's own: within rows of 16 lanes, then of the rows before.
 template <typename T, typename F>
-__device__ __forceinline__ T pg_wave_scan(T x, int lane, F add) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const T y = __shfl_up(x, d, 64);
-    if (lane >= d) x = add(x, y);
-  }
-  return x;
+__device__ __forceinline__ T pg_wave_scan(T x, F add) {
+  x = add(x, pg_dpp<0x111, 0xf>(x));  // one lane up, two, four, eight
+  x = add(x, pg_dpp<0x112, 0xf>(x));
+  x = add(x, pg_dpp<0x114, 0xf>(x));
+  x = add(x, pg_dpp<0x118, 0xf>(x));
+  x = add(x, pg_dpp<0x142, 0xa>(x));  // the last of the row before, to rows 1 and 3
+  return add(x, pg_dpp<0x143, 0xc>(x));  // the last of the first half, to the second
 }
 
-// The slot of row `row` of list r, which has `had` rows and new pages from place pos on; its new
-// pages' table entries are written by the threads of their first rows.
-__device__ __forceinline__ int32_t pg_slot(const PageResizeArgs& a, int64_t r, int32_t row,
-                                           int32_t had, int32_t pos) {
-  if (pos < 0) return -1;
-  const int32_t mask = (1 << a.lp) - 1, held = (had + mask) >> a.lp, pi = row >> a.lp;
+// The number of page pi of list r, which had `held` pages and has its new ones from place pos of
+// the ring on; -1 for one that is none of the pool's.  first: the caller's row is the page's first,
+// and writes a new page's table entry.
+__device__ __forceinline__ int32_t pg_page(const PageResizeArgs& a, int64_t r, int32_t pi, int32_t held,
+                                           int32_t pos, bool first) {
   int32_t* entry = a.table + r * a.max_pages + pi;
   int32_t id;
   if (pi < held) {
     id = *entry;
   } else {
-    id = a.ring[(uint32_t)(pos + (pi - held)) % (uint32_t)a.num_pages];
-    if ((row & mask) == 0) *entry = id;
+    const uint32_t at = (uint32_t)(pos + (pi - held)), n = (uint32_t)a.num_pages;  // below 2 n
+    id = a.ring[at < n ? at : at - n];
+    if (first) *entry = id;
   }
   if ((uint32_t)id >= (uint32_t)a.num_pages) {  // (the caller's numbers)
     report_range(a.g);
     return -1;
   }
-  return (id << a.lp) + (row & mask);
+  return id;
+}
+// The slot of row `row` of list r, which has `had` rows and new pages from place pos on (-1: it is
+// refused).
+__device__ __forceinline__ int32_t pg_slot(const PageResizeArgs& a, int64_t r, int32_t row,
+                                           int32_t had, int32_t pos) {
+  if (pos < 0) return -1;
+  const int32_t mask = (1 << a.lp) - 1, in = row & mask;
+  const int32_t id = pg_page(a, r, row >> a.lp, (had + mask) >> a.lp, pos, in == 0);
+  return id < 0 ? -1 : (id << a.lp) + in;
 }
 
 // The last r of [lo, hi] with first(r) <= x.
@@ -84,15 +109,54 @@ __device__ __forceinline__ int32_t pg_bisect(int32_t lo, int32_t hi, F first, in
   return lo;
 }
 
-template <bool SMALL>
-__global__ __launch_bounds__(kPgScan) void page_resize_kernel(PageResizeArgs a) {
-  constexpr int W = kPgScan / 64;
+// Slots j .. j + 3 of those before `end`, from the lists' sums: so(r) the first of list r's,
+// had(r) and pos(r) as pg_slot takes them; the lists of j and of the last are in [ra, rb].
+template <typename S, typename A, typename B>
+__device__ __forceinline__ void pg_slots4(const PageResizeArgs& a, int64_t j, int64_t end, int32_t ra,
+                                          int32_t rb, S so, A had, B pos) {
+  int32_t r = pg_bisect(ra, rb, so, j), h = had(r), p = pos(r), out[4];
+  int64_t first = so(r), next = so(r + 1);
+  if (j + 4 <= next && j + 4 <= end) {  // one list's: rows of one page, or of two
+    const int32_t mask = (1 << a.lp) - 1, held = (h + mask) >> a.lp, row = (int32_t)(h + (j - first));
+    const int32_t in = row & mask, pi = row >> a.lp;
+    int32_t id = -1, id2 = -1;
+    if (p >= 0) {
+      id = id2 = pg_page(a, r, pi, held, p, in == 0);
+      if (in + 3 > mask) id2 = pg_page(a, r, pi + 1, held, p, true);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int32_t x = in + i, of = x > mask ? id2 : id;
+      out[i] = of < 0 ? -1 : (of << a.lp) + (x & mask);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i > 0 && j + i >= next && j + i < end) {
+        r = pg_bisect(r + 1, rb, so, j + i);
+        first = so(r), next = so(r + 1);
+        h = had(r), p = pos(r);
+      }
+      out[i] = j + i < end ? pg_slot(a, r, (int32_t)(h + (j + i - first)), h, p) : -1;
+    }
+  }
+  if (j + 4 <= end && ((uintptr_t)(a.slots + j) & 15u) == 0) {
+    *reinterpret_cast<int4*>(a.slots + j) = make_int4(out[0], out[1], out[2], out[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (j + i < end) a.slots[j + i] = out[i];
+  }
+}
+
+// W waves scan K lists a lane at a time.  PART: 0, this is the only workgroup and does all; 1, every
+// workgroup scans, the first writes the sums; 2, the sums alone, for page_slots_kernel.
+template <int W, int K, int PART>
+__global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
+  constexpr int NT = 64 * W, STEP = NT * K, HELD = PART == 2 ? 1 : STEP;
   __shared__ int32_t need_s[W], give_s[W], taken_s;
   __shared__ int64_t add_s[W], len_s[W], end_s;
-  // (up to kPgScan lists)
-  __shared__ int32_t had_s[SMALL ? kPgScan : 1], pos_s[SMALL ? kPgScan : 1];
-  __shared__ int32_t keep_s[SMALL ? kPgScan : 1], go_s[SMALL ? kPgScan + 1 : 1];
-  __shared__ int32_t so_s[SMALL ? kPgScan + 1 : 1];
+  __shared__ int32_t had_s[HELD], pos_s[HELD], keep_s[HELD], go_s[HELD + 1], so_s[HELD + 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t R = a.lists, N = a.num_pages, mask = (1 << a.lp) - 1;
   const int64_t most_rows = (int64_t)a.max_pages << a.lp;
@@ -101,6 +165,7 @@ __global__ __launch_bounds__(kPgScan) void page_resize_kernel(PageResizeArgs a) 
   const int64_t free_pages = a.free[1];
   const int32_t count = (int32_t)(free_pages < 0 ? 0 : free_pages < N ? free_pages : N);
   const PgLists ws = pg_lists(a.ws, R);
+  const bool tells = PART != 1 || blockIdx.x == 0;
   // sums of pages stop at N + 1, more than there are
   const auto sat = [N](int32_t x, int32_t y) { return min(x + y, N + 1); };
   const auto sum = [](int64_t x, int64_t y) { return x + y; };
@@ -108,35 +173,46 @@ __global__ __launch_bounds__(kPgScan) void page_resize_kernel(PageResizeArgs a) 
   int64_t add_c = 0, len_c = 0, old_end = base;
   bool refused = free_pages != count;
   if (tid == 0) taken_s = 0;
-  for (int32_t r0 = 0; r0 < R; r0 += kPgScan) {
-    const int32_t r = r0 + tid;
-    const bool in = r < R;
+  for (int32_t r0 = 0; r0 < R; r0 += STEP) {
+    const int32_t r = r0 + tid * K;
+    int32_t had[K], need[K], give[K], add[K];
+    int64_t will[K];
+    bool fits[K];
+    int32_t need_t = 0, give_t = 0;
+    int64_t add_t = 0;
     // (offsets_out may be offsets: the step before has written this one's first)
-    const int64_t first = tid == 0 ? old_end : in ? a.offsets[r] : 0;
-    const int64_t end = in ? a.offsets[r + 1] : 0;
-    const int32_t change = in ? a.change[r] : 0;
-    const int64_t n = end - first;
-    const int32_t had = (int32_t)(n < 0 || !in ? 0 : n < most_rows ? n : most_rows);
-    const int64_t sumrows = (int64_t)had + change, will = sumrows < 0 ? 0 : sumrows;
-    const int32_t held = (had + mask) >> a.lp;
-    const int64_t want = (will + mask) >> a.lp;
-    const bool fits = want <= a.max_pages;
-    int32_t need = 0, give = 0;
-    if (want > held && fits) need = (int32_t)min(want - held, (int64_t)N + 1);
-    if (want < held) give = min(held - (int32_t)want, N + 1);
-    const int32_t add = change > 0 ? change : 0;
-    const int32_t need_i = pg_wave_scan(need, lane, sat);
-    const int32_t give_i = pg_wave_scan(give, lane, sat);
-    const int64_t add_i = pg_wave_scan((int64_t)add, lane, sum);
+    int64_t first = tid == 0 ? old_end : r < R ? a.offsets[r] : 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const bool in = r + k < R;
+      const int64_t end = in ? a.offsets[r + k + 1] : first;
+      const int32_t change = in ? a.change[r + k] : 0;
+      const int64_t n = end - first;
+      first = end;
+      had[k] = (int32_t)(n < 0 ? 0 : n < most_rows ? n : most_rows);
+      will[k] = max((int64_t)had[k] + change, (int64_t)0);
+      const int32_t held = (had[k] + mask) >> a.lp;
+      const int64_t want = (will[k] + mask) >> a.lp;
+      fits[k] = want <= a.max_pages;
+      need[k] = want > held && fits[k] ? (int32_t)min(want - held, (int64_t)N + 1) : 0;
+      give[k] = want < held ? min(held - (int32_t)want, N + 1) : 0;
+      add[k] = change > 0 ? change : 0;
+      need_t = sat(need_t, need[k]);
+      give_t = sat(give_t, give[k]);
+      add_t += add[k];
+    }
+    const int32_t need_i = pg_wave_scan(need_t, sat), give_i = pg_wave_scan(give_t, sat);
+    const int64_t add_i = pg_wave_scan(add_t, sum);
     if (lane == 63) {
       need_s[wave] = need_i;
       give_s[wave] = give_i;
       add_s[wave] = add_i;
     }
-    if (tid == kPgScan - 1) end_s = end;
+    if (tid == NT - 1) end_s = first;
     __syncthreads();
     int32_t need_b = need_c, give_b = give_c;
     int64_t add_b = add_c;
+#pragma unroll
     for (int w = 0; w < W; ++w) {
       if (w < wave) {
         need_b = sat(need_b, need_s[w]);
@@ -148,36 +224,57 @@ __global__ __launch_bounds__(kPgScan) void page_resize_kernel(PageResizeArgs a) 
       add_c += add_s[w];
     }
     old_end = end_s;
-    const int64_t add_e = add_b + add_i;  // with this list's
-    const bool room = add == 0 || add_e <= a.slot_capacity;
-    const bool ok = fits && room && (need == 0 || sat(need_b, need_i) <= count);
-    refused |= !ok;
-    if (ok && need > 0) atomicMax(&taken_s, sat(need_b, need_i));
-    const int64_t len = !in ? 0 : ok ? will : had;
-    const int64_t len_i = pg_wave_scan(len, lane, sum);
+    // of the lists before the lane's (not its sums less its own: they may have stopped)
+    const int32_t need_l = __shfl_up(need_i, 1, 64), give_l = __shfl_up(give_i, 1, 64);
+    int32_t need_e = sat(need_b, lane ? need_l : 0), give_e = sat(give_b, lane ? give_l : 0);
+    int64_t add_e = add_b + add_i - add_t, len_t = 0, len[K];
+    int32_t pos[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int32_t need_n = sat(need_e, need[k]);
+      add_e += add[k];
+      const bool ok = fits[k] && (add[k] == 0 || add_e <= a.slot_capacity) &&
+                      (need[k] == 0 || need_n <= count);
+      refused |= !ok;
+      if (ok && need[k] > 0) atomicMax(&taken_s, need_n);
+      pos[k] = ok ? (int32_t)((uint32_t)(head + need_e) % (uint32_t)N) : -1;
+      need_e = need_n;
+      len[k] = r + k >= R ? 0 : ok ? will[k] : had[k];
+      len_t += len[k];
+    }
+    const int64_t len_i = pg_wave_scan(len_t, sum);
     if (lane == 63) len_s[wave] = len_i;
     __syncthreads();
     int64_t len_b = len_c;
+#pragma unroll
     for (int w = 0; w < W; ++w) {
       if (w < wave) len_b += len_s[w];
       len_c += len_s[w];
     }
-    if (in) {
-      const int32_t pos = ok ? (int32_t)((uint32_t)(head + need_b + need_i - need) % (uint32_t)N) : -1;
-      const int32_t go = sat(give_b, give_i);
-      a.offsets_out[r + 1] = base + len_b + len_i;
-      a.slot_offsets[r + 1] = add_e;
-      if constexpr (SMALL) {
-        had_s[r] = had;
-        pos_s[r] = pos;
-        keep_s[r] = (int32_t)want;
-        go_s[r + 1] = go;
-        so_s[r + 1] = (int32_t)min(add_e, (int64_t)kPgSmallSlots + 1);
+    len_b += len_i - len_t;
+    add_e = add_b + add_i - add_t;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      add_e += add[k];
+      len_b += len[k];
+      give_e = sat(give_e, give[k]);
+      if (r + k >= R) continue;
+      if (tells) {
+        a.offsets_out[r + k + 1] = base + len_b;
+        a.slot_offsets[r + k + 1] = add_e;
+      }
+      const int32_t keep = (int32_t)min((will[k] + mask) >> a.lp, (int64_t)a.max_pages);
+      if constexpr (PART != 2) {
+        had_s[r + k] = had[k];
+        pos_s[r + k] = pos[k];
+        keep_s[r + k] = keep;
+        go_s[r + k + 1] = give_e;
+        so_s[r + k + 1] = (int32_t)min(add_e, (int64_t)INT32_MAX);
       } else {
-        ws.had[r] = had;
-        ws.pos[r] = pos;
-        ws.keep[r] = (int32_t)min(want, (int64_t)a.max_pages);
-        ws.give[r + 1] = go;
+        ws.had[r + k] = had[k];
+        ws.pos[r + k] = pos[k];
+        ws.keep[r + k] = keep;
+        ws.give[r + k + 1] = give_e;
       }
     }
   }
@@ -187,12 +284,14 @@ __global__ __launch_bounds__(kPgScan) void page_resize_kernel(PageResizeArgs a) 
   const int32_t given = min(give_c, N - count);  // (more: the ring's pages and the lists' overlap)
   const int32_t tail = (int32_t)((uint32_t)(head + count) % (uint32_t)N);
   if (tid == 0) {
-    a.offsets_out[0] = base;
-    a.slot_offsets[0] = 0;
-    a.free_out[0] = (uint32_t)(head + taken) % (uint32_t)N;
-    a.free_out[1] = count - taken + given;
-    if (give_c > given) report_range(a.g);
-    if constexpr (SMALL) {
+    if (tells) {
+      a.offsets_out[0] = base;
+      a.slot_offsets[0] = 0;
+      a.free_out[0] = (uint32_t)(head + taken) % (uint32_t)N;
+      a.free_out[1] = count - taken + given;
+      if (give_c > given) report_range(a.g);
+    }
+    if constexpr (PART != 2) {
       go_s[0] = so_s[0] = 0;
     } else {
       ws.give[0] = 0;
@@ -200,20 +299,34 @@ __global__ __launch_bounds__(kPgScan) void page_resize_kernel(PageResizeArgs a) 
       ws.tail[1] = given;
     }
   }
-  if constexpr (SMALL) {
+  if constexpr (PART != 2) {
     __syncthreads();
-    const int32_t total = (int32_t)min(add_c, a.slot_capacity);
-    for (int32_t j = tid; j < total; j += kPgScan) {
-      const int32_t r = pg_bisect(0, R - 1, [&](int32_t i) { return (int64_t)so_s[i]; }, j);
-      const int32_t row = had_s[r] + (j - so_s[r]);
-      a.slots[j] = pg_slot(a, r, row, had_s[r], pos_s[r]);
+    const uint32_t total = (uint32_t)min(add_c, a.slot_capacity);
+    const uint32_t at = (PART == 1 ? blockIdx.x : 0) * NT + tid, step = (PART == 1 ? gridDim.x : 1) * NT;
+    const auto so = [&](int32_t i) { return (int64_t)so_s[i]; };
+    if constexpr (PART == 0) {
+      for (uint32_t j = at; j < total; j += step) {
+        const int32_t r = pg_bisect(0, R - 1, so, j);
+        a.slots[j] = pg_slot(a, r, had_s[r] + (int32_t)(j - so_s[r]), had_s[r], pos_s[r]);
+      }
+    } else {
+      for (int64_t j = 4 * (int64_t)at; j < total; j += 4 * (int64_t)step)
+        pg_slots4(a, j, total, 0, R - 1, so, [&](int32_t r) { return had_s[r]; },
+                  [&](int32_t r) { return pos_s[r]; });
     }
-    for (int32_t i = tid; i < given; i += kPgScan) {
+    for (uint32_t i = at; i < (uint32_t)given; i += step) {
       const int32_t r = pg_bisect(0, R - 1, [&](int32_t q) { return (int64_t)go_s[q]; }, i);
       a.ring[(uint32_t)(tail + i) % (uint32_t)N] =
-          a.table[(int64_t)r * a.max_pages + keep_s[r] + (i - go_s[r])];
+          a.table[(int64_t)r * a.max_pages + keep_s[r] + ((int32_t)i - go_s[r])];
     }
   }
+}
+
+// The sums that a launch of many workgroups left beside the offsets that they read, in their place.
+__global__ __launch_bounds__(kPgThreads) void page_sums_kernel(PageResizeArgs a, const int64_t* offsets,
+                                                               const int64_t* free_state) {
+  for (int32_t r = threadIdx.x; r <= a.lists; r += kPgThreads) a.offsets_out[r] = offsets[r];
+  if (threadIdx.x < 2) a.free_out[threadIdx.x] = free_state[threadIdx.x];
 }
 
 // The last list r < R with first(r) <= x, by a wave: 64 lists' ends to a step.
@@ -241,20 +354,21 @@ __global__ __launch_bounds__(kPgThreads) void page_slots_kernel(PageResizeArgs a
   const auto so = [&](int32_t r) { return a.slot_offsets[r]; };
   const auto go = [&](int32_t r) { return (int64_t)ws.give[r]; };
   const int64_t total = min(a.slot_offsets[R], a.slot_capacity);
-  // a run of the slots for each wave
-  const int64_t per = ((total + waves - 1) / waves + 63) / 64 * 64;
+  // a run of the slots for each wave, four of one place in a row to a lane
+  const int64_t per = ((total + waves - 1) / waves + 255) / 256 * 256;
   const int64_t j0 = wave * per, j1 = min(total, j0 + per);
   if (j0 < j1) {
     const int32_t ra = pg_find(R, so, j0, lane), rb = pg_find(R, so, j1 - 1, lane);
-    for (int64_t j = j0 + lane; j < j1; j += 64) {
-      const int32_t r = pg_bisect(ra, rb, so, j);
-      const int32_t had = ws.had[r];
-      a.slots[j] = pg_slot(a, r, (int32_t)(had + (j - so(r))), had, ws.pos[r]);
+    for (int64_t j = j0 + 4 * lane; j < j1; j += 256) {
+      pg_slots4(a, j, j1, ra, rb, so, [&](int32_t r) { return ws.had[r]; },
+                [&](int32_t r) { return ws.pos[r]; });
     }
   }
   const int32_t tail = ws.tail[0], given = ws.tail[1];
-  for (int64_t i = wave * 64 + lane; i < given; i += waves * 64) {
-    const int32_t r = pg_bisect(0, R - 1, go, i);
+  for (int64_t i0 = wave * 64; i0 < given; i0 += waves * 64) {
+    const int64_t i = min(i0 + lane, (int64_t)given - 1);
+    const int32_t ra = pg_find(R, go, i0, lane), rb = pg_find(R, go, min(i0 + 63, (int64_t)given - 1), lane);
+    const int32_t r = pg_bisect(ra, rb, go, i);
     a.ring[(uint32_t)(tail + i) % (uint32_t)a.num_pages] =
         a.table[(int64_t)r * a.max_pages + ws.keep[r] + (i - go(r))];
   }
@@ -262,26 +376,69 @@ __global__ __launch_bounds__(kPgThreads) void page_slots_kernel(PageResizeArgs a
 
 certkv_status run_page_resize(const PageResizeArgs& a, hipStream_t s) {
   if (a.lists <= kPgScan && a.slot_capacity <= kPgSmallSlots) {
-    CERTKV_LAUNCH("page_resize", (page_resize_kernel<true>), dim3(1), dim3(kPgScan), 0, s, a);
+    if (a.lists <= 64 && a.slot_capacity <= 1024)
+      CERTKV_LAUNCH("page_resize", (page_resize_kernel<1, 1, 0>), dim3(1), dim3(64), 0, s, a);
+    else if (a.lists <= 256 && a.slot_capacity <= 4096)
+      CERTKV_LAUNCH("page_resize", (page_resize_kernel<4, 1, 0>), dim3(1), dim3(256), 0, s, a);
+    else
+      CERTKV_LAUNCH("page_resize", (page_resize_kernel<16, 1, 0>), dim3(1), dim3(1024), 0, s, a);
     return CERTKV_OK;
   }
-  CERTKV_LAUNCH("page_resize", (page_resize_kernel<false>), dim3(1), dim3(kPgScan), 0, s, a);
-  CERTKV_LAUNCH("page_slots", page_slots_kernel, dim3(4 * 256), dim3(kPgThreads), 0, s, a);
+  if (a.lists <= kPgScan) {
+    // (in place, the sums would be written while others read: they wait in the workspace)
+    const bool in_place = a.offsets_out == a.offsets || a.free_out == a.free;
+    PageResizeArgs b = a;
+    if (in_place) {
+      b.offsets_out = reinterpret_cast<int64_t*>(a.ws);
+      b.free_out = b.offsets_out + a.lists + 1;
+    }
+    const int64_t wgs = (a.slot_capacity + 1023) / 1024;
+    const dim3 grid((unsigned)(wgs < 4 * 256 ? wgs : 4 * 256));
+    if (a.lists <= 256)
+      CERTKV_LAUNCH("page_resize", (page_resize_kernel<4, 1, 1>), grid, dim3(256), 0, s, b);
+    else
+      CERTKV_LAUNCH("page_resize", (page_resize_kernel<4, 4, 1>), grid, dim3(256), 0, s, b);
+    if (in_place)
+      CERTKV_LAUNCH("page_sums", page_sums_kernel, dim3(1), dim3(kPgThreads), 0, s, a, b.offsets_out,
+                    b.free_out);
+    return CERTKV_OK;
+  }
+  CERTKV_LAUNCH("page_resize", (page_resize_kernel<16, 4, 2>), dim3(1), dim3(1024), 0, s, a);
+  CERTKV_LAUNCH("page_slots", page_slots_kernel, dim3(8 * 256), dim3(kPgThreads), 0, s, a);
   return CERTKV_OK;
 }
 
 // ---- rows to slots --------------------------------------------------------------
 
+// n / d for n < 2^31, by a product: with 2^(s-1) < d <= 2^s, n / d = (n + (n m >> 32)) >> s for
+// m = floor(2^32 (2^s - d) / d) + 1.  (The hardware has no integer division.)
+struct PgDiv {
+  uint32_t m, s;
+  explicit PgDiv(uint32_t d) : m(1), s(0) {
+    if (d == 0) return;  // (not asked)
+    while (((uint64_t)1 << s) < d) ++s;
+    m = (uint32_t)((((((uint64_t)1 << s) - d) << 32) / d) + 1);
+  }
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (n + __umulhi(n, m)) >> s; }
+};
+
+// Row r of page id of the pool (the strides but the layer's are below 2^31).
+__device__ __forceinline__ int64_t pg_place_of(const PageArgs& a, uint32_t id, uint32_t r, int l,
+                                               uint32_t h) {
+  return l * a.s_layer + (int64_t)((uint64_t)id * (uint32_t)a.s_page + (uint64_t)r * (uint32_t)a.s_row +
+                                   (uint64_t)h * (uint32_t)a.s_head);
+}
+
 // The pool's row of a slot for (layer, head); -1: none (refused rows, and numbers that are none
 // of the pool's, which are reported).
-__device__ __forceinline__ int64_t pg_row(const PageArgs& a, int32_t slot, int l, int h) {
+__device__ __forceinline__ int64_t pg_row(const PageArgs& a, int32_t slot, int l, uint32_t h) {
   if (slot < 0) return -1;
   const int32_t id = slot >> a.lp;
   if (id >= a.num_pages) {
     report_range(a.g);
     return -1;
   }
-  return l * a.s_layer + id * a.s_page + (slot & ((1 << a.lp) - 1)) * a.s_row + h * a.s_head;
+  return pg_place_of(a, id, (uint32_t)slot & ((1u << a.lp) - 1), l, h);
 }
 
 // Eight dims of a row, as they are held in format F, from the source's values.
@@ -305,57 +462,79 @@ __device__ __forceinline__ void pg_store8(const Geo& g, const MxRaw<T>& x, int64
   }
 }
 
-// D / 8 lanes to a row.  blockIdx.y: the layer; rows of a layer token by token, head by head.
+// Rows of a lane in flight, and whether keys and values are written together: microscaled rows are
+// bound by the issue of their quantisation and addresses, which keys and values share; copies by
+// memory, where one array at a time keeps more of the rows that are open (3.26M rows of 8 layers,
+// bf16: 557 us, together 630; mxfp8: 442, apart 448; mxfp4 419 and 426).
+constexpr int page_write_rows(int format) { return format == CERTKV_CACHE_BF16 ? 1 : 2; }
+constexpr int page_write_arrays(int format) { return format == CERTKV_CACHE_BF16 ? 1 : 2; }
+// D / 8 lanes to a row, UR rows of a lane in flight.  blockIdx.y: the layer, whose rows are taken
+// token by token, head by head; blockIdx.z: keys or values, where they are not written together.
 template <int D, typename T, int F>
-__global__ __launch_bounds__(kPgThreads) void page_write_kernel(PageWriteArgs a) {
-  constexpr int LPR = D / 8, RPS = kPgThreads / LPR;
+__global__ __launch_bounds__(kPgThreads) void page_write_kernel(PageWriteArgs a, PgDiv by_h, PgDiv by_tn) {
+  constexpr int LPR = D / 8, RPS = kPgThreads / LPR, UR = page_write_rows(F), NA = page_write_arrays(F);
   const Geo& g = a.p.g;
   const int l = blockIdx.y, ci = threadIdx.x % LPR;
-  const T* ks = static_cast<const T*>(a.k.ptr) + l * a.k.s_layer + ci * 8;
-  const T* vs = static_cast<const T*>(a.v.ptr) + l * a.v.s_layer + ci * 8;
-  const uint32_t H = (uint32_t)g.H, rows = (uint32_t)(a.tokens * g.H);
+  const uint32_t rows = (uint32_t)(a.tokens * g.H);
   const int64_t total = a.slot_offsets[a.p.lists];
-  for (uint32_t x = blockIdx.x * RPS + threadIdx.x / LPR; x < rows; x += gridDim.x * RPS) {
-    const uint32_t tk = x / H, h = x % H;
-    int64_t j = tk;  // its slot's place
-    bool mine = j < total;
-    if (a.tn) {
-      const uint32_t b = tk / (uint32_t)a.tn, i = tk % (uint32_t)a.tn;
-      const int64_t r = a.p.per_head ? unit_index(g, l, (int)b, (int)h) : b;
-      j = a.slot_offsets[r] + i;
-      mine = j < a.slot_offsets[r + 1];
+  for (uint32_t x0 = blockIdx.x * RPS * UR; x0 < rows; x0 += gridDim.x * RPS * UR) {
+    MxRaw<T> x8[UR][NA];
+    int64_t row[UR];
+#pragma unroll
+    for (int q = 0; q < UR; ++q) {
+      const uint32_t x = x0 + q * RPS + threadIdx.x / LPR;
+      const uint32_t tk = by_h(min(x, rows - 1)), h = min(x, rows - 1) - tk * (uint32_t)g.H;
+      int64_t j = tk;  // its slot's place
+      bool mine = x < rows && j < total;
+      if (a.tn) {
+        const uint32_t b = by_tn(tk), i = tk - b * (uint32_t)a.tn;
+        const int64_t r = a.p.per_head ? unit_index(g, l, (int)b, (int)h) : b;
+        j = a.slot_offsets[r] + i;
+        mine = x < rows && j < a.slot_offsets[r + 1];
+      }
+      if (mine && (j < 0 || j >= a.slot_count)) {
+        report_range(g);
+        mine = false;
+      }
+      row[q] = mine ? pg_row(a.p, a.slots[j], l, h) : -1;
+#pragma unroll
+      for (int n = 0; n < NA; ++n) {
+        const certkv_tensor& t = (NA == 1 ? blockIdx.z : n) ? a.v : a.k;
+        if (row[q] >= 0)
+          x8[q][n].load(static_cast<const T*>(t.ptr) + l * t.s_layer + tk * t.s_token + h * t.s_head + ci * 8);
+      }
     }
-    if (!mine) continue;
-    if (j < 0 || j >= a.slot_count) {
-      report_range(g);
-      continue;
-    }
-    const int64_t row = pg_row(a.p, a.slots[j], l, (int)h);
-    if (row < 0) continue;
-    MxRaw<T> kx, vx;
-    kx.load(ks + tk * a.k.s_token + h * a.k.s_head);
-    vx.load(vs + tk * a.v.s_token + h * a.v.s_head);
-    pg_store8<F, T>(g, kx, row * D + ci * 8, a.p.k, a.p.k_scales);
-    pg_store8<F, T>(g, vx, row * D + ci * 8, a.p.v, a.p.v_scales);
+#pragma unroll
+    for (int q = 0; q < UR; ++q)
+#pragma unroll
+      for (int n = 0; n < NA; ++n) {
+        const bool v = NA == 1 ? blockIdx.z : n;
+        if (row[q] >= 0)
+          pg_store8<F, T>(g, x8[q][n], row[q] * D + ci * 8, v ? a.p.v : a.p.k,
+                          v ? a.p.v_scales : a.p.k_scales);
+      }
   }
 }
 
 template <int D, typename T>
 static certkv_status launch_page_write(const PageWriteArgs& a, hipStream_t s) {
-  const int64_t steps = (a.tokens * a.p.g.H + kPgThreads * 8 / D - 1) / (kPgThreads * 8 / D);
-  const dim3 grid((unsigned)(steps < 8 * 256 ? steps : 8 * 256), (unsigned)a.p.g.L);
+  const int64_t step = page_write_rows(a.p.format) * (kPgThreads * 8 / D);
+  const int64_t steps = (a.tokens * a.p.g.H + step - 1) / step;
+  const dim3 grid((unsigned)(steps < 64 * 256 ? steps : 64 * 256), (unsigned)a.p.g.L,
+                  3 - page_write_arrays(a.p.format));
+  const PgDiv by_h((uint32_t)a.p.g.H), by_tn((uint32_t)a.tn);
   switch (a.p.format) {
     case CERTKV_CACHE_MXFP8:
       CERTKV_LAUNCH("page_write", (page_write_kernel<D, T, CERTKV_CACHE_MXFP8>), grid,
-                    dim3(kPgThreads), 0, s, a);
+                    dim3(kPgThreads), 0, s, a, by_h, by_tn);
       break;
     case CERTKV_CACHE_MXFP4:
       CERTKV_LAUNCH("page_write", (page_write_kernel<D, T, CERTKV_CACHE_MXFP4>), grid,
-                    dim3(kPgThreads), 0, s, a);
+                    dim3(kPgThreads), 0, s, a, by_h, by_tn);
       break;
     default:
       CERTKV_LAUNCH("page_write", (page_write_kernel<D, T, CERTKV_CACHE_BF16>), grid,
-                    dim3(kPgThreads), 0, s, a);
+                    dim3(kPgThreads), 0, s, a, by_h, by_tn);
   }
   return CERTKV_OK;
 }
@@ -414,24 +593,34 @@ certkv_status run_page_adopt(const PageAdoptArgs& a, hipStream_t s) {
 
 // ---- rows out of their pages ------------------------------------------------------
 
-// Eight dims of row `row` of the pool as bf16.
+// Eight dims of a row as they are held, and as bf16.
 template <int F, int D>
-__device__ __forceinline__ uint4 pg_load8(const uint8_t* rows, const uint8_t* scales, int64_t row,
-                                          int ci) {
-  if constexpr (F == CERTKV_CACHE_BF16) {
-    const MxU4 v = __builtin_nontemporal_load(reinterpret_cast<const MxU4*>(rows + row * (2 * D)) + ci);
-    return make_uint4(v[0], v[1], v[2], v[3]);
-  } else {
-    uint2 c = make_uint2(0u, 0u);
-    if constexpr (F == CERTKV_CACHE_MXFP8)
-      c = reinterpret_cast<const uint2*>(rows + row * D)[ci];
-    else
-      c.x = reinterpret_cast<const uint32_t*>(rows + row * (D / 2))[ci];
-    const uint32_t x = scales[row * (D / kMxBlock) + ci / 4];
-    if (x == 255u) return make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
-    return mx_decode8<F>(c, mx_scale(x));
+struct PgRaw {
+  uint4 c;
+  uint32_t x;
+  __device__ __forceinline__ void load(const uint8_t* rows, const uint8_t* scales, int64_t row, int ci) {
+    if constexpr (F == CERTKV_CACHE_BF16) {
+      const MxU4 v = __builtin_nontemporal_load(reinterpret_cast<const MxU4*>(rows + row * (2 * D)) + ci);
+      c = make_uint4(v[0], v[1], v[2], v[3]);
+    } else {
+      if constexpr (F == CERTKV_CACHE_MXFP8) {
+        const uint2 w = reinterpret_cast<const uint2*>(rows + row * D)[ci];
+        c.x = w.x, c.y = w.y;
+      } else {
+        c.x = reinterpret_cast<const uint32_t*>(rows + row * (D / 2))[ci];
+      }
+      x = scales[row * (D / kMxBlock) + ci / 4];
+    }
   }
-}
+  __device__ __forceinline__ uint4 values() const {
+    if constexpr (F == CERTKV_CACHE_BF16) {
+      return c;
+    } else {
+      if (x == 255u) return make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+      return mx_decode8<F>(make_uint2(c.x, c.y), mx_scale(x));
+    }
+  }
+};
 
 template <bool F32>
 __device__ __forceinline__ void pg_put8(void* out, int64_t at, uint4 v) {
@@ -445,59 +634,82 @@ __device__ __forceinline__ void pg_put8(void* out, int64_t at, uint4 v) {
   }
 }
 
-// A run of a layer's rows (tokens by heads; heads' lists: all rows) for each workgroup, D / 8
-// lanes to a row; the list of the run's first row by a 64-way search, the next ones by stepping
-// on.
+// Rows of a lane in flight: 32 bytes of them.
+constexpr int page_read_rows(int format) {
+  return format == CERTKV_CACHE_BF16 ? 2 : format == CERTKV_CACHE_MXFP8 ? 4 : 8;
+}
+// D / 8 lanes to a row, rows token by token, head by head (heads' lists: row by row), in blocks that
+// the workgroups of a layer take in turn; the list of a block's first row by a 64-way search, the
+// next ones by stepping on.  blockIdx.z: keys or values.
 template <int F, int D, bool F32>
-__global__ __launch_bounds__(kPgThreads) void page_read_kernel(PageReadArgs a) {
-  constexpr int LPR = D / 8, RPS = kPgThreads / LPR;
+__global__ __launch_bounds__(kPgThreads) void page_read_kernel(PageReadArgs a, PgDiv by_h) {
+  constexpr int LPR = D / 8, RPS = kPgThreads / LPR, UR = page_read_rows(F), BLOCK = RPS * UR;
   const PageArgs& p = a.p;
+  const uint8_t* src = blockIdx.z ? p.v : p.k;
+  const uint8_t* scales = blockIdx.z ? p.v_scales : p.k_scales;
+  void* out = blockIdx.z ? a.v : a.k;
+  if (!out) return;
   const int l = blockIdx.y, ci = threadIdx.x % LPR, lane = threadIdx.x & 63;
   const uint32_t H = p.per_head ? 1u : (uint32_t)p.g.H;
   const int64_t base = p.offsets[0], all = p.offsets[p.lists] - base;
   const int64_t tokens = min(all, a.rows);
   if (all > a.rows && threadIdx.x == 0 && blockIdx.x == 0) report_range(p.g);
-  const int64_t rows = tokens * H;
-  const int64_t per = ((rows + gridDim.x - 1) / gridDim.x + RPS - 1) / RPS * RPS;
-  const int64_t x0 = blockIdx.x * per, x1 = min(rows, x0 + per);
-  if (x0 >= x1) return;
+  const uint32_t rows = (uint32_t)max(tokens, (int64_t)0) * H;
   const auto first = [&](int32_t r) { return p.offsets[r] - base; };
-  int32_t r = pg_find(p.lists, first, x0 / H, lane);
-  int64_t start = first(r), end = first(r + 1);
   const int64_t out0 = p.per_head ? 0 : (int64_t)l * a.rows * H;
-  for (int64_t x = x0 + threadIdx.x / LPR; x < x1; x += RPS) {
-    const int64_t tk = x / H;
-    const int h = (int)(x - tk * H);
-    while (tk >= end && r + 1 < p.lists) {
-      ++r;
-      start = end;
-      end = first(r + 1);
+  for (uint32_t x0 = blockIdx.x * BLOCK; x0 < rows; x0 += gridDim.x * BLOCK) {
+    const uint32_t t0 = by_h(x0), h0 = x0 - t0 * H;  // (the workgroup's)
+    int32_t r = pg_find(p.lists, first, t0, lane);
+    int64_t start = first(r), end = first(r + 1);
+    {
+      int64_t row[UR];
+      int32_t id[UR];
+      uint32_t in[UR], h[UR];
+#pragma unroll
+      for (int q = 0; q < UR; ++q) {
+        const uint32_t y = h0 + threadIdx.x / LPR + q * RPS, t = by_h(y);
+        const int64_t tk = min(t0 + t, (uint32_t)(tokens - 1));
+        h[q] = y - t * H;
+        while (tk >= end && r + 1 < p.lists) {
+          ++r;
+          start = end;
+          end = first(r + 1);
+        }
+        const int64_t i = tk - start, pi = i >> p.lp;
+        in[q] = (uint32_t)i & ((1u << p.lp) - 1);
+        id[q] = i >= 0 && pi < p.max_pages ? p.table[(int64_t)r * p.max_pages + pi] : -1;
+      }
+      PgRaw<F, D> k[UR];
+#pragma unroll
+      for (int q = 0; q < UR; ++q) {
+        // (the caller's numbers: page 0's row in the place of one that is none, not kept)
+        const bool fine = (uint32_t)id[q] < (uint32_t)p.num_pages;
+        if (!fine) report_range(p.g);
+        row[q] = pg_place_of(p, fine ? (uint32_t)id[q] : 0u, in[q], l, h[q]);
+        k[q].load(src, scales, row[q], ci);
+        if (!fine) row[q] = -1;
+      }
+#pragma unroll
+      for (int q = 0; q < UR; ++q) {
+        const uint32_t x = x0 + threadIdx.x / LPR + q * RPS;
+        if (x >= rows || row[q] < 0) continue;
+        pg_put8<F32>(out, (out0 + x) * D + ci * 8, k[q].values());
+      }
     }
-    const int64_t i = tk - start, pi = i >> p.lp;
-    int32_t id = -1;
-    if (i >= 0 && pi < p.max_pages) id = p.table[(int64_t)r * p.max_pages + pi];
-    if ((uint32_t)id >= (uint32_t)p.num_pages) {  // (the caller's numbers)
-      report_range(p.g);
-      continue;
-    }
-    const int64_t row = pg_row(p, (id << p.lp) + (int32_t)(i & ((1 << p.lp) - 1)), l, h);
-    const int64_t at = (out0 + x) * D + ci * 8;
-    if (a.k) pg_put8<F32>(a.k, at, pg_load8<F, D>(p.k, p.k_scales, row, ci));
-    if (a.v) pg_put8<F32>(a.v, at, pg_load8<F, D>(p.v, p.v_scales, row, ci));
   }
 }
 
 template <int F, int D>
 static certkv_status launch_page_read(const PageReadArgs& a, hipStream_t s) {
-  const int64_t rows = a.rows * (a.p.per_head ? 1 : a.p.g.H), step = kPgThreads * 8 / D;
-  const int64_t steps = (rows + step - 1) / step;
-  const int layers = a.p.per_head ? 1 : a.p.g.L;
-  const int64_t most = 8 * 256;
-  const dim3 grid((unsigned)(steps < most ? steps : most), (unsigned)layers);
+  const int H = a.p.per_head ? 1 : a.p.g.H, layers = a.p.per_head ? 1 : a.p.g.L;
+  const int64_t rows = a.rows * H, step = page_read_rows(F) * (kPgThreads * 8 / D);
+  const int64_t wgs = (rows + step - 1) / step < 64 * 256 ? (rows + step - 1) / step : 64 * 256;
+  const dim3 grid((unsigned)wgs, (unsigned)layers, 2);
+  const PgDiv by_h((uint32_t)H);
   if (a.f32)
-    CERTKV_LAUNCH("page_read", (page_read_kernel<F, D, true>), grid, dim3(kPgThreads), 0, s, a);
+    CERTKV_LAUNCH("page_read", (page_read_kernel<F, D, true>), grid, dim3(kPgThreads), 0, s, a, by_h);
   else
-    CERTKV_LAUNCH("page_read", (page_read_kernel<F, D, false>), grid, dim3(kPgThreads), 0, s, a);
+    CERTKV_LAUNCH("page_read", (page_read_kernel<F, D, false>), grid, dim3(kPgThreads), 0, s, a, by_h);
   return CERTKV_OK;
 }
 

@@ -358,3 +358,23 @@ def test_no_tokens():
     ck.page_write(spec, cache, none, none, slots, so)
     k, v = ck.page_read(spec, cache)
     assert k.shape == v.shape == (2, 0, 2, 64)
+
+
+@pytest.mark.parametrize("lists", [200, 1000, 1200])
+def test_sums_that_stop(lists):
+    # far more pages asked for than there are, in lists before, in and behind those of one lane:
+    # nothing behind the first refused list is given any
+    spec = spec_of(B=lists)
+    rng = random.Random(lists)
+    for room in (10_000_000, 16_000):
+        ref = _pages.Lists(lists, 20, 16, 64)
+        cache = tables(lists, 20, 16, 64)
+        change = [rng.choice([0, 1, 0, 900, 16, 1000]) if i > 3 else 1 for i in range(lists)]
+        bufs = ck.ResizeBuffers(cache, room, DEV)
+        slots, so = ck.page_resize(spec, cache, torch.tensor(change, dtype=torch.int32, device=DEV),
+                                   bufs=bufs)
+        want, want_so, refused = ref.resize(change, room)
+        assert refused and so.tolist() == want_so
+        n = min(room, len(want))
+        assert slots[:n].tolist() == want[:n]
+        check_lists(cache, ref)
