@@ -1405,8 +1405,9 @@ certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* page
 // 256-byte aligned.
 struct PagedWs {
   int shape;
-  int32_t copies, cover, qgroups, mp, parts, most;
-  size_t ml_off, total;
+  int32_t copies, cover, qgroups, mp, mode, parts, most;
+  int32_t parts_weighed, most_weighed;  // where the query groups are weighed (0: never)
+  size_t ml_off, place_off, total;
 };
 static bool paged_ws_layout(const PageArgs& x, int32_t tq, int32_t max_rows, PagedWs* w) {
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
@@ -1417,24 +1418,32 @@ static bool paged_ws_layout(const PageArgs& x, int32_t tq, int32_t max_rows, Pag
   w->qgroups = (int32_t)((M + held - 1) / held);
   w->mp = (int32_t)M;
   // as many chunks as their workgroups stay resident: 256 compute units of four SIMDs
-  w->parts = 256 * 4 * attend_waves(x.g.D, w->shape) / attend_wg_waves(w->shape);
-  w->parts = (w->parts + w->qgroups - 1) / w->qgroups;
-  w->copies = x.per_head ? 1 : x.g.L * x.g.H;
+  const int resident = 256 * 4 * pg_simd_waves(x.format, x.g.D, held / 16) / pg_waves(kPgPiece);
+  w->parts = (resident + w->qgroups - 1) / w->qgroups;
   const int64_t list = (int64_t)x.max_pages << x.lp;
   w->cover = (int32_t)(max_rows > 0 && max_rows < list ? max_rows : list);
+  w->mode = pg_mode(x.per_head, x.g.H, x.s_row, x.s_head, w->cover);
+  const int heads = w->mode == kPgHeads ? 4 : 1;
+  w->copies = x.per_head ? 1 : x.g.L * x.g.H / heads;
   const int64_t by_lists = (int64_t)x.lists * ((w->cover + 31) / 32 + kPgGap);
   const int64_t by_pool = ((int64_t)x.num_pages << x.lp) / 32 + (int64_t)x.lists * (1 + kPgGap);
   const int64_t tiles = w->copies * (1 + (by_lists < by_pool ? by_lists : by_pool));
-  if (by_lists > INT32_MAX || tiles > INT32_MAX) return false;
-  int64_t most = (tiles + kPgMaxTiles - 1) / kPgMaxTiles;
-  const int64_t shortest = (tiles + kPgMinTiles - 1) / kPgMinTiles;
-  if (most < w->parts) most = w->parts;
-  if (most > shortest) most = shortest;
-  if (pg_whole(w->cover, x.lists * (int64_t)w->copies)) most = 0;
-  w->most = (int32_t)most;
-  const size_t part = most ? (size_t)(most + (int64_t)x.lists * w->copies) * w->mp : 1;
+  if (by_lists > INT32_MAX || tiles * w->qgroups > INT32_MAX) return false;
+  auto chunks = [](int64_t n, int64_t parts) {
+    int64_t most = (n + kPgMaxTiles - 1) / kPgMaxTiles;
+    const int64_t shortest = (n + kPgMinTiles - 1) / kPgMinTiles;
+    if (most < parts) most = parts;
+    return (int32_t)(most > shortest ? shortest : most);
+  };
+  w->most = chunks(tiles, w->parts);
+  const bool weighs = w->qgroups > 1 && w->mode != kPgWhole && x.lists <= kPgWeighed;
+  w->parts_weighed = weighs ? resident : 0;
+  w->most_weighed = weighs ? chunks(tiles * w->qgroups, resident) : 0;
+  const int64_t most = w->most > w->most_weighed ? w->most : w->most_weighed;
+  const size_t part = w->mode == kPgWhole ? 1 : (size_t)(most + (int64_t)x.lists * w->copies) * heads * w->mp;
   w->ml_off = up(part * (size_t)x.g.D * sizeof(float));
-  w->total = up(w->ml_off + part * sizeof(float2));
+  w->place_off = up(w->ml_off + part * sizeof(float2));
+  w->total = up(w->place_off + (weighs ? ((size_t)x.lists + 1) * sizeof(uint32_t) : 0));
   return true;
 }
 
@@ -1467,9 +1476,12 @@ certkv_status certkv_decode_paged(const certkv_problem* p, certkv_tensor q_new, 
   a.cover = W.cover;
   a.qgroups = W.qgroups;
   a.mp = W.mp;
-  a.parts = W.parts;
-  a.most = W.most;
+  a.mode = W.mode;
+  const bool weighed = q_lens && W.parts_weighed;
+  a.parts = weighed ? W.parts_weighed : W.parts;
+  a.most = weighed ? W.most_weighed : W.most;
   a.q_lens = q_lens;
+  a.place = weighed ? reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + W.place_off) : nullptr;
   a.q = q_new;
   a.part_o = static_cast<float*>(ws);
   a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + W.ml_off);

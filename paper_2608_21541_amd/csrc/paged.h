@@ -28,26 +28,35 @@ constexpr int kPgGap = 8;         // tiles between lists' places beside their ro
 constexpr int kPgMinTiles = 4;    // shortest chunk, and the unit of its length
 constexpr int kPgMaxTiles = kAtMaxKeys / kAtTile;  // longest, unless partials are short
 
-// Waves of a workgroup, by whether it has whole units.
-constexpr int pg_waves(bool whole) { return whole ? 8 : 4; }
+// What a workgroup has: a piece of a unit, whose tiles its waves take in turn; whole units; or the
+// same piece of four heads' units, a head for each wave.
+enum { kPgPiece, kPgWhole, kPgHeads };
+constexpr int pg_waves(int mode) { return mode == kPgWhole ? 8 : 4; }
 
-// Whether they have, by the most rows of a unit.
-#ifndef PG_WHOLE
-#define PG_WHOLE 1024
-#endif
-inline bool pg_whole(int64_t cover, int64_t) { return cover <= PG_WHOLE; }
+// Waves per SIMD that a kernel leaves registers for, which is also how many are launched.
+constexpr int pg_simd_waves(int format, int D, int qt) {
+  return qt == 1 && (D == 64 || format == CERTKV_CACHE_MXFP4) ? 3 : 2;
+}
+constexpr int kPgWholeRows = 1024;  // of a unit at most that a workgroup has whole
+// s_row, s_head: the pool's strides.
+inline int pg_mode(int per_head, int H, int64_t s_row, int64_t s_head, int64_t cover) {
+  if (cover <= kPgWholeRows) return kPgWhole;
+  return !per_head && H % 4 == 0 && s_head < s_row ? kPgHeads : kPgPiece;
+}
 
 struct PagedArgs {
   PageArgs p;
   int32_t tq;
-  int32_t copies;               // units of a list: L H of a sequence's, 1 of a head's
+  int32_t copies;               // units of a list: L H of a sequence's, 1 of a head's; a quarter
+                                // of them where a workgroup has four heads
   int32_t cover;                // rows of a list that are attended
   int32_t qgroups, mp;          // workgroups of a chunk, query rows of a partial
-  int32_t parts, most;          // chunks taken at once, and that the workspace has room for (0: a
-                                // workgroup has a whole unit)
+  int32_t mode;
+  int32_t parts, most;          // chunks taken at once, and that the workspace has room for
   const int32_t* q_lens;        // [B], or NULL: tq
+  uint32_t* place;              // [lists + 1]: the lists' places by their queries' groups, or NULL
   certkv_tensor q;
-  float* part_o;                // [most + U][mp][d]
+  float* part_o;                // [most + lists copies][mp][d], or four times as many for four heads
   float2* part_ml;
   float* out;
   float* lse;
@@ -67,14 +76,65 @@ __device__ __forceinline__ uint32_t pg_up(int64_t rows) { return (uint32_t)((uin
 __device__ __forceinline__ uint32_t pg_place(int64_t rows_before, uint32_t r) {
   return pg_up(rows_before) + r * (uint32_t)kPgGap;
 }
-__device__ __forceinline__ PgCut pg_cut(const PagedArgs& a, int64_t rows) {
-  const uint32_t total = (uint32_t)a.copies * pg_place(rows, (uint32_t)a.p.lists);
+__device__ __forceinline__ PgCut pg_cut(const PagedArgs& a, uint32_t tiles) {
+  const uint32_t total = (uint32_t)a.copies * tiles;
   uint32_t k = (total + (uint32_t)a.parts - 1u) / (uint32_t)a.parts;
   k = min(max(k, (uint32_t)kPgMinTiles), (uint32_t)kPgMaxTiles);
   // (more rows than the caller's bound or the pool allow for, as with pages that lists share:
   // longer chunks, so that the partials stay within the workspace)
   if (total > (uint64_t)a.most * k) k = (total + (uint32_t)a.most - 1u) / (uint32_t)a.most;
   return PgCut{(k + kPgMinTiles - 1u) / kPgMinTiles * kPgMinTiles, total};
+}
+
+// Where sequences have queries of their own number, and more than a workgroup holds, the groups of
+// 32 that they have differ, and so does what a list costs: its groups then stand one after another
+// in the order, as copies do, and the places are a scan over the lists.
+constexpr int kPgWeighed = 2048;  // lists at most
+__device__ __forceinline__ int pg_list_sequence(const PagedArgs& a, uint32_t r) {
+  return (int)(a.p.per_head ? r / (uint32_t)a.p.g.H % (uint32_t)a.p.g.B : r);
+}
+__device__ __forceinline__ int pg_queries(const PagedArgs& a, int b) {
+  return a.q_lens ? min(max(a.q_lens[b], 0), a.tq) : a.tq;
+}
+__device__ __forceinline__ uint32_t pg_groups(const PagedArgs& a, int b) {
+  return (uint32_t)(pg_queries(a, b) * a.p.g.G + 31) >> 5;
+}
+// place_s[r]: the first tile of list r, for copies = 1; and, from the first workgroup, a.place.
+template <int NT>
+__device__ __forceinline__ void pg_weigh(const PagedArgs& a, uint32_t* place_s, uint32_t* sum_s) {
+  const int tid = threadIdx.x;
+  const int64_t* off = a.p.offsets;
+  const int64_t base = off[0];
+  uint32_t before = 0;
+  for (int r0 = 0; r0 < a.p.lists; r0 += NT) {
+    const int r = r0 + tid;
+    uint32_t x = 0;
+    if (r < a.p.lists)
+      x = pg_groups(a, pg_list_sequence(a, r)) * (pg_up(off[r + 1] - base) - pg_up(off[r] - base) + kPgGap);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t y = __shfl_up(x, d, 64);
+      if ((tid & 63) >= d) x += y;
+    }
+    if ((tid & 63) == 63) sum_s[tid >> 6] = x;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      if (w < tid >> 6) x += sum_s[w];
+    }
+    x += before;
+    for (int w = 0; w < NT / 64; ++w) before += sum_s[w];
+    if (r < a.p.lists) {
+      place_s[r + 1] = x;
+      if (blockIdx.x == 0) a.place[r + 1] = x;
+    }
+    __syncthreads();
+  }
+  if (tid == 0) {
+    place_s[0] = 0;
+    if (blockIdx.x == 0) a.place[0] = 0;
+  }
+  __syncthreads();
 }
 
 // The lists' offsets, as a wave reads them: those of 64 lists at a time in its lanes.
@@ -150,15 +210,14 @@ __device__ __forceinline__ uint32_t pg_finite(uint32_t x) {
   return x;
 }
 
-// WHOLE: a workgroup of eight waves has a unit's rows from first to last, and writes its outputs
-// itself.
-template <int F, int D, int QT, bool WHOLE>
-__global__ __launch_bounds__(64 * pg_waves(WHOLE))
-__attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void paged_kernel(PagedArgs a) {
-  using Shape = AtShape<D, 1, QT>;
-  constexpr int KS = pg_waves(WHOLE), NT = 64 * KS, PARTS = Shape::PARTS;
+template <int F, int D, int QT, int MODE>
+__global__ __launch_bounds__(64 * pg_waves(MODE))
+__attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT)))) void paged_kernel(PagedArgs a) {
+  constexpr bool WHOLE = MODE == kPgWhole, HEADS = MODE == kPgHeads;
+  constexpr int KW = pg_waves(MODE), NT = 64 * KW, PARTS = AtShape<D, 1, QT>::PARTS;
+  constexpr int KS = HEADS ? 1 : KW;  // waves that take a unit's tiles in turn
   constexpr int ROW = D + 4;  // floats of a joined output row
-  constexpr int JOIN = 2 * KS * 16 * ROW, TILES = KS * AtTile<D>::V;  // bf16 elements
+  constexpr int JOIN = KS > 1 ? 2 * KS * 16 * ROW : 0, TILES = KW * AtTile<D>::V;  // bf16 elements
   constexpr int BITS = F == CERTKV_CACHE_BF16 ? 16 : F == CERTKV_CACHE_MXFP8 ? 8 : 4;
   constexpr bool MX = F != CERTKV_CACHE_BF16;
   constexpr int RB = mx_row_bytes(F, D);
@@ -170,7 +229,7 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
   constexpr int NLT = kAtTile / RPL;
   static_assert(RPL <= 16 && SK * NLK == KSTEP, "a load's rows are in one half");
   __shared__ __align__(16) uint16_t lds[TILES > JOIN ? TILES : JOIN];
-  __shared__ float2 ml_s[KS * 16];
+  __shared__ float2 ml_s[KS > 1 ? KS * 16 : 1];
 
   const PageArgs& p = a.p;
   const Geo& gm = p.g;
@@ -180,20 +239,41 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
   const float c2 = gm.scale * kAtLog2e;
   const uint32_t copies = (uint32_t)a.copies;
   // Query groups of a chunk: eight workgroups apart, on the same XCD, whose L2 then serves all
-  // but the first.
-  const int wgx = blockIdx.x;
-  const int qg = (wgx >> 3) % a.qgroups;
-  const uint32_t x0 = a.qgroups == 1 ? wgx : (wgx >> 3) / a.qgroups * 8 + (wgx & 7);
-  const uint32_t xstep = gridDim.x / a.qgroups;
-  const int row0 = qg * QT * 16;  // the first query row
+  // but the first; or, where they are weighed, in the order of the units.
+  const bool weighed = QT == 2 && !WHOLE && a.place;
+  const int groups = weighed ? 1 : a.qgroups, wgx = blockIdx.x;
+  int qg = (wgx >> 3) % groups;
+  const uint32_t x0 = groups == 1 ? wgx : (wgx >> 3) / groups * 8 + (wgx & 7);
+  const uint32_t xstep = gridDim.x / groups;
+  constexpr int PLACES = QT == 2 && !WHOLE ? kPgWeighed + 1 : 1;
+  __shared__ uint32_t place_s[PLACES], sum_s[KW];
+  if constexpr (PLACES > 1) {
+    if (weighed) pg_weigh<NT>(a, place_s, sum_s);
+  }
   uint16_t* const vt = lds + wave * AtTile<D>::V;
   // The units' pieces: of the chunks that the workgroup takes, or the whole units.
   PgOffsets off(p.offsets, WHOLE ? 0 : p.lists, lane);
-  const PgCut cut = WHOLE ? PgCut{1, 0} : pg_cut(a, off.rows);
+  const PgCut cut = WHOLE ? PgCut{1, 0}
+                          : pg_cut(a, weighed ? place_s[PLACES > 1 ? p.lists : 0] : pg_place(off.rows, off.R));
   const uint32_t nch = WHOLE ? (uint32_t)p.lists * copies : (cut.total + cut.tiles - 1) / cut.tiles;
   for (uint32_t x = x0; x < nch; x = WHOLE ? nch : x + xstep) {
     const uint32_t r0 = x * cut.tiles, r1 = min(cut.total, r0 + cut.tiles);
-    uint32_t r = WHOLE ? x / copies : off.find(r0 / copies, lane), copy = WHOLE ? x - r * copies : 0;
+    uint32_t r = 0, copy = 0;
+    if constexpr (WHOLE) {
+      r = x / copies, copy = x - r * copies;
+    } else if (weighed) {
+      for (uint32_t lo = 0, hi = (uint32_t)p.lists - 1; lo < hi;) {  // the last that begins here or before
+        const uint32_t mid = (lo + hi + 1) >> 1;
+        if (place_s[PLACES > 1 ? mid : 0] <= r0 / copies)
+          lo = mid;
+        else
+          hi = mid - 1;
+        r = lo;
+      }
+      r = __builtin_amdgcn_readfirstlane(r);
+    } else {
+      r = off.find(r0 / copies, lane);
+    }
     bool begun = false;
     while (WHOLE ? !begun : r < off.R) {
       int64_t p0, p1;
@@ -207,22 +287,27 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
         ntp = (int)pg_up(len);
       } else {
         off.list(r, lane, p0, p1);
-        const uint32_t place = copies * pg_place(p0, r);
+        uint32_t place = copies * pg_place(p0, r), times = 1;
         const uint32_t span = pg_place(p1, r + 1) - pg_place(p0, r);
+        if (weighed) {
+          place = copies * place_s[PLACES > 1 ? r : 0];
+          times = pg_groups(a, pg_list_sequence(a, r));
+        }
         if (!begun) copy = r0 > place ? (r0 - place) / span : 0;
         begun = true;
-        if (copy >= copies) {
+        if (copy >= copies * times) {
           ++r, copy = 0;
           continue;
         }
         const uint32_t vs = place + copy * span;
-        u = r * copies + copy;
         if (vs >= r1) break;
         // the piece: tiles [lo, lo + ntp) of the unit's
         len = min(page_rows(p, p0, p1), a.cover);
         lo = max(r0, vs) - vs;
         ntp = (int)min(r1 - vs, pg_up(len)) - (int)lo;
         mine = copy++;
+        if (weighed) qg = (int)(mine % times), mine /= times;
+        u = r * copies + mine;
         if (ntp <= 0) continue;  // (only what lies between units)
       }
       // (What follows from the lane is worked out for each piece: kept beyond it, it would take
@@ -242,9 +327,11 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
         h = (int)(r % (uint32_t)gm.H), b = (int)(r / gm.H % (uint32_t)gm.B);
         l = (int)(r / gm.H / gm.B);
       } else {
+        if constexpr (HEADS) mine = mine * 4 + wave;
         b = (int)r, l = (int)(mine / (uint32_t)gm.H), h = (int)(mine % (uint32_t)gm.H);
       }
-      const int own = a.q_lens ? min(max(a.q_lens[b], 0), a.tq) : a.tq;
+      const int row0 = qg * QT * 16;  // the first query row
+      const int own = pg_queries(a, b);
       const int64_t at0 = p.per_head ? 0 : l * p.s_layer + h * p.s_head;
       const uint8_t* const kp = p.k + at0 * RB;
       const uint8_t* const vp = p.v + at0 * RB;
@@ -260,13 +347,14 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
       const int t0 = row0 / gm.G;  // the first token; rows up to `whole` are seen by all
       const int whole = len - own + t0;
 
-      // The pages of the wave's tiles lo + wave + 4 n, 32 at a time: half i % 2 of the one of
+      // The wave's tiles are lo + turn + KS n.  Their pages, 32 at a time: half i % 2 of the one of
       // n = i / 2 in lane i.
+      const int turn = HEADS ? 0 : wave;
       int32_t ids = 0, window = -1;
       auto pages = [&](int n) {
         if ((n >> 5) == window) return;
         window = n >> 5;
-        const int row = (int)(lo + wave + KS * ((n & ~31) + (lane >> 1))) * kAtTile + (lane & 1) * 16;
+        const int row = (int)(lo + turn + KS * ((n & ~31) + (lane >> 1))) * kAtTile + (lane & 1) * 16;
         ids = -1;
         if (row < len) {
           const int32_t id = p.table[(int64_t)r * p.max_pages + (row >> p.lp)];
@@ -278,7 +366,7 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
       };
       // rows of half kb of the wave's tile n that are there, and their first byte behind kp and vp
       auto half = [&](int n, int kb, int& there) {
-        const int row = (int)(lo + wave + KS * n) * kAtTile + kb * 16;
+        const int row = (int)(lo + turn + KS * n) * kAtTile + kb * 16;
         const int32_t id = __builtin_amdgcn_readlane(ids, 2 * (n & 31) + kb);
         there = id < 0 ? 0 : min(max(len - row, 0), 16);
         return (uint32_t)max(id, 0) * page_bytes + (uint32_t)(row & ((1 << p.lp) - 1)) * (uint64_t)st;
@@ -328,7 +416,7 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
           }
         }
       };
-      const int own_tiles = t0 < own ? (ntp - wave + KS - 1) / KS : 0;  // of the wave
+      const int own_tiles = t0 < own ? (ntp - turn + KS - 1) / KS : 0;  // of the wave
       if (own_tiles > 0) {
         load_keys(0);
         load_values(0);
@@ -350,7 +438,7 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
       // others' loads in flight.)
       auto tile = [&](int n, auto tail_c) {
         constexpr bool TAIL = decltype(tail_c)::value;
-        const int trow = (int)(lo + wave + KS * n) * kAtTile;
+        const int trow = (int)(lo + turn + KS * n) * kAtTile;
         // (its addresses by itself too)
         int ln = lane;
         if constexpr (TAIL) asm volatile("" : "+v"(ln));
@@ -455,7 +543,7 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
         }
       };
       int n = 0;
-      for (; n < own_tiles && (int)(lo + wave + KS * n + 1) * kAtTile <= whole + 1; ++n)
+      for (; n < own_tiles && (int)(lo + turn + KS * n + 1) * kAtTile <= whole + 1; ++n)
         tile(n, std::false_type{});
       for (; n < own_tiles; ++n) tile(n, std::true_type{});
 
@@ -477,6 +565,18 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
         l_row += __shfl_xor(l_row, 32, 64);
         const int g = (tid_j & 63) >> 4, c = tid_j & 15;
         float* join = reinterpret_cast<float*>(lds);
+        if constexpr (KS == 1) {
+          const int row = row0 + qt * 16 + c;
+          if (row < M) {
+            const int64_t pr = (slot * 4 + wave) * mp + row;
+            if (g == 0) a.part_ml[pr] = make_float2(acc.m[qt], l_row);
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db)
+              *reinterpret_cast<float4*>(a.part_o + pr * D + 16 * db + 4 * g) =
+                  make_float4(acc.o[qt][db][0], acc.o[qt][db][1], acc.o[qt][db][2], acc.o[qt][db][3]);
+          }
+          continue;
+        }
         __syncthreads();  // every wave is done with its tiles (and with the tile before)
         if (g == 0) ml_s[wave * 16 + c] = make_float2(acc.m[qt], l_row);
         __syncthreads();
@@ -520,22 +620,24 @@ __attribute__((amdgpu_waves_per_eu(WHOLE ? 2 : attend_waves(D, QT - 1)))) void p
           }
         }
       }
-      __syncthreads();  // the joined tiles are read before the next piece overwrites them
+      if constexpr (KS > 1) __syncthreads();  // the joined tiles are read before the next piece's
     }
   }
 }
 
 template <int F, int D, int QT>
 static certkv_status launch_paged_d(const PagedArgs& a, hipStream_t s) {
-  if (a.most == 0) {
-    const int64_t U = (int64_t)a.p.lists * a.copies;
-    const dim3 grid((unsigned)(a.qgroups == 1 ? U : (U + 7) / 8 * 8 * a.qgroups));
-    CERTKV_LAUNCH("paged_whole", (paged_kernel<F, D, QT, true>), grid, dim3(64 * pg_waves(true)), 0, s, a);
-    return CERTKV_OK;
-  }
-  const int wgs = a.most < a.parts ? a.most : a.parts;
-  const dim3 grid(a.qgroups == 1 ? wgs : (wgs + 7) / 8 * 8 * a.qgroups);
-  CERTKV_LAUNCH("paged", (paged_kernel<F, D, QT, false>), grid, dim3(64 * pg_waves(false)), 0, s, a);
+  const int64_t U = (int64_t)a.p.lists * a.copies;
+  const int64_t wgs = a.mode == kPgWhole ? U : a.most < a.parts ? a.most : a.parts;
+  const bool one = a.qgroups == 1 || a.place;
+  const dim3 grid((unsigned)(one ? wgs : (wgs + 7) / 8 * 8 * a.qgroups));
+  const dim3 block(64 * pg_waves(a.mode));
+  if (a.mode == kPgWhole)
+    CERTKV_LAUNCH("paged_whole", (paged_kernel<F, D, QT, kPgWhole>), grid, block, 0, s, a);
+  else if (a.mode == kPgHeads)
+    CERTKV_LAUNCH("paged_heads", (paged_kernel<F, D, QT, kPgHeads>), grid, block, 0, s, a);
+  else
+    CERTKV_LAUNCH("paged", (paged_kernel<F, D, QT, kPgPiece>), grid, block, 0, s, a);
   return CERTKV_OK;
 }
 

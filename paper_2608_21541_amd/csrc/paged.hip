@@ -16,7 +16,8 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
   __shared__ float2 ml_s[GR];
   const PageArgs& p = a.p;
   const Geo& g = p.g;
-  const uint32_t u = blockIdx.x;
+  // the unit, or of four heads' units the place in common and the head's
+  const uint32_t four = a.mode == kPgHeads ? 4u : 1u, u = blockIdx.x / four, head = blockIdx.x % four;
   const uint32_t r = u / (uint32_t)a.copies, copy = u % (uint32_t)a.copies;
   const int grp = threadIdx.x / C4, c4 = threadIdx.x % C4;
   const int row = blockIdx.y * RW + grp / S, sg = grp % S;
@@ -26,10 +27,13 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
   if (p1 - p0 != len && blockIdx.y == 0 && threadIdx.x == 0) report_range(g);
   float m = kAtNone, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (row < M && len > 0) {
-    const PgCut cut = pg_cut(a, p.offsets[p.lists] - base);
+  uint32_t group = 0, groups = 1;
+  if (a.place) groups = pg_groups(a, pg_list_sequence(a, r)), group = (uint32_t)row >> 5;
+  if (row < M && len > 0 && group < groups) {
+    const PgCut cut = pg_cut(a, a.place ? a.place[p.lists] : pg_place(p.offsets[p.lists] - base, (uint32_t)p.lists));
     const uint32_t span = pg_place(p1, r + 1) - pg_place(p0, r);
-    const uint32_t vs = (uint32_t)a.copies * pg_place(p0, r) + copy * span;
+    const uint32_t place = a.place ? a.place[r] : pg_place(p0, r);
+    const uint32_t vs = (uint32_t)a.copies * place + (copy * groups + group) * span;
     // (of offsets that fall, places may lie behind the last chunk)
     const uint32_t s0 = min(vs / cut.tiles, (uint32_t)a.most - 1u);
     const uint32_t nv = min((vs + pg_up(len) - 1) / cut.tiles, (uint32_t)a.most - 1u) - s0 + 1;
@@ -39,7 +43,7 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
       float4 x[Q];
 #pragma unroll
       for (int i = 0; i < Q; ++i) {
-        const int64_t pr = ((int64_t)s0 + u + min(i0 + i * S, nv - 1)) * a.mp + row;
+        const int64_t pr = (((int64_t)s0 + u + min(i0 + i * S, nv - 1)) * four + head) * a.mp + row;
         ml[i] = a.part_ml[pr];
         x[i] = reinterpret_cast<const float4*>(a.part_o + pr * D)[c4];
       }
@@ -87,7 +91,8 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
   if (p.per_head) {
     h = (int)(r % (uint32_t)g.H), b = (int)(r / g.H % (uint32_t)g.B), l = (int)(r / g.H / g.B);
   } else {
-    b = (int)r, l = (int)(copy / (uint32_t)g.H), h = (int)(copy % (uint32_t)g.H);
+    const uint32_t x = copy * four + head;
+    b = (int)r, l = (int)(x / (uint32_t)g.H), h = (int)(x % (uint32_t)g.H);
   }
   pg_output(a, l, b, h, row, c4, D, o, m, L);
 }
@@ -96,7 +101,7 @@ template <int D>
 static certkv_status launch_paged_join(const PagedArgs& a, hipStream_t s) {
   constexpr int GR = kPgJoinThreads / (D / 4);
   const int M = a.tq * a.p.g.G;
-  const int64_t U = (int64_t)a.p.lists * a.copies;
+  const int64_t U = (int64_t)a.p.lists * a.copies * (a.mode == kPgHeads ? 4 : 1);
   // The partials of few rows are dealt out, of many taken row by row (as in attend.hip).
   if (U * M < 8192)
     CERTKV_LAUNCH("paged_join", (paged_join_kernel<D, GR>), dim3((unsigned)U, (unsigned)M),
@@ -111,7 +116,7 @@ certkv_status run_paged(const PagedArgs& a, int shape, hipStream_t s) {
   const certkv_status st = a.p.format == CERTKV_CACHE_MXFP8   ? run_paged_mxfp8(a, shape, s)
                            : a.p.format == CERTKV_CACHE_MXFP4 ? run_paged_mxfp4(a, shape, s)
                                                               : run_paged_bf16(a, shape, s);
-  if (st != CERTKV_OK || a.most == 0) return st;
+  if (st != CERTKV_OK || a.mode == kPgWhole) return st;
   return a.p.g.D == 128 ? launch_paged_join<128>(a, s) : launch_paged_join<64>(a, s);
 }
 

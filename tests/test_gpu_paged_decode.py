@@ -8,6 +8,7 @@ import paper_2608_21541_amd as ck
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
+LONG = 2000  # rows that lists have room for where a workgroup does not have a whole unit
 EDGES = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300]
 
 
@@ -42,36 +43,60 @@ def check(spec, cache, q, tq, q_lens=None, status=0, **kw):
 @pytest.mark.parametrize("fmt", ["bf16", "mxfp8", "mxfp4"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("page,head_major", [(16, False), (32, True), (256, False)])
-def test_one_token_of_every_length(fmt, d, page, head_major):
-    spec = spec_of(2, EDGES, H=3, G=4, d=d)
+@pytest.mark.parametrize("H,room", [(3, 300), (3, LONG), (4, LONG)])
+def test_one_token_of_every_length(fmt, d, page, head_major, H, room):
+    # whole units, pieces of units, and of four heads' units
+    spec = spec_of(2, EDGES, H=H, G=4, d=d)
     gen = torch.Generator().manual_seed(page + d)
-    cache = _pages.make_cache(spec, EDGES, page, fmt, DEV, gen, head_major=head_major)
+    cache = _pages.make_cache(spec, EDGES, page, fmt, DEV, gen, head_major=head_major,
+                              max_pages=-(-room // page))
     check(spec, cache, queries(spec, 1, gen), 1)
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "mxfp8", "mxfp4"])
 @pytest.mark.parametrize("d,page", [(64, 64), (128, 16)])
-def test_heads_of_their_own_lengths(fmt, d, page):
+@pytest.mark.parametrize("room", [700, LONG])
+def test_heads_of_their_own_lengths(fmt, d, page, room):
     spec = spec_of(2, B=3, H=3, G=2, d=d)
     gen = torch.Generator().manual_seed(page)
     lens = (EDGES + [700, 0, 90])[:spec.units]
-    cache = _pages.make_cache(spec, lens, page, fmt, DEV, gen, per_head=True)
+    cache = _pages.make_cache(spec, lens, page, fmt, DEV, gen, per_head=True,
+                              max_pages=-(-room // page))
     check(spec, cache, queries(spec, 1, gen), 1)
 
 
 @pytest.mark.parametrize("G,tq", [(1, 2), (1, 16), (1, 17), (3, 5), (4, 8), (8, 5), (2, 33), (16, 1),
                                   (24, 1), (8, 64)])
-@pytest.mark.parametrize("d,fmt", [(64, "bf16"), (128, "bf16"), (128, "mxfp4")])
-def test_drafts(d, fmt, G, tq):
+@pytest.mark.parametrize("d,fmt,H,room", [(64, "bf16", 2, 250), (128, "bf16", 2, LONG),
+                                          (64, "mxfp8", 4, LONG), (128, "mxfp4", 4, LONG)])
+def test_drafts(d, fmt, H, room, G, tq):
     # lengths below, at and above the drafts' own
     lens = [0, 1, tq - 1, tq, tq + 1, 40, 200]
-    spec = spec_of(1, lens, H=2, G=G, d=d)
+    spec = spec_of(1, lens, H=H, G=G, d=d)
     gen = torch.Generator().manual_seed(G * 100 + tq)
-    cache = _pages.make_cache(spec, lens, 16, fmt, DEV, gen)
+    cache = _pages.make_cache(spec, lens, 16, fmt, DEV, gen, max_pages=-(-room // 16))
     q = queries(spec, tq, gen)
     check(spec, cache, q, tq)
     q_lens = torch.tensor([0, tq, 1, tq // 2, tq, 1, tq], dtype=torch.int32, device=DEV)
     check(spec, cache, q, tq, q_lens)
+
+
+@pytest.mark.parametrize("lists", [5, 300, 2100])
+@pytest.mark.parametrize("H,per_head", [(1, False), (4, False), (2, True)])
+def test_drafts_of_their_own_lengths(lists, H, per_head):
+    # sequences with none, one, two or three groups of 32 query rows beside each other
+    B, tq, G = lists // H if per_head else lists, 12, 8
+    gen = torch.Generator().manual_seed(lists)
+    spec = spec_of(1, B=B, H=H, G=G, d=64)
+    n = B * H if per_head else B
+    lens = torch.randint(0, 70, (n,), generator=gen).tolist()
+    lens[n // 2] = 1500
+    cache = _pages.make_cache(spec, lens, 16, "mxfp4", DEV, gen, per_head=per_head,
+                              max_pages=LONG // 16)
+    q = queries(spec, tq, gen)
+    q_lens = torch.randint(0, tq + 1, (B,), generator=gen).int().to(DEV)
+    check(spec, cache, q, tq, q_lens)
+    assert bool((ck.decode_paged(spec, q, cache, tq, q_lens=torch.zeros_like(q_lens)) == 0).all())
 
 
 def test_numbers_of_queries_that_are_none():
@@ -88,12 +113,13 @@ def test_numbers_of_queries_that_are_none():
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "mxfp8"])
-@pytest.mark.parametrize("d,G", [(64, 1), (128, 6)])
-def test_rows_that_some_queries_do_not_see_may_hold_anything(fmt, d, G):
+@pytest.mark.parametrize("d,G,H,room", [(64, 1, 2, 100), (128, 6, 2, LONG), (64, 8, 4, LONG),
+                                        (128, 4, 1, 100)])
+def test_rows_that_some_queries_do_not_see_may_hold_anything(fmt, d, G, H, room):
     tq, lens = 5, [5, 29, 33, 64, 70]
-    spec = spec_of(1, lens, H=2, G=G, d=d)
+    spec = spec_of(1, lens, H=H, G=G, d=d)
     gen = torch.Generator().manual_seed(9)
-    cache = _pages.make_cache(spec, lens, 16, fmt, DEV, gen)
+    cache = _pages.make_cache(spec, lens, 16, fmt, DEV, gen, max_pages=-(-room // 16))
     q = queries(spec, tq, gen)
     good, lse = (x.clone() for x in ck.decode_paged(spec, q, cache, tq, with_lse=True))
     for b, n in enumerate(lens):  # the last two tokens' rows
@@ -112,17 +138,18 @@ def test_rows_that_some_queries_do_not_see_may_hold_anything(fmt, d, G):
     assert int(spec.status) == ck.CERTKV_ENONFINITE
 
 
-@pytest.mark.parametrize("fmt,per_head,d", [("bf16", False, 128), ("bf16", True, 64),
-                                            ("mxfp8", True, 128), ("mxfp4", False, 64)])
-def test_long_lists_are_cut_and_joined(fmt, per_head, d):
+@pytest.mark.parametrize("fmt,per_head,d,H", [("bf16", False, 128, 2), ("bf16", True, 64, 3),
+                                              ("mxfp8", True, 128, 3), ("mxfp4", False, 64, 4),
+                                              ("bf16", False, 128, 8)])
+def test_long_lists_are_cut_and_joined(fmt, per_head, d, H):
     # pieces of a list in many workgroups, and many lists' beside them
     gen = torch.Generator().manual_seed(d)
     if per_head:
-        spec = spec_of(2, B=1, H=3, G=2, d=d)
+        spec = spec_of(2, B=1, H=H, G=2, d=d)
         lens = [40_000, 3, 900, 0, 12_345, 5000]
     else:
         lens = [30_011, 1, 4097, 0, 64]
-        spec = spec_of(1, lens, H=2, G=4, d=d)
+        spec = spec_of(1, lens, H=H, G=4, d=d)
     cache = _pages.make_cache(spec, lens, 64, fmt, DEV, gen, per_head=per_head)
     q = queries(spec, 1, gen)
     a = check(spec, cache, q, 1).clone()
@@ -150,24 +177,26 @@ def test_many_lists(lists):
     check(spec, cache, queries(spec, 1, gen), 1)
 
 
-def test_rows_as_a_shorter_bound_leaves_them():
+@pytest.mark.parametrize("bound", [100, 1100])
+def test_rows_as_a_shorter_bound_leaves_them(bound):
     # the rows within the bound are attended, as if the list ended there
-    spec = spec_of(1, [500], H=2, G=2, d=64)
+    spec = spec_of(1, [1500], H=2, G=2, d=64)
     gen = torch.Generator().manual_seed(4)
-    cache = _pages.make_cache(spec, [500], 16, "bf16", DEV, gen)
+    cache = _pages.make_cache(spec, [1500], 16, "bf16", DEV, gen)
     q = queries(spec, 1, gen)
-    out = ck.decode_paged(spec, q, cache, 1, max_rows=100).clone()
+    out = ck.decode_paged(spec, q, cache, 1, max_rows=bound).clone()
     assert int(spec.status) == ck.CERTKV_ERANGE
-    cache.offsets[1] = 100
+    cache.offsets[1] = bound
     want, _, tol, _ = _pages.attend(spec, cache, q, 1)
     assert bool(((out.double().cpu() - want).abs() <= tol).all())
 
 
-def test_pages_that_are_none():
+@pytest.mark.parametrize("room", [100, LONG])
+def test_pages_that_are_none(room):
     # a page number that is none of the pool's leaves its rows out and is reported
     spec = spec_of(1, [100, 50], H=2, G=2, d=128)
     gen = torch.Generator().manual_seed(6)
-    cache = _pages.make_cache(spec, [100, 50], 16, "bf16", DEV, gen)
+    cache = _pages.make_cache(spec, [100, 50], 16, "bf16", DEV, gen, max_pages=-(-room // 16))
     q = queries(spec, 1, gen)
     good = ck.decode_paged(spec, q, cache, 1).clone()
     for bad in (-1, cache.num_pages, 2 ** 31 - 1, -2 ** 31):
@@ -189,22 +218,26 @@ def test_pages_that_are_none():
             assert bool(((out[0, 0, 2 * h:2 * h + 2].double().cpu() - o).abs() <= tol).all())
 
 
-def test_offsets_of_any_kind():
+@pytest.mark.parametrize("H,G,tq", [(1, 1, 1), (4, 1, 1), (2, 8, 9)])
+@pytest.mark.parametrize("room", [64, LONG])
+def test_offsets_of_any_kind(H, G, tq, room):
     # lengths that fall or are beyond the table: no access outside it
-    spec = spec_of(1, B=4, H=1, G=1, d=64)
+    spec = spec_of(1, B=4, H=H, G=G, d=64)
     gen = torch.Generator().manual_seed(8)
-    cache = _pages.make_cache(spec, [30, 40, 50, 20], 16, "bf16", DEV, gen)
+    cache = _pages.make_cache(spec, [30, 40, 50, 20], 16, "bf16", DEV, gen, max_pages=room // 16)
     cache.table.clamp_(max=2)
+    q_lens = torch.tensor([tq, 0, 1, tq], dtype=torch.int32, device=DEV)
     for off in ([0, 50, 20, 21, 10 ** 10], [5, 4, 3, 2, 1], [0, 0, 0, 0, 0], [7, 7, 10 ** 6, 7, 7]):
         cache.offsets.copy_(torch.tensor(off, device=DEV))
-        ck.decode_paged(spec, queries(spec, 1, gen), cache, 1)
-        torch.cuda.synchronize()
+        for n in (None, q_lens):
+            ck.decode_paged(spec, queries(spec, tq, gen), cache, tq, q_lens=n)
+            torch.cuda.synchronize()
 
 
 def test_strided_queries_and_large_scores():
     spec = spec_of(2, [70, 33], H=2, G=3, d=64)
     gen = torch.Generator().manual_seed(12)
-    cache = _pages.make_cache(spec, [70, 33], 32, "bf16", DEV, gen)
+    cache = _pages.make_cache(spec, [70, 33], 32, "bf16", DEV, gen, max_pages=LONG // 32)
     tq = 2
     q = queries(spec, tq, gen)
     big = torch.zeros((2, 6, 4, 72), dtype=torch.bfloat16, device=DEV)
