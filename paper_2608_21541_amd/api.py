@@ -89,7 +89,7 @@ class ProblemSpec:
         return p
 
     def __getstate__(self):  # (a copy describes itself anew)
-        return {k: v for k, v in self.__dict__.items() if k != "_c"}
+        return {k: v for k, v in self.__dict__.items() if k not in ("_c", "_paged")}
 
 
 def _dtype_code(dt):
@@ -678,6 +678,12 @@ class PagedCache:
         object.__setattr__(self, "_seen", None)
         object.__setattr__(self, name, value)
 
+    def __getstate__(self):  # (a copy describes itself anew)
+        return {k: v for k, v in self.__dict__.items() if k != "_seen"}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state, _seen=None)
+
     def _strides(self, t, width):
         # in rows: of layer, page, row and head
         s = t.stride()
@@ -691,17 +697,23 @@ class PagedCache:
         return [0, rows[0], rows[1], 0] if self.per_head else rows
 
     def _c_pages(self, spec):
-        """The cache as the C entry points take it.  Shapes and types are checked when a field has
-        changed, or a tensor's address, or the lists and heads that the spec says there are."""
-        k, v, ks, vs, ring = self.k, self.v, self.k_scales, self.v_scales, self.ring
-        seen = (None if k is None else (k.data_ptr(), k.shape, k.stride(), v.data_ptr(), v.stride()),
-                None if ks is None else (ks.data_ptr(), ks.stride(), vs.data_ptr(), vs.stride()),
-                self.table.data_ptr(), self.table.shape, self.offsets.data_ptr(),
-                None if ring is None else (ring.data_ptr(), self.free.data_ptr()),
-                spec.layers, len(spec.seqlens), spec.kv_heads, spec.head_dim)
+        """(what it was made from, the cache as the C entry points take it, a reference to that, the
+        tensors' GPU, their device).  Shapes and types are checked when a field has changed, or a
+        tensor's address, or the lists and heads that the spec says there are."""
+        k, ks, ring = self.k, self.k_scales, self.ring
+        seen = (self.table.data_ptr(), self.table.numel(), self.offsets.data_ptr(), spec.layers,
+                spec.kv_heads, spec.head_dim, len(spec.seqlens))
+        if k is not None:
+            v = self.v
+            seen += (k.data_ptr(), k.numel(), k.stride(), v.data_ptr(), v.stride())
+        if ks is not None:
+            vs = self.v_scales
+            seen += (ks.data_ptr(), ks.stride(), vs.data_ptr(), vs.stride())
+        if ring is not None:
+            seen += (ring.data_ptr(), self.free.data_ptr())
         kept = self._seen
         if kept is not None and kept[0] == seen:
-            return kept[1]
+            return kept
         dev = self.table.device
         strides = [0, 0, 1, 0]
         if k is not None:
@@ -736,8 +748,54 @@ class PagedCache:
                        self.k_scales.data_ptr() if mx else None,
                        self.v_scales.data_ptr() if mx else None, self.table.data_ptr(),
                        self.offsets.data_ptr(), _ptr(ring), _ptr(self.free))
-        object.__setattr__(self, "_seen", (seen, c))
-        return c
+        kept = (seen, c, ctypes.byref(c), self.table.get_device(), dev)
+        object.__setattr__(self, "_seen", kept)
+        return kept
+
+
+def _page_problem(spec):
+    # The problem as the paged calls read it, without the sequences' lengths: kept with the spec
+    # until a field changes.
+    key = (spec.layers, len(spec.seqlens), spec.kv_heads, spec.group, spec.head_dim, spec.dtype,
+           spec.softmax_scale, spec.dry_run, None if spec.status is None else spec.status.data_ptr())
+    kept = spec.__dict__.get("_paged")
+    if kept is not None and kept[0] == key:
+        return kept[1]
+    dt = _dtype_code(spec.dtype)
+    p = _lib.Problem(key[0], key[1], key[2], key[3], key[4], 1, None, dt, dt, float(key[6]),
+                     _lib.CERTKV_DRY_RUN if key[7] else 0, key[8])
+    spec.__dict__["_paged"] = (key, ctypes.byref(p))
+    return spec.__dict__["_paged"][1]
+
+
+_PAGED = {}  # the paged entry points, by name
+
+
+def _run_paged(index, what, *args):
+    """_run with the GPU's index (a call of few rows takes longer to make than to run)."""
+    fn = _PAGED.get(what)
+    if fn is None:
+        fn = _PAGED[what] = getattr(_lib.lib(), what)
+    if index < 0:
+        raise ValueError(f"{what}: expected tensors on a GPU")
+    if index == torch._C._cuda_getDevice():
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        _check(st, what)
+
+
+def _there(kept, *tensors):
+    # whether tensors are where a cache's are (kept: its _c_pages)
+    index = kept[3]
+    if index >= 0:
+        for t in tensors:
+            if t.get_device() != index:
+                return False
+        return True
+    return all(t.device == kept[4] for t in tensors)
 
 
 class ResizeBuffers:
@@ -766,92 +824,94 @@ def page_resize(spec: ProblemSpec, cache: PagedCache, change, bufs=None, into=No
     as they are and the new ones written there.  A list that does not fit is refused: its slots are
     -1, it stays as it was, and spec.status says CERTKV_ERANGE.  bufs: ResizeBuffers (without, the
     rows to append are counted on the device first)."""
-    dev = change.device
-    c = cache._c_pages(spec)
-    assert change.dtype == torch.int32 and change.is_contiguous()
-    assert change.numel() == cache.lists and cache.table.device == dev
-    assert cache.ring is not None and cache.free is not None
+    kept = cache._c_pages(spec)
+    lists = cache.lists
+    assert change.dtype == torch.int32 and change.is_contiguous() and change.numel() == lists
+    assert _there(kept, change) and cache.ring is not None and cache.free is not None
     if bufs is None:
-        bufs = ResizeBuffers(cache, int(change.clamp(min=0).sum().item()), dev)
-    offsets, free = (cache.offsets, cache.free) if into is None else into
-    if into is not None:
-        assert offsets.dtype == free.dtype == torch.int64
-        assert offsets.shape == cache.offsets.shape and free.shape == cache.free.shape
-        assert offsets.is_contiguous() and free.is_contiguous()
-        assert offsets.device == free.device == dev
-    assert bufs.slot_offsets.numel() == cache.lists + 1 and bufs.slots.device == dev
-    slots = bufs.slots
-    _run(dev, "certkv_page_resize", ctypes.byref(spec._problem()), ctypes.byref(c),
-         change.data_ptr(), offsets.data_ptr(), free.data_ptr(), slots.data_ptr(), slots.numel(),
-         bufs.slot_offsets.data_ptr(), bufs.ws.data_ptr(), bufs.ws_bytes)
-    return slots, bufs.slot_offsets
+        bufs = ResizeBuffers(cache, int(change.clamp(min=0).sum().item()), change.device)
+    if into is None:
+        offsets, free = cache.offsets, cache.free
+    else:
+        offsets, free = into
+        assert offsets.dtype == torch.int64 and offsets.numel() == lists + 1
+        assert free.dtype == torch.int64 and free.numel() == 2
+        assert offsets.is_contiguous() and free.is_contiguous() and _there(kept, offsets, free)
+    slots, slot_offsets = bufs.slots, bufs.slot_offsets
+    assert slot_offsets.numel() == lists + 1 and _there(kept, slots)
+    _run_paged(kept[3], "certkv_page_resize", _page_problem(spec), kept[2], change.data_ptr(),
+               offsets.data_ptr(), free.data_ptr(), slots.data_ptr(), slots.numel(),
+               slot_offsets.data_ptr(), bufs.ws.data_ptr(), bufs.ws_bytes)
+    return slots, slot_offsets
 
 
-def _check_slots(cache, slots, slot_offsets, dev):
-    assert slots.dtype == torch.int32 and slots.is_contiguous() and slots.device == dev
+def _check_slots(cache, kept, slots, slot_offsets):
+    assert slots.dtype == torch.int32 and slots.is_contiguous()
     assert slot_offsets.dtype == torch.int64 and slot_offsets.is_contiguous()
-    assert slot_offsets.numel() == cache.lists + 1 and slot_offsets.device == dev
+    assert slot_offsets.numel() == cache.lists + 1 and _there(kept, slots, slot_offsets)
 
 
 def page_write(spec: ProblemSpec, cache: PagedCache, k, v, slots, slot_offsets, tn=0):
     """Rows of new tokens to their slots (of page_resize): k, v [L][tokens][H][d] in spec.dtype,
     sequence after sequence, or, with tn, tn tokens of each sequence, of which a list takes as many
     as it has slots."""
-    dev = k.device
-    c = cache._c_pages(spec)
-    tokens = k.shape[1]
-    assert k.shape == v.shape == (spec.layers, tokens, spec.kv_heads, spec.head_dim)
-    assert k.dtype == v.dtype == spec.dtype and v.device == dev and cache.k.device == dev
-    _check_slots(cache, slots, slot_offsets, dev)
-    _run(dev, "certkv_page_write", ctypes.byref(spec._problem()), ctypes.byref(c), _tensor(k),
-         _tensor(v), tokens, int(tn), slots.data_ptr(), slots.numel(), slot_offsets.data_ptr())
+    kept = cache._c_pages(spec)
+    shape = k.shape
+    assert shape == v.shape and len(shape) == 4 and cache.k is not None
+    layers, tokens, heads, d = shape
+    assert layers == spec.layers and heads == spec.kv_heads and d == spec.head_dim
+    assert k.dtype == v.dtype == spec.dtype and _there(kept, k, v)
+    _check_slots(cache, kept, slots, slot_offsets)
+    _run_paged(kept[3], "certkv_page_write", _page_problem(spec), kept[2], _tensor(k), _tensor(v),
+               tokens, int(tn), slots.data_ptr(), slots.numel(), slot_offsets.data_ptr())
 
 
 def page_adopt(spec: ProblemSpec, cache: PagedCache, packed, slots, slot_offsets):
     """A packed cache's rows to the slots of lists (units') that take them whole: an MxCache, or
     (k_packed, v_packed, packed_offsets) of a bf16 one, of the pages' format."""
-    c = cache._c_pages(spec)
+    kept = cache._c_pages(spec)
+    assert cache.k is not None
     if isinstance(packed, MxCache):
-        src, rows, d, dev = packed.c_cache(), packed.rows, packed.head_dim, packed.k.device
+        src, rows, d, k = packed.c_cache(), packed.rows, packed.head_dim, packed.k
         assert packed.format == cache.format
     else:
         k, v = packed[0], packed[1]
         assert k.is_contiguous() and v.is_contiguous() and k.shape == v.shape
         assert k.dtype == v.dtype == torch.bfloat16 and v.device == k.device
         assert cache.format == "bf16"
-        (rows, d), dev = k.shape, k.device
+        rows, d = k.shape
         src = _lib.Cache(_lib.CERTKV_CACHE_BF16, k.data_ptr(), v.data_ptr(), None, None, None)
-    assert d == spec.head_dim and cache.k.device == dev
-    _check_slots(cache, slots, slot_offsets, dev)
-    _run(dev, "certkv_page_adopt", ctypes.byref(spec._problem()), ctypes.byref(c), src, rows,
-         slots.data_ptr(), slots.numel(), slot_offsets.data_ptr())
+    assert d == spec.head_dim and _there(kept, k)
+    _check_slots(cache, kept, slots, slot_offsets)
+    _run_paged(kept[3], "certkv_page_adopt", _page_problem(spec), kept[2], src, rows,
+               slots.data_ptr(), slots.numel(), slot_offsets.data_ptr())
 
 
 def page_read(spec: ProblemSpec, cache: PagedCache, dtype=torch.bfloat16, rows=None, out=None):
     """The rows of all lists, out of their pages: (k, v) [L][rows][H][d], as compress takes them, or
     of units' lists [rows][d], a packed cache.  rows: their number (None: asked of the device);
     out: the two tensors to write, whose rows past the lists' last are left as they are."""
-    c = cache._c_pages(spec)
-    dev = cache.k.device
+    kept = cache._c_pages(spec)
+    assert cache.k is not None
     if out is None:
         n = int((cache.offsets[-1] - cache.offsets[0]).item()) if rows is None else int(rows)
         shape = (n, spec.head_dim) if cache.per_head else \
             (spec.layers, n, spec.kv_heads, spec.head_dim)
-        out = [torch.empty(shape, dtype=dtype, device=dev) for _ in range(2)]
+        out = [torch.empty(shape, dtype=dtype, device=kept[4]) for _ in range(2)]
     ko, vo = out
     n = ko.shape[0 if cache.per_head else 1]
     shape = (n, spec.head_dim) if cache.per_head else (spec.layers, n, spec.kv_heads, spec.head_dim)
     assert ko.shape == vo.shape == shape and ko.dtype == vo.dtype
-    assert ko.is_contiguous() and vo.is_contiguous() and ko.device == vo.device == dev
-    _run(dev, "certkv_page_read", ctypes.byref(spec._problem()), ctypes.byref(c), n,
-         _dtype_code(ko.dtype), ko.data_ptr(), vo.data_ptr())
+    assert ko.is_contiguous() and vo.is_contiguous() and _there(kept, ko, vo)
+    _run_paged(kept[3], "certkv_page_read", _page_problem(spec), kept[2], n, _dtype_code(ko.dtype),
+               ko.data_ptr(), vo.data_ptr())
     return ko, vo
 
 
 def decode_paged_workspace_size(spec: ProblemSpec, cache: PagedCache, tq: int,
                                 max_rows: int = 0) -> int:
     return int(_lib.lib().certkv_decode_paged_workspace_size(
-        ctypes.byref(spec._problem()), ctypes.byref(cache._c_pages(spec)), int(tq), int(max_rows)))
+        _page_problem(spec), cache._c_pages(spec)[2], int(tq), int(max_rows)))
 
 
 def decode_paged(spec: ProblemSpec, q_new, cache: PagedCache, tq, q_lens=None, with_lse=False,
@@ -860,22 +920,23 @@ def decode_paged(spec: ProblemSpec, q_new, cache: PagedCache, tq, q_lens=None, w
     sequence b's n = q_lens[b] (int32 [B]; None: tq) sees the rows up to len - n + t.  Returns out
     [L][B*tq][Hq][d] fp32 (and the natural-log lse [L][B*tq][Hq] with_lse); a query that sees
     nothing (t >= n, an empty list) is out 0, lse -inf.  bufs: DecodeBuffers(..., pages=cache)."""
-    dev = q_new.device
+    kept = cache._c_pages(spec)
     _check_queries(spec, q_new, tq)
-    c = cache._c_pages(spec)
-    assert cache.k.device == dev
+    assert cache.k is not None and _there(kept, q_new)
     if q_lens is not None:
         assert q_lens.dtype == torch.int32 and q_lens.is_contiguous()
-        assert q_lens.shape == (spec.batch,) and q_lens.device == dev
+        assert q_lens.shape == (spec.batch,) and _there(kept, q_lens)
     if bufs is None:
-        bufs = DecodeBuffers(spec, tq, dev, with_lse=with_lse, max_rows=max_rows, pages=cache)
-    assert bufs.paged and bufs.tq == int(tq)
-    assert bufs.out.shape == q_new.shape and bufs.out.device == dev
-    assert bufs.lse is not None or not with_lse
-    _run(dev, "certkv_decode_paged", ctypes.byref(spec._problem()), _tensor(q_new), bufs.tq,
-         _ptr(q_lens), bufs.max_rows, ctypes.byref(c), bufs.out.data_ptr(), _ptr(bufs.lse),
-         bufs.ws.data_ptr(), bufs.ws_bytes)
-    return (bufs.out, bufs.lse) if with_lse else bufs.out
+        bufs = DecodeBuffers(spec, tq, q_new.device, with_lse=with_lse, max_rows=max_rows,
+                             pages=cache)
+    out, lse = bufs.out, bufs.lse
+    assert bufs.paged and bufs.tq == tq and out.shape == q_new.shape and _there(kept, out)
+    assert lse is not None or not with_lse
+    _run_paged(kept[3], "certkv_decode_paged", _page_problem(spec), _tensor(q_new), bufs.tq,
+               None if q_lens is None else q_lens.data_ptr(), bufs.max_rows, kept[2],
+               out.data_ptr(), None if lse is None else lse.data_ptr(), bufs.ws.data_ptr(),
+               bufs.ws_bytes)
+    return (out, lse) if with_lse else out
 
 
 class CompressBuffers:

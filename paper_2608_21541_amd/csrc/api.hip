@@ -1405,7 +1405,7 @@ certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* page
 // 256-byte aligned.
 struct PagedWs {
   int shape;
-  int32_t copies, cover, qgroups, mp, mode, parts, most;
+  int32_t copies, cover, qgroups, mp, mode, gap, parts, most;
   int32_t parts_weighed, most_weighed;  // where the query groups are weighed (0: never)
   size_t ml_off, place_off, total;
 };
@@ -1418,6 +1418,7 @@ static bool paged_ws_layout(const PageArgs& x, int32_t tq, int32_t max_rows, Pag
   w->qgroups = (int32_t)((M + held - 1) / held);
   w->mp = (int32_t)M;
   // as many chunks as their workgroups stay resident: 256 compute units of four SIMDs
+  w->gap = pg_gap(held / 16);
   const int resident = 256 * 4 * pg_simd_waves(x.format, x.g.D, held / 16) / pg_waves(kPgPiece);
   w->parts = (resident + w->qgroups - 1) / w->qgroups;
   const int64_t list = (int64_t)x.max_pages << x.lp;
@@ -1425,8 +1426,8 @@ static bool paged_ws_layout(const PageArgs& x, int32_t tq, int32_t max_rows, Pag
   w->mode = pg_mode(x.per_head, x.g.H, x.s_row, x.s_head, w->cover);
   const int heads = w->mode == kPgHeads ? 4 : 1;
   w->copies = x.per_head ? 1 : x.g.L * x.g.H / heads;
-  const int64_t by_lists = (int64_t)x.lists * ((w->cover + 31) / 32 + kPgGap);
-  const int64_t by_pool = ((int64_t)x.num_pages << x.lp) / 32 + (int64_t)x.lists * (1 + kPgGap);
+  const int64_t by_lists = (int64_t)x.lists * ((w->cover + 31) / 32 + w->gap);
+  const int64_t by_pool = ((int64_t)x.num_pages << x.lp) / 32 + (int64_t)x.lists * (1 + w->gap);
   const int64_t tiles = w->copies * (1 + (by_lists < by_pool ? by_lists : by_pool));
   if (by_lists > INT32_MAX || tiles * w->qgroups > INT32_MAX) return false;
   auto chunks = [](int64_t n, int64_t parts) {
@@ -1477,6 +1478,7 @@ certkv_status certkv_decode_paged(const certkv_problem* p, certkv_tensor q_new, 
   a.qgroups = W.qgroups;
   a.mp = W.mp;
   a.mode = W.mode;
+  a.gap = W.gap;
   const bool weighed = q_lens && W.parts_weighed;
   a.parts = weighed ? W.parts_weighed : W.parts;
   a.most = weighed ? W.most_weighed : W.most;

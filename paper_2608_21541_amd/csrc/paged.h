@@ -24,7 +24,8 @@
 
 namespace certkv {
 
-constexpr int kPgGap = 8;         // tiles between lists' places beside their rows': a piece's cost
+// Tiles between lists' places beside their rows': what a piece costs beside its tiles.
+constexpr int pg_gap(int qt) { return qt == 2 ? 16 : 8; }
 constexpr int kPgMinTiles = 4;    // shortest chunk, and the unit of its length
 constexpr int kPgMaxTiles = kAtMaxKeys / kAtTile;  // longest, unless partials are short
 
@@ -51,7 +52,7 @@ struct PagedArgs {
                                 // of them where a workgroup has four heads
   int32_t cover;                // rows of a list that are attended
   int32_t qgroups, mp;          // workgroups of a chunk, query rows of a partial
-  int32_t mode;
+  int32_t mode, gap;
   int32_t parts, most;          // chunks taken at once, and that the workspace has room for
   const int32_t* q_lens;        // [B], or NULL: tq
   uint32_t* place;              // [lists + 1]: the lists' places by their queries' groups, or NULL
@@ -73,8 +74,8 @@ struct PgCut {
 };
 __device__ __forceinline__ uint32_t pg_up(int64_t rows) { return (uint32_t)((uint64_t)(rows + 31) >> 5); }
 // The first tile of list r, for copies = 1.
-__device__ __forceinline__ uint32_t pg_place(int64_t rows_before, uint32_t r) {
-  return pg_up(rows_before) + r * (uint32_t)kPgGap;
+__device__ __forceinline__ uint32_t pg_place(int64_t rows_before, uint32_t r, int gap) {
+  return pg_up(rows_before) + r * (uint32_t)gap;
 }
 __device__ __forceinline__ PgCut pg_cut(const PagedArgs& a, uint32_t tiles) {
   const uint32_t total = (uint32_t)a.copies * tiles;
@@ -110,7 +111,7 @@ __device__ __forceinline__ void pg_weigh(const PagedArgs& a, uint32_t* place_s, 
     const int r = r0 + tid;
     uint32_t x = 0;
     if (r < a.p.lists)
-      x = pg_groups(a, pg_list_sequence(a, r)) * (pg_up(off[r + 1] - base) - pg_up(off[r] - base) + kPgGap);
+      x = pg_groups(a, pg_list_sequence(a, r)) * (pg_up(off[r + 1] - base) - pg_up(off[r] - base) + a.gap);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const uint32_t y = __shfl_up(x, d, 64);
@@ -161,17 +162,17 @@ struct PgOffsets {
     p1 = AtOffsets::lane64(end, r - at) - base;
   }
   // The list whose place holds tile x (of one copy): 64 lists' ends per step.
-  __device__ __forceinline__ uint32_t find(uint32_t x, int lane) {
+  __device__ __forceinline__ uint32_t find(uint32_t x, int gap, int lane) {
     uint32_t lo = 0, n = R;  // the answer is one of [lo, lo + n]
     while (n > 64) {
       const uint32_t step = (n + 63) / 64, i = lo + lane * step + step - 1;
-      const bool past = i >= R || pg_place(off[min(i + 1, R)] - base, i + 1) > x;
+      const bool past = i >= R || pg_place(off[min(i + 1, R)] - base, i + 1, gap) > x;
       lo += (uint32_t)__popcll(__ballot(!past)) * step;
       n = step;
     }
     if (lo != at) window(lo, lane);
     const uint32_t i = lo + lane;
-    const uint64_t past = __ballot(i >= R || pg_place(end - base, i + 1) > x);
+    const uint64_t past = __ballot(i >= R || pg_place(end - base, i + 1, gap) > x);
     return past ? min(lo + (uint32_t)__builtin_ctzll(past), R) : R;
   }
 };
@@ -254,7 +255,7 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
   // The units' pieces: of the chunks that the workgroup takes, or the whole units.
   PgOffsets off(p.offsets, WHOLE ? 0 : p.lists, lane);
   const PgCut cut = WHOLE ? PgCut{1, 0}
-                          : pg_cut(a, weighed ? place_s[PLACES > 1 ? p.lists : 0] : pg_place(off.rows, off.R));
+                          : pg_cut(a, weighed ? place_s[PLACES > 1 ? p.lists : 0] : pg_place(off.rows, off.R, pg_gap(QT)));
   const uint32_t nch = WHOLE ? (uint32_t)p.lists * copies : (cut.total + cut.tiles - 1) / cut.tiles;
   for (uint32_t x = x0; x < nch; x = WHOLE ? nch : x + xstep) {
     const uint32_t r0 = x * cut.tiles, r1 = min(cut.total, r0 + cut.tiles);
@@ -272,7 +273,7 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
       }
       r = __builtin_amdgcn_readfirstlane(r);
     } else {
-      r = off.find(r0 / copies, lane);
+      r = off.find(r0 / copies, pg_gap(QT), lane);
     }
     bool begun = false;
     while (WHOLE ? !begun : r < off.R) {
@@ -287,8 +288,8 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
         ntp = (int)pg_up(len);
       } else {
         off.list(r, lane, p0, p1);
-        uint32_t place = copies * pg_place(p0, r), times = 1;
-        const uint32_t span = pg_place(p1, r + 1) - pg_place(p0, r);
+        uint32_t place = copies * pg_place(p0, r, pg_gap(QT)), times = 1;
+        const uint32_t span = pg_place(p1, r + 1, pg_gap(QT)) - pg_place(p0, r, pg_gap(QT));
         if (weighed) {
           place = copies * place_s[PLACES > 1 ? r : 0];
           times = pg_groups(a, pg_list_sequence(a, r));

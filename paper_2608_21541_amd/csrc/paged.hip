@@ -30,9 +30,9 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
   uint32_t group = 0, groups = 1;
   if (a.place) groups = pg_groups(a, pg_list_sequence(a, r)), group = (uint32_t)row >> 5;
   if (row < M && len > 0 && group < groups) {
-    const PgCut cut = pg_cut(a, a.place ? a.place[p.lists] : pg_place(p.offsets[p.lists] - base, (uint32_t)p.lists));
-    const uint32_t span = pg_place(p1, r + 1) - pg_place(p0, r);
-    const uint32_t place = a.place ? a.place[r] : pg_place(p0, r);
+    const PgCut cut = pg_cut(a, a.place ? a.place[p.lists] : pg_place(p.offsets[p.lists] - base, (uint32_t)p.lists, a.gap));
+    const uint32_t span = pg_place(p1, r + 1, a.gap) - pg_place(p0, r, a.gap);
+    const uint32_t place = a.place ? a.place[r] : pg_place(p0, r, a.gap);
     const uint32_t vs = (uint32_t)a.copies * place + (copy * groups + group) * span;
     // (of offsets that fall, places may lie behind the last chunk)
     const uint32_t s0 = min(vs / cut.tiles, (uint32_t)a.most - 1u);

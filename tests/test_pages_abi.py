@@ -204,15 +204,15 @@ GPU = pytest.raises(ValueError, match="expected tensors on a GPU")  # (the argum
 @pytest.mark.parametrize("per_head", [False, True])
 def test_strides_are_counted_in_rows(fmt, per_head):
     spec, cache = _cpu(fmt, per_head)
-    c = cache._c_pages(spec)
+    c = cache._c_pages(spec)[1]
     got = (c.s_layer, c.s_page, c.s_row, c.s_head)
     assert got == ((0, 16, 1, 0) if per_head else (9 * 16 * 2, 32, 2, 1))
     if not per_head:
         other = ck.PagedCache.empty(spec, 9, 16, 4, "cpu", fmt, head_major=True)
-        c = other._c_pages(spec)
+        c = other._c_pages(spec)[1]
         assert (c.s_layer, c.s_page, c.s_row, c.s_head) == (9 * 32, 32, 1, 16)
         one = other.layer(1, 2)
-        c = one._c_pages(ck.ProblemSpec(1, 2, 2, 64, 1, [1, 1]))
+        c = one._c_pages(ck.ProblemSpec(1, 2, 2, 64, 1, [1, 1]))[1]
         assert (c.s_layer, c.s_page, c.s_row, c.s_head) == (0, 32, 1, 16)
         assert c.k == other.k[1].data_ptr() and c.num_pages == 9
 
