@@ -1423,7 +1423,8 @@ static bool paged_ws_layout(const PageArgs& x, int32_t tq, int32_t max_rows, Pag
   w->parts = (resident + w->qgroups - 1) / w->qgroups;
   const int64_t list = (int64_t)x.max_pages << x.lp;
   w->cover = (int32_t)(max_rows > 0 && max_rows < list ? max_rows : list);
-  w->mode = pg_mode(x.per_head, x.g.H, x.s_row, x.s_head, w->cover);
+  w->mode = pg_mode(x.per_head, x.g.H, x.g.D, (int64_t)x.g.L * x.g.B * x.g.H * w->qgroups, x.s_row,
+                    x.s_head, w->cover);
   const int heads = w->mode == kPgHeads ? 4 : 1;
   w->copies = x.per_head ? 1 : x.g.L * x.g.H / heads;
   const int64_t by_lists = (int64_t)x.lists * ((w->cover + 31) / 32 + w->gap);

@@ -38,10 +38,19 @@ constexpr int pg_waves(int mode) { return mode == kPgWhole ? 8 : 4; }
 constexpr int pg_simd_waves(int format, int D, int qt) {
   return qt == 1 && (D == 64 || format == CERTKV_CACHE_MXFP4) ? 3 : 2;
 }
-constexpr int kPgWholeRows = 1024;  // of a unit at most that a workgroup has whole
-// s_row, s_head: the pool's strides.
-inline int pg_mode(int per_head, int H, int64_t s_row, int64_t s_head, int64_t cover) {
-  if (cover <= kPgWholeRows) return kPgWhole;
+// A workgroup has whole units where they are short and not many: no partials, no second launch.
+// (In us, whole and in pieces: 8 units of 1024 rows of 128 dims, bf16, 17 and 15, 128 of them 19
+// and 23, 512 48 and 54, 2048 194 and 181; 32 units of 100 rows 9 and 15, 2048 53 and 31; of 64
+// dims 16 units of 1024 rows 10 and 14, 1024 46 and 53.)
+constexpr int kPgWholeRows = 1024, kPgWholeUnits = 1024;
+// Four heads' units where the heads of a row lie together: their rows share lines, which they then
+// read at the same time.  (64 ragged sequences, 2.4M rows of 128 dims, a head's rows by itself and
+// with three others: bf16 218 and 200 us, mxfp8 136 and 118, mxfp4 124 and 86, 4.8M rows of 64
+// dims of mxfp4 237 and 147; with the heads apart in a page, bf16, 202 and 206.)
+// units: by query group; s_row, s_head: the pool's strides.
+inline int pg_mode(int per_head, int H, int D, int64_t units, int64_t s_row, int64_t s_head,
+                   int64_t cover) {
+  if (cover <= kPgWholeRows && units * (D / 64) <= kPgWholeUnits) return kPgWhole;
   return !per_head && H % 4 == 0 && s_head < s_row ? kPgHeads : kPgPiece;
 }
 
@@ -284,7 +293,6 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
         begun = true;
         p0 = p.offsets[r], p1 = p.offsets[r + 1];
         len = min(page_rows(p, p0, p1), a.cover);
-        if (p1 - p0 != len && tid == 0) report_range(gm);
         ntp = (int)pg_up(len);
       } else {
         off.list(r, lane, p0, p1);
@@ -332,6 +340,26 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
         b = (int)r, l = (int)(mine / (uint32_t)gm.H), h = (int)(mine % (uint32_t)gm.H);
       }
       const int row0 = qg * QT * 16;  // the first query row
+      // (Query rows that are not there are another's: nothing is kept of them.)
+      uint4 q[QT][KSTEP];
+      auto load_queries = [&]() {
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          const int rc = min(row0 + qt * 16 + c, M - 1);
+          const uint16_t* src = static_cast<const uint16_t*>(a.q.ptr) + l * a.q.s_layer +
+                                (int64_t)(b * a.tq + rc / gm.G) * a.q.s_token +
+                                (int64_t)(h * gm.G + rc % gm.G) * a.q.s_head;
+#pragma unroll
+          for (int ks = 0; ks < KSTEP; ++ks) q[qt][ks] = *reinterpret_cast<const uint4*>(src + kdim(ks));
+        }
+      };
+      // A whole unit's queries and first pages are asked for before its length is known: latency.
+      int32_t first_ids = 0;
+      if constexpr (WHOLE) {
+        const int pi = ((wave + KS * (lane >> 1)) * kAtTile + (lane & 1) * 16) >> p.lp;
+        first_ids = p.table[(int64_t)r * p.max_pages + min(pi, p.max_pages - 1)];
+        load_queries();
+      }
       const int own = pg_queries(a, b);
       const int64_t at0 = p.per_head ? 0 : l * p.s_layer + h * p.s_head;
       const uint8_t* const kp = p.k + at0 * RB;
@@ -358,7 +386,7 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
         const int row = (int)(lo + turn + KS * ((n & ~31) + (lane >> 1))) * kAtTile + (lane & 1) * 16;
         ids = -1;
         if (row < len) {
-          const int32_t id = p.table[(int64_t)r * p.max_pages + (row >> p.lp)];
+          const int32_t id = WHOLE && n == 0 ? first_ids : p.table[(int64_t)r * p.max_pages + (row >> p.lp)];
           if ((uint32_t)id < (uint32_t)p.num_pages)
             ids = id;
           else
@@ -381,7 +409,6 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) acc.o[qt][db] = (at_f32x4){0.f, 0.f, 0.f, 0.f};
       }
-      uint4 q[QT][KSTEP];
       AtRaw<F, WK> kx[2][NLK];
       AtRaw<F, W> vx[NLT];
       uint32_t ksc[2] = {}, vsc[NLT] = {};
@@ -422,18 +449,7 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
         load_keys(0);
         load_values(0);
       }
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        const int row = row0 + qt * 16 + c, rc = min(row, M - 1);
-        const uint16_t* src = static_cast<const uint16_t*>(a.q.ptr) + l * a.q.s_layer +
-                              (int64_t)(b * a.tq + rc / gm.G) * a.q.s_token +
-                              (int64_t)(h * gm.G + rc % gm.G) * a.q.s_head;
-#pragma unroll
-        for (int ks = 0; ks < KSTEP; ++ks) {
-          q[qt][ks] = *reinterpret_cast<const uint4*>(src + kdim(ks));
-          if (row >= M) q[qt][ks] = make_uint4(0u, 0u, 0u, 0u);
-        }
-      }
+      if constexpr (!WHOLE) load_queries();
       // One tile, whose keys and values have been asked for; TAIL: some row of it may not be seen by
       // some query.  (Apart, so that what the few last tiles need takes no registers from the
       // others' loads in flight.)
@@ -621,6 +637,7 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
           }
         }
       }
+      if (WHOLE && tid == 0 && p.offsets[r + 1] - p.offsets[r] != len) report_range(gm);
       if constexpr (KS > 1) __syncthreads();  // the joined tiles are read before the next piece's
     }
   }
