@@ -546,7 +546,8 @@ typedef struct certkv_pages {
  *                ring's new state.  May be pages->offsets and pages->free (in
  *                place); or others, which leaves those as they are (a step planned
  *                beside the present one's attention)
- *   slots        [slot_capacity] int32 out: for each appended row, lists one after
+ *   slots        [slot_capacity] int32 out, slot_capacity at most 2^31 - 1024 (else
+ *                CERTKV_EUNSUPPORTED): for each appended row, lists one after
  *                another, its slot, page number * page + row of the page.  Entries
  *                behind the last appended row are not written
  *   slot_offsets [lists+1] int64 out: first slot of each list's

@@ -1313,6 +1313,7 @@ certkv_status certkv_page_resize(const certkv_problem* p, const certkv_pages* pa
   if (!pages->ring || !pages->free || !change || !offsets_out || !free_out || !slot_offsets)
     return CERTKV_EINVAL;
   if (slot_capacity < 0 || (slot_capacity > 0 && !slots)) return CERTKV_EINVAL;
+  if (slot_capacity > kPgMostRows) return CERTKV_EUNSUPPORTED;
   if (!ws) return CERTKV_EWORKSPACE;
   if (((uintptr_t)ws & 255u) != 0) return CERTKV_EINVAL;
   if (ws_bytes < page_resize_ws(x.lists)) return CERTKV_EWORKSPACE;

@@ -413,6 +413,10 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
       AtRaw<F, W> vx[NLT];
       uint32_t ksc[2] = {}, vsc[NLT] = {};
       int kthere[2] = {};
+      // Values are read non-temporally, but for rows of less than a line that four heads share.
+      // (32 layers of bf16 265 us, without 295; 64 sequences, four heads, bf16 200 and 219, mxfp8
+      // 117 and 127, mxfp4 94 and 87, of 64 dims 148 and 126; keys too: as without or slower.)
+      constexpr bool VNT = !HEADS || RB >= 128;
       // (rows that are not there are read as well, of the same page: their scores are replaced and
       // their values zero)
       auto load_keys = [&](int n) {
@@ -439,7 +443,7 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
 #pragma unroll
           for (int i = 0; i < NLT / 2; ++i) {
             const uint64_t ati = at + (uint32_t)(i * RPL) * (uint64_t)st;
-            pg_load<true>(vx[kb * (NLT / 2) + i].x, vp + ati, v_off);
+            pg_load<VNT>(vx[kb * (NLT / 2) + i].x, vp + ati, v_off);
             if constexpr (MX) vsc[kb * (NLT / 2) + i] = vsp[ati / (RB / (D / 32)) + vs_off];
           }
         }

@@ -310,9 +310,16 @@ __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
         a.slots[j] = pg_slot(a, r, had_s[r] + (int32_t)(j - so_s[r]), had_s[r], pos_s[r]);
       }
     } else {
-      for (int64_t j = 4 * (int64_t)at; j < total; j += 4 * (int64_t)step)
-        pg_slots4(a, j, total, 0, R - 1, so, [&](int32_t r) { return had_s[r]; },
-                  [&](int32_t r) { return pos_s[r]; });
+      // a run of the slots for each wave
+      const int64_t waves = (int64_t)gridDim.x * W, w = (int64_t)blockIdx.x * W + wave;
+      const int64_t per = ((int64_t)total + 256 * waves - 1) / (256 * waves) * 256;
+      const int64_t j0 = w * per, j1 = min((int64_t)total, j0 + per);
+      if (j0 < j1) {
+        const int32_t ra = pg_bisect(0, R - 1, so, j0), rb = pg_bisect(ra, R - 1, so, j1 - 1);
+        for (int64_t j = j0 + 4 * lane; j < j1; j += 256)
+          pg_slots4(a, j, j1, ra, rb, so, [&](int32_t r) { return had_s[r]; },
+                    [&](int32_t r) { return pos_s[r]; });
+      }
     }
     for (uint32_t i = at; i < (uint32_t)given; i += step) {
       const int32_t r = pg_bisect(0, R - 1, [&](int32_t q) { return (int64_t)go_s[q]; }, i);

@@ -71,6 +71,7 @@ def test_resize_refusals():
         assert resize(**{name: None}) == EINVAL, name
     assert resize(slots=None) == EINVAL and resize(slots=None, cap=0) == OK
     assert resize(cap=-1) == EINVAL
+    assert resize(cap=2 ** 31 - 1024) == OK and resize(cap=2 ** 31 - 1023) == EUNS
     assert resize(ws=None) == EWS and resize(size=0) == EWS and resize(ws=FAKE + 4) == EINVAL
     for name in ("table", "offsets", "ring", "free"):
         assert resize(g=pages(**{name: None}), size=1 << 20) == EINVAL, name
