@@ -102,8 +102,11 @@ static certkv_status launch_paged_join(const PagedArgs& a, hipStream_t s) {
   constexpr int GR = kPgJoinThreads / (D / 4);
   const int M = a.tq * a.p.g.G;
   const int64_t U = (int64_t)a.p.lists * a.copies * (a.mode == kPgHeads ? 4 : 1);
-  // The partials of few rows are dealt out, of many taken row by row (as in attend.hip).
-  if (U * M < 8192)
+  // The partials of few rows, or of many pieces to a unit, are dealt out, others taken row by row.
+  // (In us, dealt and not: 8 units of 64 pieces, 4 rows 8 and 38; 256 units of 4 rows 4 and 4; 1024
+  // of 4 rows 9 and 5; 64 units of 48 rows 8 and 7.)
+  const int64_t chunks = a.most < a.parts ? a.most : a.parts;
+  if (U * M < 2048 || chunks >= 8 * (int64_t)a.p.lists * a.copies)
     CERTKV_LAUNCH("paged_join", (paged_join_kernel<D, GR>), dim3((unsigned)U, (unsigned)M),
                   dim3(kPgJoinThreads), 0, s, a);
   else
