@@ -580,7 +580,7 @@ template <int D>
 static certkv_status launch_page_adopt(const PageAdoptArgs& a, hipStream_t s) {
   const int64_t step = kPgThreads / (mx_row_bytes(a.p.format, D) / 16);
   const int64_t steps = (a.rows + step - 1) / step;
-  const dim3 grid((unsigned)(steps < 8 * 256 ? steps : 8 * 256));
+  const dim3 grid((unsigned)(steps < 4 * 256 ? steps : 4 * 256));
   switch (a.p.format) {
     case CERTKV_CACHE_MXFP8:
       CERTKV_LAUNCH("page_adopt", (page_adopt_kernel<D, D / 32>), grid, dim3(kPgThreads), 0, s, a);
