@@ -8,13 +8,22 @@
 //
 // Tiles of 32 rows, products and weights are those of attend.h: S^T = K Q^T and O^T += V^T P^T on
 // v_mfma_f32_16x16x32_bf16, weights in three bf16 parts against a reference that moves only on
-// overflow.  A workgroup has 16 or 32 query rows and four waves, which take a piece's tiles in
-// turn, each by itself, and are joined at the piece's end.
+// overflow.  A workgroup has 16 or 32 query rows; every wave takes tiles by itself, keys straight
+// into operands, values through its own LDS tile, and the waves of a unit are joined at a piece's
+// end.
 //
 // A page is a power of two of 16 rows or more, so that the 16 rows of half a tile are consecutive
-// rows of one page: their place is scalar arithmetic, and each half has buffer resources of its
-// own, which end with the list's last row (rows behind it, which may hold anything, are zero).
+// rows of one page, and their place is scalar arithmetic.  Rows of that page behind the list's
+// last are read with them: their scores are replaced and their values zero, whatever they hold.
 // The table's entries of 32 tiles of a wave are one load, half a tile's to each lane.
+//
+// Bounds (calls, the join of partials included): one token, the reads (32 layers, 3.36M rows of 128
+// dims, bf16: 1.72 GB in 267 us, 6.4 TB/s; 64 ragged sequences, 1.23 GB in 204, 6.0; 8 sequences
+// over 16 layers of mxfp8, 2.1 GB in 335, 6.2), but for mxfp4, the issue of its conversions and of
+// weights in three parts (3.36M rows, 457 MB in 92 us, 5.0 TB/s); short lists, latency (9 us);
+// drafts, issue with little of matrix and vector instructions under each other (48 query rows over
+// 378k rows of mxfp4: 50 us; over 3.0M rows 236, the vector unit 43 % busy, the matrix unit 25 %).
+// Tiles two ahead in registers instead of one are no faster (64 dims: 1 to 8 % slower).
 #pragma once
 
 #include <type_traits>
@@ -24,7 +33,9 @@
 
 namespace certkv {
 
-// Tiles between lists' places beside their rows': what a piece costs beside its tiles.
+// Tiles between lists' places beside their rows': what a piece costs beside its tiles.  (48 query
+// rows over 256 uneven units, 8: 53 us, 16: 46, 24: 46, 32: 48, 48: 54; one token over 1024 units,
+// 4: 336 us, 8: 332, 16: 457.)
 constexpr int pg_gap(int qt) { return qt == 2 ? 16 : 8; }
 constexpr int kPgMinTiles = 4;    // shortest chunk, and the unit of its length
 constexpr int kPgMaxTiles = kAtMaxKeys / kAtTile;  // longest, unless partials are short
@@ -34,7 +45,9 @@ constexpr int kPgMaxTiles = kAtMaxKeys / kAtTile;  // longest, unless partials a
 enum { kPgPiece, kPgWhole, kPgHeads };
 constexpr int pg_waves(int mode) { return mode == kPgWhole ? 8 : 4; }
 
-// Waves per SIMD that a kernel leaves registers for, which is also how many are launched.
+// Waves per SIMD that a kernel leaves registers for, which is also how many are launched.  (128
+// dims, 16 query rows, two waves and three: mxfp4 93 and 86 us, mxfp8 146 and 171, bf16 266 and 376:
+// they spill.)
 constexpr int pg_simd_waves(int format, int D, int qt) {
   return qt == 1 && (D == 64 || format == CERTKV_CACHE_MXFP4) ? 3 : 2;
 }
@@ -383,9 +396,10 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
       auto pages = [&](int n) {
         if ((n >> 5) == window) return;
         window = n >> 5;
-        const int row = (int)(lo + turn + KS * ((n & ~31) + (lane >> 1))) * kAtTile + (lane & 1) * 16;
+        // (of tiles behind the last, where 31 bits may not do)
+        const uint32_t row = (lo + turn + KS * ((n & ~31) + (lane >> 1))) * kAtTile + (lane & 1) * 16;
         ids = -1;
-        if (row < len) {
+        if (row < (uint32_t)len) {
           const int32_t id = WHOLE && n == 0 ? first_ids : p.table[(int64_t)r * p.max_pages + (row >> p.lp)];
           if ((uint32_t)id < (uint32_t)p.num_pages)
             ids = id;

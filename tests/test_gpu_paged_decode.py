@@ -99,6 +99,19 @@ def test_drafts_of_their_own_lengths(lists, H, per_head):
     assert bool((ck.decode_paged(spec, q, cache, tq, q_lens=torch.zeros_like(q_lens)) == 0).all())
 
 
+@pytest.mark.parametrize("H,room", [(2, 100), (2, LONG), (4, LONG)])
+def test_empty_lists(H, room):
+    spec = spec_of(2, [0, 0, 0], H=H, G=2, d=64)
+    gen = torch.Generator().manual_seed(1)
+    cache = _pages.make_cache(spec, [0, 0, 0], 16, "bf16", DEV, gen, max_pages=room // 16)
+    for tq in (1, 20):
+        bufs = ck.DecodeBuffers(spec, tq, DEV, with_lse=True, pages=cache)
+        bufs.out.fill_(7), bufs.lse.fill_(7)
+        out, lse = ck.decode_paged(spec, queries(spec, tq, gen), cache, tq, with_lse=True, bufs=bufs)
+        assert bool((out == 0).all()) and bool((lse == -float("inf")).all())
+    assert int(spec.status) == 0
+
+
 def test_numbers_of_queries_that_are_none():
     # fewer than none, more than there are
     lens = [40, 40]
