@@ -68,7 +68,9 @@ enum {
   CERTKV_EHIP = -6,         /* a HIP runtime call or launch failed         */
   CERTKV_ERANGE = -7        /* written to *dev_status by certkv_decode     */
                             /* when a packed segment holds more rows than */
-                            /* its max_rows bound allowed for              */
+                            /* its max_rows bound allowed for, and by the  */
+                            /* paged cache's calls for numbers that are    */
+                            /* none of its pages' and lists' (below)       */
 };
 
 enum { CERTKV_F32 = 0, CERTKV_BF16 = 1 };

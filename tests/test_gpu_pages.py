@@ -145,6 +145,22 @@ def test_numbers_that_are_none(room):
     assert all(0 <= b - a <= 32 for a, b in zip(off, off[1:]))
 
 
+@pytest.mark.parametrize("room", [100, 20_000])
+@pytest.mark.parametrize("offsets", [[0, 5, 3], [0, 5, 38]])
+def test_lengths_that_are_none(room, offsets):
+    # such a list holds none, or all that it can, and the call says so
+    spec = spec_of(B=2)
+    cache = tables(2, 6, 16, 2)
+    cache.offsets.copy_(torch.tensor(offsets, dtype=torch.int64, device=DEV))
+    change = torch.zeros(2, dtype=torch.int32, device=DEV)
+    ck.page_resize(spec, cache, change, bufs=ck.ResizeBuffers(cache, room, DEV))
+    assert int(spec.status) == ck.CERTKV_ERANGE
+    assert cache.offsets.tolist() == [0, 5, 5 if offsets[2] < 5 else 37]
+    spec.status.zero_()
+    ck.page_resize(spec, cache, change, bufs=ck.ResizeBuffers(cache, room, DEV))
+    assert int(spec.status) == 0
+
+
 def test_offsets_of_a_part():
     # lists whose first row is not row 0 (a layer's of many)
     spec = spec_of(B=3)
