@@ -192,7 +192,7 @@ __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
       const int64_t n = end - first;
       first = end;
       had[k] = (int32_t)(n < 0 ? 0 : n < most_rows ? n : most_rows);
-      refused |= n != had[k];  // (the caller's numbers)
+      if ((uint64_t)n > (uint64_t)most_rows) report_range(a.g);  // (the caller's numbers)
       will[k] = max((int64_t)had[k] + change, (int64_t)0);
       const int32_t held = (had[k] + mask) >> a.lp;
       const int64_t want = (will[k] + mask) >> a.lp;
