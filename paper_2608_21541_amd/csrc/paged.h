@@ -116,11 +116,12 @@ constexpr int kPgWeighed = 2048;  // lists at most
 __device__ __forceinline__ int pg_list_sequence(const PagedArgs& a, uint32_t r) {
   return (int)(a.p.per_head ? r / (uint32_t)a.p.g.H % (uint32_t)a.p.g.B : r);
 }
+__device__ __forceinline__ int pg_own(const PagedArgs& a, int n) { return min(max(n, 0), a.tq); }
 __device__ __forceinline__ int pg_queries(const PagedArgs& a, int b) {
-  return a.q_lens ? min(max(a.q_lens[b], 0), a.tq) : a.tq;
+  return a.q_lens ? pg_own(a, a.q_lens[b]) : a.tq;
 }
-__device__ __forceinline__ uint32_t pg_groups(const PagedArgs& a, int b) {
-  return (uint32_t)(pg_queries(a, b) * a.p.g.G + 31) >> 5;
+__device__ __forceinline__ uint32_t pg_groups(const PagedArgs& a, int own) {
+  return (uint32_t)(own * a.p.g.G + 31) >> 5;
 }
 // place_s[r]: the first tile of list r, for copies = 1; and, from the first workgroup, a.place.
 template <int NT>
@@ -133,7 +134,7 @@ __device__ __forceinline__ void pg_weigh(const PagedArgs& a, uint32_t* place_s, 
     const int r = r0 + tid;
     uint32_t x = 0;
     if (r < a.p.lists)
-      x = pg_groups(a, pg_list_sequence(a, r)) * (pg_up(off[r + 1] - base) - pg_up(off[r] - base) + a.gap);
+      x = pg_groups(a, pg_queries(a, pg_list_sequence(a, r))) * (pg_up(off[r + 1] - base) - pg_up(off[r] - base) + a.gap);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const uint32_t y = __shfl_up(x, d, 64);
@@ -313,7 +314,7 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
         const uint32_t span = pg_place(p1, r + 1, pg_gap(QT)) - pg_place(p0, r, pg_gap(QT));
         if (weighed) {
           place = copies * place_s[PLACES > 1 ? r : 0];
-          times = pg_groups(a, pg_list_sequence(a, r));
+          times = pg_groups(a, pg_queries(a, pg_list_sequence(a, r)));
         }
         if (!begun) copy = r0 > place ? (r0 - place) / span : 0;
         begun = true;
@@ -584,7 +585,9 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
 
       // The piece's partial: (maximum, sum, unnormalized output) of each query row, the waves
       // joined in LDS.
+      // (of the query rows that are the sequence's)
       const int64_t slot = (int64_t)x + u;
+      const int kept = WHOLE ? M : own * gm.G;
       int tid_j = tid;
       asm volatile("" : "+v"(tid_j));
 #pragma unroll
@@ -602,7 +605,7 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
         float* join = reinterpret_cast<float*>(lds);
         if constexpr (KS == 1) {
           const int row = row0 + qt * 16 + c;
-          if (row < M) {
+          if (row < kept) {
             const int64_t pr = (slot * 4 + wave) * mp + row;
             if (g == 0) a.part_ml[pr] = make_float2(acc.m[qt], l_row);
 #pragma unroll
@@ -629,7 +632,7 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
         for (int i = tid_j; i < 16 * (D / 4); i += NT) {
           const int rr = i / (D / 4), d4 = i % (D / 4);
           const int row = row0 + qt * 16 + rr;
-          if (row >= M) continue;
+          if (row >= kept) continue;
           float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
           for (int k = 0; k < KS; ++k) {

@@ -22,17 +22,31 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
   const int grp = threadIdx.x / C4, c4 = threadIdx.x % C4;
   const int row = blockIdx.y * RW + grp / S, sg = grp % S;
   const int M = a.tq * g.G;
+  int l, b, h;
+  if (p.per_head) {
+    h = (int)(r % (uint32_t)g.H), b = (int)(r / g.H % (uint32_t)g.B), l = (int)(r / g.H / g.B);
+  } else {
+    const uint32_t x = copy * four + head;
+    b = (int)r, l = (int)(x / (uint32_t)g.H), h = (int)(x % (uint32_t)g.H);
+  }
+  // (all asked for at once, what is not there in the offsets' place: latency)
+  const uint32_t* const places = a.place ? a.place : reinterpret_cast<const uint32_t*>(p.offsets);
+  const int32_t* const q_lens = a.q_lens ? a.q_lens : reinterpret_cast<const int32_t*>(p.offsets);
   const int64_t base = p.offsets[0], p0 = p.offsets[r] - base, p1 = p.offsets[r + 1] - base;
+  const int64_t rows = p.offsets[p.lists] - base;
+  const uint32_t place_r = places[r], place_all = places[p.lists];
+  const int32_t q_len = q_lens[b];
   const int len = min(page_rows(p, p0, p1), a.cover);
   if (p1 - p0 != len && blockIdx.y == 0 && threadIdx.x == 0) report_range(g);
   float m = kAtNone, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   uint32_t group = 0, groups = 1;
-  if (a.place) groups = pg_groups(a, pg_list_sequence(a, r)), group = (uint32_t)row >> 5;
-  if (row < M && len > 0 && group < groups) {
-    const PgCut cut = pg_cut(a, a.place ? a.place[p.lists] : pg_place(p.offsets[p.lists] - base, (uint32_t)p.lists, a.gap));
+  const int own = a.q_lens ? pg_own(a, q_len) : a.tq;
+  if (a.place) groups = pg_groups(a, own), group = (uint32_t)row >> 5;
+  if (row < own * g.G && len > 0) {  // (others have no partials)
+    const PgCut cut = pg_cut(a, a.place ? place_all : pg_place(rows, (uint32_t)p.lists, a.gap));
     const uint32_t span = pg_place(p1, r + 1, a.gap) - pg_place(p0, r, a.gap);
-    const uint32_t place = a.place ? a.place[r] : pg_place(p0, r, a.gap);
+    const uint32_t place = a.place ? place_r : pg_place(p0, r, a.gap);
     const uint32_t vs = (uint32_t)a.copies * place + (copy * groups + group) * span;
     // (of offsets that fall, places may lie behind the last chunk)
     const uint32_t s0 = min(vs / cut.tiles, (uint32_t)a.most - 1u);
@@ -44,12 +58,11 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
 #pragma unroll
       for (int i = 0; i < Q; ++i) {
         const int64_t pr = (((int64_t)s0 + u + min(i0 + i * S, nv - 1)) * four + head) * a.mp + row;
-        ml[i] = a.part_ml[pr];
+        ml[i] = i0 + i * S < nv ? a.part_ml[pr] : make_float2(kAtNone, 0.f);
         x[i] = reinterpret_cast<const float4*>(a.part_o + pr * D)[c4];
       }
 #pragma unroll
       for (int i = 0; i < Q; ++i) {
-        if (i0 + i * S >= nv) continue;
         const float mn = fmaxf(m, ml[i].x);
         const float e = __builtin_amdgcn_exp2f(m - mn);
         const float w = __builtin_amdgcn_exp2f(ml[i].x - mn);
@@ -87,13 +100,6 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
     m = mx;
   }
   if (row >= M) return;
-  int l, b, h;
-  if (p.per_head) {
-    h = (int)(r % (uint32_t)g.H), b = (int)(r / g.H % (uint32_t)g.B), l = (int)(r / g.H / g.B);
-  } else {
-    const uint32_t x = copy * four + head;
-    b = (int)r, l = (int)(x / (uint32_t)g.H), h = (int)(x % (uint32_t)g.H);
-  }
   pg_output(a, l, b, h, row, c4, D, o, m, L);
 }
 
