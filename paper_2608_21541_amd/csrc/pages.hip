@@ -5,7 +5,6 @@ namespace certkv {
 
 constexpr int kPgThreads = 256;
 constexpr int kPgScan = 1024;      // lists of a step of the scan
-constexpr int kPgSmallSlots = 16384;  // slots that the scan's own workgroup fills in
 
 // ---- tables and slots ---------------------------------------------------------
 //
@@ -109,6 +108,21 @@ __device__ __forceinline__ int32_t pg_bisect(int32_t lo, int32_t hi, F first, in
       hi = mid - 1;
   }
   return lo;
+}
+
+// The last list r < R with first(r) <= x, by a wave: 64 lists' ends to a step.
+template <typename F>
+__device__ __forceinline__ int32_t pg_find(int32_t R, F first, int64_t x, int lane) {
+  int32_t u = 0;
+  for (int32_t n = R;;) {
+    const int32_t step = (n + 63) / 64;
+    const int64_t i = (int64_t)u + (int64_t)lane * step + step - 1;
+    const bool past = i >= R || first((int32_t)i + 1) > x;
+    u += (int32_t)__popcll(__ballot(!past)) * step;
+    if (step == 1) break;
+    n = step;
+  }
+  return min(u, R - 1);
 }
 
 // Slots j .. j + 3 of those before `end`, from the lists' sums: so(r) the first of list r's,
@@ -307,18 +321,19 @@ __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
     const uint32_t total = (uint32_t)min(add_c, a.slot_capacity);
     const uint32_t at = (PART == 1 ? blockIdx.x : 0) * NT + tid, step = (PART == 1 ? gridDim.x : 1) * NT;
     const auto so = [&](int32_t i) { return (int64_t)so_s[i]; };
-    if constexpr (PART == 0) {
-      for (uint32_t j = at; j < total; j += step) {
-        const int32_t r = pg_bisect(0, R - 1, so, j);
-        a.slots[j] = pg_slot(a, r, had_s[r] + (int32_t)(j - so_s[r]), had_s[r], pos_s[r]);
+    if (PART == 0 && total <= NT) {  // (a row or few to a list: a slot to a lane)
+      if (at < total) {
+        const int32_t r = pg_bisect(0, R - 1, so, at);
+        a.slots[at] = pg_slot(a, r, had_s[r] + (int32_t)(at - so_s[r]), had_s[r], pos_s[r]);
       }
     } else {
       // a run of the slots for each wave
-      const int64_t waves = (int64_t)gridDim.x * W, w = (int64_t)blockIdx.x * W + wave;
+      const int64_t wgs = PART == 1 ? gridDim.x : 1, waves = wgs * W;
+      const int64_t w = (PART == 1 ? blockIdx.x : 0) * (int64_t)W + wave;
       const int64_t per = ((int64_t)total + 256 * waves - 1) / (256 * waves) * 256;
       const int64_t j0 = w * per, j1 = min((int64_t)total, j0 + per);
       if (j0 < j1) {
-        const int32_t ra = pg_bisect(0, R - 1, so, j0), rb = pg_bisect(ra, R - 1, so, j1 - 1);
+        const int32_t ra = pg_find(R, so, j0, lane), rb = pg_find(R, so, j1 - 1, lane);
         for (int64_t j = j0 + 4 * lane; j < j1; j += 256)
           pg_slots4(a, j, j1, ra, rb, so, [&](int32_t r) { return had_s[r]; },
                     [&](int32_t r) { return pos_s[r]; });
@@ -337,21 +352,6 @@ __global__ __launch_bounds__(kPgThreads) void page_sums_kernel(PageResizeArgs a,
                                                                const int64_t* free_state) {
   for (int32_t r = threadIdx.x; r <= a.lists; r += kPgThreads) a.offsets_out[r] = offsets[r];
   if (threadIdx.x < 2) a.free_out[threadIdx.x] = free_state[threadIdx.x];
-}
-
-// The last list r < R with first(r) <= x, by a wave: 64 lists' ends to a step.
-template <typename F>
-__device__ __forceinline__ int32_t pg_find(int32_t R, F first, int64_t x, int lane) {
-  int32_t u = 0;
-  for (int32_t n = R;;) {
-    const int32_t step = (n + 63) / 64;
-    const int64_t i = (int64_t)u + (int64_t)lane * step + step - 1;
-    const bool past = i >= R || first((int32_t)i + 1) > x;
-    u += (int32_t)__popcll(__ballot(!past)) * step;
-    if (step == 1) break;
-    n = step;
-  }
-  return min(u, R - 1);
 }
 
 // Slots, table entries and the pages given back, 64 at a time to a wave.
@@ -384,9 +384,18 @@ __global__ __launch_bounds__(kPgThreads) void page_slots_kernel(PageResizeArgs a
   }
 }
 
+// Slots that the scan's own workgroup fills in: in place more, where the sums of many workgroups
+// wait for a launch of their own.  (In us, one workgroup and many: 250 lists of 8 rows each 10.0 and
+// 9.9, of 16 12.2 and 9.6, of 64 16.5 and 9.2, in place 12.9 and 14.8; 1000 lists of 4 14.9 and 16.4,
+// of 8 17 and 16.3, of 16 19.8 and 16.6, in place 15.1 and 19.)
+static int64_t pg_small_slots(int32_t lists, bool in_place) {
+  return in_place ? 16384 : lists <= 256 ? 2048 : 8192;
+}
+
 certkv_status run_page_resize(const PageResizeArgs& a, hipStream_t s) {
-  if (a.lists <= kPgScan && a.slot_capacity <= kPgSmallSlots) {
-    if (a.lists <= 64 && a.slot_capacity <= 1024)
+  const bool in_place = a.offsets_out == a.offsets || a.free_out == a.free;
+  if (a.lists <= kPgScan && a.slot_capacity <= pg_small_slots(a.lists, in_place)) {
+    if (a.lists <= 64 && a.slot_capacity <= 256)
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<1, 1, 0>), dim3(1), dim3(64), 0, s, a);
     else if (a.lists <= 256 && a.slot_capacity <= 4096)
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<4, 1, 0>), dim3(1), dim3(256), 0, s, a);
@@ -396,7 +405,6 @@ certkv_status run_page_resize(const PageResizeArgs& a, hipStream_t s) {
   }
   if (a.lists <= kPgScan) {
     // (in place, the sums would be written while others read: they wait in the workspace)
-    const bool in_place = a.offsets_out == a.offsets || a.free_out == a.free;
     PageResizeArgs b = a;
     if (in_place) {
       b.offsets_out = reinterpret_cast<int64_t*>(a.ws);

@@ -41,7 +41,8 @@ def check_lists(cache, ref, table_too=True):
     assert len(set(held + free)) == len(held) + len(free)
 
 
-@pytest.mark.parametrize("room", [10_000, 60_000])  # filled in by the scan's workgroup, or not
+# filled in by the scan's workgroup, of one wave, four or sixteen, or by many
+@pytest.mark.parametrize("room", [200, 3000, 10_000, 60_000])
 @pytest.mark.parametrize("lists,page", [(1, 16), (2, 1024), (5, 16), (63, 32), (64, 16), (65, 64),
                                         (1023, 16), (1024, 128), (1025, 16), (3000, 32)])
 def test_steps_in_place(lists, page, room):
@@ -76,7 +77,8 @@ def test_steps_in_place(lists, page, room):
     assert refused or lists < 60
 
 
-@pytest.mark.parametrize("lists,room", [(40, 500), (40, 20_000), (1500, 20_000)])
+@pytest.mark.parametrize("lists,room", [(40, 200), (40, 500), (40, 20_000), (300, 5000), (300, 9000),
+                                        (1500, 20_000)])
 def test_a_step_beside_the_present_one(lists, room):
     # other offsets and free are written, the cache's own left; the same call gives the same again
     spec = spec_of(B=lists)
