@@ -4,7 +4,8 @@
 namespace certkv {
 
 constexpr int kPgThreads = 256;
-constexpr int kPgScan = 1024;      // lists of a step of the scan
+constexpr int kPgScan = 2048;      // lists that a workgroup scans by itself
+constexpr int kPgBlock = 1024;     // of more, lists to a workgroup
 
 // ---- tables and slots ---------------------------------------------------------
 //
@@ -16,34 +17,52 @@ constexpr int kPgScan = 1024;      // lists of a step of the scan
 // their number before it, and the places taken have no gap.  (Refused for its own length: need
 // counts as 0.)
 //
-// The sums are a scan of the lists, a workgroup's; the slots and table entries follow from them.
-// Up to 1024 lists one launch does both: few slots by the scan's own workgroup, many by workgroups
-// that each scan all lists and take a share of the slots.  More lists: a second launch.
+// The sums are a scan of the lists; the slots and table entries follow from them.  Up to 2048 lists
+// one launch does both: few slots by one workgroup, many by workgroups that each scan all lists and
+// take a share of the slots.  More lists: the sums of blocks of them, then a scan of each block
+// behind those, then the slots.
 // Bound by latency: a launch, loads in turn (offsets, then entries of the table or ring) and the
 // scan.  64 lists that get a row each 3.5 us (a call 7.0, the host's); 1024 lists of which an
 // eighth each end, begin, grow by four rows and lose three, 371k slots 11 us, in two launches 15;
-// 256 empty lists that get 3.36M rows 14 us, in two launches 22, the scan alone 6.
+// 256 empty lists that get 3.36M rows 14 us, in two launches 22, the scan alone 6; lists that get a
+// row each, with events, 2048 of them 22 us (three launches 33), 16384 30, 65536 32 (a scan of all by
+// one workgroup 102 and 357).
 
-// What the second part needs of each list, in the workspace or LDS.
+// What the second part needs of each list, in the workspace or LDS; and, of many lists, the sums of
+// each block of kPgBlock.
 struct PgLists {
   int32_t* had;
   int32_t* pos;   // place of the ring of its first new page, or -1: refused
   int32_t* keep;  // pages that are left to a list that gives some
   int32_t* give;  // [lists + 1] sums of the pages given
-  int32_t* tail;  // place of the ring where they go, and how many
+  int32_t* tail;  // place of the ring where they go, how many, first free place, free pages
+  int64_t* base;  // offsets[0]
+  int32_t* need_b;   // of a block: pages needed and given, the last place of the ring taken,
+  int32_t* give_b;
+  int32_t* taken_b;
+  int64_t* add_b;    // rows appended, and rows after the step
+  int64_t* len_b;
 };
 constexpr int64_t pg_pad(int64_t n) { return (n + 63) & ~(int64_t)63; }
+__host__ __device__ constexpr int64_t pg_blocks(int64_t lists) { return (lists + kPgBlock - 1) / kPgBlock; }
 __host__ __device__ static inline PgLists pg_lists(int32_t* ws, int64_t lists) {
+  const int64_t nb = pg_pad(pg_blocks(lists));
   PgLists x;
   x.tail = ws;
+  x.base = reinterpret_cast<int64_t*>(ws + 8);
   x.had = ws + 64;
   x.pos = x.had + pg_pad(lists);
   x.keep = x.pos + pg_pad(lists);
   x.give = x.keep + pg_pad(lists);
+  x.need_b = x.give + pg_pad(lists + 1);
+  x.give_b = x.need_b + nb;
+  x.taken_b = x.give_b + nb;
+  x.add_b = reinterpret_cast<int64_t*>(x.taken_b + nb);
+  x.len_b = x.add_b + nb;
   return x;
 }
 size_t page_resize_ws(int64_t lists) {
-  return (size_t)(64 + 3 * pg_pad(lists) + pg_pad(lists + 1)) * sizeof(int32_t);
+  return (size_t)(64 + 3 * pg_pad(lists) + pg_pad(lists + 1) + 7 * pg_pad(pg_blocks(lists))) * sizeof(int32_t);
 }
 
 // x of the lane that a data-parallel step takes it from, 0 where there is none.
@@ -165,8 +184,71 @@ __device__ __forceinline__ void pg_slots4(const PageResizeArgs& a, int64_t j, in
   }
 }
 
+// What a list of rows [first, end) of the offsets asks for.
+struct PgStep {
+  int32_t had, need, give, add;
+  int64_t will;
+  bool fits;
+};
+__device__ __forceinline__ PgStep pg_step(const PageResizeArgs& a, int64_t first, int64_t end, int32_t change) {
+  const int32_t N = a.num_pages, mask = (1 << a.lp) - 1;
+  const int64_t most_rows = (int64_t)a.max_pages << a.lp, n = end - first;
+  PgStep x;
+  x.had = (int32_t)(n < 0 ? 0 : n < most_rows ? n : most_rows);
+  x.will = max((int64_t)x.had + change, (int64_t)0);
+  const int32_t held = (x.had + mask) >> a.lp;
+  const int64_t want = (x.will + mask) >> a.lp;
+  x.fits = want <= a.max_pages;
+  x.need = want > held && x.fits ? (int32_t)min(want - held, (int64_t)N + 1) : 0;
+  x.give = want < held ? min(held - (int32_t)want, N + 1) : 0;
+  x.add = change > 0 ? change : 0;
+  return x;
+}
+
+// The sum of a workgroup's values, to all of them.  part: W words of LDS.
+template <int W, typename T, typename F>
+__device__ __forceinline__ T pg_total(T x, F add, T* part) {
+  x = pg_wave_scan(x, add);
+  if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = x;
+  __syncthreads();
+  T t = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) t = add(t, part[w]);
+  __syncthreads();
+  return t;
+}
+
+// Many lists: the sums of a block of them.
+__global__ __launch_bounds__(kPgThreads) void page_blocks_kernel(PageResizeArgs a) {
+  __shared__ int32_t part[kPgThreads / 64];
+  __shared__ int64_t part64[kPgThreads / 64];
+  const int32_t N = a.num_pages;
+  const PgLists ws = pg_lists(a.ws, a.lists);
+  const auto sat = [N](int32_t x, int32_t y) { return min(x + y, N + 1); };
+  int32_t need = 0, give = 0;
+  int64_t add = 0;
+#pragma unroll
+  for (int k = 0; k < kPgBlock / kPgThreads; ++k) {
+    const int64_t r = (int64_t)blockIdx.x * kPgBlock + k * kPgThreads + threadIdx.x;
+    if (r >= a.lists) continue;
+    const PgStep x = pg_step(a, a.offsets[r], a.offsets[r + 1], a.change[r]);
+    need = sat(need, x.need);
+    give = sat(give, x.give);
+    add += x.add;
+  }
+  need = pg_total<kPgThreads / 64>(need, sat, part);
+  give = pg_total<kPgThreads / 64>(give, sat, part);
+  add = pg_total<kPgThreads / 64>(add, [](int64_t x, int64_t y) { return x + y; }, part64);
+  if (threadIdx.x == 0) {
+    ws.need_b[blockIdx.x] = need;
+    ws.give_b[blockIdx.x] = give;
+    ws.add_b[blockIdx.x] = add;
+  }
+}
+
 // W waves scan K lists a lane at a time.  PART: 0, this is the only workgroup and does all; 1, every
-// workgroup scans, the first writes the sums; 2, the sums alone, for page_slots_kernel.
+// workgroup scans, the first writes the sums; 2, each scans a block behind those of
+// page_blocks_kernel, for page_slots_kernel.
 template <int W, int K, int PART>
 __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
   constexpr int NT = 64 * W, STEP = NT * K, HELD = PART == 2 ? 1 : STEP;
@@ -175,21 +257,32 @@ __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
   __shared__ int32_t had_s[HELD], pos_s[HELD], keep_s[HELD], go_s[HELD + 1], so_s[HELD + 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t R = a.lists, N = a.num_pages, mask = (1 << a.lp) - 1;
-  const int64_t most_rows = (int64_t)a.max_pages << a.lp;
   const int64_t base = a.offsets[0];
   const int32_t head = (int32_t)((uint64_t)a.free[0] % (uint64_t)N);
   const int64_t free_pages = a.free[1];
   const int32_t count = (int32_t)(free_pages < 0 ? 0 : free_pages < N ? free_pages : N);
   const PgLists ws = pg_lists(a.ws, R);
   const bool tells = PART != 1 || blockIdx.x == 0;
+  const int32_t begin = PART == 2 ? (int32_t)blockIdx.x * STEP : 0;
   // sums of pages stop at N + 1, more than there are
   const auto sat = [N](int32_t x, int32_t y) { return min(x + y, N + 1); };
   const auto sum = [](int64_t x, int64_t y) { return x + y; };
   int32_t need_c = 0, give_c = 0;
-  int64_t add_c = 0, len_c = 0, old_end = base;
+  int64_t add_c = 0, len_c = 0, old_end = PART == 2 ? a.offsets[begin] : base;
   bool refused = free_pages != count;
   if (tid == 0) taken_s = 0;
-  for (int32_t r0 = 0; r0 < R; r0 += STEP) {
+  if constexpr (PART == 2) {
+    static_assert(STEP == kPgBlock, "a workgroup's lists");
+    for (int32_t i = tid; i < (int32_t)blockIdx.x; i += NT) {
+      need_c = sat(need_c, ws.need_b[i]);
+      give_c = sat(give_c, ws.give_b[i]);
+      add_c += ws.add_b[i];
+    }
+    need_c = pg_total<W>(need_c, sat, need_s);
+    give_c = pg_total<W>(give_c, sat, give_s);
+    add_c = pg_total<W>(add_c, sum, add_s);
+  }
+  for (int32_t r0 = begin; r0 < (PART == 2 ? min(R, begin + STEP) : R); r0 += STEP) {
     const int32_t r = r0 + tid * K;
     int32_t had[K], need[K], give[K], add[K];
     int64_t will[K];
@@ -202,18 +295,11 @@ __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
     for (int k = 0; k < K; ++k) {
       const bool in = r + k < R;
       const int64_t end = in ? a.offsets[r + k + 1] : first;
-      const int32_t change = in ? a.change[r + k] : 0;
-      const int64_t n = end - first;
+      const PgStep x = pg_step(a, first, end, in ? a.change[r + k] : 0);
+      if (end - first != x.had) report_range(a.g);  // (the caller's numbers)
       first = end;
-      had[k] = (int32_t)(n < 0 ? 0 : n < most_rows ? n : most_rows);
-      if ((uint64_t)n > (uint64_t)most_rows) report_range(a.g);  // (the caller's numbers)
-      will[k] = max((int64_t)had[k] + change, (int64_t)0);
-      const int32_t held = (had[k] + mask) >> a.lp;
-      const int64_t want = (will[k] + mask) >> a.lp;
-      fits[k] = want <= a.max_pages;
-      need[k] = want > held && fits[k] ? (int32_t)min(want - held, (int64_t)N + 1) : 0;
-      give[k] = want < held ? min(held - (int32_t)want, N + 1) : 0;
-      add[k] = change > 0 ? change : 0;
+      had[k] = x.had, will[k] = x.will, fits[k] = x.fits;
+      need[k] = x.need, give[k] = x.give, add[k] = x.add;
       need_t = sat(need_t, need[k]);
       give_t = sat(give_t, give[k]);
       add_t += add[k];
@@ -277,7 +363,7 @@ __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
       give_e = sat(give_e, give[k]);
       if (r + k >= R) continue;
       if (tells) {
-        a.offsets_out[r + k + 1] = base + len_b;
+        if (PART != 2) a.offsets_out[r + k + 1] = base + len_b;
         a.slot_offsets[r + k + 1] = add_e;
       }
       const int32_t keep = (int32_t)min((will[k] + mask) >> a.lp, (int64_t)a.max_pages);
@@ -300,7 +386,20 @@ __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
   const int32_t taken = taken_s;
   const int32_t given = min(give_c, N - count);  // (more: the ring's pages and the lists' overlap)
   const int32_t tail = (int32_t)((uint32_t)(head + count) % (uint32_t)N);
-  if (tid == 0) {
+  if (PART == 2 && tid == 0) {
+    ws.taken_b[blockIdx.x] = taken;
+    ws.len_b[blockIdx.x] = len_c;
+    if (blockIdx.x == 0) {
+      a.slot_offsets[0] = 0;
+      ws.give[0] = 0;
+    }
+    if (blockIdx.x == gridDim.x - 1) {
+      ws.tail[0] = tail, ws.tail[1] = given;
+      ws.tail[2] = head, ws.tail[3] = count;
+      ws.base[0] = base;
+      if (give_c > given) report_range(a.g);
+    }
+  } else if (tid == 0) {
     if (tells) {
       a.offsets_out[0] = base;
       a.slot_offsets[0] = 0;
@@ -308,13 +407,7 @@ __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
       a.free_out[1] = count - taken + given;
       if (give_c > given) report_range(a.g);
     }
-    if constexpr (PART != 2) {
-      go_s[0] = so_s[0] = 0;
-    } else {
-      ws.give[0] = 0;
-      ws.tail[0] = tail;
-      ws.tail[1] = given;
-    }
+    go_s[0] = so_s[0] = 0;
   }
   if constexpr (PART != 2) {
     __syncthreads();
@@ -354,9 +447,60 @@ __global__ __launch_bounds__(kPgThreads) void page_sums_kernel(PageResizeArgs a,
   if (threadIdx.x < 2) a.free_out[threadIdx.x] = free_state[threadIdx.x];
 }
 
-// Slots, table entries and the pages given back, 64 at a time to a wave.
+// The new offsets of a block of lists, behind its sums' (and the ring's new state).
+__device__ __forceinline__ void pg_offsets(const PageResizeArgs& a, const PgLists& ws, int32_t block,
+                                           int64_t* part) {
+  constexpr int W = kPgThreads / 64, K = kPgBlock / kPgThreads;
+  const int tid = threadIdx.x;
+  const auto sum = [](int64_t x, int64_t y) { return x + y; };
+  const int64_t base = ws.base[0];
+  if (block == 0) {
+    int64_t taken = 0;
+    for (int32_t i = tid; i < (int32_t)pg_blocks(a.lists); i += kPgThreads)
+      taken = max(taken, (int64_t)ws.taken_b[i]);
+    taken = pg_total<W>(taken, [](int64_t x, int64_t y) { return max(x, y); }, part);
+    if (tid == 0) {
+      a.offsets_out[0] = base;
+      a.free_out[0] = (uint32_t)(ws.tail[2] + (int32_t)taken) % (uint32_t)a.num_pages;
+      a.free_out[1] = ws.tail[3] - taken + ws.tail[1];
+    }
+  }
+  int64_t before = base, len[K], mine = 0;
+  const int32_t r = block * kPgBlock + tid * K;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    len[k] = 0;
+    if (r + k < a.lists) {
+      const int32_t had = ws.had[r + k];
+      len[k] = ws.pos[r + k] < 0 ? had : max((int64_t)had + a.change[r + k], (int64_t)0);
+    }
+    mine += len[k];
+  }
+  int64_t s = 0;
+  for (int32_t i = tid; i < block; i += kPgThreads) s += ws.len_b[i];
+  before += pg_total<W>(s, sum, part);
+  s = pg_wave_scan(mine, sum);
+  if ((tid & 63) == 63) part[tid >> 6] = s;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < W; ++w)
+    if (w < tid >> 6) before += part[w];
+  __syncthreads();
+  before += s - mine;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    before += len[k];
+    if (r + k < a.lists) a.offsets_out[r + k + 1] = before;
+  }
+}
+
+// Offsets, slots, table entries and the pages given back, the slots 256 at a time to a wave.
 __global__ __launch_bounds__(kPgThreads) void page_slots_kernel(PageResizeArgs a) {
   const PgLists ws = pg_lists(a.ws, a.lists);
+  __shared__ int64_t part[kPgThreads / 64];
+  // (by the last workgroups, whose share of few slots is none)
+  for (int64_t i = (int64_t)gridDim.x - 1 - blockIdx.x; i < pg_blocks(a.lists); i += gridDim.x)
+    pg_offsets(a, ws, (int32_t)i, part);
   const int lane = threadIdx.x & 63;
   const int64_t wave = (int64_t)blockIdx.x * (kPgThreads / 64) + (threadIdx.x >> 6);
   const int64_t waves = (int64_t)gridDim.x * (kPgThreads / 64);
@@ -394,7 +538,7 @@ static int64_t pg_small_slots(int32_t lists, bool in_place) {
 
 certkv_status run_page_resize(const PageResizeArgs& a, hipStream_t s) {
   const bool in_place = a.offsets_out == a.offsets || a.free_out == a.free;
-  if (a.lists <= kPgScan && a.slot_capacity <= pg_small_slots(a.lists, in_place)) {
+  if (a.lists <= 1024 && a.slot_capacity <= pg_small_slots(a.lists, in_place)) {
     if (a.lists <= 64 && a.slot_capacity <= 256)
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<1, 1, 0>), dim3(1), dim3(64), 0, s, a);
     else if (a.lists <= 256 && a.slot_capacity <= 4096)
@@ -414,14 +558,18 @@ certkv_status run_page_resize(const PageResizeArgs& a, hipStream_t s) {
     const dim3 grid((unsigned)(wgs < 4 * 256 ? wgs : 4 * 256));
     if (a.lists <= 256)
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<4, 1, 1>), grid, dim3(256), 0, s, b);
-    else
+    else if (a.lists <= 1024)
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<4, 4, 1>), grid, dim3(256), 0, s, b);
+    else
+      CERTKV_LAUNCH("page_resize", (page_resize_kernel<8, 4, 1>), grid, dim3(512), 0, s, b);
     if (in_place)
       CERTKV_LAUNCH("page_sums", page_sums_kernel, dim3(1), dim3(kPgThreads), 0, s, a, b.offsets_out,
                     b.free_out);
     return CERTKV_OK;
   }
-  CERTKV_LAUNCH("page_resize", (page_resize_kernel<16, 4, 2>), dim3(1), dim3(1024), 0, s, a);
+  const dim3 blocks((unsigned)pg_blocks(a.lists));
+  CERTKV_LAUNCH("page_blocks", page_blocks_kernel, blocks, dim3(kPgThreads), 0, s, a);
+  CERTKV_LAUNCH("page_resize", (page_resize_kernel<16, 1, 2>), blocks, dim3(1024), 0, s, a);
   CERTKV_LAUNCH("page_slots", page_slots_kernel, dim3(8 * 256), dim3(kPgThreads), 0, s, a);
   return CERTKV_OK;
 }

@@ -44,7 +44,7 @@ def check_lists(cache, ref, table_too=True):
 # filled in by the scan's workgroup, of one wave, four or sixteen, or by many
 @pytest.mark.parametrize("room", [200, 3000, 10_000, 60_000])
 @pytest.mark.parametrize("lists,page", [(1, 16), (2, 1024), (5, 16), (63, 32), (64, 16), (65, 64),
-                                        (1023, 16), (1024, 128), (1025, 16), (3000, 32)])
+                                        (1023, 16), (1024, 128), (1025, 16), (3000, 32), (7169, 16)])
 def test_steps_in_place(lists, page, room):
     rng = random.Random(lists * 7 + page)
     most = 9 if page < 1024 else 3
@@ -100,6 +100,43 @@ def test_a_step_beside_the_present_one(lists, room):
         assert torch.equal(cache.offsets, offsets) and torch.equal(cache.free, free)
     cache.offsets, cache.free = into
     check_lists(cache, ref)
+
+
+@pytest.mark.parametrize("lists", [1025, 300_000])
+def test_many_lists(lists):
+    # of numbers of rows that repeat, the last ones refused
+    page, most, per = 16, 3, torch.tensor([1, 17, 0, 33, 48, 16], device=DEV)
+    spec = spec_of(B=lists)
+    change = per.repeat(lists // 6 + 1)[:lists].int()
+    need = (change.long() + 15) // 16
+    have = int(need.sum()) - 5
+    cache = tables(lists, have, page, most)
+    cache.ring.copy_(torch.randperm(have, device=DEV))
+    cache.free[0] = 77
+    bufs = ck.ResizeBuffers(cache, int(change.sum()), DEV)
+    taken = need.cumsum(0)
+    fits = (need == 0) | (taken <= have)
+    slots, so = ck.page_resize(spec, cache, change, bufs=bufs)
+    assert int(spec.status) == ck.CERTKV_ERANGE
+    kept = torch.where(fits, change.long(), 0)
+    assert torch.equal(cache.offsets[1:], kept.cumsum(0)) and int(cache.offsets[0]) == 0
+    assert torch.equal(so[1:], change.long().cumsum(0)) and int(so[0]) == 0
+    last = int(taken[fits].max())
+    assert cache.free.tolist() == [(77 + last) % have, have - last]
+    r = torch.repeat_interleave(torch.arange(lists, device=DEV), change.long())
+    row = torch.arange(len(slots), device=DEV) - so[:-1][r]
+    place = (taken - need)[r] + row // page
+    want = cache.ring[(77 + place) % have].long() * page + row % page
+    assert torch.equal(slots.long(), torch.where(fits[r], want, -1))
+    # and all dropped again: pages go back in the lists' order
+    ring = cache.ring.clone()
+    held = cache.table[(torch.arange(most, device=DEV) < (need * fits)[:, None])]
+    spec.status.zero_()
+    ck.page_resize(spec, cache, torch.full_like(change, DROP), bufs=bufs)
+    assert int(spec.status) == 0 and not bool(cache.offsets.any())
+    at = (77 + have + torch.arange(last, device=DEV)) % have
+    ring[at] = held
+    assert torch.equal(cache.ring, ring) and cache.free.tolist() == [(77 + last) % have, have]
 
 
 def test_room_for_no_slot_and_for_some():

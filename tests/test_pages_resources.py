@@ -13,6 +13,7 @@ from test_kernel_resources import _device_asm, _symbols
 
 # (source, kernel symbol prefix, largest VGPR count, scratch bytes a lane at most)
 KERNELS = [("pages.hip", "_ZN6certkv18page_resize_kernelI", 128, 0),
+           ("pages.hip", "_ZN6certkv18page_blocks_kernelE", 64, 0),
            ("pages.hip", "_ZN6certkv17page_slots_kernelE", 64, 0),
            ("pages.hip", "_ZN6certkv17page_write_kernelI", 64, 0),
            ("pages.hip", "_ZN6certkv17page_adopt_kernelI", 64, 0),
