@@ -554,7 +554,8 @@ certkv_status run_page_resize(const PageResizeArgs& a, hipStream_t s) {
       b.offsets_out = reinterpret_cast<int64_t*>(a.ws);
       b.free_out = b.offsets_out + a.lists + 1;
     }
-    const int64_t wgs = (a.slot_capacity + 1023) / 1024;
+    // (room for no slot, as where lists only shrink: the sums and the pages given back all the same)
+    const int64_t wgs = a.slot_capacity < 1024 ? 1 : (a.slot_capacity + 1023) / 1024;
     const dim3 grid((unsigned)(wgs < 4 * 256 ? wgs : 4 * 256));
     if (a.lists <= 256)
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<4, 1, 1>), grid, dim3(256), 0, s, b);
