@@ -615,9 +615,12 @@ certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* page
  *                    *dev_status and its rows past the bound are left out
  * Rows are summed in chunks as in certkv_decode; the problem's dtypes are
  * CERTKV_BF16, the queries'.  Tiles of 32 rows of all units, by the lists' bounds or
- * the pool's pages, must be fewer than 2^31 (else CERTKV_EUNSUPPORTED).  The workspace
- * is certkv_decode_paged_workspace_size(p, pages, tq, max_rows) bytes, 256-byte
- * aligned. */
+ * the pool's pages, must be fewer than 2^31 (else CERTKV_EUNSUPPORTED).  Lists that
+ * share pages may have more rows than the pool.  Where the tiles that they have (a
+ * unit's with up to 16 more; with q_lens, once for every 32 query rows of a sequence)
+ * are 2^31 - 1 or more, the device stores CERTKV_ERANGE and no query sees anything (out = 0,
+ * lse = -infinity).  The workspace is certkv_decode_paged_workspace_size(p, pages, tq,
+ * max_rows) bytes, 256-byte aligned. */
 size_t certkv_decode_paged_workspace_size(const certkv_problem* p, const certkv_pages* pages,
                                           int32_t tq, int32_t max_rows);
 certkv_status certkv_decode_paged(const certkv_problem* p, certkv_tensor q_new, int32_t tq,

@@ -30,6 +30,7 @@
 
 #include "attend.h"
 #include "pages.h"
+#include "places.h"
 
 namespace certkv {
 
@@ -37,8 +38,7 @@ namespace certkv {
 // rows over 256 uneven units, 8: 53 us, 16: 46, 24: 46, 32: 48, 48: 54; one token over 1024 units,
 // 4: 336 us, 8: 332, 16: 457.)
 constexpr int pg_gap(int qt) { return qt == 2 ? 16 : 8; }
-constexpr int kPgMinTiles = 4;    // shortest chunk, and the unit of its length
-constexpr int kPgMaxTiles = kAtMaxKeys / kAtTile;  // longest, unless partials are short
+static_assert(kPgMaxTiles == kAtMaxKeys / kAtTile, "the longest chunk is the packed cache's");
 
 // What a workgroup has: a piece of a unit, whose tiles its waves take in turn; whole units; or the
 // same piece of four heads' units, a head for each wave.
@@ -89,24 +89,9 @@ certkv_status run_paged_bf16(const PagedArgs& a, int shape, hipStream_t s);   //
 certkv_status run_paged_mxfp8(const PagedArgs& a, int shape, hipStream_t s);
 certkv_status run_paged_mxfp4(const PagedArgs& a, int shape, hipStream_t s);
 
-// The units in one order (a list's copies one after another), each at a place, in tiles, that
-// follows from its list's first row alone; chunks of equal length are cut from it.
-struct PgCut {
-  uint32_t tiles, total;        // of a chunk, of all
-};
-__device__ __forceinline__ uint32_t pg_up(int64_t rows) { return (uint32_t)((uint64_t)(rows + 31) >> 5); }
-// The first tile of list r, for copies = 1.
-__device__ __forceinline__ uint32_t pg_place(int64_t rows_before, uint32_t r, int gap) {
-  return pg_up(rows_before) + r * (uint32_t)gap;
-}
+// The chunks of a call whose lists have `tiles` tiles, for one copy.
 __device__ __forceinline__ PgCut pg_cut(const PagedArgs& a, uint32_t tiles) {
-  const uint32_t total = (uint32_t)a.copies * tiles;
-  uint32_t k = (total + (uint32_t)a.parts - 1u) / (uint32_t)a.parts;
-  k = min(max(k, (uint32_t)kPgMinTiles), (uint32_t)kPgMaxTiles);
-  // (more rows than the caller's bound or the pool allow for, as with pages that lists share:
-  // longer chunks, so that the partials stay within the workspace)
-  if (total > (uint64_t)a.most * k) k = (total + (uint32_t)a.most - 1u) / (uint32_t)a.most;
-  return PgCut{(k + kPgMinTiles - 1u) / kPgMinTiles * kPgMinTiles, total};
+  return pg_cut((uint32_t)a.copies, tiles, (uint32_t)a.parts, (uint32_t)a.most);
 }
 
 // Where sequences have queries of their own number, and more than a workgroup holds, the groups of
@@ -124,6 +109,7 @@ __device__ __forceinline__ uint32_t pg_groups(const PagedArgs& a, int own) {
   return (uint32_t)(own * a.p.g.G + 31) >> 5;
 }
 // place_s[r]: the first tile of list r, for copies = 1; and, from the first workgroup, a.place.
+// (Sums stop at kPgMostTiles.)
 template <int NT>
 __device__ __forceinline__ void pg_weigh(const PagedArgs& a, uint32_t* place_s, uint32_t* sum_s) {
   const int tid = threadIdx.x;
@@ -133,21 +119,24 @@ __device__ __forceinline__ void pg_weigh(const PagedArgs& a, uint32_t* place_s, 
   for (int r0 = 0; r0 < a.p.lists; r0 += NT) {
     const int r = r0 + tid;
     uint32_t x = 0;
-    if (r < a.p.lists)
-      x = pg_groups(a, pg_queries(a, pg_list_sequence(a, r))) * (pg_up(off[r + 1] - base) - pg_up(off[r] - base) + a.gap);
+    if (r < a.p.lists) {
+      const uint64_t n = (uint64_t)pg_groups(a, pg_queries(a, pg_list_sequence(a, r))) *
+                         (pg_up(off[r + 1] - base) - pg_up(off[r] - base) + a.gap);
+      x = (uint32_t)min(n, kPgMostTiles);
+    }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const uint32_t y = __shfl_up(x, d, 64);
-      if ((tid & 63) >= d) x += y;
+      if ((tid & 63) >= d) x = pg_add(x, y);
     }
     if ((tid & 63) == 63) sum_s[tid >> 6] = x;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) {
-      if (w < tid >> 6) x += sum_s[w];
+      if (w < tid >> 6) x = pg_add(x, sum_s[w]);
     }
-    x += before;
-    for (int w = 0; w < NT / 64; ++w) before += sum_s[w];
+    x = pg_add(x, before);
+    for (int w = 0; w < NT / 64; ++w) before = pg_add(before, sum_s[w]);
     if (r < a.p.lists) {
       place_s[r + 1] = x;
       if (blockIdx.x == 0) a.place[r + 1] = x;
@@ -277,8 +266,8 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
   uint16_t* const vt = lds + wave * AtTile<D>::V;
   // The units' pieces: of the chunks that the workgroup takes, or the whole units.
   PgOffsets off(p.offsets, WHOLE ? 0 : p.lists, lane);
-  const PgCut cut = WHOLE ? PgCut{1, 0}
-                          : pg_cut(a, weighed ? place_s[PLACES > 1 ? p.lists : 0] : pg_place(off.rows, off.R, pg_gap(QT)));
+  const PgCut cut = WHOLE ? PgCut{1, 0, true}
+                          : pg_cut(a, weighed ? place_s[PLACES > 1 ? p.lists : 0] : pg_tiles(off.rows, off.R, pg_gap(QT)));
   const uint32_t nch = WHOLE ? (uint32_t)p.lists * copies : (cut.total + cut.tiles - 1) / cut.tiles;
   for (uint32_t x = x0; x < nch; x = WHOLE ? nch : x + xstep) {
     const uint32_t r0 = x * cut.tiles, r1 = min(cut.total, r0 + cut.tiles);

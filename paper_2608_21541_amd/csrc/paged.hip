@@ -37,14 +37,14 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
   const uint32_t place_r = places[r], place_all = places[p.lists];
   const int32_t q_len = q_lens[b];
   const int len = min(page_rows(p, p0, p1), a.cover);
-  if (p1 - p0 != len && blockIdx.y == 0 && threadIdx.x == 0) report_range(g);
+  const PgCut cut = pg_cut(a, a.place ? place_all : pg_tiles(rows, (uint32_t)p.lists, a.gap));
+  if ((p1 - p0 != len || !cut.fits) && blockIdx.y == 0 && threadIdx.x == 0) report_range(g);
   float m = kAtNone, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   uint32_t group = 0, groups = 1;
   const int own = a.q_lens ? pg_own(a, q_len) : a.tq;
   if (a.place) groups = pg_groups(a, own), group = (uint32_t)row >> 5;
-  if (row < own * g.G && len > 0) {  // (others have no partials)
-    const PgCut cut = pg_cut(a, a.place ? place_all : pg_place(rows, (uint32_t)p.lists, a.gap));
+  if (row < own * g.G && len > 0 && cut.fits) {  // (others have no partials)
     const uint32_t span = pg_place(p1, r + 1, a.gap) - pg_place(p0, r, a.gap);
     const uint32_t place = a.place ? place_r : pg_place(p0, r, a.gap);
     const uint32_t vs = (uint32_t)a.copies * place + (copy * groups + group) * span;
