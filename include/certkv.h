@@ -607,7 +607,9 @@ certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* page
  * queries' own tokens: query t < n sees rows j <= len - n + t, len the rows of the
  * unit's list.  A row that a query does not see has no part in its output, whatever
  * it holds, and what lies behind a list's last row is not read.  A query that sees
- * nothing (t >= n, or len - n + t < 0) is out = 0, lse = -infinity.
+ * nothing (t >= n, or len - n + t < 0) is out = 0, lse = -infinity.  Offsets that fall
+ * store CERTKV_ERANGE, their lists' queries see nothing, and what the other lists'
+ * outputs hold is not defined.
  *   q_new, out, lse  as certkv_decode; tq * G <= 512
  *   q_lens           optional [B] int32, device
  *   max_rows         bound on the rows of any list, or 0 for max_pages * page; it

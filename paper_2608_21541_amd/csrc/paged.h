@@ -114,14 +114,15 @@ template <int NT>
 __device__ __forceinline__ void pg_weigh(const PagedArgs& a, uint32_t* place_s, uint32_t* sum_s) {
   const int tid = threadIdx.x;
   const int64_t* off = a.p.offsets;
-  const int64_t base = off[0];
+  const int64_t base = off[0], rows = off[a.p.lists] - base;
   uint32_t before = 0;
   for (int r0 = 0; r0 < a.p.lists; r0 += NT) {
     const int r = r0 + tid;
     uint32_t x = 0;
     if (r < a.p.lists) {
-      const uint64_t n = (uint64_t)pg_groups(a, pg_queries(a, pg_list_sequence(a, r))) *
-                         (pg_up(off[r + 1] - base) - pg_up(off[r] - base) + a.gap);
+      const int64_t p0 = off[r] - base, p1 = off[r + 1] - base;
+      const uint32_t held = pg_held(p0, p1, rows) ? pg_up(p1) - pg_up(p0) : 0u;
+      const uint64_t n = (uint64_t)pg_groups(a, pg_queries(a, pg_list_sequence(a, r))) * (held + a.gap);
       x = (uint32_t)min(n, kPgMostTiles);
     }
 #pragma unroll
@@ -299,6 +300,10 @@ __attribute__((amdgpu_waves_per_eu(MODE == kPgWhole ? 2 : pg_simd_waves(F, D, QT
         ntp = (int)pg_up(len);
       } else {
         off.list(r, lane, p0, p1);
+        if (!pg_held(p0, p1, off.rows)) {
+          ++r, copy = 0;
+          continue;
+        }
         uint32_t place = copies * pg_place(p0, r, pg_gap(QT)), times = 1;
         const uint32_t span = pg_place(p1, r + 1, pg_gap(QT)) - pg_place(p0, r, pg_gap(QT));
         if (weighed) {

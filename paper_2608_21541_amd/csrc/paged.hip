@@ -36,7 +36,7 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
   const int64_t rows = p.offsets[p.lists] - base;
   const uint32_t place_r = places[r], place_all = places[p.lists];
   const int32_t q_len = q_lens[b];
-  const int len = min(page_rows(p, p0, p1), a.cover);
+  const int len = pg_held(p0, p1, rows) ? min(page_rows(p, p0, p1), a.cover) : 0;
   const PgCut cut = pg_cut(a, a.place ? place_all : pg_tiles(rows, (uint32_t)p.lists, a.gap));
   if ((p1 - p0 != len || !cut.fits) && blockIdx.y == 0 && threadIdx.x == 0) report_range(g);
   float m = kAtNone, L = 0.f;
@@ -48,9 +48,8 @@ __global__ __launch_bounds__(kPgJoinThreads) void paged_join_kernel(PagedArgs a)
     const uint32_t span = pg_place(p1, r + 1, a.gap) - pg_place(p0, r, a.gap);
     const uint32_t place = a.place ? place_r : pg_place(p0, r, a.gap);
     const uint32_t vs = (uint32_t)a.copies * place + (copy * groups + group) * span;
-    // (of offsets that fall, places may lie behind the last chunk)
-    const uint32_t s0 = min(vs / cut.tiles, (uint32_t)a.most - 1u);
-    const uint32_t nv = min((vs + pg_up(len) - 1) / cut.tiles, (uint32_t)a.most - 1u) - s0 + 1;
+    const PgPieces own_pieces = pg_pieces(vs, pg_up(len), cut.tiles);
+    const uint32_t s0 = own_pieces.first, nv = own_pieces.n;
     constexpr int Q = 4;
     for (uint32_t i0 = sg; i0 < nv; i0 += Q * S) {
       float2 ml[Q];

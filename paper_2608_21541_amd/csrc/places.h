@@ -27,6 +27,11 @@ __host__ __device__ __forceinline__ uint32_t pg_tiles(int64_t rows, uint32_t lis
   const uint64_t n = (((uint64_t)rows + 31) >> 5) + (uint64_t)lists * (uint32_t)gap;
   return (uint32_t)(rows >= 0 && n < kPgMostTiles ? n : kPgMostTiles);
 }
+// Whether [p0, p1) are rows of a list, of `rows` of all: offsets that fall, or lie outside the first
+// and the last, are the caller's mistake.  A list of such is as one without a row: it has no place.
+__host__ __device__ __forceinline__ bool pg_held(int64_t p0, int64_t p1, int64_t rows) {
+  return p0 >= 0 && p1 >= p0 && p1 <= rows;
+}
 // Sums of tiles stop there too.
 __host__ __device__ __forceinline__ uint32_t pg_add(uint32_t x, uint32_t y) {
   const uint32_t n = x + y;
@@ -49,6 +54,16 @@ __host__ __device__ __forceinline__ PgCut pg_cut(uint32_t copies, uint32_t tiles
   // longer chunks, so that the partials stay within the workspace)
   if (total > (uint64_t)most * k) k = (total + most - 1u) / most;
   return PgCut{(k + kPgMinTiles - 1u) / kPgMinTiles * kPgMinTiles, total, true};
+}
+
+// The chunks that a unit's tiles, one or more, lie in: n from `first` on.  (Of a list that is held
+// their end is no later than the total's: below 2^31, and the last of the chunks at most.)
+struct PgPieces {
+  uint32_t first, n;
+};
+__host__ __device__ __forceinline__ PgPieces pg_pieces(uint32_t place, uint32_t tiles, uint32_t chunk) {
+  const uint32_t first = place / chunk;
+  return PgPieces{first, (place + tiles - 1u) / chunk - first + 1u};
 }
 
 }  // namespace certkv

@@ -58,3 +58,48 @@ def test_more_tiles_than_are_counted(L, H, G, tq, copies):
     out = ck.decode_paged(spec, q, cache, tq)
     # (a sum of n weights is off by half a step for each of its n terms, and so is theirs)
     assert int(spec.status) == 0 and bool(((out - 1).abs() <= 2 * LONG * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("H,G,tq", [(1, 1, 1), (4, 1, 1), (2, 8, 9)])
+def test_offsets_below_the_first(H, G, tq):
+    # lists that begin before the first offset, or end behind the last: none has a row to see
+    spec = spec_of(1, B=4, H=H, G=G, d=64)
+    gen = torch.Generator().manual_seed(8)
+    cache = _pages.make_cache(spec, [30, 40, 50, 20], 16, "bf16", DEV, gen, max_pages=LONG // 16)
+    cache.table.clamp_(max=2)
+    q = queries(spec, tq, gen)
+    q_lens = torch.tensor([tq, tq, 1, tq], dtype=torch.int32, device=DEV)
+    for off in ([1000, 488, 1088, 1088, 1088], [5, 4, 3, 2, 1], [10 ** 6, 10 ** 6 + 50, 0, 50, 20],
+                [0, 2 ** 40, 2 ** 40 + 7, 2 ** 40, 0], [2 ** 62, -2 ** 62, 2 ** 62, -2 ** 62, 2 ** 62],
+                [7, 7, 10 ** 6, 7, 7]):
+        cache.offsets.copy_(torch.tensor(off, device=DEV))
+        nothing(spec, q, cache, tq)
+        nothing(spec, q, cache, tq, q_lens)
+
+
+@pytest.mark.parametrize("room", [300, LONG])
+@pytest.mark.parametrize("H,G,tq", [(1, 1, 1), (4, 1, 1), (2, 8, 9)])
+def test_a_list_that_is_longer_than_its_table(H, G, tq, room):
+    # the rows that the table has room for are attended, the others reported; empty ones are neither
+    spec = spec_of(1, B=4, H=H, G=G, d=64)
+    gen = torch.Generator().manual_seed(8)
+    lens = [50, 0, room // 16 * 16, 20]
+    cache = _pages.make_cache(spec, lens, 16, "bf16", DEV, gen, max_pages=room // 16)
+    q = queries(spec, tq, gen)
+    q_lens = torch.tensor([tq, tq, tq, min(1, tq)], dtype=torch.int32, device=DEV)
+    for lens_q in (None, q_lens):
+        good, lse = (x.clone() for x in ck.decode_paged(spec, q, cache, tq, q_lens=lens_q, with_lse=True))
+        assert int(spec.status) == 0
+        was = cache.offsets.clone()
+        cache.offsets.copy_(torch.tensor([9, 59, 59, 59 + 10 ** 9, 59 + 10 ** 9 + 20], device=DEV))
+        spec.status.zero_()
+        out, lse2 = ck.decode_paged(spec, q, cache, tq, q_lens=lens_q, with_lse=True)
+        assert int(spec.status) == ck.CERTKV_ERANGE
+        spec.status.zero_()
+        cache.offsets.copy_(was)
+        keep = torch.tensor([b != 2 for b in range(4) for _ in range(tq)], device=DEV)
+        # (cut elsewhere: sums in another order)
+        assert torch.allclose(out[:, keep], good[:, keep], rtol=0, atol=1e-5)
+        fin = torch.isfinite(lse[:, keep])
+        assert torch.equal(fin, torch.isfinite(lse2[:, keep]))
+        assert torch.allclose(lse2[:, keep][fin], lse[:, keep][fin], rtol=0, atol=1e-5)

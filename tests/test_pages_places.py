@@ -21,6 +21,28 @@ int main() {
       scanf("%u %u %u %u", &copies, &tiles, &parts, &most);
       const PgCut c = pg_cut(copies, tiles, parts, most);
       printf("%u %u %d\n", c.tiles, c.total, (int)c.fits);
+    } else if (!strcmp(what, "lists")) {
+      // the pieces of every list's copies, as the join takes them
+      int lists, gap;
+      unsigned copies, cover, parts, most;
+      scanf("%d %u %u %d %u %u", &lists, &copies, &cover, &gap, &parts, &most);
+      long long off[64];
+      for (int r = 0; r <= lists; ++r) scanf("%lld", off + r);
+      const long long base = off[0], rows = off[lists] - base;
+      const PgCut c = pg_cut(copies, pg_tiles(rows, lists, gap), parts, most);
+      printf("%u", c.tiles);
+      for (int r = 0; r < lists; ++r) {
+        const long long p0 = off[r] - base, p1 = off[r + 1] - base;
+        const bool held = c.fits && pg_held(p0, p1, rows) && p1 > p0;
+        const uint32_t n = held ? pg_up(p1 - p0 < cover ? p1 - p0 : cover) : 0;
+        const uint32_t span = held ? pg_place(p1, r + 1, gap) - pg_place(p0, r, gap) : 0;
+        for (unsigned x = 0; x < copies; ++x) {
+          PgPieces y = {0, 0};
+          if (held) y = pg_pieces(copies * pg_place(p0, r, gap) + x * span, n, c.tiles);
+          printf(" %u %u", y.first, y.n);
+        }
+      }
+      printf("\n");
     } else if (!strcmp(what, "tiles")) {
       long long rows;
       unsigned lists;
@@ -88,6 +110,53 @@ def test_tiles_of_the_lists(ask):
     cases += [(2 ** 63 - 1, 1, 8), (-2 ** 63, 1, 8), (0, 1, 8), (-1, 1, 8)]
     for (rows, lists, gap), (got,) in zip(cases, ask(["tiles %d %d %d" % c for c in cases])):
         assert got == (min(MOST, -(-rows // 32) + lists * gap) if rows >= 0 else MOST)
+
+
+def pieces(off, copies, cover, gap, chunk):
+    """(first chunk, chunks) of every list's copies, their places counted without a width."""
+    up, out = lambda n: -(-n // 32), []  # noqa: E731
+    base, end = off[0], off[-1] - off[0]
+    place = lambda rows, r: up(rows) + r * gap  # noqa: E731
+    fits = end >= 0 and copies * place(end, len(off) - 1) < MOST
+    for r in range(len(off) - 1):
+        p0, p1 = off[r] - base, off[r + 1] - base
+        for x in range(copies):
+            if not fits or not 0 <= p0 < p1 <= end:
+                out.append((0, 0))
+                continue
+            at = copies * place(p0, r) + x * (place(p1, r + 1) - place(p0, r))
+            first = at // chunk
+            out.append((first, (at + up(min(p1 - p0, cover)) - 1) // chunk - first + 1))
+    return out
+
+
+@pytest.mark.parametrize("kind", ["fall", "rise"])
+def test_pieces_of_lists(ask, kind):
+    # lists below the first offset, behind the last, that fall, and that are as they should be: no
+    # partial outside the workspace, and none that two units share
+    rng = random.Random(kind)
+    cases = [([1000, 488, 1088, 1088, 1088], 1, 2000, 8, 512, 71)] if kind == "fall" else []
+    for _ in range(3000):
+        n = rng.randint(1, 8)
+        step = lambda: int(2 ** rng.uniform(0, rng.choice([4, 12, 40])))  # noqa: E731
+        off = [rng.choice([0, step()])]
+        for _ in range(n):
+            off.append(off[-1] + (rng.choice([1, 1, 1, -1]) if kind == "fall" else 1) * step() * rng.randint(0, 1))
+        cases.append((off, rng.choice([1, 2, 16]), rng.choice([64, 2000, 2 ** 31 - 1024]), rng.choice([8, 16]),
+                      rng.choice([1, 512, 1024]), rng.choice([1, 71, 5000])))
+    lines = ["lists %d %d %d %d %d %d %s" % (len(o) - 1, c, cover, gap, parts, most, " ".join(map(str, o)))
+             for o, c, cover, gap, parts, most in cases]
+    some = 0
+    for (off, copies, cover, gap, parts, most), got in zip(cases, ask(lines)):
+        chunk, got = got[0], list(zip(got[1::2], got[2::2]))
+        assert got == pieces(off, copies, cover, gap, chunk)
+        # partial (chunk + unit): within chunks + units
+        kept = [first + u + i for u, (first, n) in enumerate(got) for i in range(min(n, 10 ** 4))]
+        assert all(first + n <= most for first, n in got)
+        some += len(kept)
+        if kind == "rise":
+            assert len(set(kept)) == len(kept)
+    assert some > 1000
 
 
 def test_sums_that_stop(ask):
