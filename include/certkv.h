@@ -572,7 +572,9 @@ certkv_status certkv_page_resize(const certkv_problem* p, const certkv_pages* pa
  *   tokens, tn   tn = 0 (sequences' lists): sequence after sequence, token j of
  *                all has slots[j]; tokens behind the last slot are left out.
  *                tn >= 1: tokens = B * tn, tn of each sequence (decode's layout),
- *                of which list r takes its slots' number from the first on
+ *                of which list r takes its slots' number from the first on.
+ *                Slots that no token fills (more than tokens, or than tn of a list)
+ *                are rows that nobody writes: they store CERTKV_ERANGE
  *   slots, slot_offsets  as certkv_page_resize writes them, slot_count entries; a
  *                slot of -1 leaves its row out.  Slots must differ
  * bf16 pages: rows copied (from fp32 rounded to nearest, ties to even); mxfp8 and

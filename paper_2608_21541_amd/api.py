@@ -854,7 +854,7 @@ def _check_slots(cache, kept, slots, slot_offsets):
 def page_write(spec: ProblemSpec, cache: PagedCache, k, v, slots, slot_offsets, tn=0):
     """Rows of new tokens to their slots (of page_resize): k, v [L][tokens][H][d] in spec.dtype,
     sequence after sequence, or, with tn, tn tokens of each sequence, of which a list takes as many
-    as it has slots."""
+    as it has slots.  Slots that no token fills are reported (CERTKV_ERANGE)."""
     kept = cache._c_pages(spec)
     shape = k.shape
     assert shape == v.shape and len(shape) == 4 and cache.k is not None

@@ -1352,7 +1352,7 @@ certkv_status certkv_page_write(const certkv_problem* p, const certkv_pages* pag
   if (slot_count > 0 && !slots) return CERTKV_EINVAL;
   if (tn ? tokens != (int64_t)tn * a.p.g.B : a.p.per_head != 0) return CERTKV_EINVAL;
   if (tokens > kPgMostRows / a.p.g.H) return CERTKV_EUNSUPPORTED;
-  if ((p->flags & CERTKV_DRY_RUN) || tokens == 0) return CERTKV_OK;
+  if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
   a.dtype = p->kv_dtype;
   a.k = k;
   a.v = v;

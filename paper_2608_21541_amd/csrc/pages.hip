@@ -684,13 +684,23 @@ __global__ __launch_bounds__(kPgThreads) void page_write_kernel(PageWriteArgs a,
                           v ? a.p.v_scales : a.p.k_scales);
       }
   }
+  // Slots that no token fills, rows that a list counts and nobody wrote, are reported.  (By the first
+  // layer's workgroups, behind their rows: a list to a thread.)
+  if (blockIdx.y == 0 && blockIdx.z == 0) {
+    const int32_t lists = a.tn ? a.p.lists : 1;
+    for (int64_t r = (int64_t)blockIdx.x * kPgThreads + threadIdx.x; r < lists; r += (int64_t)gridDim.x * kPgThreads) {
+      const int64_t n = a.tn ? a.slot_offsets[r + 1] - a.slot_offsets[r] : total;
+      if (n > (a.tn ? (int64_t)a.tn : a.tokens)) report_range(g);
+    }
+  }
 }
 
 template <int D, typename T>
 static certkv_status launch_page_write(const PageWriteArgs& a, hipStream_t s) {
   const int64_t step = page_write_rows(a.p.format) * (kPgThreads * 8 / D);
-  const int64_t steps = (a.tokens * a.p.g.H + step - 1) / step;
-  const dim3 grid((unsigned)(steps < 64 * 256 ? steps : 64 * 256), (unsigned)a.p.g.L,
+  // (no token: slots are looked at all the same)
+  const int64_t steps = a.tokens > 0 ? (a.tokens * a.p.g.H + step - 1) / step : 1;
+  const dim3 grid((unsigned)(steps < 64 * 256 ? steps : 64 * 256), a.tokens > 0 ? (unsigned)a.p.g.L : 1u,
                   3 - page_write_arrays(a.p.format));
   const PgDiv by_h((uint32_t)a.p.g.H), by_tn((uint32_t)a.tn);
   switch (a.p.format) {

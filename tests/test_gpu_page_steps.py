@@ -44,3 +44,42 @@ def test_lists_that_only_shrink(lists, beside):
     ref.resize([1] * lists, 0)
     check_lists(cache, ref)
     assert int(spec.status) == ck.CERTKV_ERANGE
+
+
+def write(spec, cache, tokens, slots, so, tn=0):
+    rows = torch.ones((spec.layers, tokens, spec.kv_heads, spec.head_dim), dtype=spec.dtype, device=DEV)
+    spec.status.zero_()
+    ck.page_write(spec, cache, rows, rows, slots, so, tn=tn)
+    return int(spec.status)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8"])
+def test_slots_that_no_token_fills(fmt):
+    # rows that the lists count and nobody wrote are reported; the tokens that are there are written
+    spec = spec_of(L=2, B=3, H=2, d=64)
+    for given, tokens, tn, bad in (([3, 0, 4], 7, 0, False), ([3, 0, 4], 6, 0, True),
+                                   ([3, 0, 4], 9, 0, False), ([3, 0, 4], 0, 0, True),
+                                   ([0, 0, 0], 0, 0, False), ([3, 0, 4], 12, 4, False),
+                                   ([3, 0, 4], 9, 3, True), ([2, 1, 1], 3, 1, True),
+                                   ([1, 0, 1], 3, 1, False)):
+        cache = ck.PagedCache.empty(spec, 8, 16, 2, DEV, fmt)
+        cache.k.zero_()
+        slots, so = step(spec, cache, given, ck.ResizeBuffers(cache, 20, DEV))
+        got = write(spec, cache, tokens, slots, so, tn)
+        assert (got == ck.CERTKV_ERANGE) == bad and got in (0, ck.CERTKV_ERANGE)
+        rows = int(cache.k[0].any(-1).any(-1).sum())
+        assert rows == (sum(min(n, tn) for n in given) if tn else min(tokens, sum(given)))
+
+
+@pytest.mark.parametrize("lists", [1, 300, 5000])
+def test_one_list_of_many_with_a_slot_too_many(lists):
+    # the last list's, by tokens of a number for each sequence
+    spec = spec_of(B=lists, H=1, d=64)
+    cache = ck.PagedCache.empty(spec, lists + 4, 16, 2, DEV)
+    change = torch.ones(lists, dtype=torch.int32, device=DEV)
+    slots, so = ck.page_resize(spec, cache, change)
+    assert write(spec, cache, lists, slots, so, tn=1) == 0
+    change[-1] = 2
+    slots, so = ck.page_resize(spec, cache, change)
+    assert write(spec, cache, lists, slots, so, tn=1) == ck.CERTKV_ERANGE
+    assert write(spec, cache, 2 * lists, slots, so, tn=2) == 0
