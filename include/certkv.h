@@ -589,7 +589,7 @@ certkv_status certkv_page_write(const certkv_problem* p, const certkv_pages* pag
  * into pages of its format, units' lists: its row j, j < rows, to slots[j], as they
  * are held.  cache.offsets is not read: the rows' order is that of slots written for
  * lists that were empty and take packed_offsets[u+1] - packed_offsets[u] rows each.
- * Rows behind the last slot are left out. */
+ * Rows behind the last slot are left out, slots behind the last row store CERTKV_ERANGE. */
 certkv_status certkv_page_adopt(const certkv_problem* p, const certkv_pages* pages,
                                 certkv_cache cache, int64_t rows, const int32_t* slots,
                                 int64_t slot_count, const int64_t* slot_offsets, void* stream);

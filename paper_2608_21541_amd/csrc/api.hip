@@ -1373,7 +1373,7 @@ certkv_status certkv_page_adopt(const certkv_problem* p, const certkv_pages* pag
   if (!a.p.per_head || cache.format != pages->format) return CERTKV_EINVAL;
   if (rows < 0 || slot_count < 0 || !slot_offsets || (slot_count > 0 && !slots))
     return CERTKV_EINVAL;
-  if ((p->flags & CERTKV_DRY_RUN) || rows == 0) return CERTKV_OK;
+  if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
   a.k = static_cast<const uint8_t*>(cache.k);
   a.v = static_cast<const uint8_t*>(cache.v);
   a.k_scales = cache.k_scales;
@@ -1394,7 +1394,7 @@ certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* page
   if (rows > kPgMostRows / (a.p.per_head ? 1 : a.p.g.H)) return CERTKV_EUNSUPPORTED;
   if ((rows > 0 && !k_out && !v_out) || ((uintptr_t)k_out & 15u) || ((uintptr_t)v_out & 15u))
     return CERTKV_EINVAL;
-  if ((p->flags & CERTKV_DRY_RUN) || rows == 0) return CERTKV_OK;
+  if (p->flags & CERTKV_DRY_RUN) return CERTKV_OK;
   a.f32 = out_dtype == CERTKV_F32;
   a.rows = rows;
   a.k = k_out;

@@ -755,7 +755,7 @@ __global__ __launch_bounds__(kPgThreads) void page_adopt_kernel(PageAdoptArgs a)
 template <int D>
 static certkv_status launch_page_adopt(const PageAdoptArgs& a, hipStream_t s) {
   const int64_t step = kPgThreads / (mx_row_bytes(a.p.format, D) / 16);
-  const int64_t steps = (a.rows + step - 1) / step;
+  const int64_t steps = a.rows > 0 ? (a.rows + step - 1) / step : 1;  // (no row: slots are looked at)
   const dim3 grid((unsigned)(steps < 4 * 256 ? steps : 4 * 256));
   switch (a.p.format) {
     case CERTKV_CACHE_MXFP8:
@@ -836,12 +836,12 @@ __global__ __launch_bounds__(kPgThreads) void page_read_kernel(PageReadArgs a, P
   const uint8_t* src = blockIdx.z ? p.v : p.k;
   const uint8_t* scales = blockIdx.z ? p.v_scales : p.k_scales;
   void* out = blockIdx.z ? a.v : a.k;
-  if (!out) return;
   const int l = blockIdx.y, ci = threadIdx.x % LPR, lane = threadIdx.x & 63;
   const uint32_t H = p.per_head ? 1u : (uint32_t)p.g.H;
   const int64_t base = p.offsets[0], all = p.offsets[p.lists] - base;
   const int64_t tokens = min(all, a.rows);
   if (all > a.rows && threadIdx.x == 0 && blockIdx.x == 0) report_range(p.g);
+  if (!out) return;
   const uint32_t rows = (uint32_t)max(tokens, (int64_t)0) * H;
   const auto first = [&](int32_t r) { return p.offsets[r] - base; };
   const int64_t out0 = p.per_head ? 0 : (int64_t)l * a.rows * H;
@@ -891,7 +891,8 @@ template <int F, int D>
 static certkv_status launch_page_read(const PageReadArgs& a, hipStream_t s) {
   const int H = a.p.per_head ? 1 : a.p.g.H, layers = a.p.per_head ? 1 : a.p.g.L;
   const int64_t rows = a.rows * H, step = page_read_rows(F) * (kPgThreads * 8 / D);
-  const int64_t wgs = (rows + step - 1) / step < 64 * 256 ? (rows + step - 1) / step : 64 * 256;
+  const int64_t steps = rows > 0 ? (rows + step - 1) / step : 1;  // (no room: what is left out is told)
+  const int64_t wgs = steps < 64 * 256 ? steps : 64 * 256;
   const dim3 grid((unsigned)wgs, (unsigned)layers, 2);
   const PgDiv by_h((uint32_t)H);
   if (a.f32)

@@ -83,3 +83,31 @@ def test_one_list_of_many_with_a_slot_too_many(lists):
     slots, so = ck.page_resize(spec, cache, change)
     assert write(spec, cache, lists, slots, so, tn=1) == ck.CERTKV_ERANGE
     assert write(spec, cache, 2 * lists, slots, so, tn=2) == 0
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8"])
+def test_calls_of_no_rows(fmt):
+    # slots that a packed cache of no rows leaves, and lists that a read has no room for
+    spec = spec_of(L=1, B=3, H=2, d=64)
+    cache = ck.PagedCache.empty(spec, 8, 16, 2, DEV, fmt, per_head=True)
+    for t in (cache.k, cache.v):
+        t.fill_(3)
+    packed = ck.MxCache.empty(spec, 0, fmt, DEV) if fmt != "bf16" else \
+        tuple(torch.empty((0, 64), dtype=torch.bfloat16, device=DEV) for _ in range(2)) + (None,)
+    none = [torch.empty((0, 64), dtype=torch.float32, device=DEV) for _ in range(2)]
+    for change, bad in (([0] * 6, False), ([0, 3, 0, 0, 1, 0], True)):
+        slots, so = step(spec, cache, change, ck.ResizeBuffers(cache, 20, DEV))
+        spec.status.zero_()
+        ck.page_adopt(spec, cache, packed, slots, so)
+        assert int(spec.status) == (ck.CERTKV_ERANGE if bad else 0)
+        spec.status.zero_()
+        ck.page_read(spec, cache, out=none)
+        assert int(spec.status) == (ck.CERTKV_ERANGE if bad else 0)
+    assert bool((cache.k == 3).all()) and bool((cache.v == 3).all())
+    cache = ck.PagedCache.empty(spec, 8, 16, 2, DEV, fmt)  # and of sequences' lists
+    none = [torch.empty((1, 0, 2, 64), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    for change, bad in (([0] * 3, False), ([0, 3, 0], True)):
+        step(spec, cache, change)
+        spec.status.zero_()
+        ck.page_read(spec, cache, out=none)
+        assert int(spec.status) == (ck.CERTKV_ERANGE if bad else 0)
