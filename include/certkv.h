@@ -599,8 +599,8 @@ certkv_status certkv_page_adopt(const certkv_problem* p, const certkv_pages* pag
  * packed cache whose offsets are the lists' (units' lists: [rows][d]), contiguous, in
  * out_dtype (CERTKV_BF16 or CERTKV_F32; microscaled rows are exact in both),
  * 16-byte aligned; either may be NULL.  rows: the outputs' room; rows behind it are
- * left out and store CERTKV_ERANGE in *dev_status, and what the lists do not fill is
- * not written. */
+ * left out and store CERTKV_ERANGE in *dev_status, as do offsets that fall and lists of
+ * more rows than the table has pages for, and what the lists do not fill is not written. */
 certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* pages, int64_t rows,
                                int32_t out_dtype, void* k_out, void* v_out, void* stream);
 

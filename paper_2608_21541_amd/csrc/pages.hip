@@ -841,8 +841,7 @@ __global__ __launch_bounds__(kPgThreads) void page_read_kernel(PageReadArgs a, P
   const int64_t base = p.offsets[0], all = p.offsets[p.lists] - base;
   const int64_t tokens = min(all, a.rows);
   if (all > a.rows && threadIdx.x == 0 && blockIdx.x == 0) report_range(p.g);
-  if (!out) return;
-  const uint32_t rows = (uint32_t)max(tokens, (int64_t)0) * H;
+  const uint32_t rows = out ? (uint32_t)max(tokens, (int64_t)0) * H : 0u;
   const auto first = [&](int32_t r) { return p.offsets[r] - base; };
   const int64_t out0 = p.per_head ? 0 : (int64_t)l * a.rows * H;
   for (uint32_t x0 = blockIdx.x * BLOCK; x0 < rows; x0 += gridDim.x * BLOCK) {
@@ -883,6 +882,14 @@ __global__ __launch_bounds__(kPgThreads) void page_read_kernel(PageReadArgs a, P
         if (x >= rows || row[q] < 0) continue;
         pg_put8<F32>(out, (out0 + x) * D + ci * 8, k[q].values());
       }
+    }
+  }
+  // Lengths that are none (offsets that fall, more rows than a table has) are reported, also where no
+  // row of the output is such a list's.  (Behind the rows: a list to a thread.)
+  if (blockIdx.y == 0 && blockIdx.z == 0) {
+    for (int64_t r = (int64_t)blockIdx.x * kPgThreads + threadIdx.x; r < p.lists; r += (int64_t)gridDim.x * kPgThreads) {
+      const int64_t p0 = p.offsets[r], p1 = p.offsets[r + 1];
+      if (page_rows(p, p0, p1) != p1 - p0) report_range(p.g);
     }
   }
 }

@@ -111,3 +111,31 @@ def test_calls_of_no_rows(fmt):
         spec.status.zero_()
         ck.page_read(spec, cache, out=none)
         assert int(spec.status) == (ck.CERTKV_ERANGE if bad else 0)
+
+
+@pytest.mark.parametrize("per_head", [False, True])
+def test_a_read_of_offsets_that_are_none(per_head):
+    # offsets that fall, or that say more than a table holds, are reported, also behind or between
+    # the rows that are read; nothing outside the outputs is written
+    spec = spec_of(L=1, B=2, H=2, d=64)
+    cache = ck.PagedCache.empty(spec, 8, 16, 2, DEV, per_head=per_head)
+    cache.k.fill_(1), cache.v.fill_(1), cache.table.zero_()
+    lists = cache.lists
+    room = [torch.full((80 * (1 if per_head else 2), 64), 5.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    shape = (40, 64) if per_head else (1, 40, 2, 64)
+    n = 40 * (1 if per_head else 2)
+    out = [t[:n].view(shape) for t in room]
+    for off in ([0, 20], [7, 39], [0, 20, 15], [0, -5, 20], [0, 33], [30, 20], [2 ** 40, 2 ** 40 + 9],
+                [0, 10, 10 ** 12], [0, 30, 25]):
+        full = (off + [off[-1]] * lists)[:lists + 1]
+        cache.offsets.copy_(torch.tensor(full, device=DEV))
+        for t in room:
+            t.fill_(5)
+        spec.status.zero_()
+        ck.page_read(spec, cache, out=out)
+        bad = any(not 0 <= b - a <= 32 for a, b in zip(full, full[1:]))
+        assert int(spec.status) == (ck.CERTKV_ERANGE if bad else 0), full
+        assert all(bool((t[n:] == 5).all()) for t in room)
+        if not bad:
+            m = (full[-1] - full[0]) * (1 if per_head else 2)
+            assert all(bool((t[:m] == 1).all()) and bool((t[m:] == 5).all()) for t in room)
