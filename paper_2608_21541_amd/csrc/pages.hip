@@ -6,6 +6,9 @@ namespace certkv {
 constexpr int kPgThreads = 256;
 constexpr int kPgScan = 2048;      // lists that a workgroup scans by itself
 constexpr int kPgBlock = 1024;     // of more, lists to a workgroup
+// Pages of a lane that are given back at a time.  (65536 pages of 8 lists of 64, with events, one wave
+// 695 us and with 16 123, eight waves 26; 131072 of 64 lists of 250, four waves 413 and 76.)
+constexpr int kPgGives = 16;
 
 // ---- tables and slots ---------------------------------------------------------
 //
@@ -432,10 +435,26 @@ __global__ __launch_bounds__(64 * W) void page_resize_kernel(PageResizeArgs a) {
                     [&](int32_t r) { return pos_s[r]; });
       }
     }
-    for (uint32_t i = at; i < (uint32_t)given; i += step) {
-      const int32_t r = pg_bisect(0, R - 1, [&](int32_t q) { return (int64_t)go_s[q]; }, i);
-      a.ring[(uint32_t)(tail + i) % (uint32_t)N] =
-          a.table[(int64_t)r * a.max_pages + keep_s[r] + ((int32_t)i - go_s[r])];
+    // Pages given back, in runs of a wave's, all of a run in flight.  The run's lists are found first:
+    // mostly one (a long list that ends), else each lane searches between them.
+    constexpr int GIVES = PART == 0 ? kPgGives : 1, RUN = 64 * GIVES;
+    const auto go = [&](int32_t i) { return (int64_t)go_s[i]; };
+    for (int64_t i0 = ((PART == 1 ? blockIdx.x : 0) * (int64_t)W + wave) * RUN; i0 < given; i0 += (int64_t)step * GIVES) {
+      const int32_t end = (int32_t)min(i0 + RUN, (int64_t)given) - 1;
+      const int32_t ra = pg_find(R, go, i0, lane), rb = pg_find(R, go, end, lane);
+      int32_t id[GIVES];
+#pragma unroll
+      for (int k = 0; k < GIVES; ++k) {
+        const int32_t i = min((int32_t)i0 + 64 * k + lane, end);
+        const int32_t r = ra == rb ? ra : pg_bisect(ra, rb, go, i);
+        id[k] = a.table[(int64_t)r * a.max_pages + keep_s[r] + (i - go_s[r])];
+      }
+#pragma unroll
+      for (int k = 0; k < GIVES; ++k) {
+        const int32_t i = (int32_t)i0 + 64 * k + lane;
+        const uint32_t to = (uint32_t)(tail + i);
+        if (i <= end) a.ring[to < (uint32_t)N ? to : to - (uint32_t)N] = id[k];
+      }
     }
   }
 }
@@ -536,13 +555,25 @@ static int64_t pg_small_slots(int32_t lists, bool in_place) {
   return in_place ? 16384 : lists <= 256 ? 2048 : 8192;
 }
 
+// And the pages that its lists may give back, whose number only the device knows: up to these few of a
+// short step one wave moves them all (3.4 us for a row to each of 64 lists, four waves 3.9, eight 4.2,
+// sixteen 6.3), of more eight waves (8192 pages of one list 23 us and 11, 65536 of eight 123 and 26,
+// 524288 of 64 914 and 131; a grid of workgroups 14, but 6.4 for a row to each, in place 7.9).  Where
+// the sums are a grid's anyhow, it is one for each 1024 of them (2048 lists that get a row each 11.7 us
+// by 2 workgroups and by 256; 400 of them that end, 204800 pages, with events, 211 and 24).
+constexpr int64_t kPgFewPages = 32768;
+
 certkv_status run_page_resize(const PageResizeArgs& a, hipStream_t s) {
   const bool in_place = a.offsets_out == a.offsets || a.free_out == a.free;
+  const int64_t held = (int64_t)a.lists * a.max_pages;
   if (a.lists <= 1024 && a.slot_capacity <= pg_small_slots(a.lists, in_place)) {
-    if (a.lists <= 64 && a.slot_capacity <= 256)
+    const bool few = held <= kPgFewPages || a.num_pages <= kPgFewPages;
+    if (few && a.lists <= 64 && a.slot_capacity <= 256)
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<1, 1, 0>), dim3(1), dim3(64), 0, s, a);
-    else if (a.lists <= 256 && a.slot_capacity <= 4096)
+    else if (few && a.lists <= 256 && a.slot_capacity <= 4096)
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<4, 1, 0>), dim3(1), dim3(256), 0, s, a);
+    else if (a.lists <= 256 && a.slot_capacity <= 4096)
+      CERTKV_LAUNCH("page_resize", (page_resize_kernel<8, 1, 0>), dim3(1), dim3(512), 0, s, a);
     else
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<16, 1, 0>), dim3(1), dim3(1024), 0, s, a);
     return CERTKV_OK;
@@ -554,8 +585,10 @@ certkv_status run_page_resize(const PageResizeArgs& a, hipStream_t s) {
       b.offsets_out = reinterpret_cast<int64_t*>(a.ws);
       b.free_out = b.offsets_out + a.lists + 1;
     }
-    // (room for no slot, as where lists only shrink: the sums and the pages given back all the same)
-    const int64_t wgs = a.slot_capacity < 1024 ? 1 : (a.slot_capacity + 1023) / 1024;
+    // (of few slots, or of room for none, as where lists only shrink: by the pages given back)
+    int64_t most = held < a.num_pages ? held : a.num_pages;
+    if (most > 256 * 1024) most = 256 * 1024;
+    const int64_t wgs = ((most > a.slot_capacity ? most : a.slot_capacity) + 1023) / 1024;
     const dim3 grid((unsigned)(wgs < 4 * 256 ? wgs : 4 * 256));
     if (a.lists <= 256)
       CERTKV_LAUNCH("page_resize", (page_resize_kernel<4, 1, 1>), grid, dim3(256), 0, s, b);

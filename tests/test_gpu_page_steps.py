@@ -46,6 +46,31 @@ def test_lists_that_only_shrink(lists, beside):
     assert int(spec.status) == ck.CERTKV_ERANGE
 
 
+# pages given back by the workgroup of a short step, of one wave, four, eight or sixteen, and by many
+@pytest.mark.parametrize("room", [0, 256, 4096, 40_000])
+@pytest.mark.parametrize("lists,most", [(1, 3000), (1, 40_000), (3, 1500), (60, 500), (64, 700), (250, 90),
+                                        (250, 140), (700, 30), (1500, 20), (2100, 20)])
+def test_many_pages_given_back(lists, most, room):
+    rng, page = random.Random(lists + most), 16
+    spec, num = spec_of(B=lists), lists * most + 5
+    ring = rng.sample(range(num), num)
+    ref = _pages.Lists(lists, num, page, most, ring=ring, head=num - 3)
+    cache = tables(lists, num, page, most, ring=ring, head=num - 3)
+    full = [rng.choice([most * page, rng.randint(0, most * page), 0]) for _ in range(lists)]
+    full[-1] = most * page
+    step(spec, cache, full, ck.ResizeBuffers(cache, sum(full), DEV))
+    ref.resize(full, sum(full))
+    bufs = ck.ResizeBuffers(cache, room, DEV)
+    for kind in (lambda r: rng.choice([0, 0, -1, -page * most // 3]), lambda r: 0 if r % 9 else DROP,
+                 lambda r: DROP if r % 2 else -5, lambda r: DROP):
+        change = [kind(r) for r in range(lists)]
+        if room >= lists:  # (and a row for some)
+            change = [c or 1 for c in change]
+        step(spec, cache, change, bufs)
+        ref.resize(change, room)
+        check_lists(cache, ref)
+
+
 def write(spec, cache, tokens, slots, so, tn=0):
     rows = torch.ones((spec.layers, tokens, spec.kv_heads, spec.head_dim), dtype=spec.dtype, device=DEV)
     spec.status.zero_()
