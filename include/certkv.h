@@ -509,7 +509,8 @@ certkv_status certkv_decode_tree(const certkv_problem* p, certkv_tensor q_new, i
  *                at most 2^31 - 1024, 16 s_row rows of k below 2^31 bytes, s_page
  *                and s_head below 2^31
  *   table        [lists][max_pages] int32: the page of row i of a list is
- *                table[list][i / page]; entries behind its last page are not read
+ *                table[list][i / page]; what entries behind its last page hold has no
+ *                effect (they may be read, never followed)
  *   offsets      [lists+1] int64: list r holds offsets[r+1] - offsets[r] rows
  *                (offsets[0] may be any)
  *   ring, free   [num_pages] int32 and [2] int64: the pages that no list has are
@@ -608,10 +609,11 @@ certkv_status certkv_page_read(const certkv_problem* p, const certkv_pages* page
  * which q_lens[b] are sequence b's own (NULL: tq), its list's last rows being the
  * queries' own tokens: query t < n sees rows j <= len - n + t, len the rows of the
  * unit's list.  A row that a query does not see has no part in its output, whatever
- * it holds, and what lies behind a list's last row is not read.  A query that sees
- * nothing (t >= n, or len - n + t < 0) is out = 0, lse = -infinity.  Offsets that fall
- * store CERTKV_ERANGE, their lists' queries see nothing, and what the other lists'
- * outputs hold is not defined.
+ * it holds, nor have the rows of its page behind a list's last one, which may be read.
+ * New tokens are a chain: a mask over them, as certkv_decode_tree's, is not taken.  A
+ * query that sees nothing (t >= n, or len - n + t < 0) is out = 0, lse = -infinity.
+ * Offsets that fall store CERTKV_ERANGE (or the CERTKV_ENONFINITE of another list), such
+ * lists' queries see nothing, and what the other lists' outputs hold is not defined.
  *   q_new, out, lse  as certkv_decode; tq * G <= 512
  *   q_lens           optional [B] int32, device
  *   max_rows         bound on the rows of any list, or 0 for max_pages * page; it

@@ -917,7 +917,8 @@ def decode_paged_workspace_size(spec: ProblemSpec, cache: PagedCache, tq: int,
 def decode_paged(spec: ProblemSpec, q_new, cache: PagedCache, tq, q_lens=None, with_lse=False,
                  bufs=None, max_rows=0):
     """decode over a paged cache, whose lists' last rows are the new tokens' own: query t of
-    sequence b's n = q_lens[b] (int32 [B]; None: tq) sees the rows up to len - n + t.  Returns out
+    sequence b's n = q_lens[b] (int32 [B]; None: tq) sees the rows up to len - n + t (a chain: no
+    mask over the new tokens, as decode_tree's).  Returns out
     [L][B*tq][Hq][d] fp32 (and the natural-log lse [L][B*tq][Hq] with_lse); a query that sees
     nothing (t >= n, an empty list) is out 0, lse -inf.  bufs: DecodeBuffers(..., pages=cache)."""
     kept = cache._c_pages(spec)

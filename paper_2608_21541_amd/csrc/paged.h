@@ -22,7 +22,8 @@
 // over 16 layers of mxfp8, 2.1 GB in 335, 6.2), but for mxfp4, the issue of its conversions and of
 // weights in three parts (3.36M rows, 457 MB in 92 us, 5.0 TB/s); short lists, latency (9 us);
 // drafts, issue with little of matrix and vector instructions under each other (48 query rows over
-// 378k rows of mxfp4: 50 us; over 3.0M rows 236, the vector unit 43 % busy, the matrix unit 25 %).
+// 378k rows of mxfp4: 48 us; over 3.0M rows 236, the vector unit 43 % busy, the matrix unit 25 %: two
+// groups of 32 query rows each convert every tile).
 // Tiles two ahead in registers instead of one are no faster (64 dims: 1 to 8 % slower).
 #pragma once
 
@@ -54,7 +55,8 @@ constexpr int pg_simd_waves(int format, int D, int qt) {
 // A workgroup has whole units where they are short and not many: no partials, no second launch.
 // (In us, whole and in pieces: 8 units of 1024 rows of 128 dims, bf16, 17 and 15, 128 of them 19
 // and 23, 512 48 and 54, 2048 194 and 181; 32 units of 100 rows 9 and 15, 2048 53 and 31; of 64
-// dims 16 units of 1024 rows 10 and 14, 1024 46 and 53.)
+// dims 16 units of 1024 rows 10 and 14, 1024 46 and 53.  The 2 us that few long units of 128 dims
+// lose have no rule of their own.)
 constexpr int kPgWholeRows = 1024, kPgWholeUnits = 1024;
 // Four heads' units where the heads of a row lie together: their rows share lines, which they then
 // read at the same time.  (64 ragged sequences, 2.4M rows of 128 dims, a head's rows by itself and
