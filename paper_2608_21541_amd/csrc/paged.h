@@ -122,9 +122,8 @@ __device__ __forceinline__ void pg_weigh(const PagedArgs& a, uint32_t* place_s, 
     const int r = r0 + tid;
     uint32_t x = 0;
     if (r < a.p.lists) {
-      const int64_t p0 = off[r] - base, p1 = off[r + 1] - base;
-      const uint32_t held = pg_held(p0, p1, rows) ? pg_up(p1) - pg_up(p0) : 0u;
-      const uint64_t n = (uint64_t)pg_groups(a, pg_queries(a, pg_list_sequence(a, r))) * (held + a.gap);
+      const uint32_t tiles = pg_list_tiles(off[r] - base, off[r + 1] - base, rows);
+      const uint64_t n = (uint64_t)pg_groups(a, pg_queries(a, pg_list_sequence(a, r))) * (tiles + a.gap);
       x = (uint32_t)min(n, kPgMostTiles);
     }
 #pragma unroll

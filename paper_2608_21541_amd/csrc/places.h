@@ -32,6 +32,13 @@ __host__ __device__ __forceinline__ uint32_t pg_tiles(int64_t rows, uint32_t lis
 __host__ __device__ __forceinline__ bool pg_held(int64_t p0, int64_t p1, int64_t rows) {
   return p0 >= 0 && p1 >= p0 && p1 <= rows;
 }
+// The tiles from a list's first row to the next one's, none of one that is not held: they stop there
+// as well.
+__host__ __device__ __forceinline__ uint32_t pg_list_tiles(int64_t p0, int64_t p1, int64_t rows) {
+  if (!pg_held(p0, p1, rows)) return 0;
+  const uint64_t n = (((uint64_t)p1 + 31) >> 5) - (((uint64_t)p0 + 31) >> 5);
+  return (uint32_t)(n < kPgMostTiles ? n : kPgMostTiles);
+}
 // Sums of tiles stop there too.
 __host__ __device__ __forceinline__ uint32_t pg_add(uint32_t x, uint32_t y) {
   const uint32_t n = x + y;

@@ -62,7 +62,8 @@ def test_more_tiles_than_are_counted(L, H, G, tq, copies):
 
 @pytest.mark.parametrize("H,G,tq", [(1, 1, 1), (4, 1, 1), (2, 8, 9)])
 def test_offsets_below_the_first(H, G, tq):
-    # lists that begin before the first offset, or end behind the last: none has a row to see
+    # lists that begin before the first offset, or end behind the last: none has a row to see; and
+    # lists of more rows than there are places for
     spec = spec_of(1, B=4, H=H, G=G, d=64)
     gen = torch.Generator().manual_seed(8)
     cache = _pages.make_cache(spec, [30, 40, 50, 20], 16, "bf16", DEV, gen, max_pages=LONG // 16)
@@ -71,7 +72,8 @@ def test_offsets_below_the_first(H, G, tq):
     q_lens = torch.tensor([tq, tq, 1, tq], dtype=torch.int32, device=DEV)
     for off in ([1000, 488, 1088, 1088, 1088], [5, 4, 3, 2, 1], [10 ** 6, 10 ** 6 + 50, 0, 50, 20],
                 [0, 2 ** 40, 2 ** 40 + 7, 2 ** 40, 0], [2 ** 62, -2 ** 62, 2 ** 62, -2 ** 62, 2 ** 62],
-                [7, 7, 10 ** 6, 7, 7]):
+                [7, 7, 10 ** 6, 7, 7], [0, 2 ** 37, 2 ** 37 + 50, 2 ** 37 + 50, 2 ** 37 + 70],
+                [9, 50, 50 + 2 ** 42, 2 ** 43, 2 ** 43]):
         cache.offsets.copy_(torch.tensor(off, device=DEV))
         nothing(spec, q, cache, tq)
         nothing(spec, q, cache, tq, q_lens)

@@ -43,6 +43,10 @@ int main() {
         }
       }
       printf("\n");
+    } else if (!strcmp(what, "list")) {
+      long long p0, p1, rows;
+      scanf("%lld %lld %lld", &p0, &p1, &rows);
+      printf("%u\n", pg_list_tiles(p0, p1, rows));
     } else if (!strcmp(what, "tiles")) {
       long long rows;
       unsigned lists;
@@ -110,6 +114,22 @@ def test_tiles_of_the_lists(ask):
     cases += [(2 ** 63 - 1, 1, 8), (-2 ** 63, 1, 8), (0, 1, 8), (-1, 1, 8)]
     for (rows, lists, gap), (got,) in zip(cases, ask(["tiles %d %d %d" % c for c in cases])):
         assert got == (min(MOST, -(-rows // 32) + lists * gap) if rows >= 0 else MOST)
+
+
+def test_tiles_of_a_list(ask):
+    # from its first row to the next one's, where 32 bits do not hold them either
+    rng = random.Random(3)
+    far = lambda: rng.choice([0, int(2 ** rng.uniform(0, 62.9)), 2 ** rng.randint(30, 62)])  # noqa: E731
+    cases = [(0, 2 ** 37, 2 ** 37 + 70), (0, 2 ** 37 + 70, 2 ** 37 + 70), (2 ** 37, 2 ** 37 + 50, 2 ** 38),
+             (-1, 5, 5), (6, 5, 9), (0, 6, 5), (0, 2 ** 63 - 1, 2 ** 63 - 1), (0, 2 ** 36 - 1, 2 ** 36)]
+    for _ in range(3000):
+        p0 = rng.choice([1, 1, 1, -1]) * far()
+        p1 = p0 + rng.choice([1, 1, 1, -1]) * rng.choice([far(), rng.randint(0, 99)])
+        cases.append((p0, p1, rng.choice([p1, p1 + 5, p1 - 1, far()])))
+    cases = [c for c in cases if all(-2 ** 63 <= x < 2 ** 63 for x in c)]
+    for (p0, p1, rows), (got,) in zip(cases, ask(["list %d %d %d" % c for c in cases])):
+        held = 0 <= p0 <= p1 <= rows
+        assert got == (min(MOST, -(-p1 // 32) - -(-p0 // 32)) if held else 0)
 
 
 def pieces(off, copies, cover, gap, chunk):
